@@ -141,6 +141,14 @@ def _flat(sizes):
     return offs, at
 
 
+def _gaps(buf, offs, sizes):
+    """buf with zeros between its tensors: what lies there belongs to none and stays zero."""
+    used = torch.zeros_like(buf)
+    for o, n in zip(offs, sizes):
+        used[o:o + n] = 1
+    return buf * used
+
+
 def _gradients(shapes, offs, total, g, noise):
     """Weight gradients of the sort a batch gives: a few strong directions in broadband noise, every matrix of a
     size of its own."""
@@ -212,14 +220,15 @@ def prepare(case, seed):
         s["w"][o:o + r * c] = math.sqrt(2 / c) * torch.randn(r * c, device="cuda", generator=g)
         s["o"][o:o + r * c] = torch.randn(r * c, device="cuda", generator=g) / math.sqrt(max(r, c))
     s["w16"] = s["w"].bfloat16() if half else None
-    s["b"] = 0.1 * torch.randn(vtotal, device="cuda", generator=g)
-    s["db"] = 1e-3 * torch.randn(vtotal, device="cuda", generator=g)
-    both = [("b", "db", voffs, [r for r, _ in shapes], vtotal)]
+    rows = [r for r, _ in shapes]
+    s["b"] = _gaps(0.1 * torch.randn(vtotal, device="cuda", generator=g), voffs, rows)
+    s["db"] = _gaps(1e-3 * torch.randn(vtotal, device="cuda", generator=g), voffs, rows)
+    both = [("b", "db", voffs, rows, vtotal)]
     if case["rule"] == "adamw":
         both.append(("w", "grad", offs, [r * c for r, c in shapes], total))
-    for w, grad, _, _, n in both:
-        s[w + "_m"] = 1e-3 * torch.randn(n, device="cuda", generator=g)
-        s[w + "_v"] = 1e-6 * torch.rand(n, device="cuda", generator=g) + 1e-8
+    for w, _, of, sizes, n in both:
+        s[w + "_m"] = _gaps(1e-3 * torch.randn(n, device="cuda", generator=g), of, sizes)
+        s[w + "_v"] = _gaps(1e-6 * torch.rand(n, device="cuda", generator=g) + 1e-8, of, sizes)
     if own:
         import paper_2004_09910_amd as tgp
 
