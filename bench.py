@@ -70,7 +70,8 @@ KERNEL_FILES = {
     "conv1x1_tile": "conv1x1_tile.hip", "wgrad1x1_tile": "conv1x1_tile.hip",
     "conv1x1_res": "conv_mfma.hip", "conv_fwd_dma": "conv_mfma.hip",
     "conv_wgrad_mfma": "conv_mfma.hip", "splitk_reduce": "conv_mfma.hip",
-    "wtransform": "conv_mfma.hip", "": "elementwise.hip",
+    "wtransform": "conv_mfma.hip", "norm_": "layer_norm.hip", "muon_": "muon.hip",
+    "weight_step": "weight_step.hip", "adamw": "weight_step.hip", "": "elementwise.hip",
 }
 
 

@@ -335,6 +335,128 @@ tgp_status tgp_pipeline_step_static(tgp_net* net, const void* x, const void* tar
  * the number of ops.  EINVAL if cap is too small (count still set). */
 tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap, int* count);
 
+/* ------------------------------------------------------------------------
+ * Layer normalisation and the weights' update: what a training program does
+ * between stage calls and after the last accumulation of a step.
+ *
+ * These calls keep no state of their own: tensors, statistics and workspaces
+ * are the caller's, every argument check runs on the host before anything is
+ * enqueued, and work goes to `stream`.  They may be captured into a HIP
+ * graph.  Calls with different buffers may run from several threads.
+ *
+ * Layer normalisation over the channels of each pixel (no statistic crosses
+ * a pixel, so a micro-batched run equals the full-batch one, and a recompute
+ * gives the forward's bits):
+ *
+ *   mean = sum_c x_c / C        rstd = 1 / sqrt(sum_c (x_c - mean)^2 / C + eps)
+ *   y_c = gain_c (x_c - mean) rstd + bias_c
+ *
+ * rows pixels of C channels (rows = 0 is allowed; C >= 1).  Consecutive rows
+ * of x and y are ldx and ldy elements apart (>= C), so that either may be a
+ * channel slice of a wider tensor.  x and y have the type `dtype`; gain and
+ * bias are float32 (NULL: ones, zeros).  stats, rows pairs of float32 (mean,
+ * rstd), is what the backward reads; NULL where none will run.  Sums are
+ * float32, the variance is that of the differences from the mean, and y is
+ * rounded once.  y may be x itself (ldy = ldx); other overlaps are not
+ * allowed.  An infinity or NaN in a row makes that row NaN and no other.
+ * Alignment: elements of x and y at multiples of their size, gain and bias at
+ * 4 bytes, stats at 8.  Pointers and row distances at multiples of 16 bytes
+ * are read and written in 16-byte vectors.  EINVAL otherwise. */
+tgp_status tgp_layer_norm_forward(int64_t rows, int C, int dtype, const void* x, int64_t ldx,
+                                  const float* gain, const float* bias, float eps, void* y,
+                                  int64_t ldy, float* stats, void* stream);
+
+/* The gradients, with xhat = (x - mean) rstd from stats and g = gain dy:
+ *
+ *   dx_c = rstd (g_c - sum_c g_c / C - xhat_c sum_c g_c xhat_c / C)
+ *   dgain_c (+)= sum_rows dy_c xhat_c        dbias_c (+)= sum_rows dy_c
+ *
+ * dx (rows lddx apart; NULL where it is not wanted) has the type `dtype`, and
+ * may be dy or x itself at the same row distance.  dgain and dbias are
+ * float32 accumulators like tgp_bind_params' (both set, or both NULL):
+ * overwrite = 1 for a step's first micro-batch, 0 to add to them.  The sums
+ * over rows run in an order fixed by (rows, C, dtype) and the alignment.
+ * They need `ws`, device memory of at least the size that
+ * tgp_layer_norm_backward_workspace returns, at a multiple of 16 bytes
+ * (unused, and may be NULL, where dgain is NULL); ENOSPACE if it is smaller.
+ * rows = 0 leaves the accumulators as they are, or zeroes them (overwrite). */
+tgp_status tgp_layer_norm_backward_workspace(int64_t rows, int C, int dtype, size_t* bytes);
+tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* dy, int64_t lddy,
+                                   const void* x, int64_t ldx, const float* gain,
+                                   const float* stats, void* dx, int64_t lddx, float* dgain,
+                                   float* dbias, int overwrite, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/* Orthogonalised updates of weight matrices (the Muon rule): for each of n
+ * matrices of rows x cols float32 values (a convolution's cout x (kh kw cin),
+ * dense),
+ *
+ *   M = mu M + G;  U = G + mu M (nesterov) or M;  X = U / (|U|_F + eps)
+ *   `steps` times:  A = X X^T;  X = (a I + b A + c A A) X
+ *   update = X, rounded to bfloat16
+ *
+ * with a, b, c = 3.4445, -4.7750, 2.0315 (X^T in place of X where rows >
+ * cols), which brings the singular values of X near one.  grad and the
+ * momentum M are float32; M is updated in place (momentum NULL: U = G).
+ * update is written densely, rows x cols.  A zero U gives a zero update; an
+ * infinity or NaN anywhere in U makes that matrix's whole update NaN and no
+ * other's.  M, U and |U| are exact to float32 (|U| is summed in float64).
+ * Products are taken on matrix instructions: operands rounded to float16 at
+ * fixed power-of-two scales with their diagonals kept to float32, sums
+ * float32.  A singular direction of U is thus kept where it is more than
+ * about 2^-11 of the largest, as against 2^-8 for bfloat16 products.
+ * steps >= 1; 1 <= rows, cols, and rows x cols (each rounded up to a multiple
+ * of 128) < 2^30 (EUNSUPPORTED beyond).  grad, momentum and update at
+ * multiples of 16 bytes; ws at a multiple of 256, of at least the size that
+ * tgp_muon_workspace returns for the same shapes (ENOSPACE if smaller).
+ * `t` is read on the host before the call returns. */
+typedef struct {
+  int32_t rows, cols;
+  const float* grad;
+  float* momentum;
+  void* update;      /* bfloat16 */
+} tgp_muon_tensor;
+tgp_status tgp_muon_workspace(int n, const tgp_muon_tensor* t, size_t* bytes);
+tgp_status tgp_muon_update(int n, const tgp_muon_tensor* t, float mu, int nesterov, int steps,
+                           float eps, void* ws, size_t ws_bytes, void* stream);
+
+/* The weights' step, for n tensors of count values each (n, count >= 0):
+ *
+ *   w = w (1 - decay) - rate update;   w16 = bfloat16(w)
+ *
+ * w: float32 weights (a TGP_FP32 net's own; a TGP_BF16 net's master copy);
+ * w16: the bfloat16 weights a TGP_BF16 net reads (NULL for none); update:
+ * bfloat16, as tgp_muon_update writes it.  All at multiples of 16 bytes.
+ * `t` is read on the host before the call returns. */
+typedef struct {
+  int64_t count;
+  float* w;
+  void* w16;
+  const void* update;
+  float rate;
+} tgp_step_tensor;
+tgp_status tgp_weight_step(int n, const tgp_step_tensor* t, float decay, void* stream);
+
+/* AdamW, for what has no matrix to orthogonalise (biases, gains, depthwise
+ * weights), for n tensors of count values each:
+ *
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - decay) - rate (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *   w16 = bfloat16(w)
+ *
+ * All float32 but w16 (may be NULL); step counts from 1; 0 <= beta1, beta2 <
+ * 1.  All at multiples of 16 bytes. */
+typedef struct {
+  int64_t count;
+  float* w;
+  void* w16;
+  const float* grad;
+  float* m;
+  float* v;
+} tgp_adamw_tensor;
+tgp_status tgp_adamw_step(int n, const tgp_adamw_tensor* t, float rate, float beta1, float beta2,
+                          float eps, float decay, int64_t step, void* stream);
+
 /* Measurement hooks (outside the method).  While enabled on the calling
  * thread, each kernel launch is bracketed by two HIP events on its stream.
  * tgp_profile_read waits for the recorded events, returns one entry per

@@ -49,8 +49,26 @@ class Layer(ctypes.Structure):
                 ("stash_id", ctypes.c_int32), ("pop_id", ctypes.c_int32)]
 
 
+class MuonTensor(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("grad", ctypes.c_void_p),
+                ("momentum", ctypes.c_void_p), ("update", ctypes.c_void_p)]
+
+
+class StepTensor(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("w", ctypes.c_void_p), ("w16", ctypes.c_void_p),
+                ("update", ctypes.c_void_p), ("rate", ctypes.c_float)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("w", ctypes.c_void_p), ("w16", ctypes.c_void_p),
+                ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_L = ctypes.c_int64
+_F = ctypes.c_float
+_Z = ctypes.c_size_t
 _SIG = {
     "tgp_net_create": [ctypes.POINTER(Layer), _I, _I, _I, _I, _I, ctypes.POINTER(_P)],
     "tgp_layer_flops": [_P, _I, ctypes.POINTER(ctypes.c_int64)],
@@ -76,6 +94,13 @@ _SIG = {
                                        _P],
     "tgp_layer_times_plan": [_P, _I, _I, ctypes.POINTER(ctypes.c_size_t)],
     "tgp_layer_times": [_P, _P, ctypes.c_size_t, _I, ctypes.POINTER(ctypes.c_float), _P],
+    "tgp_layer_norm_forward": [_L, _I, _I, _P, _L, _P, _P, _F, _P, _L, _P, _P],
+    "tgp_layer_norm_backward_workspace": [_L, _I, _I, ctypes.POINTER(_Z)],
+    "tgp_layer_norm_backward": [_L, _I, _I, _P, _L, _P, _L, _P, _P, _P, _L, _P, _P, _I, _P, _Z, _P],
+    "tgp_muon_workspace": [_I, ctypes.POINTER(MuonTensor), ctypes.POINTER(_Z)],
+    "tgp_muon_update": [_I, ctypes.POINTER(MuonTensor), _F, _I, _I, _F, _P, _Z, _P],
+    "tgp_weight_step": [_I, ctypes.POINTER(StepTensor), _F, _P],
+    "tgp_adamw_step": [_I, ctypes.POINTER(AdamwTensor), _F, _F, _F, _F, _F, _L, _P],
     "tgp_balance_by_time": [_P, _P, ctypes.c_size_t, _I, _I, ctypes.POINTER(_I),
                             ctypes.POINTER(ctypes.c_float), _P],
 }
@@ -299,6 +324,80 @@ def schedule_trace(m: int, n: int, ckpt_mode: int) -> List[Tuple[int, int, int]]
     _check(_lib.tgp_schedule_trace(m, n, ckpt_mode, buf, cnt.value, ctypes.byref(cnt)),
            "tgp_schedule_trace")
     return [tuple(buf[3 * k:3 * k + 3]) for k in range(cnt.value)]
+
+
+def layer_norm_forward(rows: int, C: int, dtype: int, x: int, ldx: int, gain: Optional[int],
+                       bias: Optional[int], eps: float, y: int, ldy: int,
+                       stats: Optional[int] = None, stream: int = 0) -> None:
+    """Layer norm over the channels of `rows` pixels; stats (rows x 2 float32) for the backward."""
+    _check(_lib.tgp_layer_norm_forward(rows, C, dtype, _vp(x), ldx, _vp(gain), _vp(bias), eps,
+                                       _vp(y), ldy, _vp(stats), _vp(stream)),
+           "tgp_layer_norm_forward")
+
+
+def layer_norm_backward_workspace(rows: int, C: int, dtype: int) -> int:
+    v = ctypes.c_size_t()
+    _check(_lib.tgp_layer_norm_backward_workspace(rows, C, dtype, ctypes.byref(v)),
+           "tgp_layer_norm_backward_workspace")
+    return v.value
+
+
+def layer_norm_backward(rows: int, C: int, dtype: int, dy: int, lddy: int, x: int, ldx: int,
+                        gain: Optional[int], stats: int, dx: Optional[int], lddx: int,
+                        dgain: Optional[int], dbias: Optional[int], overwrite: bool,
+                        ws: Optional[int], ws_bytes: int, stream: int = 0) -> None:
+    """dx, and the gain's and bias's gradients into (overwrite) or added to dgain and dbias."""
+    _check(_lib.tgp_layer_norm_backward(rows, C, dtype, _vp(dy), lddy, _vp(x), ldx, _vp(gain),
+                                        _vp(stats), _vp(dx), lddx, _vp(dgain), _vp(dbias),
+                                        int(overwrite), _vp(ws), ws_bytes, _vp(stream)),
+           "tgp_layer_norm_backward")
+
+
+def _descriptors(cls, rows):
+    rows = list(rows)
+    return (cls * len(rows))(*[cls(*r) for r in rows])
+
+
+def muon_tensors(tensors: Sequence[Tuple]):
+    """The list that muon_workspace and muon_update take, of (rows, cols, grad, momentum or None,
+    update) for each matrix: device addresses of float32, float32 and bfloat16 values.  A program
+    makes it once and keeps it."""
+    return _descriptors(MuonTensor, tensors)
+
+
+def muon_workspace(tensors) -> int:
+    v = ctypes.c_size_t()
+    _check(_lib.tgp_muon_workspace(len(tensors), tensors, ctypes.byref(v)), "tgp_muon_workspace")
+    return v.value
+
+
+def muon_update(tensors, mu: float, nesterov: bool, steps: int, eps: float, ws: int,
+                ws_bytes: int, stream: int = 0) -> None:
+    """Momentum and the orthogonalised update of every matrix of muon_tensors()."""
+    _check(_lib.tgp_muon_update(len(tensors), tensors, mu, int(nesterov), steps, eps, _vp(ws),
+                                ws_bytes, _vp(stream)), "tgp_muon_update")
+
+
+def step_tensors(tensors: Sequence[Tuple]):
+    """The list that weight_step takes, of (count, w, w16 or None, update, rate) for each tensor."""
+    return _descriptors(StepTensor, tensors)
+
+
+def weight_step(tensors, decay: float, stream: int = 0) -> None:
+    """w = w (1 - decay) - rate update (and its bfloat16 copy), for every tensor of step_tensors()."""
+    _check(_lib.tgp_weight_step(len(tensors), tensors, decay, _vp(stream)), "tgp_weight_step")
+
+
+def adamw_tensors(tensors: Sequence[Tuple]):
+    """The list that adamw_step takes, of (count, w, w16 or None, grad, m, v) for each tensor."""
+    return _descriptors(AdamwTensor, tensors)
+
+
+def adamw_step(tensors, rate: float, beta1: float, beta2: float, eps: float, decay: float,
+               step: int, stream: int = 0) -> None:
+    """AdamW's step number `step` (from 1) for every tensor of adamw_tensors()."""
+    _check(_lib.tgp_adamw_step(len(tensors), tensors, rate, beta1, beta2, eps, decay, step,
+                               _vp(stream)), "tgp_adamw_step")
 
 
 def profile_enable(enable: bool) -> None:

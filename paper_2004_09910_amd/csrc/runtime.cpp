@@ -17,12 +17,15 @@
 #include <string>
 #include <vector>
 
+#include "error.h"
 #include "kernels.h"
 #include "tgp.h"
 
 namespace {
-
 thread_local std::string g_err;
+}
+
+namespace tgpk {
 
 tgp_status fail(tgp_status s, const char* fmt, ...) {
   char buf[512];
@@ -33,6 +36,12 @@ tgp_status fail(tgp_status s, const char* fmt, ...) {
   g_err = buf;
   return s;
 }
+
+}  // namespace tgpk
+
+namespace {
+
+using tgpk::fail;
 
 inline size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -228,13 +237,6 @@ bool ckpt_of(int mode, int i, int m) {
 int cell(const tgp_net* N, int i, int j) { return (i - 1) * N->n + (j - 1); }
 
 hipStream_t S(void* s) { return (hipStream_t)s; }
-
-#define HIPCHK(expr, name)                                                         \
-  do {                                                                             \
-    hipError_t e_ = (expr);                                                        \
-    if (e_ != hipSuccess)                                                          \
-      return fail(TGP_EHIP, "%s: %s", name, hipGetErrorString(e_));                \
-  } while (0)
 
 char* W_(tgp_net* N, size_t off) { return N->ws + off; }
 // Gradient slot buffer at slot-relative offset off, for micro-batch i.
