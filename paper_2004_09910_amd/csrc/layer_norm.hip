@@ -8,6 +8,7 @@
 // Column sums are partial sums of row ranges, left in a workspace and added
 // up in a fixed order by a second launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "prof.h"
@@ -17,7 +18,8 @@ namespace tgpk {
 namespace {
 
 constexpr int kT = 256;          // threads of a block
-constexpr int kColBlocks = 256;  // most row ranges of the column sums
+constexpr int kFwdBlocks = 2048; // most blocks of a forward launch
+constexpr int kColBlocks = 1024; // most row ranges of the column sums
 
 // Sum over the block's kT threads, the same value in every thread: a wave's
 // xor tree, then the waves' sums in order.
@@ -61,6 +63,249 @@ __global__ __launch_bounds__(kT) void norm_fwd_any(const T* __restrict__ x, long
     if (stats && threadIdx.x == 0) stats[r] = make_float2(mean, rstd);
   }
 }
+
+// ------------------------------------------------- rows held in registers
+
+// VB bytes of T as one access, and their values as floats.
+template <typename T, int VB> struct Vec;
+template <> struct Vec<bf16_t, 16> {
+  typedef uint4 raw;
+  static __device__ __forceinline__ void un(raw v, float* f) {
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = bf2f(d[i] & 0xffffu); f[2 * i + 1] = bf2f(d[i] >> 16); }
+  }
+  static __device__ __forceinline__ raw pk(const float* f) {
+    uint32_t d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = f2bf(f[2 * i]) | (f2bf(f[2 * i + 1]) << 16);
+    return make_uint4(d[0], d[1], d[2], d[3]);
+  }
+};
+template <> struct Vec<bf16_t, 4> {
+  typedef uint32_t raw;
+  static __device__ __forceinline__ void un(raw v, float* f) { f[0] = bf2f(v & 0xffffu); f[1] = bf2f(v >> 16); }
+  static __device__ __forceinline__ raw pk(const float* f) { return f2bf(f[0]) | (f2bf(f[1]) << 16); }
+};
+template <> struct Vec<bf16_t, 2> {
+  typedef uint16_t raw;
+  static __device__ __forceinline__ void un(raw v, float* f) { f[0] = bf2f(v); }
+  static __device__ __forceinline__ raw pk(const float* f) { return (uint16_t)f2bf(f[0]); }
+};
+template <> struct Vec<float, 16> {
+  typedef float4 raw;
+  static __device__ __forceinline__ void un(raw v, float* f) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+  static __device__ __forceinline__ raw pk(const float* f) { return make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Vec<float, 4> {
+  typedef float raw;
+  static __device__ __forceinline__ void un(raw v, float* f) { f[0] = v; }
+  static __device__ __forceinline__ raw pk(const float* f) { return f[0]; }
+};
+
+// Sum over the lanes of one row: the G lanes of a group (G a power of two,
+// xor tree), or the whole block.
+template <bool BLK>
+__device__ __forceinline__ float row_sum(float v, int G, float* s4) {
+  if constexpr (BLK) {
+    return block_sum(v, s4);
+  } else {
+    for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+  }
+}
+
+// How the lanes of a block share rows.  A row's nvec vectors of VB bytes lie
+// on G lanes of a wave (64 / G rows side by side), or (BLK) on the block's
+// 256 lanes, NV a lane: vector k of lane l is number l + G k.
+template <typename T, int VB, int NV, bool BLK>
+struct Share {
+  static constexpr int V = VB / (int)sizeof(T);
+  int l, G, nvec;
+  long row0, step;   // first row of this lane, rows from one turn to the next
+  __device__ __forceinline__ Share(int C, int g) : G(BLK ? kT : g), nvec(C / V) {
+    const int per = BLK ? 1 : 64 / G, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    l = BLK ? threadIdx.x : lane & (G - 1);
+    row0 = BLK ? blockIdx.x : ((long)blockIdx.x * 4 + wave) * per + lane / G;
+    step = (long)gridDim.x * (BLK ? 1 : 4 * per);
+  }
+  __device__ __forceinline__ bool has(int k) const { return l + G * k < nvec; }
+  __device__ __forceinline__ int vec(int k) const { return l + G * k; }
+  // the lane's channels of a float32 vector over channels (NULL: `none`)
+  __device__ __forceinline__ void channels(const float* p, float none, float (&f)[NV][V]) const {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) f[k][v] = p && has(k) ? p[(long)vec(k) * V + v] : none;
+  }
+};
+
+// U rows of a lane are in flight at a time.
+template <typename T, int VB, int NV, bool BLK, int U>
+__global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float* __restrict__ gain,
+                                               const float* __restrict__ bias, float eps, T* y,
+                                               long ldy, float2* __restrict__ stats, long rows,
+                                               int C, int G) {
+  typedef Vec<T, VB> VT;
+  typedef Share<T, VB, NV, BLK> SH;
+  constexpr int V = SH::V;
+  __shared__ float s4[4];
+  const SH sh(C, G);
+  float gn[NV][V], bs[NV][V];
+  sh.channels(gain, 1.f, gn);
+  sh.channels(bias, 0.f, bs);
+  // the trip count is the same for every lane of the block (block_sum meets a barrier)
+  for (long base = 0; base + (BLK ? sh.row0 : (long)blockIdx.x * 4 * (64 / sh.G)) < rows; base += U * sh.step) {
+    typename VT::raw raw[U][NV];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long r = sh.row0 + base + u * sh.step;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (r < rows && sh.has(k)) raw[u][k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
+        else raw[u][k] = typename VT::raw{};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long r = sh.row0 + base + u * sh.step;
+      float f[NV][V], s = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        VT::un(raw[u][k], f[k]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) s += f[k][v];
+      }
+      const float mean = row_sum<BLK>(s, sh.G, s4) / C;
+      float q = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          f[k][v] -= mean;
+          if (sh.has(k)) q += f[k][v] * f[k][v];
+        }
+      const float rstd = 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps);
+      if (r < rows) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) f[k][v] = f[k][v] * rstd * gn[k][v] + bs[k][v];
+          if (sh.has(k)) ((typename VT::raw*)(y + r * ldy))[sh.vec(k)] = VT::pk(f[k]);
+        }
+        if (stats && sh.l == 0) stats[r] = make_float2(mean, rstd);
+      }
+    }
+  }
+}
+
+// dx, and this block's column sums in part[block][2][C] (part NULL: none).
+template <typename T, int VB, int NV, bool BLK, int U>
+__global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* x, long ldx,
+                                               const float* __restrict__ gain,
+                                               const float2* __restrict__ stats, T* dx, long lddx,
+                                               float* __restrict__ part, long rows, int C, int G) {
+  typedef Vec<T, VB> VT;
+  typedef Share<T, VB, NV, BLK> SH;
+  constexpr int V = SH::V;
+  __shared__ float s4[4];
+  const SH sh(C, G);
+  float gn[NV][V], a[NV][V], b[NV][V];
+  sh.channels(gain, 1.f, gn);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) a[k][v] = b[k][v] = 0.f;
+  const float inv_c = 1.f / C;
+  for (long base = 0; base + (BLK ? sh.row0 : (long)blockIdx.x * 4 * (64 / sh.G)) < rows; base += U * sh.step) {
+    typename VT::raw rd[U][NV], rx[U][NV];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long r = sh.row0 + base + u * sh.step;
+      st[u] = r < rows ? stats[r] : make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (r < rows && sh.has(k)) {
+          rd[u][k] = ((const typename VT::raw*)(dy + r * lddy))[sh.vec(k)];
+          rx[u][k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
+        } else {
+          rd[u][k] = rx[u][k] = typename VT::raw{};
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long r = sh.row0 + base + u * sh.step;
+      float d[NV][V], xh[NV][V], s = 0.f, p = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        VT::un(rd[u][k], d[k]);
+        VT::un(rx[u][k], xh[k]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          xh[k][v] = (xh[k][v] - st[u].x) * st[u].y;
+          a[k][v] += d[k][v] * xh[k][v];
+          b[k][v] += d[k][v];
+          const float g = d[k][v] * gn[k][v];
+          s += g;
+          p += g * xh[k][v];
+        }
+      }
+      if (!dx) continue;
+      const float ms = row_sum<BLK>(s, sh.G, s4) * inv_c, mp = row_sum<BLK>(p, sh.G, s4) * inv_c;
+      if (r < rows) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          float o[V];
+#pragma unroll
+          for (int v = 0; v < V; ++v) o[v] = st[u].y * (d[k][v] * gn[k][v] - ms - xh[k][v] * mp);
+          if (sh.has(k)) ((typename VT::raw*)(dx + r * lddx))[sh.vec(k)] = VT::pk(o);
+        }
+      }
+    }
+  }
+  if (!part) return;
+  float* out = part + (long)blockIdx.x * 2 * C;
+  if constexpr (BLK) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (sh.has(k))
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          out[(long)sh.vec(k) * V + v] = a[k][v];
+          out[C + (long)sh.vec(k) * V + v] = b[k][v];
+        }
+  } else {
+    // the wave's rows, then the four waves' sums in order
+    __shared__ float ws[3][2 * NV * V][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        for (int o = sh.G; o < 64; o <<= 1) {
+          a[k][v] += __shfl_xor(a[k][v], o);
+          b[k][v] += __shfl_xor(b[k][v], o);
+        }
+        if (wave > 0) {
+          ws[wave - 1][k * V + v][lane] = a[k][v];
+          ws[wave - 1][NV * V + k * V + v][lane] = b[k][v];
+        }
+      }
+    __syncthreads();
+    if (wave == 0 && lane < sh.G)
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (sh.has(k))
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const int e = k * V + v, f = NV * V + e;
+            out[(long)sh.vec(k) * V + v] = ((a[k][v] + ws[0][e][lane]) + ws[1][e][lane]) + ws[2][e][lane];
+            out[C + (long)sh.vec(k) * V + v] = ((b[k][v] + ws[0][f][lane]) + ws[1][f][lane]) + ws[2][f][lane];
+          }
+  }
+}
+
+// ------------------------------------------------- any row
 
 template <typename T>
 __global__ __launch_bounds__(kT) void norm_dx_any(const T* dy, long lddy, const T* x, long ldx,
@@ -141,12 +386,103 @@ __global__ void norm_zero(float* a, float* b, int C) {
   if (c < C) a[c] = b[c] = 0.f;
 }
 
-int row_ranges(const NormShape& s) { return (int)std::min<long>(kColBlocks, std::max<long>(1, s.rows / 32)); }
+// The plan of a register kernel: VB bytes a vector, NV vectors a lane, G lanes
+// a row (0: the whole block); VB = 0 where no register kernel takes the row.
+struct Plan {
+  int vb, nv, g;
+};
+
+// The widest vectors that every row's start and length allow; then the lanes
+// and vectors a lane that leave the fewest lanes idle, more lanes where two
+// leave the same (a row's vectors then lie side by side in one access).  A
+// row of more than 4 x 64 vectors takes a block, of more than 4 x 256 none.
+Plan plan_of(int dt, int C, uintptr_t bits) {
+  const int esz = dt == TGP_BF16 ? 2 : 4;
+  bits |= (uintptr_t)C * esz;
+  const int vb = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+  const int nvec = C * (long)esz / vb > 1 << 20 ? 1 << 20 : (int)(C * (long)esz / vb);
+  if (nvec > 4 * kT) return {0, 0, 0};
+  if (nvec > 4 * 64) return {vb, cdiv(nvec, kT), 0};
+  Plan best{vb, 1, 64};
+  int room = 1 << 30;
+  for (int g = 64; g >= 1; g >>= 1) {
+    const int nv = cdiv(nvec, g);
+    if (nv > 4) break;
+    if (nv * g < room) room = nv * g, best = {vb, nv, g};
+  }
+  return best;
+}
+
+// Calls f(Plan's NV, BLK as constants).
+template <typename F>
+void with_plan(const Plan& p, F f) {
+  auto nv = [&](auto blk) {
+    switch (p.nv) {
+      case 1: f(std::integral_constant<int, 1>(), blk); break;
+      case 2: f(std::integral_constant<int, 2>(), blk); break;
+      case 3: f(std::integral_constant<int, 3>(), blk); break;
+      default: f(std::integral_constant<int, 4>(), blk); break;
+    }
+  };
+  if (p.g == 0) nv(std::true_type());
+  else nv(std::false_type());
+}
+
+long rows_of_block(const Plan& p) { return p.g == 0 ? 1 : 4 * (64 / p.g); }
+
+template <typename T, int VB>
+void forward_regs(const Plan& p, const NormShape& s, const T* x, long ldx, const float* gain,
+                  const float* bias, float eps, T* y, long ldy, float2* stats, hipStream_t st) {
+  const double n = (double)s.rows * s.C;
+  const unsigned grid = (unsigned)std::min<long>(kFwdBlocks, cdiv(s.rows, rows_of_block(p)));
+  with_plan(p, [&](auto nv, auto blk) {
+    constexpr int NV = decltype(nv)::value, U = NV == 1 ? 4 : NV == 2 ? 2 : 1;
+    constexpr bool BLK = decltype(blk)::value;
+    ProfScope ps("layer_norm_fwd", 8 * n, 2 * n * sizeof(T), st);
+    TGP_LAUNCH(ps, (norm_fwd<T, VB, NV, BLK, U>), dim3(grid), dim3(kT), 0, st, x, ldx, gain, bias,
+               eps, y, ldy, stats, s.rows, s.C, p.g);
+  });
+}
+
+template <typename T, int VB>
+void backward_regs(const Plan& p, unsigned grid, const NormShape& s, const T* dy, long lddy,
+                   const T* x, long ldx, const float* gain, const float2* stats, T* dx, long lddx,
+                   float* part, hipStream_t st) {
+  const double n = (double)s.rows * s.C;
+  with_plan(p, [&](auto nv, auto blk) {
+    constexpr int NV = decltype(nv)::value, U = NV == 1 ? 2 : 1;
+    constexpr bool BLK = decltype(blk)::value;
+    ProfScope ps("layer_norm_bwd", 14 * n, (dx ? 3 : 2) * n * sizeof(T), st);
+    TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK, U>), dim3(grid), dim3(kT), 0, st, dy, lddy, x, ldx,
+               gain, stats, dx, lddx, part, s.rows, s.C, p.g);
+  });
+}
+
+// Row ranges (partial column sums) of the backward, at most: enough to fill
+// the chip; beyond that 16 rows each, so that the sums' traffic (16 bytes a
+// channel and range) stays a sixth of the rows' own.
+int row_ranges(const NormShape& s) {
+  return (int)std::min<long>(std::min<long>(kColBlocks, std::max<long>(256, s.rows / 16)), s.rows);
+}
+
+// Element size, and the bits of every address and row distance that the
+// widest vector has to divide.
+template <typename T>
+uintptr_t place(const void* p, long ld) { return (uintptr_t)p | (uintptr_t)ld * sizeof(T); }
 
 template <typename T>
 hipError_t forward_t(const NormShape& s, const void* x, long ldx, const float* gain,
                      const float* bias, float eps, void* y, long ldy, float* stats,
                      hipStream_t st) {
+  const Plan p = plan_of(sizeof(T) == 2 ? TGP_BF16 : TGP_FP32, s.C, place<T>(x, ldx) | place<T>(y, ldy));
+  auto regs = [&](auto vb) {
+    forward_regs<T, decltype(vb)::value>(p, s, (const T*)x, ldx, gain, bias, eps, (T*)y, ldy,
+                                         (float2*)stats, st);
+  };
+  if (p.vb == 16) regs(std::integral_constant<int, 16>());
+  else if (p.vb == 4) regs(std::integral_constant<int, 4>());
+  else if (p.vb == 2) regs(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
+  if (p.vb) return launch_status();
   const double n = (double)s.rows * s.C;
   ProfScope ps("layer_norm_fwd_any", 8 * n, 2 * n * sizeof(T), st);
   TGP_LAUNCH(ps, norm_fwd_any<T>, dim3((unsigned)std::min<long>(s.rows, 2048)), dim3(kT), 0, st,
@@ -154,21 +490,42 @@ hipError_t forward_t(const NormShape& s, const void* x, long ldx, const float* g
   return launch_status();
 }
 
+void sum_columns(int S, int C, const float* part, float* dgain, float* dbias, bool overwrite,
+                 hipStream_t st) {
+  ProfScope ps("layer_norm_cols_sum", 2.0 * S * C, 8.0 * S * C, st);
+  TGP_LAUNCH(ps, norm_cols_sum, dim3(cdiv(2L * C, 16)), dim3(512), 0, st, part, S, C, dgain, dbias,
+             (int)overwrite);
+}
+
 template <typename T>
 hipError_t backward_t(const NormShape& s, const void* dy, long lddy, const void* x, long ldx,
                       const float* gain, const float* stats, void* dx, long lddx, float* dgain,
                       float* dbias, bool overwrite, float* part, hipStream_t st) {
   const double n = (double)s.rows * s.C;
+  const int most = row_ranges(s);
+  const Plan p = plan_of(sizeof(T) == 2 ? TGP_BF16 : TGP_FP32, s.C,
+                         place<T>(dy, lddy) | place<T>(x, ldx) | (dx ? place<T>(dx, lddx) : 0));
+  if (p.vb) {
+    const int S = (int)std::min<long>(most, cdiv(s.rows, rows_of_block(p)));
+    auto regs = [&](auto vb) {
+      backward_regs<T, decltype(vb)::value>(p, (unsigned)S, s, (const T*)dy, lddy, (const T*)x, ldx,
+                                            gain, (const float2*)stats, (T*)dx, lddx,
+                                            dgain ? part : nullptr, st);
+    };
+    if (p.vb == 16) regs(std::integral_constant<int, 16>());
+    else if (p.vb == 4) regs(std::integral_constant<int, 4>());
+    else regs(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
+    if (dgain) sum_columns(S, s.C, part, dgain, dbias, overwrite, st);
+    return launch_status();
+  }
   if (dgain) {   // first: dx may be written over dy or x
-    const int S = row_ranges(s);
+    const int S = (int)std::min<long>(most, std::max<long>(1, s.rows / 32));
     {
       ProfScope ps("layer_norm_cols_any", 5 * n, 2 * n * sizeof(T), st);
       TGP_LAUNCH(ps, norm_cols_any<T>, dim3(cdiv(s.C, 64), S), dim3(kT), 0, st, (const T*)dy, lddy,
                  (const T*)x, ldx, (const float2*)stats, part, s.rows, s.C);
     }
-    ProfScope ps("layer_norm_cols_sum", 2.0 * S * s.C, 8.0 * S * s.C, st);
-    TGP_LAUNCH(ps, norm_cols_sum, dim3(cdiv(2L * s.C, 16)), dim3(512), 0, st, (const float*)part, S,
-               s.C, dgain, dbias, (int)overwrite);
+    sum_columns(S, s.C, part, dgain, dbias, overwrite, st);
   }
   if (dx) {
     ProfScope ps("layer_norm_dx_any", 9 * n, 3 * n * sizeof(T), st);
