@@ -103,14 +103,26 @@ template <> struct Vec<float, 4> {
   static __device__ __forceinline__ raw pk(const float* f) { return f[0]; }
 };
 
+// v of the lane that DPP control CTRL pairs with this one.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
 // Sum over the lanes of one row: the G lanes of a group (G a power of two,
-// xor tree), or the whole block.
+// the same for the whole launch), or the whole block.  Neighbours are added
+// first; once the lanes of a half agree, mirroring reaches the other half.
 template <bool BLK>
 __device__ __forceinline__ float row_sum(float v, int G, float* s4) {
   if constexpr (BLK) {
     return block_sum(v, s4);
   } else {
-    for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if (G >= 2) v += dpp<0xB1>(v);     // lanes 1 0 3 2
+    if (G >= 4) v += dpp<0x4E>(v);     // lanes 2 3 0 1
+    if (G >= 8) v += dpp<0x141>(v);    // mirror of 8
+    if (G >= 16) v += dpp<0x140>(v);   // mirror of 16
+    if (G >= 32) v += __shfl_xor(v, 16);
+    if (G >= 64) v += __shfl_xor(v, 32);
     return v;
   }
 }
@@ -133,10 +145,24 @@ struct Share {
   __device__ __forceinline__ int vec(int k) const { return l + G * k; }
   // the lane's channels of a float32 vector over channels (NULL: `none`)
   __device__ __forceinline__ void channels(const float* p, float none, float (&f)[NV][V]) const {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));   // p is at a multiple of 4 only
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) f[k][v] = p && has(k) ? p[(long)vec(k) * V + v] : none;
+      for (int v = 0; v < V; ++v) f[k][v] = none;
+      if (!p || !has(k)) continue;
+      const float* q = p + (long)vec(k) * V;
+      if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int v = 0; v < V; v += 4) {
+          const f4 t = *(const f4*)(q + v);
+          f[k][v] = t.x; f[k][v + 1] = t.y; f[k][v + 2] = t.z; f[k][v + 3] = t.w;
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) f[k][v] = q[v];
+      }
+    }
   }
 };
 
@@ -360,18 +386,23 @@ __global__ __launch_bounds__(kT) void norm_cols_any(const T* __restrict__ dy, lo
 }
 
 // dgain, dbias (+)= the sum over S ranges of part[s][2][C]: 16 sums a block,
-// 32 threads a sum (ranges s, s + 32, ..), then their xor tree.
-__global__ __launch_bounds__(512) void norm_cols_sum(const float* __restrict__ part, int S, int C,
-                                                     float* dgain, float* dbias, int overwrite) {
-  __shared__ float sh[32][17];
+// 64 threads a sum (ranges s, s + 64, .., eight loads in flight), then a tree.
+__global__ __launch_bounds__(1024) void norm_cols_sum(const float* __restrict__ part, int S, int C,
+                                                      float* dgain, float* dbias, int overwrite) {
+  __shared__ float sh[64][17];
   const int l = threadIdx.x & 15, k = threadIdx.x >> 4;
   const long e = (long)blockIdx.x * 16 + l, E = 2L * C;
   float s = 0.f;
   if (e < E)
-    for (int q = k; q < S; q += 32) s += part[q * E + e];
+    for (int q0 = k; q0 < S; q0 += 8 * 64) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = q0 + 64 * i < S ? part[(q0 + 64 * i) * E + e] : 0.f;
+      s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
   sh[k][l] = s;
   __syncthreads();
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = 32; o > 0; o >>= 1) {
     if (k < o) sh[k][l] += sh[k + o][l];
     __syncthreads();
   }
@@ -428,13 +459,19 @@ void with_plan(const Plan& p, F f) {
   else nv(std::false_type());
 }
 
+// At most `most` blocks, each with as many turns over its rows as the others.
+unsigned even_grid(long rows, long per_block, long most) {
+  const long blocks = (rows + per_block - 1) / per_block, turns = (blocks + most - 1) / most;
+  return (unsigned)((blocks + turns - 1) / turns);
+}
+
 long rows_of_block(const Plan& p) { return p.g == 0 ? 1 : 4 * (64 / p.g); }
 
 template <typename T, int VB>
 void forward_regs(const Plan& p, const NormShape& s, const T* x, long ldx, const float* gain,
                   const float* bias, float eps, T* y, long ldy, float2* stats, hipStream_t st) {
   const double n = (double)s.rows * s.C;
-  const unsigned grid = (unsigned)std::min<long>(kFwdBlocks, cdiv(s.rows, rows_of_block(p)));
+  const unsigned grid = even_grid(s.rows, rows_of_block(p), kFwdBlocks);
   with_plan(p, [&](auto nv, auto blk) {
     constexpr int NV = decltype(nv)::value, U = NV == 1 ? 4 : NV == 2 ? 2 : 1;
     constexpr bool BLK = decltype(blk)::value;
@@ -493,7 +530,7 @@ hipError_t forward_t(const NormShape& s, const void* x, long ldx, const float* g
 void sum_columns(int S, int C, const float* part, float* dgain, float* dbias, bool overwrite,
                  hipStream_t st) {
   ProfScope ps("layer_norm_cols_sum", 2.0 * S * C, 8.0 * S * C, st);
-  TGP_LAUNCH(ps, norm_cols_sum, dim3(cdiv(2L * C, 16)), dim3(512), 0, st, part, S, C, dgain, dbias,
+  TGP_LAUNCH(ps, norm_cols_sum, dim3(cdiv(2L * C, 16)), dim3(1024), 0, st, part, S, C, dgain, dbias,
              (int)overwrite);
 }
 
@@ -506,7 +543,7 @@ hipError_t backward_t(const NormShape& s, const void* dy, long lddy, const void*
   const Plan p = plan_of(sizeof(T) == 2 ? TGP_BF16 : TGP_FP32, s.C,
                          place<T>(dy, lddy) | place<T>(x, ldx) | (dx ? place<T>(dx, lddx) : 0));
   if (p.vb) {
-    const int S = (int)std::min<long>(most, cdiv(s.rows, rows_of_block(p)));
+    const int S = (int)even_grid(s.rows, rows_of_block(p), most);
     auto regs = [&](auto vb) {
       backward_regs<T, decltype(vb)::value>(p, (unsigned)S, s, (const T*)dy, lddy, (const T*)x, ldx,
                                             gain, (const float2*)stats, (T*)dx, lddx,
