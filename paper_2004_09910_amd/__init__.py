@@ -330,8 +330,8 @@ def layer_norm_forward(rows: int, C: int, dtype: int, x: int, ldx: int, gain: Op
                        bias: Optional[int], eps: float, y: int, ldy: int,
                        stats: Optional[int] = None, stream: int = 0) -> None:
     """Layer norm over the channels of `rows` pixels; stats (rows x 2 float32) for the backward."""
-    _check(_lib.tgp_layer_norm_forward(rows, C, dtype, _vp(x), ldx, _vp(gain), _vp(bias), eps,
-                                       _vp(y), ldy, _vp(stats), _vp(stream)),
+    _check(_lib.tgp_layer_norm_forward(rows, C, dtype, x, ldx, gain, bias, eps,
+                                       y, ldy, stats, stream),
            "tgp_layer_norm_forward")
 
 
@@ -347,9 +347,9 @@ def layer_norm_backward(rows: int, C: int, dtype: int, dy: int, lddy: int, x: in
                         dgain: Optional[int], dbias: Optional[int], overwrite: bool,
                         ws: Optional[int], ws_bytes: int, stream: int = 0) -> None:
     """dx, and the gain's and bias's gradients into (overwrite) or added to dgain and dbias."""
-    _check(_lib.tgp_layer_norm_backward(rows, C, dtype, _vp(dy), lddy, _vp(x), ldx, _vp(gain),
-                                        _vp(stats), _vp(dx), lddx, _vp(dgain), _vp(dbias),
-                                        int(overwrite), _vp(ws), ws_bytes, _vp(stream)),
+    _check(_lib.tgp_layer_norm_backward(rows, C, dtype, dy, lddy, x, ldx, gain,
+                                        stats, dx, lddx, dgain, dbias,
+                                        int(overwrite), ws, ws_bytes, stream),
            "tgp_layer_norm_backward")
 
 
@@ -374,8 +374,8 @@ def muon_workspace(tensors) -> int:
 def muon_update(tensors, mu: float, nesterov: bool, steps: int, eps: float, ws: int,
                 ws_bytes: int, stream: int = 0) -> None:
     """Momentum and the orthogonalised update of every matrix of muon_tensors()."""
-    _check(_lib.tgp_muon_update(len(tensors), tensors, mu, int(nesterov), steps, eps, _vp(ws),
-                                ws_bytes, _vp(stream)), "tgp_muon_update")
+    _check(_lib.tgp_muon_update(len(tensors), tensors, mu, int(nesterov), steps, eps, ws,
+                                ws_bytes, stream), "tgp_muon_update")
 
 
 def step_tensors(tensors: Sequence[Tuple]):
@@ -385,7 +385,7 @@ def step_tensors(tensors: Sequence[Tuple]):
 
 def weight_step(tensors, decay: float, stream: int = 0) -> None:
     """w = w (1 - decay) - rate update (and its bfloat16 copy), for every tensor of step_tensors()."""
-    _check(_lib.tgp_weight_step(len(tensors), tensors, decay, _vp(stream)), "tgp_weight_step")
+    _check(_lib.tgp_weight_step(len(tensors), tensors, decay, stream), "tgp_weight_step")
 
 
 def adamw_tensors(tensors: Sequence[Tuple]):
@@ -397,7 +397,7 @@ def adamw_step(tensors, rate: float, beta1: float, beta2: float, eps: float, dec
                step: int, stream: int = 0) -> None:
     """AdamW's step number `step` (from 1) for every tensor of adamw_tensors()."""
     _check(_lib.tgp_adamw_step(len(tensors), tensors, rate, beta1, beta2, eps, decay, step,
-                               _vp(stream)), "tgp_adamw_step")
+                               stream), "tgp_adamw_step")
 
 
 def profile_enable(enable: bool) -> None:
