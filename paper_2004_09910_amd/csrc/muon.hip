@@ -3,7 +3,10 @@
 //
 // With m the shorter and n the longer side of a matrix, X is held m x n (a
 // matrix of more rows than columns transposed), in float16 at a fixed scale,
-// padded with zeros to multiples of 128.  One step is
+// padded with zeros to multiples of 128.  All matrices lie in panels of 32
+// columns, a panel's rows (64 bytes) one after the other: what a product's
+// stage takes of an operand, 32 sum values of some rows or 32 sum rows of
+// some panels, is then contiguous in pieces of 1 KiB and more.  One step is
 //
 //   A = X X^T          P = a I + b A + c A A          X' = P X
 //
@@ -34,7 +37,6 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kSX = 2048.f, kSM = 1024.f;
 
 constexpr int kNormBlocks = 1024;  // most partial sums of |U|^2 of a matrix
-constexpr int kNormPer = 4;         // pieces of 4096 values a block of the normalisation takes
 constexpr int kMaxMats = 20;       // matrices of one launch
 
 struct Mat {
@@ -45,7 +47,8 @@ struct Mat {
   f16 *x[2], *a, *p;   // X (mp x np, ping-pong), A and P (mp x mp)
   float *da, *dp;      // diagonals' rounding errors
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
-  int rows, cols, m, n, mp, np, norm_blocks, split;
+  int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;
+  int bm;              // rows of a tile of X X^T and P X
 };
 
 struct Mats {
@@ -53,6 +56,9 @@ struct Mats {
   Mat t[kMaxMats];
   int blk0[kMaxMats + 1];   // first block of each matrix in the launch
 };
+
+// Place of row i, column j of a matrix of mp rows.
+__device__ __forceinline__ long at(int mp, int i, int j) { return ((long)(j >> 5) * mp + i) * 32 + (j & 31); }
 
 __device__ __forceinline__ int find(const Mats& l, int blk) {
   int k = 0;
@@ -124,9 +130,9 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, float mu, int neste
   if (threadIdx.x == 0) t.norm[b] = s;
 }
 
-// X = U / (|U| + eps) as float16, kNormPer pieces of 4096 values a block, zeros
+// X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
 // in the padding: a piece is 64 rows x 64 columns through LDS where the matrix
-// is transposed, else 512 consecutive chunks of eight.
+// is transposed, else 32 rows x 128 columns.
 __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nesterov, float eps) {
   __shared__ double sh[4];
   __shared__ float tile[64][65];
@@ -143,10 +149,10 @@ __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nest
     f16x8 h;
 #pragma unroll
     for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(f[v] * inv);
-    *(f16x8*)(t.x[0] + (long)i * t.np + j) = h;
+    *(f16x8*)(t.x[0] + at(t.mp, i, j)) = h;
   };
-  const int b0 = (blockIdx.x - l.blk0[k]) * kNormPer;
-  for (int b = b0; b < b0 + kNormPer; ++b) {
+  const int b0 = (blockIdx.x - l.blk0[k]) * t.norm_per;
+  for (int b = b0; b < b0 + t.norm_per; ++b) {
     if (flip) {
       const int nt = t.np / 64, i0 = b / nt * 64, j0 = b % nt * 64;
       float u[16];
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nest
       __syncthreads();
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        const int i = (z * 256 + threadIdx.x) / 8, j = threadIdx.x % 8 * 8;
+        const int i = threadIdx.x / 4, j = 32 * z + threadIdx.x % 4 * 8;
         float f[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) f[v] = tile[j + v][i];
@@ -169,16 +175,17 @@ __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nest
       }
       continue;
     }
+    const int nt = t.np / 128, i0 = b / nt * 32, j0 = b % nt * 128;
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const int e = (b * 512 + z * 256 + threadIdx.x) * 8, i = e / t.np, j = e - i * t.np;
-      const long at = (long)i * t.cols + j;
+      const int i = i0 + 16 * z + threadIdx.x / 16, j = j0 + threadIdx.x % 16 * 8;
+      const long src = (long)i * t.cols + j;
       float u[8];
       if (i < t.rows && j + 8 <= t.cols && t.cols % 4 == 0) {
-        const float4 g0 = *(const float4*)(t.grad + at), g1 = *(const float4*)(t.grad + at + 4);
+        const float4 g0 = *(const float4*)(t.grad + src), g1 = *(const float4*)(t.grad + src + 4);
         const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
         if (t.mom) {
-          const float4 m0 = *(const float4*)(t.mom + at), m1 = *(const float4*)(t.mom + at + 4);
+          const float4 m0 = *(const float4*)(t.mom + src), m1 = *(const float4*)(t.mom + src + 4);
           const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
 #pragma unroll
           for (int v = 0; v < 8; ++v) u[v] = nesterov ? g[v] + mu * m[v] : m[v];
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nest
       } else {
 #pragma unroll
         for (int v = 0; v < 8; ++v)
-          u[v] = i < t.rows && j + v < t.cols ? update_of(t, at + v, mu, nesterov) : 0.f;
+          u[v] = i < t.rows && j + v < t.cols ? update_of(t, src + v, mu, nesterov) : 0.f;
       }
       put(i, j, u);
     }
@@ -204,57 +211,56 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // The tile product of a block: WM x WN waves, each MT x NT fragments of 32 x
-// 32, over stages of 64 sum values in a ring of NS LDS slots.  L is a panel
-// of BM rows, R of BN rows, both contiguous in the sum (128-byte LDS rows,
-// 16-byte chunks XOR-swizzled); with TR, R's panel is 64 sum rows of BN
-// columns and its fragments are gathered by transpose loads.  With SWAP the
-// accumulators hold the transposed tile: a lane has column (row with SWAP)
-// l % 32 of a fragment and rows (columns) 8 (v / 4) + 4 (l / 32) + v % 4.
+// 32, over stages of 32 sum values in a ring of NS LDS slots.  L is BM rows
+// from row i0 on, contiguous in the sum, R BN rows from j0 on likewise; with
+// TR, R is the 32 sum rows of BN columns from j0 on, and its fragments are
+// gathered by transpose loads.  A slot holds 64-byte rows, whose 16-byte
+// chunks are XOR-swizzled.  With SWAP the accumulators hold the transposed
+// tile: a lane has column (row with SWAP) l % 32 of a fragment and rows
+// (columns) 8 (v / 4) + 4 (l / 32) + v % 4.
+//
+// A stage is visible to all waves one turn before it is multiplied, so that
+// fragments are always read one step ahead of their products, over the
+// stages' barriers too.
 template <int MT, int NT, int WM, int WN, int NS, bool TR, bool SWAP>
 struct Tile {
   static constexpr int NW = WM * WN, BM = 32 * MT * WM, BN = 32 * NT * WN;
-  static constexpr int LCH = BM / 8, RCH = BN / 8, CH = LCH + RCH;   // 1 KiB DMA chunks of a stage
-  static constexpr int SB = CH * 1024, PER = CH / NW;
-  static constexpr int RROW = 2 * BN, RPI = 1024 / RROW;             // (TR) bytes of a sum row, rows of a chunk
+  static constexpr int LCH = BM / 16, RCH = BN / 16;   // 1 KiB DMA chunks of a stage: 16 rows
+  static constexpr int CH = LCH + RCH, SB = CH * 1024, PER = CH / NW;
   static_assert(LCH % NW == 0 && RCH % NW == 0 && NS * SB <= 160 * 1024, "whole DMA rounds, LDS ring");
+  static_assert(NS >= 3, "a stage ahead");
 
   f32x16 acc[MT][NT];
 
-  __device__ __forceinline__ static int rswz(int row) { return 2 * (row & 3); }
+  // Chunk q's slot in row `row`: eight consecutive rows read at one chunk, and
+  // (TR) half rows of four consecutive rows, hit distinct banks.
+  __device__ __forceinline__ static int kswz(int row, int q) { return q ^ ((row >> 1) & 3); }
+  __device__ __forceinline__ static int rswz(int row, int q) { return q ^ (row & 2); }
 
-  // L: first row of the panel (ldl values a row); R: likewise, or (TR) row 0
-  // at the panel's first column (ldr values a row); stages k0 .. k1 of the sum.
-  __device__ __forceinline__ void run(unsigned char* ring, const f16* L, int ldl, const f16* R, int ldr,
-                                      int k0, int k1) {
+  // L and R: matrices of lrows and rrows rows; stages k0 .. k1 of the sum.
+  __device__ __forceinline__ void run(unsigned char* ring, const f16* L, int lrows, int i0, const f16* R,
+                                      int rrows, int j0, int k0, int k1) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const u32x4 rl = make_rsrc(L, 0x7fffffff), rr = make_rsrc(R, 0x7fffffff);
-    int lo[LCH / NW], ro[RCH / NW];
-#pragma unroll
-    for (int u = 0; u < LCH / NW; ++u) {
-      const int row = (NW * u + wave) * 8 + (lane >> 3);
-      lo[u] = (row * ldl + 8 * swz(row, lane & 7)) * 2;
-    }
-#pragma unroll
-    for (int u = 0; u < RCH / NW; ++u) {
-      const int c = NW * u + wave;
-      if constexpr (TR) {
-        const int row = c * RPI + lane / (64 / RPI);
-        ro[u] = (row * ldr + 8 * ((lane % (64 / RPI)) ^ rswz(row))) * 2;
-      } else {
-        const int row = c * 8 + (lane >> 3);
-        ro[u] = (row * ldr + 8 * swz(row, lane & 7)) * 2;
-      }
-    }
+    const u32x4 rl = make_rsrc(L + (long)i0 * 32, 0x7fffffff);
+    const u32x4 rr = make_rsrc(TR ? R + (long)j0 * rrows : R + (long)j0 * 32, 0x7fffffff);
+    // this lane's byte offset in chunk `wave` and the distance to its next
+    // ones; rows of chunks NW apart agree in their swizzle (NW is even)
+    const int r16 = wave * 16 + (lane >> 2);
+    const int lo = r16 * 64 + 16 * kswz(r16, lane & 3);
+    const int rrow = (wave & 1) * 16 + (lane >> 2);
+    const int ro = TR ? (wave >> 1) * rrows * 64 + rrow * 64 + 16 * rswz(rrow, lane & 3)
+                      : r16 * 64 + 16 * kswz(r16, lane & 3);
+    static_assert(NW % 2 == 0, "pairs of chunks");
     auto issue = [&](int k, int slot) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < LCH / NW; ++u)
-        dma16(rl, TGP_LDS(ring + slot * SB + (NW * u + wave) * 1024), lo[u], k * 128);
+        dma16(rl, TGP_LDS(ring + slot * SB + (NW * u + wave) * 1024), lo, k * lrows * 64 + u * NW * 1024);
 #pragma unroll
       for (int u = 0; u < RCH / NW; ++u)
-        dma16(rr, TGP_LDS(ring + slot * SB + (LCH + NW * u + wave) * 1024), ro[u],
-              TR ? k * 128 * ldr : k * 128);
+        dma16(rr, TGP_LDS(ring + slot * SB + (LCH + NW * u + wave) * 1024), ro,
+              TR ? k * 2048 + u * (NW / 2) * rrows * 64 : k * rrows * 64 + u * NW * 1024);
     };
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -264,43 +270,42 @@ struct Tile {
 #pragma unroll
     for (int k = 0; k < NS - 1; ++k)
       if (k < total) issue(k0 + k, k);
+    u32x4 a[2][MT], b[2][NT];
+    const int fr = lane & 31;                              // row of a fragment
     const int kb = 8 * (lane >> 5) + ((lane & 15) >> 2);   // (TR) row of the transpose load
+    const int cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);   // (TR) its chunk
+    auto load = [&](int slot, int kk, int buf) __attribute__((always_inline)) {
+      const unsigned char* Ls = ring + slot * SB;
+      const unsigned char* Rs = Ls + LCH * 1024;
+      const int q = kswz(fr, 2 * kk + (lane >> 5)) * 16;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[buf][i] = *(const u32x4*)(Ls + ((wm * MT + i) * 32 + fr) * 64 + q);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if constexpr (TR)
+          b[buf][j] = frag_tr(Rs + (wn * NT + j) * 2048 + (16 * kk + kb) * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1), 64);
+        else
+          b[buf][j] = *(const u32x4*)(Rs + ((wn * NT + j) * 32 + fr) * 64 + q);
+      }
+    };
+    wait_stages<NS, PER>(min(NS - 2, total - 1));
+    ring_barrier();
+    if (total > 0) load(0, 0, 0);
     for (int idx = 0; idx < total; ++idx) {
-      wait_stages<NS, PER>(min(NS - 2, total - 1 - idx));
+      // stage idx + 1 has landed, for every wave; slot idx - 1 has been read
+      wait_stages<NS - 1, PER>(min(NS - 3, total - 2 - idx));
       ring_barrier();
       if (idx + NS - 1 < total) issue(k0 + idx + NS - 1, (idx + NS - 1) % NS);
-      const unsigned char* Ls = ring + (idx % NS) * SB;
-      const unsigned char* Rs = Ls + LCH * 1024;
-      u32x4 a[2][MT], b[2][NT];
-      auto load = [&](int kk, int buf) __attribute__((always_inline)) {
-        const int q = 2 * kk + (lane >> 5);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const int row = (wm * MT + i) * 32 + (lane & 31);
-          a[buf][i] = *(const u32x4*)(Ls + row * 128 + swz(row, q) * 16);
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          if constexpr (TR) {
-            const int cb = ((wn * NT + j) * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-            b[buf][j] = frag_tr(Rs + (16 * kk + kb) * RROW + (((cb >> 4) ^ rswz(kb)) << 4) + (cb & 15), RROW);
-          } else {
-            const int row = (wn * NT + j) * 32 + (lane & 31);
-            b[buf][j] = *(const u32x4*)(Rs + row * 128 + swz(row, q) * 16);
-          }
-        }
-      };
-      load(0, 0);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if (kk + 1 < 4) load(kk + 1, (kk + 1) & 1);
+      for (int kk = 0; kk < 2; ++kk) {
+        if (kk == 0) load(idx % NS, 1, 1);
+        else if (idx + 1 < total) load((idx + 1) % NS, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            acc[i][j] = SWAP ? mfma(b[kk & 1][j], a[kk & 1][i], acc[i][j])
-                             : mfma(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
+            acc[i][j] = SWAP ? mfma(b[kk][j], a[kk][i], acc[i][j]) : mfma(a[kk][i], b[kk][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -332,9 +337,10 @@ __device__ __forceinline__ f32x4_t from_f16(const f16* p) {
   return __builtin_convertvector(*(const f16x4*)p, f32x4_t);
 }
 
-// Stores one 32 x 32 fragment of a symmetric matrix at rows i0, columns j0,
-// and its mirror image where the tile is off the diagonal.  value(g, i, j) is
-// what elements 4 g .. 4 g + 3 (rows i .. i + 3, column j) become.
+// Stores one 32 x 32 fragment of a symmetric matrix of mp rows at rows i0,
+// columns j0, and its mirror image where the tile does not hold it already.
+// value(g, i, j) is what elements 4 g .. 4 g + 3 (rows i .. i + 3, column j)
+// become.
 template <typename F>
 __device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int j0, bool mirror, F value) {
   const int lane = threadIdx.x & 63, j = j0 + (lane & 31);
@@ -347,27 +353,29 @@ __device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int 
     for (int z = 0; z < 4; ++z) {
       const f16 h = (f16)(f[z] * kSM);
       if (i + z == j) d[j] = f[z] - (float)h * (1.f / kSM);
-      if (mirror) m[(long)(i + z) * mp + j] = h;
+      if (mirror) m[at(mp, i + z, j)] = h;
     }
     pk[2 * g] = pack_f16(f[0] * kSM, f[1] * kSM);
     pk[2 * g + 1] = pack_f16(f[2] * kSM, f[3] * kSM);
   }
-  put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + (long)j * mp + i0 + 16 * h + 8 * (lane >> 5)) = c; });
+  put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * (lane >> 5))) = c; });
 }
 
 __device__ __forceinline__ f32x4_t part_of(const f32x16& a, int g) {
   return f32x4_t{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
 }
 
-// Row and column of tile b of the upper triangle (row <= column), row by row
-// of an nt x nt grid.
-__device__ __forceinline__ void upper(int b, int nt, int& r, int& c) {
+// Row and column of tile b of the upper triangle, row by row of a grid of nr
+// x nc tiles, nc / nr of which make a square: row r has the columns from
+// r nc / nr on.
+__device__ __forceinline__ void upper(int b, int nr, int nc, int& r, int& c) {
+  const int w = nc / nr;
   r = 0;
-  while (b >= nt - r) {
-    b -= nt - r;
+  while (b >= nc - r * w) {
+    b -= nc - r * w;
     ++r;
   }
-  c = r + b;
+  c = r * w + b;
 }
 
 enum { GRAM, POLY };
@@ -375,42 +383,43 @@ enum { GRAM, POLY };
 // Symmetric products, upper tiles only: A = X X^T (GRAM) or P = a I + b A + c
 // A A (POLY).  Where GRAM's sum is split, its ranges' partial tiles go to
 // t.part as the accumulators lie, [range][tile][wave][fragment][g][lane].
-template <int MODE, int MT, int WM, int NS>
-__global__ __launch_bounds__(64 * WM * WM) void muon_sym(Mats l, int from) {
-  typedef Tile<MT, MT, WM, WM, NS, false, false> TL;
+template <int MODE, int MT, int NT, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(Mats l, int from) {
+  typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
   const int k = find(l, blk);
   const Mat& t = l.t[k];
-  const int nt = t.mp / TL::BM, tiles = nt * (nt + 1) / 2;
+  const int nr = t.mp / TL::BM, nc = t.mp / TL::BN, w = nc / nr, tiles = nr * nc - w * (nr * (nr - 1) / 2);
   const int b = blk - l.blk0[k], sp = MODE == GRAM ? b / tiles : 0, tile = b - sp * tiles;
   int ti, tj;
-  upper(tile, nt, ti, tj);
-  const int i0 = ti * TL::BM, j0 = tj * TL::BM, K = MODE == GRAM ? t.np : t.mp, nk = K / 64;
+  upper(tile, nr, nc, ti, tj);
+  const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
   const int k0 = MODE == GRAM ? (int)((long)nk * sp / t.split) : 0;
   const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
   const f16* src = MODE == GRAM ? t.x[from] : t.a;
+  const bool mirror = tj >= (ti + 1) * w;
   TL tl;
-  tl.run(ring, src + (long)i0 * K, K, src + (long)j0 * K, K, k0, k1);
-  const int wave = threadIdx.x >> 6, wi = i0 + wave / WM * MT * 32, wj = j0 + wave % WM * MT * 32;
+  tl.run(ring, src, t.mp, i0, src, t.mp, j0, k0, k1);
+  const int wave = threadIdx.x >> 6, wi = i0 + wave / WN * MT * 32, wj = j0 + wave % WN * NT * 32;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
+    for (int j = 0; j < NT; ++j) {
       const f32x16& acc = tl.acc[i][j];
       if constexpr (MODE == GRAM) {
         if (t.split > 1) {
           f32x4_t* out = (f32x4_t*)t.part +
-                         ((((long)b * WM * WM + wave) * MT + i) * MT + j) * 256 + (threadIdx.x & 63);
+                         ((((long)b * WM * WN + wave) * MT + i) * NT + j) * 256 + (threadIdx.x & 63);
 #pragma unroll
           for (int g = 0; g < 4; ++g) out[64 * g] = part_of(acc, g);
         } else {
-          store_sym(t.a, t.da, t.mp, wi + 32 * i, wj + 32 * j, ti != tj,
+          store_sym(t.a, t.da, t.mp, wi + 32 * i, wj + 32 * j, mirror,
                     [&](int g, int, int) { return part_of(acc, g) * (1.f / (kSX * kSX)); });
         }
       } else {
-        store_sym(t.p, t.dp, t.mp, wi + 32 * i, wj + 32 * j, ti != tj, [&](int g, int r, int c) {
-          const f32x4_t a = from_f16(t.a + (long)c * t.mp + r) * (1.f / kSM);   // A is symmetric
+        store_sym(t.p, t.dp, t.mp, wi + 32 * i, wj + 32 * j, mirror, [&](int g, int r, int c) {
+          const f32x4_t a = from_f16(t.a + at(t.mp, c, r)) * (1.f / kSM);   // A is symmetric
           const f32x4_t dr = *(const f32x4_t*)(t.da + r);
           const float dc = t.da[c];
           f32x4_t p = kC * (part_of(acc, g) * (1.f / (kSM * kSM)) + a * (dr + dc)) + kB * a;
@@ -424,30 +433,30 @@ __global__ __launch_bounds__(64 * WM * WM) void muon_sym(Mats l, int from) {
 }
 
 // A from the ranges' partial tiles, added in order: a wave takes one fragment.
-template <int MT, int WM>
+template <int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(256) void muon_gram_sum(Mats l) {
   const int k = find(l, blockIdx.x);
   const Mat& t = l.t[k];
-  constexpr int BM = 32 * MT * WM, FR = WM * WM * MT * MT;
-  const int nt = t.mp / BM, tiles = nt * (nt + 1) / 2;
+  constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, FR = WM * WN * MT * NT;
+  const int nr = t.mp / BM, nc = t.mp / BN, w = nc / nr, tiles = nr * nc - w * (nr * (nr - 1) / 2);
   const int f = (blockIdx.x - l.blk0[k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
-  const int lane = threadIdx.x & 63, wave = q / (MT * MT), i = q / MT % MT, j = q % MT;
+  const int lane = threadIdx.x & 63, wave = q / (MT * NT), i = q / NT % MT, j = q % NT;
   int ti, tj;
-  upper(tile, nt, ti, tj);
+  upper(tile, nr, nc, ti, tj);
   const f32x4_t* in = (const f32x4_t*)t.part + ((long)tile * FR + q) * 256 + lane;
   const long step = (long)tiles * FR * 256;
   f32x4_t acc[4] = {};
   for (int s = 0; s < t.split; ++s)
 #pragma unroll
     for (int g = 0; g < 4; ++g) acc[g] += in[s * step + 64 * g];
-  store_sym(t.a, t.da, t.mp, ti * BM + (wave / WM * MT + i) * 32, tj * BM + (wave % WM * MT + j) * 32,
-            ti != tj, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
+  store_sym(t.a, t.da, t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BN + (wave % WN * NT + j) * 32,
+            tj >= (ti + 1) * w, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 
 // X' = P X, or (last) the update itself.
-template <int MT, int WM, int NS>
-__global__ __launch_bounds__(64 * WM * WM) void muon_apply(Mats l, int from, int last) {
-  typedef Tile<MT, MT, WM, WM, NS, true, true> TL;
+template <int MT, int NT, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int from, int last) {
+  typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
   const int k = find(l, blk);
@@ -456,31 +465,30 @@ __global__ __launch_bounds__(64 * WM * WM) void muon_apply(Mats l, int from, int
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
   const f16* x = t.x[from];
   TL tl;
-  tl.run(ring, t.p + (long)i0 * t.mp, t.mp, x + j0, t.np, 0, t.mp / 64);
+  tl.run(ring, t.p, t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool flip = t.rows > t.cols, whole = !flip && t.cols % 8 == 0;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int r = i0 + (wave / WM * MT + i) * 32 + (lane & 31);
+    const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31);
     const float d = t.dp[r] * (1.f / kSX);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      const int c0 = j0 + (wave % WM * MT + j) * 32;
+    for (int j = 0; j < NT; ++j) {
+      const int c0 = j0 + (wave % WN * NT + j) * 32;
       const f32x16& acc = tl.acc[i][j];
       unsigned pk[8];
       float y[16];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int c = c0 + 8 * g + 4 * (lane >> 5);
-        const f32x4_t xv = from_f16(x + (long)r * t.np + c);
+        const f32x4_t xv = from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5)));
 #pragma unroll
         for (int z = 0; z < 4; ++z) y[4 * g + z] = acc[4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
       }
       if (!last) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
-        f16* out = t.x[from ^ 1] + (long)r * t.np + c0;
-        put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + 16 * h + 8 * (lane >> 5)) = c; });
+        f16* out = t.x[from ^ 1];
+        put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
       } else if (whole) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = f2bf(y[2 * g]) | (f2bf(y[2 * g + 1]) << 16);
@@ -500,23 +508,33 @@ __global__ __launch_bounds__(64 * WM * WM) void muon_apply(Mats l, int from, int
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
-constexpr int kTile = 128;         // X, A and P are padded to multiples of it
-int up(int x) { return (x + kTile - 1) / kTile * kTile; }
-constexpr int kGramBlocks = 512;
-int uppers(int nt) { return nt * (nt + 1) / 2; }
+// The two tiles of X X^T and P X: 128 x 128 and 256 x 128 values of the result
+// on four waves.  The larger one takes a quarter less from the caches and
+// from LDS for each product; matrices whose padded side is no multiple of 256
+// take the smaller one, and so does a list that the larger one would deal out
+// to less than two blocks a CU.
+constexpr int kPad = 128;
+constexpr int kBlocks = 512;   // two a CU
+int up(int x) { return (x + kPad - 1) / kPad * kPad; }
+// Upper tiles of BM = bm, BN = 128 of an mp x mp matrix.
+int uppers(int mp, int bm) {
+  const int nr = mp / bm, nc = mp / 128, w = nc / nr;
+  return nr * nc - w * (nr * (nr - 1) / 2);
+}
+int tiles_apply(const Mat& t, int bm) { return (t.mp / bm) * (t.np / 128); }
 
-// Describes n (at most kMaxMats) matrices laid out from byte `at` of the
+// Describes n (at most kMaxMats) matrices laid out from byte `pos` of the
 // workspace ws on; returns their end.  The sums of A = X X^T are split where
 // the launch has too few tiles to fill the chip: into ranges of about one
-// length over all matrices, for kGramBlocks blocks, of 512 values at least.
-size_t lay_out(int n, const tgp_muon_tensor* d, char* ws, size_t at, Mats& l) {
+// length over all matrices, for kBlocks blocks, of 512 values at least.
+size_t lay_out(int n, const tgp_muon_tensor* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
-    char* p = ws + at;
-    at += al256(bytes);
+    char* p = ws + pos;
+    pos += al256(bytes);
     return p;
   };
   l.count = n;
-  long work = 0;
+  long large = 0, work = 0;
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
     t.grad = d[k].grad;
@@ -528,24 +546,31 @@ size_t lay_out(int n, const tgp_muon_tensor* d, char* ws, size_t at, Mats& l) {
     t.n = std::max(t.rows, t.cols);
     t.mp = up(t.m);
     t.np = up(t.n);
-    t.norm_blocks = (int)std::min<long>(kNormBlocks, cdiv((long)t.rows * t.cols, 4096));
+    const long size = (long)t.rows * t.cols;
+    t.norm_blocks = (int)std::min<long>(kNormBlocks, cdiv(size, 4096));
+    t.norm_per = size >= 1 << 22 ? 4 : 1;   // where it is large, |U| is summed up by fewer blocks
     t.norm = (double*)take(kNormBlocks * sizeof(double));
     for (int z = 0; z < 2; ++z) t.x[z] = (f16*)take((size_t)t.mp * t.np * 2);
     t.a = (f16*)take((size_t)t.mp * t.mp * 2);
     t.p = (f16*)take((size_t)t.mp * t.mp * 2);
     t.da = (float*)take((size_t)t.mp * 4);
     t.dp = (float*)take((size_t)t.mp * 4);
-    work += (long)uppers(t.mp / kTile) * (t.np / 64);
+    if (t.mp % 256 == 0) large += tiles_apply(t, 256);
   }
-  const long range = std::max<long>(8, (work + kGramBlocks - 1) / kGramBlocks);
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
-    t.split = (int)((t.np / 64 + range - 1) / range);
+    t.bm = t.mp % 256 == 0 && large >= kBlocks ? 256 : 128;
+    work += (long)uppers(t.mp, t.bm) * (t.bm / 128) * (t.np / 32);
+  }
+  const long range = std::max<long>(16, (work + kBlocks - 1) / kBlocks);
+  for (int k = 0; k < n; ++k) {
+    Mat& t = l.t[k];
+    t.split = (int)((t.np / 32 * (t.bm / 128) + range - 1) / range);
     t.part = nullptr;
     if (t.split > 1)
-      t.part = (float*)take((size_t)t.split * uppers(t.mp / kTile) * kTile * kTile * sizeof(float));
+      t.part = (float*)take((size_t)t.split * uppers(t.mp, t.bm) * t.bm * 128 * sizeof(float));
   }
-  return at;
+  return pos;
 }
 
 // Fills blk0 with blocks(t) of each matrix; returns the grid.
@@ -575,32 +600,50 @@ hipError_t update_list(Mats& l, float mu, bool nesterov, int steps, float eps, h
     TGP_LAUNCH(ps, muon_momentum, dim3(g), dim3(256), 0, st, l, mu, (int)nesterov);
   }
   {
-    const unsigned g = deal(l, [](const Mat& t) { return (t.mp / 64) * (t.np / 64) / kNormPer; });
+    const unsigned g = deal(l, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
     TGP_LAUNCH(ps, muon_normalize, dim3(g), dim3(256), 0, st, l, mu, (int)nesterov, eps);
   }
-  Mats lp = l, lsum = l, la = l;   // the same matrices, blocks dealt for each product
-  const unsigned gg = deal(l, [](const Mat& t) { return uppers(t.mp / kTile) * t.split; });
-  const unsigned gsum = deal(lsum, [](const Mat& t) {
-    return t.split > 1 ? uppers(t.mp / kTile) * (kTile / 32) * (kTile / 32) / 4 : 0;
-  });
-  const unsigned gp = deal(lp, [](const Mat& t) { return uppers(t.mp / 64); });
-  const unsigned ga = deal(la, [](const Mat& t) { return (t.mp / kTile) * (t.np / kTile); });
+  // the same matrices, blocks dealt for each product and tile
+  Mats lp = l, lg[2] = {l, l}, ls[2] = {l, l}, la[2] = {l, l};
+  unsigned gg[2], gs[2], ga[2];
+  for (int z = 0; z < 2; ++z) {
+    const int bm = z ? 256 : 128;
+    gg[z] = deal(lg[z], [&](const Mat& t) { return t.bm == bm ? uppers(t.mp, bm) * t.split : 0; });
+    gs[z] = deal(ls[z], [&](const Mat& t) { return t.bm == bm && t.split > 1 ? uppers(t.mp, bm) * bm / 32 : 0; });
+    ga[z] = deal(la[z], [&](const Mat& t) { return t.bm == bm ? tiles_apply(t, bm) : 0; });
+  }
+  const unsigned gp = deal(lp, [](const Mat& t) { const int nt = t.mp / 64; return nt * (nt + 1) / 2; });
   for (int s = 0; s < steps; ++s) {
-    {
-      ProfScope ps("muon_gram", gram / 2, 2 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2>), dim3(gg), dim3(256), 0, st, l, s & 1);
+    const int from = s & 1, last = s + 1 == steps;
+    if (gg[0]) {
+      ProfScope ps("muon_gram<128>", gram / 2, 2 * n + 2 * cells, st);
+      TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg[0]), dim3(256), 0, st, lg[0], from);
     }
-    if (gsum) {
-      ProfScope ps("muon_gram_sum", 0, 4.0 * gsum * 4096, st);
-      TGP_LAUNCH(ps, (muon_gram_sum<2, 2>), dim3(gsum), dim3(256), 0, st, lsum);
+    if (gg[1]) {
+      ProfScope ps("muon_gram<256>", gram / 2, 2 * n + 2 * cells, st);
+      TGP_LAUNCH(ps, (muon_sym<GRAM, 4, 2, 2, 2, 3>), dim3(gg[1]), dim3(256), 0, st, lg[1], from);
+    }
+    if (gs[0]) {
+      ProfScope ps("muon_gram_sum<128>", 0, 0, st);
+      TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs[0]), dim3(256), 0, st, ls[0]);
+    }
+    if (gs[1]) {
+      ProfScope ps("muon_gram_sum<256>", 0, 0, st);
+      TGP_LAUNCH(ps, (muon_gram_sum<4, 2, 2, 2>), dim3(gs[1]), dim3(256), 0, st, ls[1]);
     }
     {
       ProfScope ps("muon_poly", poly / 2, 4 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 2, 4>), dim3(gp), dim3(256), 0, st, lp, s & 1);
+      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, from);
     }
-    ProfScope ps("muon_apply", gram, 4 * n + 2 * cells, st);
-    TGP_LAUNCH(ps, (muon_apply<2, 2, 2>), dim3(ga), dim3(256), 0, st, la, s & 1, (int)(s + 1 == steps));
+    if (ga[0]) {
+      ProfScope ps("muon_apply<128>", gram, 4 * n + 2 * cells, st);
+      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga[0]), dim3(256), 0, st, la[0], from, last);
+    }
+    if (ga[1]) {
+      ProfScope ps("muon_apply<256>", gram, 4 * n + 2 * cells, st);
+      TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga[1]), dim3(256), 0, st, la[1], from, last);
+    }
   }
   return launch_status();
 }
