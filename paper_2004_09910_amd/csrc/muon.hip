@@ -10,11 +10,19 @@
 //
 //   A = X X^T          P = a I + b A + c A A          X' = P X
 //
-// three launches over the tiles of all matrices.  A and P are float16 with the
+// launches over the tiles of all matrices.  A and P are float16 with the
 // rounding error of their diagonals beside them in float32: near convergence
 // A is nearly a multiple of I, whose one rounding would shift every singular
 // value alike and be multiplied by b / p(1) = 7.  A product of two such
 // matrices (L + dL)(R + dR), dL and dR diagonal, is taken as L R + dL R + L dR.
+//
+// Two steps at once, for long matrices: X'' = P(A') P(A) X, and as P(A) and A
+// commute, A' = X' X'^T = P A P.  That replaces the first step's product with X
+// and the second's X X^T, 3 m^2 n operations, by four products of m x m
+// matrices, 4 m^3.  (More than two at once would take fewer still, but A's
+// eigenvalues span the square of X's range, which P^2 stretches 12-fold a
+// step: three at once lose small singular values to float16's 11 bits, 8e-3
+// of the update's norm where two leave 1.5e-3.)
 #include <algorithm>
 
 #include "common.h"
@@ -44,12 +52,10 @@ struct Mat {
   float* mom;
   bf16_t* out;
   double* norm;        // partial sums of |U|^2
-  f16 *x[2], *a, *p;   // X (mp x np, ping-pong), A and P (mp x mp)
-  float *da, *dp;      // diagonals' rounding errors
+  f16 *x[2], *s[3];    // X (mp x np, ping-pong), A, P and their products (mp x mp)
+  float* d[3];         // their diagonals' rounding errors
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
-  int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;
-  int bm;              // rows of a tile of X X^T and P X
-};
+  int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;};
 
 struct Mats {
   int count;
@@ -365,97 +371,109 @@ __device__ __forceinline__ f32x4_t part_of(const f32x16& a, int g) {
   return f32x4_t{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
 }
 
-// Row and column of tile b of the upper triangle, row by row of a grid of nr
-// x nc tiles, nc / nr of which make a square: row r has the columns from
-// r nc / nr on.
-__device__ __forceinline__ void upper(int b, int nr, int nc, int& r, int& c) {
-  const int w = nc / nr;
+// Row and column of tile b of the upper triangle (row <= column) of nt x nt,
+// row by row.
+__device__ __forceinline__ void upper(int b, int nt, int& r, int& c) {
   r = 0;
-  while (b >= nc - r * w) {
-    b -= nc - r * w;
+  while (b >= nt - r) {
+    b -= nt - r;
     ++r;
   }
-  c = r * w + b;
+  c = r + b;
 }
 
-enum { GRAM, POLY };
+enum { GRAM, POLY, MUL };
 
-// Symmetric products, upper tiles only: A = X X^T (GRAM) or P = a I + b A + c
-// A A (POLY).  Where GRAM's sum is split, its ranges' partial tiles go to
-// t.part as the accumulators lie, [range][tile][wave][fragment][g][lane].
+// Symmetric products, upper tiles only.  GRAM: s[0] = X X^T; where its sum is
+// split, the ranges' partial tiles go to t.part as the accumulators lie,
+// [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
+// s[a].  MUL: s[c] = s[a] s[b], of matrices that commute.
 template <int MODE, int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(Mats l, int from) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(Mats l, int a, int b, int c) {
   typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
+  static_assert(TL::BM == TL::BN, "square tiles");
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
   const int k = find(l, blk);
   const Mat& t = l.t[k];
-  const int nr = t.mp / TL::BM, nc = t.mp / TL::BN, w = nc / nr, tiles = nr * nc - w * (nr * (nr - 1) / 2);
-  const int b = blk - l.blk0[k], sp = MODE == GRAM ? b / tiles : 0, tile = b - sp * tiles;
+  const int nt = t.mp / TL::BM, tiles = nt * (nt + 1) / 2;
+  const int q = blk - l.blk0[k], sp = MODE == GRAM ? q / tiles : 0;
   int ti, tj;
-  upper(tile, nr, nc, ti, tj);
+  upper(q - sp * tiles, nt, ti, tj);
   const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
   const int k0 = MODE == GRAM ? (int)((long)nk * sp / t.split) : 0;
   const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
-  const f16* src = MODE == GRAM ? t.x[from] : t.a;
-  const bool mirror = tj >= (ti + 1) * w;
+  const f16* L = MODE == GRAM ? pickg(t.x, a) : pickg(t.s, a);
+  const f16* R = MODE == MUL ? pickg(t.s, b) : L;
   TL tl;
-  tl.run(ring, src, t.mp, i0, src, t.mp, j0, k0, k1);
+  tl.run(ring, L, t.mp, i0, R, t.mp, j0, k0, k1);
+  const float* dl = pickg(t.d, a);
+  const float* dr = MODE == MUL ? pickg(t.d, b) : dl;
+  f16* out = pickg(t.s, c);
+  float* dout = pickg(t.d, c);
   const int wave = threadIdx.x >> 6, wi = i0 + wave / WN * MT * 32, wj = j0 + wave % WN * NT * 32;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const f32x16& acc = tl.acc[i][j];
-      if constexpr (MODE == GRAM) {
-        if (t.split > 1) {
-          f32x4_t* out = (f32x4_t*)t.part +
-                         ((((long)b * WM * WN + wave) * MT + i) * NT + j) * 256 + (threadIdx.x & 63);
+      if (MODE == GRAM && t.split > 1) {
+        f32x4_t* part = (f32x4_t*)t.part +
+                        ((((long)q * WM * WN + wave) * MT + i) * NT + j) * 256 + (threadIdx.x & 63);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) out[64 * g] = part_of(acc, g);
+        for (int g = 0; g < 4; ++g) part[64 * g] = part_of(acc, g);
+        continue;
+      }
+      store_sym(out, dout, t.mp, wi + 32 * i, wj + 32 * j, ti != tj, [&](int g, int r, int col) {
+        if constexpr (MODE == GRAM) {
+          return part_of(acc, g) * (1.f / (kSX * kSX));
         } else {
-          store_sym(t.a, t.da, t.mp, wi + 32 * i, wj + 32 * j, mirror,
-                    [&](int g, int, int) { return part_of(acc, g) * (1.f / (kSX * kSX)); });
-        }
-      } else {
-        store_sym(t.p, t.dp, t.mp, wi + 32 * i, wj + 32 * j, mirror, [&](int g, int r, int c) {
-          const f32x4_t a = from_f16(t.a + at(t.mp, c, r)) * (1.f / kSM);   // A is symmetric
-          const f32x4_t dr = *(const f32x4_t*)(t.da + r);
-          const float dc = t.da[c];
-          f32x4_t p = kC * (part_of(acc, g) * (1.f / (kSM * kSM)) + a * (dr + dc)) + kB * a;
+          // element (r .. r + 3, col) of L and R, read where symmetry has it
+          const f32x4_t lv = from_f16(L + at(t.mp, col, r)) * (1.f / kSM);
+          const f32x4_t rv = MODE == POLY ? lv : from_f16(R + at(t.mp, col, r)) * (1.f / kSM);
+          const f32x4_t dlr = *(const f32x4_t*)(dl + r);
+          const float dlc = dl[col], drc = dr[col];
+          f32x4_t p = part_of(acc, g) * (1.f / (kSM * kSM)) + dlr * rv + lv * drc;
 #pragma unroll
           for (int z = 0; z < 4; ++z)
-            if (r + z == c) p[z] += kA + kB * dc;
+            if (r + z == col) p[z] += dlc * drc;
+          if constexpr (MODE == POLY) {
+            p = kC * p + kB * lv;
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+              if (r + z == col) p[z] += kA + kB * dlc;
+          }
           return p;
-        });
-      }
+        }
+      });
     }
 }
 
-// A from the ranges' partial tiles, added in order: a wave takes one fragment.
+// s[0] from the ranges' partial tiles, added in order: a wave takes one
+// fragment.
 template <int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(256) void muon_gram_sum(Mats l) {
   const int k = find(l, blockIdx.x);
   const Mat& t = l.t[k];
-  constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, FR = WM * WN * MT * NT;
-  const int nr = t.mp / BM, nc = t.mp / BN, w = nc / nr, tiles = nr * nc - w * (nr * (nr - 1) / 2);
+  constexpr int BM = 32 * MT * WM, FR = WM * WN * MT * NT;
+  const int nt = t.mp / BM, tiles = nt * (nt + 1) / 2;
   const int f = (blockIdx.x - l.blk0[k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
   const int lane = threadIdx.x & 63, wave = q / (MT * NT), i = q / NT % MT, j = q % NT;
   int ti, tj;
-  upper(tile, nr, nc, ti, tj);
+  upper(tile, nt, ti, tj);
   const f32x4_t* in = (const f32x4_t*)t.part + ((long)tile * FR + q) * 256 + lane;
   const long step = (long)tiles * FR * 256;
   f32x4_t acc[4] = {};
   for (int s = 0; s < t.split; ++s)
 #pragma unroll
     for (int g = 0; g < 4; ++g) acc[g] += in[s * step + 64 * g];
-  store_sym(t.a, t.da, t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BN + (wave % WN * NT + j) * 32,
-            tj >= (ti + 1) * w, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
+  store_sym(t.s[0], t.d[0], t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BM + (wave % WN * NT + j) * 32,
+            ti != tj, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 
-// X' = P X, or (last) the update itself.
+// X' = s[p] X, or (last) the update itself.
 template <int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int from, int last) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int from, int last) {
   typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
@@ -463,15 +481,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int from, 
   const Mat& t = l.t[k];
   const int b = blk - l.blk0[k], nt = t.mp / TL::BM;
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
-  const f16* x = t.x[from];
+  const f16* x = pickg(t.x, from);
+  const float* dp = pickg(t.d, p);
   TL tl;
-  tl.run(ring, t.p, t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
+  tl.run(ring, pickg(t.s, p), t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool flip = t.rows > t.cols, whole = !flip && t.cols % 8 == 0;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31);
-    const float d = t.dp[r] * (1.f / kSX);
+    const float d = dp[r] * (1.f / kSX);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int c0 = j0 + (wave % WN * NT + j) * 32;
@@ -487,7 +506,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int from, 
       if (!last) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
-        f16* out = t.x[from ^ 1];
+        f16* out = pickg(t.x, from ^ 1);
         put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
       } else if (whole) {
 #pragma unroll
@@ -508,40 +527,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int from, 
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
-// The two tiles of X X^T and P X: 128 x 128 and 256 x 128 values of the result
-// on four waves.  The larger one takes a quarter less from the caches and
-// from LDS for each product; matrices whose padded side is no multiple of 256
-// take the smaller one, and so does a list that the larger one would deal out
-// to less than two blocks a CU.
 constexpr int kPad = 128;
 constexpr int kBlocks = 512;   // two a CU
 int up(int x) { return (x + kPad - 1) / kPad * kPad; }
-// Upper tiles of BM = bm, BN = 128 of an mp x mp matrix.
-int uppers(int mp, int bm) {
-  const int nr = mp / bm, nc = mp / 128, w = nc / nr;
-  return nr * nc - w * (nr * (nr - 1) / 2);
+int uppers(int nt) { return nt * (nt + 1) / 2; }
+
+// Whether two steps are taken at once.  The products with X that this saves
+// run at about twice the rate of the m x m ones that replace them, on fewer
+// tiles: from n = 4 m on (a 3 x 3 layer has 9 m and more).
+bool pairs(const tgp_muon_tensor& d) {
+  return std::max(d.rows, d.cols) >= 4 * (long)std::min(d.rows, d.cols);
 }
-int tiles_apply(const Mat& t, int bm) { return (t.mp / bm) * (t.np / 128); }
 
 // Describes n (at most kMaxMats) matrices laid out from byte `pos` of the
 // workspace ws on; returns their end.  The sums of A = X X^T are split where
 // the launch has too few tiles to fill the chip: into ranges of about one
 // length over all matrices, for kBlocks blocks, of 512 values at least.
-size_t lay_out(int n, const tgp_muon_tensor* d, char* ws, size_t pos, Mats& l) {
+size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
     char* p = ws + pos;
     pos += al256(bytes);
     return p;
   };
   l.count = n;
-  long large = 0, work = 0;
+  long work = 0;
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
-    t.grad = d[k].grad;
-    t.mom = d[k].momentum;
-    t.out = (bf16_t*)d[k].update;
-    t.rows = d[k].rows;
-    t.cols = d[k].cols;
+    t.grad = d[k]->grad;
+    t.mom = d[k]->momentum;
+    t.out = (bf16_t*)d[k]->update;
+    t.rows = d[k]->rows;
+    t.cols = d[k]->cols;
     t.m = std::min(t.rows, t.cols);
     t.n = std::max(t.rows, t.cols);
     t.mp = up(t.m);
@@ -551,26 +567,37 @@ size_t lay_out(int n, const tgp_muon_tensor* d, char* ws, size_t pos, Mats& l) {
     t.norm_per = size >= 1 << 22 ? 4 : 1;   // where it is large, |U| is summed up by fewer blocks
     t.norm = (double*)take(kNormBlocks * sizeof(double));
     for (int z = 0; z < 2; ++z) t.x[z] = (f16*)take((size_t)t.mp * t.np * 2);
-    t.a = (f16*)take((size_t)t.mp * t.mp * 2);
-    t.p = (f16*)take((size_t)t.mp * t.mp * 2);
-    t.da = (float*)take((size_t)t.mp * 4);
-    t.dp = (float*)take((size_t)t.mp * 4);
-    if (t.mp % 256 == 0) large += tiles_apply(t, 256);
-  }
-  for (int k = 0; k < n; ++k) {
-    Mat& t = l.t[k];
-    t.bm = t.mp % 256 == 0 && large >= kBlocks ? 256 : 128;
-    work += (long)uppers(t.mp, t.bm) * (t.bm / 128) * (t.np / 32);
+    for (int z = 0; z < 3; ++z) {
+      t.s[z] = (f16*)take((size_t)t.mp * t.mp * 2);
+      t.d[z] = (float*)take((size_t)t.mp * 4);
+    }
+    work += (long)uppers(t.mp / 128) * (t.np / 32);
   }
   const long range = std::max<long>(16, (work + kBlocks - 1) / kBlocks);
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
-    t.split = (int)((t.np / 32 * (t.bm / 128) + range - 1) / range);
+    t.split = (int)((t.np / 32 + range - 1) / range);
     t.part = nullptr;
-    if (t.split > 1)
-      t.part = (float*)take((size_t)t.split * uppers(t.mp, t.bm) * t.bm * 128 * sizeof(float));
+    if (t.split > 1) t.part = (float*)take((size_t)t.split * uppers(t.mp / 128) * 128 * 128 * sizeof(float));
   }
   return pos;
+}
+
+// Deals the matrices into lists of one launch each: those of one step at a
+// time, then those of two, in their order.  Calls go(list of pointers, count,
+// whether in pairs).
+template <typename F>
+void each_list(int n, const tgp_muon_tensor* t, F go) {
+  for (int z = 0; z < 2; ++z) {
+    const tgp_muon_tensor* list[kMaxMats];
+    int count = 0;
+    for (int k = 0; k < n; ++k) {
+      if (pairs(t[k]) != (z == 1)) continue;
+      list[count++] = t + k;
+      if (count == kMaxMats) go(list, count, z == 1), count = 0;
+    }
+    if (count) go(list, count, z == 1);
+  }
 }
 
 // Fills blk0 with blocks(t) of each matrix; returns the grid.
@@ -585,14 +612,18 @@ unsigned deal(Mats& l, F blocks) {
   return (unsigned)at;
 }
 
-hipError_t update_list(Mats& l, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
-  double n = 0, gram = 0, poly = 0, cells = 0;
+hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
+  double n = 0, gram = 0, cube = 0, cells = 0;
+  bool wide = true;
+  long large = 0;
   for (int k = 0; k < l.count; ++k) {
     const Mat& t = l.t[k];
     n += (double)t.rows * t.cols;
-    gram += 2.0 * t.m * t.m * t.n;
-    poly += 2.0 * t.m * t.m * t.m;
+    gram += (double)t.m * t.m * t.n;
+    cube += (double)t.m * t.m * t.m;
     cells += (double)t.m * t.m;
+    wide = wide && t.mp % 256 == 0;
+    large += (long)(t.mp / 256) * (t.np / 128);
   }
   {
     const unsigned g = deal(l, [](const Mat& t) { return t.norm_blocks; });
@@ -604,46 +635,54 @@ hipError_t update_list(Mats& l, float mu, bool nesterov, int steps, float eps, h
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
     TGP_LAUNCH(ps, muon_normalize, dim3(g), dim3(256), 0, st, l, mu, (int)nesterov, eps);
   }
-  // the same matrices, blocks dealt for each product and tile
-  Mats lp = l, lg[2] = {l, l}, ls[2] = {l, l}, la[2] = {l, l};
-  unsigned gg[2], gs[2], ga[2];
-  for (int z = 0; z < 2; ++z) {
-    const int bm = z ? 256 : 128;
-    gg[z] = deal(lg[z], [&](const Mat& t) { return t.bm == bm ? uppers(t.mp, bm) * t.split : 0; });
-    gs[z] = deal(ls[z], [&](const Mat& t) { return t.bm == bm && t.split > 1 ? uppers(t.mp, bm) * bm / 32 : 0; });
-    ga[z] = deal(la[z], [&](const Mat& t) { return t.bm == bm ? tiles_apply(t, bm) : 0; });
-  }
-  const unsigned gp = deal(lp, [](const Mat& t) { const int nt = t.mp / 64; return nt * (nt + 1) / 2; });
-  for (int s = 0; s < steps; ++s) {
-    const int from = s & 1, last = s + 1 == steps;
-    if (gg[0]) {
-      ProfScope ps("muon_gram<128>", gram / 2, 2 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg[0]), dim3(256), 0, st, lg[0], from);
-    }
-    if (gg[1]) {
-      ProfScope ps("muon_gram<256>", gram / 2, 2 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<GRAM, 4, 2, 2, 2, 3>), dim3(gg[1]), dim3(256), 0, st, lg[1], from);
-    }
-    if (gs[0]) {
-      ProfScope ps("muon_gram_sum<128>", 0, 0, st);
-      TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs[0]), dim3(256), 0, st, ls[0]);
-    }
-    if (gs[1]) {
-      ProfScope ps("muon_gram_sum<256>", 0, 0, st);
-      TGP_LAUNCH(ps, (muon_gram_sum<4, 2, 2, 2>), dim3(gs[1]), dim3(256), 0, st, ls[1]);
-    }
+  // the same matrices, blocks dealt for each product.  P X on tiles of 256 x
+  // 128 takes a quarter less from the caches and LDS than on 128 x 128 (2048
+  // x 18432: 173 us, 178); it is taken where every matrix is cut into whole
+  // ones and they make two blocks a CU.
+  const int bm = wide && large >= kBlocks ? 256 : 128;
+  Mats lp = l, lg = l, ls = l, la = l;
+  const unsigned gg = deal(lg, [](const Mat& t) { return uppers(t.mp / 128) * t.split; });
+  const unsigned gs = deal(ls, [](const Mat& t) { return t.split > 1 ? uppers(t.mp / 128) * 4 : 0; });
+  const unsigned gp = deal(lp, [](const Mat& t) { return uppers(t.mp / 64); });
+  const unsigned ga = deal(la, [&](const Mat& t) { return (t.mp / bm) * (t.np / 128); });
+  auto poly = [&](int a, int c) {
+    ProfScope ps("muon_poly", cube, 4 * cells, st);
+    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, a, 0, c);
+  };
+  auto mul = [&](int a, int b, int c) {
+    ProfScope ps("muon_mul", cube, 6 * cells, st);
+    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, a, b, c);
+  };
+  int from = 0;
+  for (int s = 0; s < steps;) {
     {
-      ProfScope ps("muon_poly", poly / 2, 4 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, from);
+      ProfScope ps("muon_gram", gram, 2 * n + 2 * cells, st);
+      TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg), dim3(256), 0, st, lg, from, 0, 0);
     }
-    if (ga[0]) {
-      ProfScope ps("muon_apply<128>", gram, 4 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga[0]), dim3(256), 0, st, la[0], from, last);
+    if (gs) {
+      ProfScope ps("muon_gram_sum", 0, 0, st);
+      TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs), dim3(256), 0, st, ls);
     }
-    if (ga[1]) {
-      ProfScope ps("muon_apply<256>", gram, 4 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga[1]), dim3(256), 0, st, la[1], from, last);
+    poly(0, 1);
+    int p = 1;
+    if (two && s + 2 <= steps) {
+      mul(1, 0, 2);    // P A
+      mul(2, 1, 0);    // A' = P A P
+      poly(0, 2);      // P'
+      mul(2, 1, 0);    // P' P
+      p = 0;
+      ++s;
     }
+    ++s;
+    {
+      const int last = s == steps;
+      ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
+      if (bm == 256)
+        TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga), dim3(256), 0, st, la, p, from, last);
+      else
+        TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga), dim3(256), 0, st, la, p, from, last);
+    }
+    from ^= 1;
   }
   return launch_status();
 }
@@ -651,22 +690,25 @@ hipError_t update_list(Mats& l, float mu, bool nesterov, int steps, float eps, h
 }  // namespace
 
 size_t muon_bytes(int n, const tgp_muon_tensor* t) {
-  size_t at = 0;
+  size_t pos = 0;
   Mats l;
-  for (int k = 0; k < n; k += kMaxMats) at = lay_out(std::min(kMaxMats, n - k), t + k, nullptr, at, l);
-  return at;
+  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count, bool) {
+    pos = lay_out(count, d, nullptr, pos, l);
+  });
+  return pos;
 }
 
 hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov, int steps,
                        float eps, void* ws, hipStream_t st) {
-  size_t at = 0;
-  for (int k = 0; k < n; k += kMaxMats) {
+  size_t pos = 0;
+  hipError_t e = hipSuccess;
+  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count, bool two) {
+    if (e != hipSuccess) return;
     Mats l;
-    at = lay_out(std::min(kMaxMats, n - k), t + k, (char*)ws, at, l);
-    const hipError_t e = update_list(l, mu, nesterov, steps, eps, st);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+    pos = lay_out(count, d, (char*)ws, pos, l);
+    e = update_list(l, two, mu, nesterov, steps, eps, st);
+  });
+  return e;
 }
 
 }  // namespace tgpk
