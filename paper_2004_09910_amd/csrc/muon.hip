@@ -471,6 +471,28 @@ __global__ __launch_bounds__(256) void muon_gram_sum(Mats l) {
             ti != tj, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 
+// Stores values of row r of X, columns c0 .. c0 + 31 (as the accumulators of a
+// transposed fragment lie), as the update.
+__device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const float (&y)[16]) {
+  const int hi = (threadIdx.x & 63) >> 5;
+  const bool flip = t.rows > t.cols;
+  if (!flip && t.cols % 8 == 0) {
+    unsigned pk[8];
+#pragma unroll
+    for (int g = 0; g < 8; ++g) pk[g] = f2bf(y[2 * g]) | (f2bf(y[2 * g + 1]) << 16);
+    put8(pk, [&](int h, u32x4 c) {
+      const int cc = c0 + 16 * h + 8 * hi;
+      if (r < t.m && cc < t.n) *(u32x4*)(t.out + (long)r * t.cols + cc) = c;
+    });
+  } else {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = c0 + 8 * (v / 4) + 4 * hi + v % 4;
+      if (r < t.m && c < t.n) t.out[flip ? (long)c * t.cols + r : (long)r * t.cols + c] = (bf16_t)f2bf(y[v]);
+    }
+  }
+}
+
 // X' = s[p] X, or (last) the update itself.
 template <int MT, int NT, int WM, int WN, int NS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int from, int last) {
@@ -486,7 +508,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int
   TL tl;
   tl.run(ring, pickg(t.s, p), t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool flip = t.rows > t.cols, whole = !flip && t.cols % 8 == 0;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31);
@@ -508,27 +529,228 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
         f16* out = pickg(t.x, from ^ 1);
         put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
-      } else if (whole) {
+      } else {
+        store_update(t, r, c0, y);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------- small matrices, whole
+
+// A matrix whose X fits in LDS: the whole update by one block of eight waves,
+// X, A and P staying in LDS (panels of 32 columns, a row's 64 bytes 80 apart:
+// eight rows read at one chunk hit distinct banks).  MS: m rounded up to 32 or
+// 64.  What it does is bound by the latencies between its barriers, four a
+// step; five launches a step take five times as long.
+constexpr int kSmallT = 512, kSmallX = 16384, kRow = 80;   // threads, most values of X, bytes of a row
+constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT;
+
+template <int MS>
+__global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
+  constexpr int Q = MS / 32, F = Q * Q, KS = 8 / F;   // fragments of A's side and of A, waves a fragment
+  __shared__ __attribute__((aligned(16))) unsigned char xs[kSmallX / 32 * kRow];
+  __shared__ __attribute__((aligned(16))) unsigned char as[Q * MS * kRow], pms[Q * MS * kRow];
+  __shared__ __attribute__((aligned(16))) f32x4_t part[8 * 256];
+  __shared__ __attribute__((aligned(16))) float da[MS], dp[MS];
+  __shared__ double sh[8];
+  const Mat& t = l.t[blockIdx.x];
+  const int ns = (t.n + 31) / 32 * 32, chunks = MS * ns / 8;
+  const bool flip = t.rows > t.cols, vec = !flip && t.cols % 4 == 0;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // U in registers: chunk z of this thread is 8 columns from j of row i
+  auto place = [&](int z, int& i, int& j) {
+    const int c = z * kSmallT + tid;
+    if (flip) {
+      i = c % MS;
+      j = c / MS * 8;
+    } else {
+      i = c / (ns / 8);
+      j = c % (ns / 8) * 8;
+    }
+    return c < chunks;
+  };
+  float u[kSmallChunks][8], m[kSmallChunks][8];
 #pragma unroll
-        for (int g = 0; g < 8; ++g) pk[g] = f2bf(y[2 * g]) | (f2bf(y[2 * g + 1]) << 16);
-        put8(pk, [&](int h, u32x4 c) {
-          const int cc = c0 + 16 * h + 8 * (lane >> 5);
-          if (r < t.m && cc < t.n) *(u32x4*)(t.out + (long)r * t.cols + cc) = c;
-        });
+  for (int z = 0; z < kSmallChunks; ++z) {
+    int i, j;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) u[z][v] = m[z][v] = 0.f;
+    if (z * kSmallT >= chunks) break;
+    if (!place(z, i, j) || i >= t.m) continue;
+    if (vec && j + 8 <= t.n) {
+      const float4* g = (const float4*)(t.grad + i * t.cols + j);
+      const float4 g0 = g[0], g1 = g[1];
+      u[z][0] = g0.x; u[z][1] = g0.y; u[z][2] = g0.z; u[z][3] = g0.w;
+      u[z][4] = g1.x; u[z][5] = g1.y; u[z][6] = g1.z; u[z][7] = g1.w;
+      if (t.mom) {
+        const float4* q = (const float4*)(t.mom + i * t.cols + j);
+        const float4 m0 = q[0], m1 = q[1];
+        m[z][0] = m0.x; m[z][1] = m0.y; m[z][2] = m0.z; m[z][3] = m0.w;
+        m[z][4] = m1.x; m[z][5] = m1.y; m[z][6] = m1.z; m[z][7] = m1.w;
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 8; ++v)
+        if (j + v < t.n) {
+          const int e = flip ? (j + v) * t.cols + i : i * t.cols + j + v;
+          u[z][v] = t.grad[e];
+          if (t.mom) m[z][v] = t.mom[e];
+        }
+    }
+  }
+  double sum = 0;
+#pragma unroll
+  for (int z = 0; z < kSmallChunks; ++z) {
+    int i, j;
+    if (z * kSmallT >= chunks) break;
+    if (!place(z, i, j) || i >= t.m) continue;
+    if (t.mom) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        m[z][v] = mu * m[z][v] + u[z][v];
+        u[z][v] = nesterov ? u[z][v] + mu * m[z][v] : m[z][v];
+      }
+      if (vec && j + 8 <= t.n) {
+        float4* q = (float4*)(t.mom + i * t.cols + j);
+        q[0] = make_float4(m[z][0], m[z][1], m[z][2], m[z][3]);
+        q[1] = make_float4(m[z][4], m[z][5], m[z][6], m[z][7]);
       } else {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int c = c0 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-          if (r < t.m && c < t.n) t.out[flip ? (long)c * t.cols + r : (long)r * t.cols + c] = (bf16_t)f2bf(y[v]);
+        for (int v = 0; v < 8; ++v)
+          if (j + v < t.n) t.mom[flip ? (j + v) * t.cols + i : i * t.cols + j + v] = m[z][v];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < 8; ++v) sum += (double)u[z][v] * u[z][v];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) sh[wave] = sum;
+  __syncthreads();
+  const double norm = sqrt(((sh[0] + sh[1]) + (sh[2] + sh[3])) + ((sh[4] + sh[5]) + (sh[6] + sh[7]))) + eps;
+  const double inv = norm > 0 || norm != norm ? kSX / norm : 0.0;
+#pragma unroll
+  for (int z = 0; z < kSmallChunks; ++z) {
+    int i, j;
+    if (z * kSmallT >= chunks) break;
+    if (!place(z, i, j)) continue;
+    f16x8 h;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(u[z][v] * inv);
+    *(f16x8*)(xs + ((j >> 5) * MS + i) * kRow + (j & 31) * 2) = h;
+  }
+  __syncthreads();
+
+  const int fr = lane & 31, hi = lane >> 5;
+  const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  // fragment of 32 rows from r0 on, sum values 16 kk .. of panel p
+  auto rows_of = [&](const unsigned char* b, int p, int r0, int kk) {
+    return *(const u32x4*)(b + (p * MS + r0 + fr) * kRow + (2 * kk + hi) * 16);
+  };
+  // place of four values of row r from column c on
+  auto four = [&](unsigned char* b, int r, int c) { return b + ((c >> 5) * MS + r) * kRow + (c & 31) * 2; };
+  // stores a fragment of a symmetric matrix (rows i0, columns j0) and its diagonal's errors
+  auto store = [&](unsigned char* b, float* d, int i0, int j0, const f32x4_t (&f)[4]) {
+    const int j = j0 + fr;
+    unsigned pk[8];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int i = i0 + 8 * g + 4 * hi;
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        if (i + z == j) d[j] = f[g][z] - (float)(f16)(f[g][z] * kSM) * (1.f / kSM);
+      pk[2 * g] = pack_f16(f[g][0] * kSM, f[g][1] * kSM);
+      pk[2 * g + 1] = pack_f16(f[g][2] * kSM, f[g][3] * kSM);
+    }
+    put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(b, j, i0 + 16 * h + 8 * hi) = c; });
+  };
+  for (int s = 0; s < steps; ++s) {
+    // A = X X^T: each fragment's panels dealt over KS waves
+    {
+      const int f = wave % F, i0 = f / Q * 32, j0 = f % Q * 32;
+      f32x16 acc = {};
+      for (int p = wave / F; p < ns / 32; p += KS)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) acc = mfma(rows_of(xs, p, i0, kk), rows_of(xs, p, j0, kk), acc);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) part[wave * 256 + 64 * g + lane] = part_of(acc, g);
+    }
+    __syncthreads();
+    if (wave < F) {
+      f32x4_t a[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        a[g] = part[wave * 256 + 64 * g + lane];
+#pragma unroll
+        for (int k = 1; k < KS; ++k) a[g] += part[(k * F + wave) * 256 + 64 * g + lane];
+        a[g] = a[g] * (1.f / (kSX * kSX));
+      }
+      store(as, da, wave / Q * 32, wave % Q * 32, a);
+    }
+    __syncthreads();
+    // P = a I + b A + c A A
+    if (wave < F) {
+      const int i0 = wave / Q * 32, j0 = wave % Q * 32, c = j0 + fr;
+      f32x16 acc = {};
+#pragma unroll
+      for (int p = 0; p < Q; ++p)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) acc = mfma(rows_of(as, p, i0, kk), rows_of(as, p, j0, kk), acc);
+      f32x4_t f[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int r = i0 + 8 * g + 4 * hi;
+        const f32x4_t a = from_f16((const f16*)four(as, c, r)) * (1.f / kSM);
+        f[g] = kC * (part_of(acc, g) * (1.f / (kSM * kSM)) + a * (*(const f32x4_t*)(da + r) + da[c])) + kB * a;
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+          if (r + z == c) f[g][z] += kA + (kB + kC * da[c]) * da[c];
+      }
+      store(pms, dp, i0, j0, f);
+    }
+    __syncthreads();
+    // X = P X, a panel a wave and turn, in place
+    for (int pj = wave; pj < ns / 32; pj += 8) {
+      f32x16 acc[Q] = {};
+#pragma unroll
+      for (int p = 0; p < Q; ++p)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const u32x4 b = frag_tr(xs + (pj * MS + 32 * p + 16 * kk + kb) * kRow + cb * 16 + 8 * (lane & 1), kRow);
+#pragma unroll
+          for (int i = 0; i < Q; ++i) acc[i] = mfma(b, rows_of(pms, p, 32 * i, kk), acc[i]);
+        }
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        const int r = 32 * i + fr;
+        const float d = dp[r] * (1.f / kSX);
+        float y[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4_t xv = from_f16((const f16*)four(xs, r, 32 * pj + 8 * g + 4 * hi));
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[4 * g + z] = acc[i][4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
+        }
+        if (s + 1 < steps) {
+          unsigned pk[8];
+#pragma unroll
+          for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
+          put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(xs, r, 32 * pj + 16 * h + 8 * hi) = c; });
+        } else {
+          store_update(t, r, 32 * pj, y);
         }
       }
     }
+    __syncthreads();
   }
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kPad = 128;
 constexpr int kBlocks = 512;   // two a CU
+constexpr int kRange = 48;     // stages of 32 sum values
 int up(int x) { return (x + kPad - 1) / kPad * kPad; }
 int uppers(int nt) { return nt * (nt + 1) / 2; }
 
@@ -539,27 +761,50 @@ bool pairs(const tgp_muon_tensor& d) {
   return std::max(d.rows, d.cols) >= 4 * (long)std::min(d.rows, d.cols);
 }
 
+// Whether one block does the whole update (muon_small).
+bool small(const tgp_muon_tensor& d) {
+  const long m = std::min(d.rows, d.cols), n = std::max(d.rows, d.cols);
+  return m <= 64 && (m <= 32 ? 32 : 64) * ((n + 31) / 32 * 32) <= kSmallX;
+}
+// How a matrix is taken: whole by one block (of 32 or 64 rows), or by tiles,
+// one or two steps at a time.
+enum { WHOLE32, WHOLE64, SINGLES, PAIRS, KINDS };
+int kind_of(const tgp_muon_tensor& d) {
+  if (small(d)) return std::min(d.rows, d.cols) <= 32 ? WHOLE32 : WHOLE64;
+  return pairs(d) ? PAIRS : SINGLES;
+}
+
+void describe(const tgp_muon_tensor& d, Mat& t) {
+  t = Mat{};
+  t.grad = d.grad;
+  t.mom = d.momentum;
+  t.out = (bf16_t*)d.update;
+  t.rows = d.rows;
+  t.cols = d.cols;
+  t.m = std::min(t.rows, t.cols);
+  t.n = std::max(t.rows, t.cols);
+}
+
 // Describes n (at most kMaxMats) matrices laid out from byte `pos` of the
-// workspace ws on; returns their end.  The sums of A = X X^T are split where
-// the launch has too few tiles to fill the chip: into ranges of about one
-// length over all matrices, for kBlocks blocks, of 512 values at least.
-size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
+// workspace ws on; returns their end.  The sum of A = X X^T is split where a
+// matrix has too few tiles to fill the chip: into ranges for about kBlocks
+// blocks of kRange stages at least (writing and reading back a partial tile
+// takes the time of 20 stages).  The ranges depend on the matrix alone, so
+// that its update does not depend on the others of the call.
+size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
     char* p = ws + pos;
     pos += al256(bytes);
     return p;
   };
   l.count = n;
-  long work = 0;
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
-    t.grad = d[k]->grad;
-    t.mom = d[k]->momentum;
-    t.out = (bf16_t*)d[k]->update;
-    t.rows = d[k]->rows;
-    t.cols = d[k]->cols;
-    t.m = std::min(t.rows, t.cols);
-    t.n = std::max(t.rows, t.cols);
+    describe(*d[k], t);
+    if (kind == WHOLE32 || kind == WHOLE64) {
+      pos += 256;   // unused: a call asks for a workspace whatever its sizes
+      continue;
+    }
     t.mp = up(t.m);
     t.np = up(t.n);
     const long size = (long)t.rows * t.cols;
@@ -571,11 +816,7 @@ size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mat
       t.s[z] = (f16*)take((size_t)t.mp * t.mp * 2);
       t.d[z] = (float*)take((size_t)t.mp * 4);
     }
-    work += (long)uppers(t.mp / 128) * (t.np / 32);
-  }
-  const long range = std::max<long>(16, (work + kBlocks - 1) / kBlocks);
-  for (int k = 0; k < n; ++k) {
-    Mat& t = l.t[k];
+    const long range = std::max<long>(kRange, cdiv((long)uppers(t.mp / 128) * (t.np / 32), kBlocks));
     t.split = (int)((t.np / 32 + range - 1) / range);
     t.part = nullptr;
     if (t.split > 1) t.part = (float*)take((size_t)t.split * uppers(t.mp / 128) * 128 * 128 * sizeof(float));
@@ -583,20 +824,19 @@ size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mat
   return pos;
 }
 
-// Deals the matrices into lists of one launch each: those of one step at a
-// time, then those of two, in their order.  Calls go(list of pointers, count,
-// whether in pairs).
+// Deals the matrices into lists of one kind each, in their order.  Calls
+// go(kind, list of pointers, count).
 template <typename F>
 void each_list(int n, const tgp_muon_tensor* t, F go) {
-  for (int z = 0; z < 2; ++z) {
+  for (int kind = 0; kind < KINDS; ++kind) {
     const tgp_muon_tensor* list[kMaxMats];
     int count = 0;
     for (int k = 0; k < n; ++k) {
-      if (pairs(t[k]) != (z == 1)) continue;
+      if (kind_of(t[k]) != kind) continue;
       list[count++] = t + k;
-      if (count == kMaxMats) go(list, count, z == 1), count = 0;
+      if (count == kMaxMats) go(kind, list, count), count = 0;
     }
-    if (count) go(list, count, z == 1);
+    if (count) go(kind, list, count);
   }
 }
 
@@ -610,6 +850,21 @@ unsigned deal(Mats& l, F blocks) {
   }
   l.blk0[l.count] = at;
   return (unsigned)at;
+}
+
+hipError_t update_small(const Mats& l, bool m64, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
+  double n = 0, flops = 0;
+  for (int k = 0; k < l.count; ++k) {
+    const double m = l.t[k].m;
+    n += m * l.t[k].n;
+    flops += steps * (3 * m * m * l.t[k].n + m * m * m);
+  }
+  ProfScope ps(m64 ? "muon_small<64>" : "muon_small<32>", flops, (l.t[0].mom ? 14 : 6) * n, st);
+  if (m64)
+    TGP_LAUNCH(ps, muon_small<64>, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
+  else
+    TGP_LAUNCH(ps, muon_small<32>, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
+  return launch_status();
 }
 
 hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
@@ -692,8 +947,8 @@ hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, fl
 size_t muon_bytes(int n, const tgp_muon_tensor* t) {
   size_t pos = 0;
   Mats l;
-  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count, bool) {
-    pos = lay_out(count, d, nullptr, pos, l);
+  each_list(n, t, [&](int kind, const tgp_muon_tensor* const* d, int count) {
+    pos = lay_out(kind, count, d, nullptr, pos, l);
   });
   return pos;
 }
@@ -702,11 +957,12 @@ hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov,
                        float eps, void* ws, hipStream_t st) {
   size_t pos = 0;
   hipError_t e = hipSuccess;
-  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count, bool two) {
+  each_list(n, t, [&](int kind, const tgp_muon_tensor* const* d, int count) {
     if (e != hipSuccess) return;
     Mats l;
-    pos = lay_out(count, d, (char*)ws, pos, l);
-    e = update_list(l, two, mu, nesterov, steps, eps, st);
+    pos = lay_out(kind, count, d, (char*)ws, pos, l);
+    e = kind == WHOLE32 || kind == WHOLE64 ? update_small(l, kind == WHOLE64, mu, nesterov, steps, eps, st)
+                                           : update_list(l, kind == PAIRS, mu, nesterov, steps, eps, st);
   });
   return e;
 }
