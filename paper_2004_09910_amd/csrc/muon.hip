@@ -57,19 +57,27 @@ struct Mat {
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
   int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;};
 
+// The matrices of a list and, for each kind of launch, the first block of each
+// (and the number of blocks).  The first launch gets it as an argument and
+// leaves it in the workspace for the others: arguments lie in host memory,
+// which every block would have to reach for.
+enum { L_MOMENTUM, L_NORMALIZE, L_GRAM, L_SUM, L_SYM, L_APPLY, LAUNCHES };
 struct Mats {
   int count;
+  int blk0[LAUNCHES][kMaxMats + 1];
   Mat t[kMaxMats];
-  int blk0[kMaxMats + 1];   // first block of each matrix in the launch
 };
+static_assert(sizeof(Mats) <= 3800, "kernel arguments");
 
 // Place of row i, column j of a matrix of mp rows.
 __device__ __forceinline__ long at(int mp, int i, int j) { return ((long)(j >> 5) * mp + i) * 32 + (j & 31); }
 
-__device__ __forceinline__ int find(const Mats& l, int blk) {
-  int k = 0;
-  while (k + 1 < l.count && blk >= l.blk0[k + 1]) ++k;
-  return k;
+// The matrix that block blk of a launch works on: the last to start at or
+// before it.
+__device__ __forceinline__ int find(const Mats* l, int launch, int blk) {
+  const int lane = threadIdx.x & 63;
+  const bool at_or_before = lane < l->count && l->blk0[launch][min(lane, kMaxMats)] <= blk;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(at_or_before)) - 1);
 }
 
 __device__ __forceinline__ float update_of(const Mat& t, long i, float mu, int nesterov) {
@@ -90,11 +98,13 @@ __device__ __forceinline__ double block_sum(double s, double* sh) {
 // M = mu M + G, and partial sums of U^2 (in float64: squares of float32 values
 // neither overflow nor vanish).  Purely a matter of memory: 16-byte accesses,
 // two of each tensor in flight a thread.
-__global__ __launch_bounds__(256) void muon_momentum(Mats l, float mu, int nesterov) {
+__global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float mu, int nesterov) {
   __shared__ double sh[4];
-  const int k = find(l, blockIdx.x);
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < (int)(sizeof(Mats) / 4); i += 256) ((int*)table)[i] = ((const int*)&l)[i];
+  const int k = find(&l, L_MOMENTUM, blockIdx.x);
   const Mat& t = l.t[k];
-  const int b = blockIdx.x - l.blk0[k];
+  const int b = blockIdx.x - l.blk0[L_MOMENTUM][k];
   const long N = (long)t.rows * t.cols, N4 = N / 4, step = (long)t.norm_blocks * 256;
   const float4* g4 = (const float4*)t.grad;
   float4* m4 = (float4*)t.mom;
@@ -139,11 +149,11 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, float mu, int neste
 // X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
 // in the padding: a piece is 64 rows x 64 columns through LDS where the matrix
 // is transposed, else 32 rows x 128 columns.
-__global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nesterov, float eps) {
+__global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l, float mu, int nesterov, float eps) {
   __shared__ double sh[4];
   __shared__ float tile[64][65];
-  const int k = find(l, blockIdx.x);
-  const Mat& t = l.t[k];
+  const int k = find(l, L_NORMALIZE, blockIdx.x);
+  const Mat& t = l->t[k];
   const bool flip = t.rows > t.cols;
   double s = 0;
   for (int q = threadIdx.x; q < t.norm_blocks; q += 256) s += t.norm[q];
@@ -157,7 +167,7 @@ __global__ __launch_bounds__(256) void muon_normalize(Mats l, float mu, int nest
     for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(f[v] * inv);
     *(f16x8*)(t.x[0] + at(t.mp, i, j)) = h;
   };
-  const int b0 = (blockIdx.x - l.blk0[k]) * t.norm_per;
+  const int b0 = (blockIdx.x - l->blk0[L_NORMALIZE][k]) * t.norm_per;
   for (int b = b0; b < b0 + t.norm_per; ++b) {
     if (flip) {
       const int nt = t.np / 64, i0 = b / nt * 64, j0 = b % nt * 64;
@@ -389,28 +399,29 @@ enum { GRAM, POLY, MUL };
 // [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
 // s[a].  MUL: s[c] = s[a] s[b], of matrices that commute.
 template <int MODE, int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(Mats l, int a, int b, int c) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int a, int b, int c) {
   typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
   static_assert(TL::BM == TL::BN, "square tiles");
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
-  const int k = find(l, blk);
-  const Mat& t = l.t[k];
+  constexpr int LAUNCH = MODE == GRAM ? L_GRAM : L_SYM;
+  const int k = find(l, LAUNCH, blk);
+  const Mat& t = l->t[k];
   const int nt = t.mp / TL::BM, tiles = nt * (nt + 1) / 2;
-  const int q = blk - l.blk0[k], sp = MODE == GRAM ? q / tiles : 0;
+  const int q = blk - l->blk0[LAUNCH][k], sp = MODE == GRAM ? q / tiles : 0;
   int ti, tj;
   upper(q - sp * tiles, nt, ti, tj);
   const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
   const int k0 = MODE == GRAM ? (int)((long)nk * sp / t.split) : 0;
   const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
-  const f16* L = MODE == GRAM ? pickg(t.x, a) : pickg(t.s, a);
-  const f16* R = MODE == MUL ? pickg(t.s, b) : L;
+  const f16* L = MODE == GRAM ? t.x[a] : t.s[a];
+  const f16* R = MODE == MUL ? t.s[b] : L;
   TL tl;
   tl.run(ring, L, t.mp, i0, R, t.mp, j0, k0, k1);
-  const float* dl = pickg(t.d, a);
-  const float* dr = MODE == MUL ? pickg(t.d, b) : dl;
-  f16* out = pickg(t.s, c);
-  float* dout = pickg(t.d, c);
+  const float* dl = t.d[a];
+  const float* dr = MODE == MUL ? t.d[b] : dl;
+  f16* out = t.s[c];
+  float* dout = t.d[c];
   const int wave = threadIdx.x >> 6, wi = i0 + wave / WN * MT * 32, wj = j0 + wave % WN * NT * 32;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -452,12 +463,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(Mats l, int a, int b
 // s[0] from the ranges' partial tiles, added in order: a wave takes one
 // fragment.
 template <int MT, int NT, int WM, int WN>
-__global__ __launch_bounds__(256) void muon_gram_sum(Mats l) {
-  const int k = find(l, blockIdx.x);
-  const Mat& t = l.t[k];
+__global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l) {
+  const int k = find(l, L_SUM, blockIdx.x);
+  const Mat& t = l->t[k];
   constexpr int BM = 32 * MT * WM, FR = WM * WN * MT * NT;
   const int nt = t.mp / BM, tiles = nt * (nt + 1) / 2;
-  const int f = (blockIdx.x - l.blk0[k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
+  const int f = (blockIdx.x - l->blk0[L_SUM][k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
   const int lane = threadIdx.x & 63, wave = q / (MT * NT), i = q / NT % MT, j = q % NT;
   int ti, tj;
   upper(tile, nt, ti, tj);
@@ -495,18 +506,18 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
 
 // X' = s[p] X, or (last) the update itself.
 template <int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int from, int last) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int p, int from, int last) {
   typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
-  const int k = find(l, blk);
-  const Mat& t = l.t[k];
-  const int b = blk - l.blk0[k], nt = t.mp / TL::BM;
+  const int k = find(l, L_APPLY, blk);
+  const Mat& t = l->t[k];
+  const int b = blk - l->blk0[L_APPLY][k], nt = t.mp / TL::BM;
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
-  const f16* x = pickg(t.x, from);
-  const float* dp = pickg(t.d, p);
+  const f16* x = t.x[from];
+  const float* dp = t.d[p];
   TL tl;
-  tl.run(ring, pickg(t.s, p), t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
+  tl.run(ring, t.s[p], t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
@@ -527,7 +538,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(Mats l, int p, int
       if (!last) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
-        f16* out = pickg(t.x, from ^ 1);
+        f16* out = t.x[from ^ 1];
         put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
       } else {
         store_update(t, r, c0, y);
@@ -798,13 +809,11 @@ size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_
     return p;
   };
   l.count = n;
+  take(sizeof(Mats));   // the launches' table
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
     describe(*d[k], t);
-    if (kind == WHOLE32 || kind == WHOLE64) {
-      pos += 256;   // unused: a call asks for a workspace whatever its sizes
-      continue;
-    }
+    if (kind == WHOLE32 || kind == WHOLE64) continue;
     t.mp = up(t.m);
     t.np = up(t.n);
     const long size = (long)t.rows * t.cols;
@@ -840,16 +849,16 @@ void each_list(int n, const tgp_muon_tensor* t, F go) {
   }
 }
 
-// Fills blk0 with blocks(t) of each matrix; returns the grid.
+// Fills blk0 of a launch with blocks(t) of each matrix; returns the grid.
 template <typename F>
-unsigned deal(Mats& l, F blocks) {
-  int at = 0;
+unsigned deal(Mats& l, int launch, F blocks) {
+  int pos = 0;
   for (int k = 0; k < l.count; ++k) {
-    l.blk0[k] = at;
-    at += blocks(l.t[k]);
+    l.blk0[launch][k] = pos;
+    pos += blocks(l.t[k]);
   }
-  l.blk0[l.count] = at;
-  return (unsigned)at;
+  l.blk0[launch][l.count] = pos;
+  return (unsigned)pos;
 }
 
 hipError_t update_small(const Mats& l, bool m64, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
@@ -867,10 +876,11 @@ hipError_t update_small(const Mats& l, bool m64, float mu, bool nesterov, int st
   return launch_status();
 }
 
-hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
+hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, int steps, float eps,
+                       hipStream_t st) {
   double n = 0, gram = 0, cube = 0, cells = 0;
   bool wide = true;
-  long large = 0;
+  long t256 = 0, t128 = 0, g128 = 0;   // tiles of P X, of X X^T
   for (int k = 0; k < l.count; ++k) {
     const Mat& t = l.t[k];
     n += (double)t.rows * t.cols;
@@ -878,45 +888,53 @@ hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, fl
     cube += (double)t.m * t.m * t.m;
     cells += (double)t.m * t.m;
     wide = wide && t.mp % 256 == 0;
-    large += (long)(t.mp / 256) * (t.np / 128);
+    t256 += (long)(t.mp / 256) * (t.np / 128);
+    t128 += (long)(t.mp / 128) * (t.np / 128);
+    g128 += (long)uppers(t.mp / 128) * t.split;
   }
+  // Rows of a tile.  P X on tiles of 256 x 128 takes a quarter less from the
+  // caches and LDS than on 128 x 128 (2048 x 18432: 173 us, 178); it is taken
+  // where every matrix is cut into whole ones and they make two blocks a CU.
+  // Where 128 x 128 leaves CUs without one, 64 x 64 with twice the stages in
+  // flight.  The sums' order is the same in all of them.
+  const int ba = wide && t256 >= kBlocks ? 256 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
+  const unsigned gm = deal(l, L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
+  const unsigned gn = deal(l, L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
+  const unsigned gg = deal(l, L_GRAM, [&](const Mat& t) { return uppers(t.mp / bg) * t.split; });
+  const unsigned gs = deal(l, L_SUM, [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; });
+  const unsigned gp = deal(l, L_SYM, [](const Mat& t) { return uppers(t.mp / 64); });
+  const unsigned ga = deal(l, L_APPLY, [&](const Mat& t) { return (t.mp / ba) * (t.np / std::min(ba, 128)); });
   {
-    const unsigned g = deal(l, [](const Mat& t) { return t.norm_blocks; });
     ProfScope ps("muon_momentum", 4 * n, 12 * n, st);
-    TGP_LAUNCH(ps, muon_momentum, dim3(g), dim3(256), 0, st, l, mu, (int)nesterov);
+    TGP_LAUNCH(ps, muon_momentum, dim3(gm), dim3(256), 0, st, l, table, mu, (int)nesterov);
   }
   {
-    const unsigned g = deal(l, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
-    TGP_LAUNCH(ps, muon_normalize, dim3(g), dim3(256), 0, st, l, mu, (int)nesterov, eps);
+    TGP_LAUNCH(ps, muon_normalize, dim3(gn), dim3(256), 0, st, (const Mats*)table, mu, (int)nesterov, eps);
   }
-  // the same matrices, blocks dealt for each product.  P X on tiles of 256 x
-  // 128 takes a quarter less from the caches and LDS than on 128 x 128 (2048
-  // x 18432: 173 us, 178); it is taken where every matrix is cut into whole
-  // ones and they make two blocks a CU.
-  const int bm = wide && large >= kBlocks ? 256 : 128;
-  Mats lp = l, lg = l, ls = l, la = l;
-  const unsigned gg = deal(lg, [](const Mat& t) { return uppers(t.mp / 128) * t.split; });
-  const unsigned gs = deal(ls, [](const Mat& t) { return t.split > 1 ? uppers(t.mp / 128) * 4 : 0; });
-  const unsigned gp = deal(lp, [](const Mat& t) { return uppers(t.mp / 64); });
-  const unsigned ga = deal(la, [&](const Mat& t) { return (t.mp / bm) * (t.np / 128); });
   auto poly = [&](int a, int c) {
     ProfScope ps("muon_poly", cube, 4 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, a, 0, c);
+    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, (const Mats*)table, a, 0, c);
   };
   auto mul = [&](int a, int b, int c) {
     ProfScope ps("muon_mul", cube, 6 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, lp, a, b, c);
+    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, (const Mats*)table, a, b, c);
   };
   int from = 0;
   for (int s = 0; s < steps;) {
     {
       ProfScope ps("muon_gram", gram, 2 * n + 2 * cells, st);
-      TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg), dim3(256), 0, st, lg, from, 0, 0);
+      if (bg == 128)
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg), dim3(256), 0, st, (const Mats*)table, from, 0, 0);
+      else
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 1, 1, 2, 2, 8>), dim3(gg), dim3(256), 0, st, (const Mats*)table, from, 0, 0);
     }
     if (gs) {
       ProfScope ps("muon_gram_sum", 0, 0, st);
-      TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs), dim3(256), 0, st, ls);
+      if (bg == 128)
+        TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs), dim3(256), 0, st, (const Mats*)table);
+      else
+        TGP_LAUNCH(ps, (muon_gram_sum<1, 1, 2, 2>), dim3(gs), dim3(256), 0, st, (const Mats*)table);
     }
     poly(0, 1);
     int p = 1;
@@ -932,10 +950,12 @@ hipError_t update_list(Mats& l, bool two, float mu, bool nesterov, int steps, fl
     {
       const int last = s == steps;
       ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
-      if (bm == 256)
-        TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga), dim3(256), 0, st, la, p, from, last);
+      if (ba == 256)
+        TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
+      else if (ba == 128)
+        TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
       else
-        TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga), dim3(256), 0, st, la, p, from, last);
+        TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 8>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
     }
     from ^= 1;
   }
@@ -960,9 +980,10 @@ hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov,
   each_list(n, t, [&](int kind, const tgp_muon_tensor* const* d, int count) {
     if (e != hipSuccess) return;
     Mats l;
+    Mats* table = (Mats*)((char*)ws + pos);
     pos = lay_out(kind, count, d, (char*)ws, pos, l);
     e = kind == WHOLE32 || kind == WHOLE64 ? update_small(l, kind == WHOLE64, mu, nesterov, steps, eps, st)
-                                           : update_list(l, kind == PAIRS, mu, nesterov, steps, eps, st);
+                                           : update_list(l, table, kind == PAIRS, mu, nesterov, steps, eps, st);
   });
   return e;
 }
