@@ -248,9 +248,10 @@ struct Tile {
 
   f32x16 acc[MT][NT];
 
-  // Chunk q's slot in row `row`: eight consecutive rows read at one chunk, and
-  // (TR) half rows of four consecutive rows, hit distinct banks.
-  __device__ __forceinline__ static int kswz(int row, int q) { return q ^ ((row >> 1) & 3); }
+  // Chunk q's slot in row `row`: sixteen rows read at one chunk, four each of
+  // any remainder by 4, and (TR) half rows of four consecutive rows, hit
+  // distinct banks (256 bytes).
+  __device__ __forceinline__ static int kswz(int row, int q) { return q ^ ((row >> 2) & 3); }
   __device__ __forceinline__ static int rswz(int row, int q) { return q ^ (row & 2); }
 
   // L and R: matrices of lrows and rrows rows; stages k0 .. k1 of the sum.
