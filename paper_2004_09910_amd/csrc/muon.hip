@@ -80,10 +80,17 @@ __device__ __forceinline__ int find(const Mats* l, int launch, int blk) {
   return __builtin_amdgcn_readfirstlane(__popcll(__ballot(at_or_before)) - 1);
 }
 
+// A pointer read from the table, as one to global memory (else the compiler
+// takes generic loads and stores).
+template <typename T>
+__device__ __forceinline__ T* gm(T* p) {
+  return (T*)(__attribute__((address_space(1))) T*)(uintptr_t)p;
+}
+
 __device__ __forceinline__ float update_of(const Mat& t, long i, float mu, int nesterov) {
-  const float g = t.grad[i];
-  if (!t.mom) return g;
-  return nesterov ? g + mu * t.mom[i] : t.mom[i];
+  const float g = gm(t.grad)[i];
+  if (!gm(t.mom)) return g;
+  return nesterov ? g + mu * gm(t.mom)[i] : gm(t.mom)[i];
 }
 
 // Sum over the block's 256 threads (the same value in all of them).
@@ -106,8 +113,8 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float 
   const Mat& t = l.t[k];
   const int b = blockIdx.x - l.blk0[L_MOMENTUM][k];
   const long N = (long)t.rows * t.cols, N4 = N / 4, step = (long)t.norm_blocks * 256;
-  const float4* g4 = (const float4*)t.grad;
-  float4* m4 = (float4*)t.mom;
+  const float4* g4 = (const float4*)gm(t.grad);
+  float4* m4 = (float4*)gm(t.mom);
   double s = 0;
   auto one = [&](float g, float& m) {
     float u = g;
@@ -138,12 +145,12 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float 
   }
   const long e = 4 * N4 + threadIdx.x;   // the last one to three values
   if (b == 0 && e < N) {
-    float m = t.mom ? t.mom[e] : 0.f;
-    one(t.grad[e], m);
-    if (t.mom) t.mom[e] = m;
+    float m = gm(t.mom) ? gm(t.mom)[e] : 0.f;
+    one(gm(t.grad)[e], m);
+    if (gm(t.mom)) gm(t.mom)[e] = m;
   }
   s = block_sum(s, sh);
-  if (threadIdx.x == 0) t.norm[b] = s;
+  if (threadIdx.x == 0) gm(t.norm)[b] = s;
 }
 
 // X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
@@ -156,7 +163,7 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
   const Mat& t = l->t[k];
   const bool flip = t.rows > t.cols;
   double s = 0;
-  for (int q = threadIdx.x; q < t.norm_blocks; q += 256) s += t.norm[q];
+  for (int q = threadIdx.x; q < t.norm_blocks; q += 256) s += gm(t.norm)[q];
   const double norm = sqrt(block_sum(s, sh)) + eps;
   // a zero matrix stays zero; 1 / |U| may pass float32's range, so the product
   // below is taken in float64
@@ -165,7 +172,7 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
     f16x8 h;
 #pragma unroll
     for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(f[v] * inv);
-    *(f16x8*)(t.x[0] + at(t.mp, i, j)) = h;
+    *(f16x8*)(gm(t.x[0]) + at(t.mp, i, j)) = h;
   };
   const int b0 = (blockIdx.x - l->blk0[L_NORMALIZE][k]) * t.norm_per;
   for (int b = b0; b < b0 + t.norm_per; ++b) {
@@ -198,10 +205,10 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
       const long src = (long)i * t.cols + j;
       float u[8];
       if (i < t.rows && j + 8 <= t.cols && t.cols % 4 == 0) {
-        const float4 g0 = *(const float4*)(t.grad + src), g1 = *(const float4*)(t.grad + src + 4);
+        const float4 g0 = *(const float4*)(gm(t.grad) + src), g1 = *(const float4*)(gm(t.grad) + src + 4);
         const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
-        if (t.mom) {
-          const float4 m0 = *(const float4*)(t.mom + src), m1 = *(const float4*)(t.mom + src + 4);
+        if (gm(t.mom)) {
+          const float4 m0 = *(const float4*)(gm(t.mom) + src), m1 = *(const float4*)(gm(t.mom) + src + 4);
           const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
 #pragma unroll
           for (int v = 0; v < 8; ++v) u[v] = nesterov ? g[v] + mu * m[v] : m[v];
@@ -236,8 +243,9 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 // (columns) 8 (v / 4) + 4 (l / 32) + v % 4.
 //
 // A stage is visible to all waves one turn before it is multiplied, so that
-// fragments are always read one step ahead of their products, over the
-// stages' barriers too.
+// its fragments are read while the stage before it is (a step of 16 ahead, the
+// 4 products of a 64 x 64 wave tile do not cover the reads: X X^T of 2048 x
+// 18432 109 us, 101 with a stage ahead).
 template <int MT, int NT, int WM, int WN, int NS, bool TR, bool SWAP>
 struct Tile {
   static constexpr int NW = WM * WN, BM = 32 * MT * WM, BN = 32 * NT * WN;
@@ -254,14 +262,17 @@ struct Tile {
   __device__ __forceinline__ static int kswz(int row, int q) { return q ^ ((row >> 2) & 3); }
   __device__ __forceinline__ static int rswz(int row, int q) { return q ^ (row & 2); }
 
-  // L and R: matrices of lrows and rrows rows; stages k0 .. k1 of the sum.
+  // L and R: matrices of lrows and rrows rows, R of rcols columns (what a TR
+  // tile has beyond them reads as zeros); stages k0 .. k1 (one at least) of the
+  // sum.
   __device__ __forceinline__ void run(unsigned char* ring, const f16* L, int lrows, int i0, const f16* R,
-                                      int rrows, int j0, int k0, int k1) {
+                                      int rrows, int rcols, int j0, int k0, int k1) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const u32x4 rl = make_rsrc(L + (long)i0 * 32, 0x7fffffff);
-    const u32x4 rr = make_rsrc(TR ? R + (long)j0 * rrows : R + (long)j0 * 32, 0x7fffffff);
+    const u32x4 rr = TR ? make_rsrc(R + (long)j0 * rrows, (rcols - j0) * rrows * 2)
+                        : make_rsrc(R + (long)j0 * 32, 0x7fffffff);
     // this lane's byte offset in chunk `wave` and the distance to its next
     // ones; rows of chunks NW apart agree in their swizzle (NW is even)
     const int r16 = wave * 16 + (lane >> 2);
@@ -287,44 +298,51 @@ struct Tile {
 #pragma unroll
     for (int k = 0; k < NS - 1; ++k)
       if (k < total) issue(k0 + k, k);
-    u32x4 a[2][MT], b[2][NT];
+    // fragments of two stages in turn: those of the next are read while this
+    // one's are multiplied
+    u32x4 a[2][2][MT], b[2][2][NT];
     const int fr = lane & 31;                              // row of a fragment
     const int kb = 8 * (lane >> 5) + ((lane & 15) >> 2);   // (TR) row of the transpose load
     const int cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);   // (TR) its chunk
-    auto load = [&](int slot, int kk, int buf) __attribute__((always_inline)) {
+    auto load = [&](int slot, int z) __attribute__((always_inline)) {
       const unsigned char* Ls = ring + slot * SB;
       const unsigned char* Rs = Ls + LCH * 1024;
-      const int q = kswz(fr, 2 * kk + (lane >> 5)) * 16;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[buf][i] = *(const u32x4*)(Ls + ((wm * MT + i) * 32 + fr) * 64 + q);
+      for (int kk = 0; kk < 2; ++kk) {
+        const int q = kswz(fr, 2 * kk + (lane >> 5)) * 16;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if constexpr (TR)
-          b[buf][j] = frag_tr(Rs + (wn * NT + j) * 2048 + (16 * kk + kb) * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1), 64);
-        else
-          b[buf][j] = *(const u32x4*)(Rs + ((wn * NT + j) * 32 + fr) * 64 + q);
+        for (int i = 0; i < MT; ++i) a[z][kk][i] = *(const u32x4*)(Ls + ((wm * MT + i) * 32 + fr) * 64 + q);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if constexpr (TR)
+            b[z][kk][j] = frag_tr(Rs + (wn * NT + j) * 2048 + (16 * kk + kb) * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1), 64);
+          else
+            b[z][kk][j] = *(const u32x4*)(Rs + ((wn * NT + j) * 32 + fr) * 64 + q);
+        }
       }
     };
     wait_stages<NS, PER>(min(NS - 2, total - 1));
     ring_barrier();
-    if (total > 0) load(0, 0, 0);
-    for (int idx = 0; idx < total; ++idx) {
+    load(0, 0);
+    auto turn = [&](int idx, int z) __attribute__((always_inline)) {
       // stage idx + 1 has landed, for every wave; slot idx - 1 has been read
       wait_stages<NS - 1, PER>(min(NS - 3, total - 2 - idx));
       ring_barrier();
       if (idx + NS - 1 < total) issue(k0 + idx + NS - 1, (idx + NS - 1) % NS);
+      if (idx + 1 < total) load((idx + 1) % NS, z ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        if (kk == 0) load(idx % NS, 1, 1);
-        else if (idx + 1 < total) load((idx + 1) % NS, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            acc[i][j] = SWAP ? mfma(b[kk][j], a[kk][i], acc[i][j]) : mfma(a[kk][i], b[kk][j], acc[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+            acc[i][j] = SWAP ? mfma(b[z][kk][j], a[z][kk][i], acc[i][j]) : mfma(a[z][kk][i], b[z][kk][j], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int idx = 0; idx < total; idx += 2) {
+      turn(idx, 0);
+      if (idx + 1 < total) turn(idx + 1, 1);
     }
   }
 };
@@ -415,14 +433,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
   const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
   const int k0 = MODE == GRAM ? (int)((long)nk * sp / t.split) : 0;
   const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
-  const f16* L = MODE == GRAM ? t.x[a] : t.s[a];
-  const f16* R = MODE == MUL ? t.s[b] : L;
+  const f16* L = MODE == GRAM ? gm(t.x[a]) : gm(t.s[a]);
+  const f16* R = MODE == MUL ? gm(t.s[b]) : L;
   TL tl;
-  tl.run(ring, L, t.mp, i0, R, t.mp, j0, k0, k1);
-  const float* dl = t.d[a];
-  const float* dr = MODE == MUL ? t.d[b] : dl;
-  f16* out = t.s[c];
-  float* dout = t.d[c];
+  tl.run(ring, L, t.mp, i0, R, t.mp, 0, j0, k0, k1);
+  const float* dl = gm(t.d[a]);
+  const float* dr = MODE == MUL ? gm(t.d[b]) : dl;
+  f16* out = gm(t.s[c]);
+  float* dout = gm(t.d[c]);
   const int wave = threadIdx.x >> 6, wi = i0 + wave / WN * MT * 32, wj = j0 + wave % WN * NT * 32;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -430,7 +448,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
     for (int j = 0; j < NT; ++j) {
       const f32x16& acc = tl.acc[i][j];
       if (MODE == GRAM && t.split > 1) {
-        f32x4_t* part = (f32x4_t*)t.part +
+        f32x4_t* part = (f32x4_t*)gm(t.part) +
                         ((((long)q * WM * WN + wave) * MT + i) * NT + j) * 256 + (threadIdx.x & 63);
 #pragma unroll
         for (int g = 0; g < 4; ++g) part[64 * g] = part_of(acc, g);
@@ -479,7 +497,7 @@ __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l)
   for (int s = 0; s < t.split; ++s)
 #pragma unroll
     for (int g = 0; g < 4; ++g) acc[g] += in[s * step + 64 * g];
-  store_sym(t.s[0], t.d[0], t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BM + (wave % WN * NT + j) * 32,
+  store_sym(gm(t.s[0]), gm(t.d[0]), t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BM + (wave % WN * NT + j) * 32,
             ti != tj, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 
@@ -494,13 +512,13 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
     for (int g = 0; g < 8; ++g) pk[g] = f2bf(y[2 * g]) | (f2bf(y[2 * g + 1]) << 16);
     put8(pk, [&](int h, u32x4 c) {
       const int cc = c0 + 16 * h + 8 * hi;
-      if (r < t.m && cc < t.n) *(u32x4*)(t.out + (long)r * t.cols + cc) = c;
+      if (r < t.m && cc < t.n) *(u32x4*)(gm(t.out) + (long)r * t.cols + cc) = c;
     });
   } else {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int c = c0 + 8 * (v / 4) + 4 * hi + v % 4;
-      if (r < t.m && c < t.n) t.out[flip ? (long)c * t.cols + r : (long)r * t.cols + c] = (bf16_t)f2bf(y[v]);
+      if (r < t.m && c < t.n) gm(t.out)[flip ? (long)c * t.cols + r : (long)r * t.cols + c] = (bf16_t)f2bf(y[v]);
     }
   }
 }
@@ -515,10 +533,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
   const Mat& t = l->t[k];
   const int b = blk - l->blk0[L_APPLY][k], nt = t.mp / TL::BM;
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
-  const f16* x = t.x[from];
-  const float* dp = t.d[p];
+  const f16* x = gm(t.x[from]);
+  const float* dp = gm(t.d[p]);
   TL tl;
-  tl.run(ring, t.s[p], t.mp, i0, x, t.mp, j0, 0, t.mp / 32);
+  tl.run(ring, gm(t.s[p]), t.mp, i0, x, t.mp, t.np, j0, 0, t.mp / 32);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
@@ -527,6 +545,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int c0 = j0 + (wave % WN * NT + j) * 32;
+      if (c0 >= t.np) continue;
       const f32x16& acc = tl.acc[i][j];
       unsigned pk[8];
       float y[16];
@@ -539,7 +558,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
       if (!last) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
-        f16* out = t.x[from ^ 1];
+        f16* out = gm(t.x[from ^ 1]);
         put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
       } else {
         store_update(t, r, c0, y);
@@ -592,12 +611,12 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
     if (z * kSmallT >= chunks) break;
     if (!place(z, i, j) || i >= t.m) continue;
     if (vec && j + 8 <= t.n) {
-      const float4* g = (const float4*)(t.grad + i * t.cols + j);
+      const float4* g = (const float4*)(gm(t.grad) + i * t.cols + j);
       const float4 g0 = g[0], g1 = g[1];
       u[z][0] = g0.x; u[z][1] = g0.y; u[z][2] = g0.z; u[z][3] = g0.w;
       u[z][4] = g1.x; u[z][5] = g1.y; u[z][6] = g1.z; u[z][7] = g1.w;
-      if (t.mom) {
-        const float4* q = (const float4*)(t.mom + i * t.cols + j);
+      if (gm(t.mom)) {
+        const float4* q = (const float4*)(gm(t.mom) + i * t.cols + j);
         const float4 m0 = q[0], m1 = q[1];
         m[z][0] = m0.x; m[z][1] = m0.y; m[z][2] = m0.z; m[z][3] = m0.w;
         m[z][4] = m1.x; m[z][5] = m1.y; m[z][6] = m1.z; m[z][7] = m1.w;
@@ -607,8 +626,8 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
       for (int v = 0; v < 8; ++v)
         if (j + v < t.n) {
           const int e = flip ? (j + v) * t.cols + i : i * t.cols + j + v;
-          u[z][v] = t.grad[e];
-          if (t.mom) m[z][v] = t.mom[e];
+          u[z][v] = gm(t.grad)[e];
+          if (gm(t.mom)) m[z][v] = gm(t.mom)[e];
         }
     }
   }
@@ -618,20 +637,20 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
     int i, j;
     if (z * kSmallT >= chunks) break;
     if (!place(z, i, j) || i >= t.m) continue;
-    if (t.mom) {
+    if (gm(t.mom)) {
 #pragma unroll
       for (int v = 0; v < 8; ++v) {
         m[z][v] = mu * m[z][v] + u[z][v];
         u[z][v] = nesterov ? u[z][v] + mu * m[z][v] : m[z][v];
       }
       if (vec && j + 8 <= t.n) {
-        float4* q = (float4*)(t.mom + i * t.cols + j);
+        float4* q = (float4*)(gm(t.mom) + i * t.cols + j);
         q[0] = make_float4(m[z][0], m[z][1], m[z][2], m[z][3]);
         q[1] = make_float4(m[z][4], m[z][5], m[z][6], m[z][7]);
       } else {
 #pragma unroll
         for (int v = 0; v < 8; ++v)
-          if (j + v < t.n) t.mom[flip ? (j + v) * t.cols + i : i * t.cols + j + v] = m[z][v];
+          if (j + v < t.n) gm(t.mom)[flip ? (j + v) * t.cols + i : i * t.cols + j + v] = m[z][v];
       }
     }
 #pragma unroll
@@ -799,10 +818,12 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 
 // Describes n (at most kMaxMats) matrices laid out from byte `pos` of the
 // workspace ws on; returns their end.  The sum of A = X X^T is split where a
-// matrix has too few tiles to fill the chip: into ranges for about kBlocks
-// blocks of kRange stages at least (writing and reading back a partial tile
-// takes the time of 20 stages).  The ranges depend on the matrix alone, so
-// that its update does not depend on the others of the call.
+// matrix has too few tiles to fill the chip: into as many ranges as make at
+// most kBlocks blocks (one more than run at once waits for all of them: 2048 x
+// 18432 in 3 ranges 105 us, in 4 126, in 7 99 and 5 more to add them up), of
+// kRange stages at least (writing and reading back a partial tile takes the
+// time of 20 stages).  The ranges depend on the matrix alone, so that its
+// update does not depend on the others of the call.
 size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
     char* p = ws + pos;
@@ -826,8 +847,7 @@ size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_
       t.s[z] = (f16*)take((size_t)t.mp * t.mp * 2);
       t.d[z] = (float*)take((size_t)t.mp * 4);
     }
-    const long range = std::max<long>(kRange, cdiv((long)uppers(t.mp / 128) * (t.np / 32), kBlocks));
-    t.split = (int)((t.np / 32 + range - 1) / range);
+    t.split = std::max(1, std::min(kBlocks / uppers(t.mp / 128), t.np / 32 / kRange));
     t.part = nullptr;
     if (t.split > 1) t.part = (float*)take((size_t)t.split * uppers(t.mp / 128) * 128 * 128 * sizeof(float));
   }
@@ -880,31 +900,29 @@ hipError_t update_small(const Mats& l, bool m64, float mu, bool nesterov, int st
 hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, int steps, float eps,
                        hipStream_t st) {
   double n = 0, gram = 0, cube = 0, cells = 0;
-  bool wide = true;
-  long t256 = 0, t128 = 0, g128 = 0;   // tiles of P X, of X X^T
+  long t192 = 0, t128 = 0, g128 = 0;   // tiles of P X, of X X^T
   for (int k = 0; k < l.count; ++k) {
     const Mat& t = l.t[k];
     n += (double)t.rows * t.cols;
     gram += (double)t.m * t.m * t.n;
     cube += (double)t.m * t.m * t.m;
     cells += (double)t.m * t.m;
-    wide = wide && t.mp % 256 == 0;
-    t256 += (long)(t.mp / 256) * (t.np / 128);
+    t192 += (long)(t.mp / 128) * cdiv(t.np, 192);
     t128 += (long)(t.mp / 128) * (t.np / 128);
     g128 += (long)uppers(t.mp / 128) * t.split;
   }
-  // Rows of a tile.  P X on tiles of 256 x 128 takes a quarter less from the
-  // caches and LDS than on 128 x 128 (2048 x 18432: 173 us, 178); it is taken
-  // where every matrix is cut into whole ones and they make two blocks a CU.
-  // Where 128 x 128 leaves CUs without one, 64 x 64 with twice the stages in
-  // flight.  The sums' order is the same in all of them.
-  const int ba = wide && t256 >= kBlocks ? 256 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
+  // Columns of a tile of P X and X X^T.  P X on tiles of 128 x 192 takes a
+  // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 158 us,
+  // 184); it is taken where the tiles make two blocks a CU.  Where 128 x 128
+  // leaves CUs without one, 64 x 64 with twice the stages in flight.  The sums'
+  // order is the same in all of them.
+  const int ba = t192 >= kBlocks ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
   const unsigned gm = deal(l, L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
   const unsigned gn = deal(l, L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
   const unsigned gg = deal(l, L_GRAM, [&](const Mat& t) { return uppers(t.mp / bg) * t.split; });
   const unsigned gs = deal(l, L_SUM, [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; });
   const unsigned gp = deal(l, L_SYM, [](const Mat& t) { return uppers(t.mp / 64); });
-  const unsigned ga = deal(l, L_APPLY, [&](const Mat& t) { return (t.mp / ba) * (t.np / std::min(ba, 128)); });
+  const unsigned ga = deal(l, L_APPLY, [&](const Mat& t) { return (t.mp / std::min(ba, 128)) * cdiv(t.np, ba); });
   {
     ProfScope ps("muon_momentum", 4 * n, 12 * n, st);
     TGP_LAUNCH(ps, muon_momentum, dim3(gm), dim3(256), 0, st, l, table, mu, (int)nesterov);
@@ -951,8 +969,8 @@ hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, 
     {
       const int last = s == steps;
       ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
-      if (ba == 256)
-        TGP_LAUNCH(ps, (muon_apply<4, 2, 2, 2, 3>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
+      if (ba == 192)
+        TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
       else if (ba == 128)
         TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
       else
