@@ -347,6 +347,16 @@ struct Tile {
   }
 };
 
+// The tile that block `blk` of n takes.  Workgroups are dealt round-robin over
+// the 8 XCDs, each with its own L2: sixteen consecutive tiles, which share a
+// panel of X, go to one XCD, and every 128 tiles are spread over all of them,
+// since tiles of one launch differ in length (a contiguous eighth for each XCD
+// leaves some with the long ones).
+__device__ __forceinline__ int grouped(int blk, int n) {
+  const int w = blk & ~127, r = blk & 127;
+  return w + 128 <= n ? w + (r & 7) * 16 + (r >> 3) : blk;
+}
+
 // Eight consecutive values of a fragment's lane as one 16-byte chunk: lanes l
 // and l + 32 hold values 8 g + 0..3 and 8 g + 4..7; swapping the halves of
 // groups 2 h and 2 h + 1 leaves each lane one whole group, 2 h + l / 32.
@@ -422,7 +432,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
   typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
   static_assert(TL::BM == TL::BN, "square tiles");
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
-  const int blk = xcd_remap(blockIdx.x, gridDim.x);
+  const int blk = grouped(blockIdx.x, gridDim.x);
   constexpr int LAUNCH = MODE == GRAM ? L_GRAM : L_SYM;
   const int k = find(l, LAUNCH, blk);
   const Mat& t = l->t[k];
@@ -491,7 +501,7 @@ __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l)
   const int lane = threadIdx.x & 63, wave = q / (MT * NT), i = q / NT % MT, j = q % NT;
   int ti, tj;
   upper(tile, nt, ti, tj);
-  const f32x4_t* in = (const f32x4_t*)t.part + ((long)tile * FR + q) * 256 + lane;
+  const f32x4_t* in = (const f32x4_t*)gm(t.part) + ((long)tile * FR + q) * 256 + lane;
   const long step = (long)tiles * FR * 256;
   f32x4_t acc[4] = {};
   for (int s = 0; s < t.split; ++s)
@@ -528,7 +538,7 @@ template <int MT, int NT, int WM, int WN, int NS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int p, int from, int last) {
   typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
-  const int blk = xcd_remap(blockIdx.x, gridDim.x);
+  const int blk = grouped(blockIdx.x, gridDim.x);
   const int k = find(l, L_APPLY, blk);
   const Mat& t = l->t[k];
   const int b = blk - l->blk0[L_APPLY][k], nt = t.mp / TL::BM;
@@ -781,7 +791,7 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kPad = 128;
 constexpr int kBlocks = 512;   // two a CU
-constexpr int kRange = 48;     // stages of 32 sum values
+constexpr int kRange = 64;     // stages of 32 sum values
 int up(int x) { return (x + kPad - 1) / kPad * kPad; }
 int uppers(int nt) { return nt * (nt + 1) / 2; }
 
@@ -854,19 +864,27 @@ size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_
   return pos;
 }
 
-// Deals the matrices into lists of one kind each, in their order.  Calls
-// go(kind, list of pointers, count).
+// Deals the matrices into lists of one kind each; within a list those of the
+// longest sums come first (stable), so that the short ones fill up its
+// launches' ends.  Calls go(kind, list of pointers, count).
 template <typename F>
 void each_list(int n, const tgp_muon_tensor* t, F go) {
   for (int kind = 0; kind < KINDS; ++kind) {
     const tgp_muon_tensor* list[kMaxMats];
     int count = 0;
+    auto flush = [&]() {
+      std::stable_sort(list, list + count, [](const tgp_muon_tensor* a, const tgp_muon_tensor* b) {
+        return std::min(a->rows, a->cols) > std::min(b->rows, b->cols);
+      });
+      if (count) go(kind, list, count);
+      count = 0;
+    };
     for (int k = 0; k < n; ++k) {
       if (kind_of(t[k]) != kind) continue;
       list[count++] = t + k;
-      if (count == kMaxMats) go(kind, list, count), count = 0;
+      if (count == kMaxMats) flush();
     }
-    if (count) go(kind, list, count);
+    flush();
   }
 }
 
