@@ -24,6 +24,7 @@
 // step: three at once lose small singular values to float16's 11 bits, 8e-3
 // of the update's norm where two leave 1.5e-3.)
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "mfma_util.h"
@@ -254,6 +255,8 @@ struct Tile {
   static_assert(LCH % NW == 0 && RCH % NW == 0 && NS * SB <= 160 * 1024, "whole DMA rounds, LDS ring");
   static_assert(NS >= 3, "a stage ahead");
 
+  static constexpr int NL = LCH / NW, NR = RCH / NW;   // chunks of L and R a wave
+
   f32x16 acc[MT][NT];
 
   // Chunk q's slot in row `row`: sixteen rows read at one chunk, four each of
@@ -273,77 +276,139 @@ struct Tile {
     const u32x4 rl = make_rsrc(L + (long)i0 * 32, 0x7fffffff);
     const u32x4 rr = TR ? make_rsrc(R + (long)j0 * rrows, (rcols - j0) * rrows * 2)
                         : make_rsrc(R + (long)j0 * 32, 0x7fffffff);
-    // this lane's byte offset in chunk `wave` and the distance to its next
-    // ones; rows of chunks NW apart agree in their swizzle (NW is even)
-    const int r16 = wave * 16 + (lane >> 2);
-    const int lo = r16 * 64 + 16 * kswz(r16, lane & 3);
-    const int rrow = (wave & 1) * 16 + (lane >> 2);
-    const int ro = TR ? (wave >> 1) * rrows * 64 + rrow * 64 + 16 * rswz(rrow, lane & 3)
-                      : r16 * 64 + 16 * kswz(r16, lane & 3);
+    // byte offsets of this lane in its chunks of a stage (rows of chunks NW
+    // apart agree in their swizzle, NW being even), and of the next stage
     static_assert(NW % 2 == 0, "pairs of chunks");
-    auto issue = [&](int k, int slot) __attribute__((always_inline)) {
+    const int r16 = wave * 16 + (lane >> 2), rrow = (wave & 1) * 16 + (lane >> 2);
+    int vl[3] = {}, vr[3] = {};
 #pragma unroll
-      for (int u = 0; u < LCH / NW; ++u)
-        dma16(rl, TGP_LDS(ring + slot * SB + (NW * u + wave) * 1024), lo, k * lrows * 64 + u * NW * 1024);
+    for (int u = 0; u < NL; ++u) vl[u] = r16 * 64 + 16 * kswz(r16, lane & 3) + u * NW * 1024;
 #pragma unroll
-      for (int u = 0; u < RCH / NW; ++u)
-        dma16(rr, TGP_LDS(ring + slot * SB + (LCH + NW * u + wave) * 1024), ro,
-              TR ? k * 2048 + u * (NW / 2) * rrows * 64 : k * rrows * 64 + u * NW * 1024);
+    for (int u = 0; u < NR; ++u)
+      vr[u] = TR ? ((wave >> 1) + u * (NW / 2)) * rrows * 64 + rrow * 64 + 16 * rswz(rrow, lane & 3)
+                 : r16 * 64 + 16 * kswz(r16, lane & 3) + u * NW * 1024;
+    const int stl = lrows * 64, str = TR ? 2048 : rrows * 64;
+    int sl = __builtin_amdgcn_readfirstlane(k0 * stl), sr = __builtin_amdgcn_readfirstlane(k0 * str);
+    const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
+    auto issue = [&](auto slot) __attribute__((always_inline)) {
+      issue_stage<decltype(slot)::value * SB>(dst, vl, vr, rl, rr, sl, sr);
+      sl += stl;
+      sr += str;
     };
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{};
     const int total = k1 - k0;
-#pragma unroll
-    for (int k = 0; k < NS - 1; ++k)
-      if (k < total) issue(k0 + k, k);
     // fragments of two stages in turn: those of the next are read while this
     // one's are multiplied
     u32x4 a[2][2][MT], b[2][2][NT];
-    const int fr = lane & 31;                              // row of a fragment
-    const int kb = 8 * (lane >> 5) + ((lane & 15) >> 2);   // (TR) row of the transpose load
+    const int fr = lane & 31;                                   // row of a fragment
+    const int kb = 8 * (lane >> 5) + ((lane & 15) >> 2);        // (TR) row of the transpose load
     const int cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);   // (TR) its chunk
-    auto load = [&](int slot, int z) __attribute__((always_inline)) {
-      const unsigned char* Ls = ring + slot * SB;
-      const unsigned char* Rs = Ls + LCH * 1024;
+    const int la = (wm * MT * 32 + fr) * 64 + kswz(fr, lane >> 5) * 16;
+    const int lb = LCH * 1024 + (TR ? wn * NT * 2048 + kb * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1)
+                                    : (wn * NT * 32 + fr) * 64 + kswz(fr, lane >> 5) * 16);
+    auto load = [&](auto slot, int z) __attribute__((always_inline)) {
+      const unsigned char* s = ring + decltype(slot)::value * SB;
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        const int q = kswz(fr, 2 * kk + (lane >> 5)) * 16;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[z][kk][i] = *(const u32x4*)(Ls + ((wm * MT + i) * 32 + fr) * 64 + q);
+        for (int i = 0; i < MT; ++i) a[z][kk][i] = *(const u32x4*)(s + (la ^ (32 * kk)) + i * 2048);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          if constexpr (TR)
-            b[z][kk][j] = frag_tr(Rs + (wn * NT + j) * 2048 + (16 * kk + kb) * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1), 64);
-          else
-            b[z][kk][j] = *(const u32x4*)(Rs + ((wn * NT + j) * 32 + fr) * 64 + q);
+          if constexpr (TR) b[z][kk][j] = frag_tr(s + lb + j * 2048 + kk * 1024, 64);
+          else b[z][kk][j] = *(const u32x4*)(s + (lb ^ (32 * kk)) + j * 2048);
         }
       }
     };
+    each<NS - 1>([&](auto k) {
+      if (decltype(k)::value < total) issue(k);
+    });
     wait_stages<NS, PER>(min(NS - 2, total - 1));
     ring_barrier();
-    load(0, 0);
-    auto turn = [&](int idx, int z) __attribute__((always_inline)) {
-      // stage idx + 1 has landed, for every wave; slot idx - 1 has been read
-      wait_stages<NS - 1, PER>(min(NS - 3, total - 2 - idx));
+    load(std::integral_constant<int, 0>(), 0);
+    // Stage idx (slot Z).  At its barrier stage idx + 1 has landed, for every
+    // wave, and slot idx - 1 has been read.  A wave issues an instruction every
+    // few clocks, so what surrounds the products is kept to a handful: slots
+    // are constants, and addresses advance by two additions.  STEADY: the stage
+    // to be issued exists.
+    auto turn = [&](int idx, auto zc, auto steady) __attribute__((always_inline)) {
+      constexpr int Z = decltype(zc)::value;
+      constexpr bool STEADY = decltype(steady)::value;
+      if constexpr (STEADY) wait_vmcnt<(NS - 3) * PER>();
+      else wait_stages<NS - 1, PER>(min(NS - 3, total - 2 - idx));
       ring_barrier();
-      if (idx + NS - 1 < total) issue(k0 + idx + NS - 1, (idx + NS - 1) % NS);
-      if (idx + 1 < total) load((idx + 1) % NS, z ^ 1);
-      __builtin_amdgcn_sched_barrier(0);
+      if (STEADY || idx + NS - 1 < total) issue(std::integral_constant<int, (Z + NS - 1) % NS>());
+      if (STEADY || idx + 1 < total) load(std::integral_constant<int, (Z + 1) % NS>(), (Z + 1) % 2);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            acc[i][j] = SWAP ? mfma(b[z][kk][j], a[z][kk][i], acc[i][j]) : mfma(a[z][kk][i], b[z][kk][j], acc[i][j]);
+            acc[i][j] = SWAP ? mfma(b[Z % 2][kk][j], a[Z % 2][kk][i], acc[i][j])
+                             : mfma(a[Z % 2][kk][i], b[Z % 2][kk][j], acc[i][j]);
+      // reads between the products
+      if constexpr (STEADY) {
+        constexpr int MF = 2 * MT * NT, RD = 2 * (MT + (TR ? 2 : 1) * NT), PM = (RD + MF - 1) / MF;
+#pragma unroll
+        for (int m = 0; m < MF; ++m) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // a product
+          __builtin_amdgcn_sched_group_barrier(0x100, PM, 0);   // LDS reads
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
     };
-    for (int idx = 0; idx < total; idx += 2) {
-      turn(idx, 0);
-      if (idx + 1 < total) turn(idx + 1, 1);
+    static_assert(NS % 2 == 0, "fragment buffers in turn");
+    int idx = 0;
+    for (; idx + 2 * NS - 1 <= total; idx += NS)
+      each<NS>([&](auto z) { turn(idx + decltype(z)::value, z, std::true_type()); });
+    for (; idx < total; idx += NS)
+      each<NS>([&](auto z) {
+        if (idx + decltype(z)::value < total) turn(idx + decltype(z)::value, z, std::false_type());
+      });
+  }
+
+ private:
+  // f(0), f(1), .. f(N - 1), as constants
+  template <int N, typename F>
+  __device__ __forceinline__ static void each(F f) {
+    if constexpr (N > 0) {
+      each<N - 1>(f);
+      f(std::integral_constant<int, N - 1>());
     }
+  }
+
+  // The wave's chunks of one stage, global to LDS at dst + AT, NW KiB apart:
+  // L's at offsets vl + sl, then R's at vr + sr.  M0 holds the destination only
+  // inside (as in dma16, one wait state between writing it and the load).
+  template <int AT>
+  __device__ __forceinline__ static void issue_stage(unsigned dst, const int (&vl)[3], const int (&vr)[3],
+                                                     u32x4 rl, u32x4 rr, int sl, int sr) {
+    unsigned saved;
+#define TGP_FIRST "s_mov_b32 %0, m0\n\ts_add_u32 m0, %1, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 "
+#define TGP_NEXT "s_add_u32 m0, m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 "
+#define TGP_LAST "s_mov_b32 m0, %0"
+#define TGP_OPS "=&s"(saved) : "s"(dst), "i"(AT), "i"(NW * 1024), "s"(rl), "s"(rr), "s"(sl), "s"(sr)
+    if constexpr (NL == 1 && NR == 1)
+      asm volatile(TGP_FIRST "%8, %4, %6 offen lds\n\t" TGP_NEXT "%9, %5, %7 offen lds\n\t" TGP_LAST
+                   : TGP_OPS, "v"(vl[0]), "v"(vr[0]) : "memory", "scc");
+    else if constexpr (NL == 2 && NR == 2)
+      asm volatile(TGP_FIRST "%8, %4, %6 offen lds\n\t" TGP_NEXT "%9, %4, %6 offen lds\n\t"
+                   TGP_NEXT "%10, %5, %7 offen lds\n\t" TGP_NEXT "%11, %5, %7 offen lds\n\t" TGP_LAST
+                   : TGP_OPS, "v"(vl[0]), "v"(vl[1]), "v"(vr[0]), "v"(vr[1]) : "memory", "scc");
+    else {
+      static_assert(NL == 2 && NR == 3, "a tile of another shape");
+      asm volatile(TGP_FIRST "%8, %4, %6 offen lds\n\t" TGP_NEXT "%9, %4, %6 offen lds\n\t"
+                   TGP_NEXT "%10, %5, %7 offen lds\n\t" TGP_NEXT "%11, %5, %7 offen lds\n\t"
+                   TGP_NEXT "%12, %5, %7 offen lds\n\t" TGP_LAST
+                   : TGP_OPS, "v"(vl[0]), "v"(vl[1]), "v"(vr[0]), "v"(vr[1]), "v"(vr[2]) : "memory", "scc");
+    }
+#undef TGP_FIRST
+#undef TGP_NEXT
+#undef TGP_LAST
+#undef TGP_OPS
   }
 };
 
