@@ -475,14 +475,25 @@ __device__ __forceinline__ f32x4_t part_of(const f32x16& a, int g) {
   return f32x4_t{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
 }
 
-// Row and column of tile b of the upper triangle (row <= column) of nt x nt,
-// row by row.
+// Row and column of tile b of the upper triangle (row <= column) of nt x nt
+// tiles: bands of four rows, in a band the triangle on the diagonal, then
+// squares of 4 x 4, whose sixteen tiles share eight panels.
 __device__ __forceinline__ void upper(int b, int nt, int& r, int& c) {
-  r = 0;
-  while (b >= nt - r) {
-    b -= nt - r;
-    ++r;
+  int r0 = 0, h = min(4, nt);
+  for (int n; b >= (n = h * (h + 1) / 2 + h * (nt - r0 - h)); h = min(4, nt - r0)) {
+    b -= n;
+    r0 += 4;
   }
+  const int tri = h * (h + 1) / 2;
+  if (b >= tri) {   // only a band of four rows has columns beyond its triangle
+    b -= tri;
+    r = r0 + (b & 3);
+    c = r0 + 4 + (b >> 2);
+    return;
+  }
+  int k = 0;
+  while (b >= h - k) b -= h - k++;
+  r = r0 + k;
   c = r + b;
 }
 
