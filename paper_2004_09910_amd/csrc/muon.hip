@@ -448,27 +448,44 @@ __device__ __forceinline__ f32x4_t from_f16(const f16* p) {
 }
 
 // Stores one 32 x 32 fragment of a symmetric matrix of mp rows at rows i0,
-// columns j0, and its mirror image where the tile does not hold it already.
-// value(g, i, j) is what elements 4 g .. 4 g + 3 (rows i .. i + 3, column j)
-// become.
+// columns j0, and its mirror image where the tile does not hold it already:
+// eight consecutive rows of a column are eight columns of the mirror's row as
+// they are, and eight columns of a row come by way of `lds` (2 KiB of this
+// wave's).  value(g, i, j) is what elements 4 g .. 4 g + 3 (rows i .. i + 3,
+// column j) become.
 template <typename F>
-__device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int j0, bool mirror, F value) {
-  const int lane = threadIdx.x & 63, j = j0 + (lane & 31);
+__device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int j0, bool mirror,
+                                          unsigned char* lds, F value) {
+  const int lane = threadIdx.x & 63, hi = lane >> 5, fr = lane & 31, j = j0 + fr;
   unsigned pk[8];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const int i = i0 + 8 * g + 4 * (lane >> 5);
+    const int i = i0 + 8 * g + 4 * hi;
     const f32x4_t f = value(g, i, j);
-#pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      const f16 h = (f16)(f[z] * kSM);
-      if (i + z == j) d[j] = f[z] - (float)h * (1.f / kSM);
-      if (mirror) m[at(mp, i + z, j)] = h;
-    }
     pk[2 * g] = pack_f16(f[0] * kSM, f[1] * kSM);
     pk[2 * g + 1] = pack_f16(f[2] * kSM, f[3] * kSM);
+    if (i0 == j0)
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        if (i + z == j) d[j] = f[z] - (float)(f16)(f[z] * kSM) * (1.f / kSM);
+    // rows of 64 bytes, chunks swizzled so that neither the writes nor the
+    // transpose reads meet in a bank more than they must
+    if (mirror) *(uint2*)(lds + fr * 64 + (g ^ ((fr >> 2) & 3)) * 16 + 8 * hi) = make_uint2(pk[2 * g], pk[2 * g + 1]);
   }
-  put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * (lane >> 5))) = c; });
+  put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * hi)) = c; });
+  if (mirror) {
+    const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      uint2 v[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int row = 16 * kk + kb + 4 * z;
+        v[z] = lds_tr16(lds + row * 64 + (cb ^ ((row >> 2) & 3)) * 16 + 8 * (lane & 1));
+      }
+      *(u32x4*)(m + at(mp, i0 + fr, j0 + 16 * kk + 8 * hi)) = u32x4{v[0].x, v[0].y, v[1].x, v[1].y};
+    }
+  }
 }
 
 __device__ __forceinline__ f32x4_t part_of(const f32x16& a, int g) {
@@ -521,13 +538,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
   const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
   const f16* L = MODE == GRAM ? gm(t.x[a]) : gm(t.s[a]);
   const f16* R = MODE == MUL ? gm(t.s[b]) : L;
-  TL tl;
-  tl.run(ring, L, t.mp, i0, R, t.mp, 0, j0, k0, k1);
   const float* dl = gm(t.d[a]);
   const float* dr = MODE == MUL ? gm(t.d[b]) : dl;
   f16* out = gm(t.s[c]);
   float* dout = gm(t.d[c]);
   const int wave = threadIdx.x >> 6, wi = i0 + wave / WN * MT * 32, wj = j0 + wave % WN * NT * 32;
+  // L's and R's own elements of this wave's fragment (read where symmetry has
+  // them) and their diagonals' errors, on their way while the sum runs
+  static_assert(MODE == GRAM || MT * NT == 1, "one fragment's elements in registers");
+  const int lane = threadIdx.x & 63, col = wj + (lane & 31);
+  f32x4_t lv[4], rv[4], dlr[4];
+  float dlc = 0.f, drc = 0.f;
+  if constexpr (MODE != GRAM) {
+    dlc = dl[col];
+    drc = dr[col];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int r = wi + 8 * g + 4 * (lane >> 5);
+      lv[g] = from_f16(L + at(t.mp, col, r)) * (1.f / kSM);
+      rv[g] = MODE == POLY ? lv[g] : from_f16(R + at(t.mp, col, r)) * (1.f / kSM);
+      dlr[g] = *(const f32x4_t*)(dl + r);
+    }
+  }
+  TL tl;
+  tl.run(ring, L, t.mp, i0, R, t.mp, 0, j0, k0, k1);
+  ring_barrier();   // the ring is free
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -540,25 +575,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
         for (int g = 0; g < 4; ++g) part[64 * g] = part_of(acc, g);
         continue;
       }
-      store_sym(out, dout, t.mp, wi + 32 * i, wj + 32 * j, ti != tj, [&](int g, int r, int col) {
+      store_sym(out, dout, t.mp, wi + 32 * i, wj + 32 * j, ti != tj, ring + wave * 2048,
+                [&](int g, int r, int c) {
         if constexpr (MODE == GRAM) {
           return part_of(acc, g) * (1.f / (kSX * kSX));
         } else {
-          // element (r .. r + 3, col) of L and R, read where symmetry has it
-          const f32x4_t lv = from_f16(L + at(t.mp, col, r)) * (1.f / kSM);
-          const f32x4_t rv = MODE == POLY ? lv : from_f16(R + at(t.mp, col, r)) * (1.f / kSM);
-          const f32x4_t dlr = *(const f32x4_t*)(dl + r);
-          const float dlc = dl[col], drc = dr[col];
-          f32x4_t p = part_of(acc, g) * (1.f / (kSM * kSM)) + dlr * rv + lv * drc;
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            if (r + z == col) p[z] += dlc * drc;
-          if constexpr (MODE == POLY) {
-            p = kC * p + kB * lv;
+          f32x4_t p = part_of(acc, g) * (1.f / (kSM * kSM)) + dlr[g] * rv[g] + lv[g] * drc;
+          if constexpr (MODE == POLY) p = kC * p + kB * lv[g];
+          if (wi == wj)
 #pragma unroll
             for (int z = 0; z < 4; ++z)
-              if (r + z == col) p[z] += kA + kB * dlc;
-          }
+              if (r + z == c) p[z] += MODE == POLY ? kA + (kB + kC * drc) * dlc : dlc * drc;
           return p;
         }
       });
@@ -569,6 +596,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
 // fragment.
 template <int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * 2048];
   const int k = find(l, L_SUM, blockIdx.x);
   const Mat& t = l->t[k];
   constexpr int BM = 32 * MT * WM, FR = WM * WN * MT * NT;
@@ -584,7 +612,8 @@ __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l)
 #pragma unroll
     for (int g = 0; g < 4; ++g) acc[g] += in[s * step + 64 * g];
   store_sym(gm(t.s[0]), gm(t.d[0]), t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BM + (wave % WN * NT + j) * 32,
-            ti != tj, [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
+            ti != tj, lds + (threadIdx.x >> 6) * 2048,
+            [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 
 // Stores values of row r of X, columns c0 .. c0 + 31 (as the accumulators of a
@@ -621,9 +650,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
   const f16* x = gm(t.x[from]);
   const float* dp = gm(t.d[p]);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // X's own elements of a wave with one fragment, on their way while the sum
+  // runs; with more there are the others' products to hide them
+  constexpr bool EARLY = MT * NT == 1;
+  f32x4_t xe[4];
+  if constexpr (EARLY) {
+    const int r = i0 + wave / WN * 32 + (lane & 31), c0 = j0 + wave % WN * 32;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      xe[g] = c0 < t.np ? from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5))) : f32x4_t{};
+  }
   TL tl;
   tl.run(ring, gm(t.s[p]), t.mp, i0, x, t.mp, t.np, j0, 0, t.mp / 32);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31);
@@ -637,7 +676,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
       float y[16];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4_t xv = from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5)));
+        const f32x4_t xv = EARLY ? xe[g] : from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5)));
 #pragma unroll
         for (int z = 0; z < 4; ++z) y[4 * g + z] = acc[4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
       }
