@@ -447,6 +447,23 @@ __device__ __forceinline__ f32x4_t from_f16(const f16* p) {
   return __builtin_convertvector(*(const f16x4*)p, f32x4_t);
 }
 
+// Of a fragment on the diagonal (f[g][z]: row 8 g + 4 (l / 32) + z, column l %
+// 32), this lane's diagonal element, if it has one (diagonal_here).
+__device__ __forceinline__ bool diagonal_here() { return ((threadIdx.x >> 5) & 1) == ((threadIdx.x >> 2) & 1); }
+__device__ __forceinline__ float diagonal(const f32x4_t (&f)[4]) {
+  // selects of values (a select of array elements is one of addresses, which
+  // puts the array in memory)
+  auto pick = [](bool second, float a, float b) { return second ? b : a; };
+  const int z = threadIdx.x & 3, g = (threadIdx.x >> 3) & 3;
+  float c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    c[k] = pick(g & 2, pick(g & 1, f[0][k], f[1][k]), pick(g & 1, f[2][k], f[3][k]));
+  return pick(z & 2, pick(z & 1, c[0], c[1]), pick(z & 1, c[2], c[3]));
+}
+// What rounding v to a stored float16 leaves out.
+__device__ __forceinline__ float lost(float v) { return v - (float)(f16)(v * kSM) * (1.f / kSM); }
+
 // Stores one 32 x 32 fragment of a symmetric matrix of mp rows at rows i0,
 // columns j0, and its mirror image where the tile does not hold it already:
 // eight consecutive rows of a column are eight columns of the mirror's row as
@@ -458,20 +475,17 @@ __device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int 
                                           unsigned char* lds, F value) {
   const int lane = threadIdx.x & 63, hi = lane >> 5, fr = lane & 31, j = j0 + fr;
   unsigned pk[8];
+  f32x4_t f[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const int i = i0 + 8 * g + 4 * hi;
-    const f32x4_t f = value(g, i, j);
-    pk[2 * g] = pack_f16(f[0] * kSM, f[1] * kSM);
-    pk[2 * g + 1] = pack_f16(f[2] * kSM, f[3] * kSM);
-    if (i0 == j0)
-#pragma unroll
-      for (int z = 0; z < 4; ++z)
-        if (i + z == j) d[j] = f[z] - (float)(f16)(f[z] * kSM) * (1.f / kSM);
+    f[g] = value(g, i0 + 8 * g + 4 * hi, j);
+    pk[2 * g] = pack_f16(f[g][0] * kSM, f[g][1] * kSM);
+    pk[2 * g + 1] = pack_f16(f[g][2] * kSM, f[g][3] * kSM);
     // rows of 64 bytes, chunks swizzled so that neither the writes nor the
     // transpose reads meet in a bank more than they must
     if (mirror) *(uint2*)(lds + fr * 64 + (g ^ ((fr >> 2) & 3)) * 16 + 8 * hi) = make_uint2(pk[2 * g], pk[2 * g + 1]);
   }
+  if (i0 == j0 && diagonal_here()) d[j] = lost(diagonal(f));
   put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * hi)) = c; });
   if (mirror) {
     const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -704,10 +718,9 @@ constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT;
 
 template <int MS>
 __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
-  constexpr int Q = MS / 32, F = Q * Q, KS = 8 / F;   // fragments of A's side and of A, waves a fragment
+  constexpr int Q = MS / 32, F = Q * Q;   // fragments of A's side and of A
   __shared__ __attribute__((aligned(16))) unsigned char xs[kSmallX / 32 * kRow];
   __shared__ __attribute__((aligned(16))) unsigned char as[Q * MS * kRow], pms[Q * MS * kRow];
-  __shared__ __attribute__((aligned(16))) f32x4_t part[8 * 256];
   __shared__ __attribute__((aligned(16))) float da[MS], dp[MS];
   __shared__ double sh[8];
   const Mat& t = l.t[blockIdx.x];
@@ -809,60 +822,52 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
   auto four = [&](unsigned char* b, int r, int c) { return b + ((c >> 5) * MS + r) * kRow + (c & 31) * 2; };
   // stores a fragment of a symmetric matrix (rows i0, columns j0) and its diagonal's errors
   auto store = [&](unsigned char* b, float* d, int i0, int j0, const f32x4_t (&f)[4]) {
-    const int j = j0 + fr;
     unsigned pk[8];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int i = i0 + 8 * g + 4 * hi;
-#pragma unroll
-      for (int z = 0; z < 4; ++z)
-        if (i + z == j) d[j] = f[g][z] - (float)(f16)(f[g][z] * kSM) * (1.f / kSM);
       pk[2 * g] = pack_f16(f[g][0] * kSM, f[g][1] * kSM);
       pk[2 * g + 1] = pack_f16(f[g][2] * kSM, f[g][3] * kSM);
     }
-    put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(b, j, i0 + 16 * h + 8 * hi) = c; });
+    if (i0 == j0 && diagonal_here()) d[j0 + fr] = lost(diagonal(f));
+    put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(b, j0 + fr, i0 + 16 * h + 8 * hi) = c; });
   };
+  const int i0 = wave % F / Q * 32, j0 = wave % Q * 32;   // this wave's fragment of A and P
   for (int s = 0; s < steps; ++s) {
-    // A = X X^T: each fragment's panels dealt over KS waves
-    {
-      const int f = wave % F, i0 = f / Q * 32, j0 = f % Q * 32;
-      f32x16 acc = {};
-      for (int p = wave / F; p < ns / 32; p += KS)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) acc = mfma(rows_of(xs, p, i0, kk), rows_of(xs, p, j0, kk), acc);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) part[wave * 256 + 64 * g + lane] = part_of(acc, g);
-    }
-    __syncthreads();
+    // A = X X^T, the even and the odd panels' sums apart
+    f32x4_t f[4];
     if (wave < F) {
-      f32x4_t a[4];
+      f32x16 acc = {}, odd = {};
+      for (int p = 0; p < ns / 32; p += 2) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        a[g] = part[wave * 256 + 64 * g + lane];
-#pragma unroll
-        for (int k = 1; k < KS; ++k) a[g] += part[(k * F + wave) * 256 + 64 * g + lane];
-        a[g] = a[g] * (1.f / (kSX * kSX));
+        for (int kk = 0; kk < 2; ++kk) {
+          acc = mfma(rows_of(xs, p, i0, kk), rows_of(xs, p, j0, kk), acc);
+          if (p + 1 < ns / 32) odd = mfma(rows_of(xs, p + 1, i0, kk), rows_of(xs, p + 1, j0, kk), odd);
+        }
       }
-      store(as, da, wave / Q * 32, wave % Q * 32, a);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) f[g] = (part_of(acc, g) + part_of(odd, g)) * (1.f / (kSX * kSX));
+      store(as, da, i0, j0, f);
     }
-    __syncthreads();
+    // one wave reads what its other lanes wrote: LDS keeps a wave's order, and
+    // the compiler has to
+    if constexpr (F > 1) __syncthreads();
+    else asm volatile("" ::: "memory");
     // P = a I + b A + c A A
     if (wave < F) {
-      const int i0 = wave / Q * 32, j0 = wave % Q * 32, c = j0 + fr;
+      const int c = j0 + fr;
       f32x16 acc = {};
 #pragma unroll
       for (int p = 0; p < Q; ++p)
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) acc = mfma(rows_of(as, p, i0, kk), rows_of(as, p, j0, kk), acc);
-      f32x4_t f[4];
+      const float dc = da[c], diag = i0 == j0 ? kA + (kB + kC * dc) * dc : 0.f;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int r = i0 + 8 * g + 4 * hi;
         const f32x4_t a = from_f16((const f16*)four(as, c, r)) * (1.f / kSM);
-        f[g] = kC * (part_of(acc, g) * (1.f / (kSM * kSM)) + a * (*(const f32x4_t*)(da + r) + da[c])) + kB * a;
+        f[g] = kC * (part_of(acc, g) * (1.f / (kSM * kSM)) + a * (*(const f32x4_t*)(da + r) + dc)) + kB * a;
 #pragma unroll
-        for (int z = 0; z < 4; ++z)
-          if (r + z == c) f[g][z] += kA + (kB + kC * da[c]) * da[c];
+        for (int z = 0; z < 4; ++z) f[g][z] += r + z == c ? diag : 0.f;
       }
       store(pms, dp, i0, j0, f);
     }
