@@ -141,6 +141,8 @@ struct Share {
     row0 = BLK ? blockIdx.x : ((long)blockIdx.x * 4 + wave) * per + lane / G;
     step = (long)gridDim.x * (BLK ? 1 : 4 * per);
   }
+  // first row of the block's first turn
+  __device__ __forceinline__ long first() const { return BLK ? row0 : (long)blockIdx.x * 4 * (64 / G); }
   __device__ __forceinline__ bool has(int k) const { return l + G * k < nvec; }
   __device__ __forceinline__ int vec(int k) const { return l + G * k; }
   // the lane's channels of a float32 vector over channels (NULL: `none`)
@@ -166,8 +168,11 @@ struct Share {
   }
 };
 
-// U rows of a lane are in flight at a time.
-template <typename T, int VB, int NV, bool BLK, int U>
+// Memory bounds it: 147456 x 64 bf16 take 9.5 us (4.1 TB/s of what has to be
+// read and written; a copy of that size, out of the caches, 4.7 us and a
+// launch), 144 x 1024 3.6.  One row a lane is on its way at a time: two or
+// four cost registers and waves, and come out slower (10.4 us).
+template <typename T, int VB, int NV, bool BLK>
 __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float* __restrict__ gain,
                                                const float* __restrict__ bias, float eps, T* y,
                                                long ldy, float2* __restrict__ stats, long rows,
@@ -181,51 +186,46 @@ __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float
   sh.channels(gain, 1.f, gn);
   sh.channels(bias, 0.f, bs);
   // the trip count is the same for every lane of the block (block_sum meets a barrier)
-  for (long base = 0; base + (BLK ? sh.row0 : (long)blockIdx.x * 4 * (64 / sh.G)) < rows; base += U * sh.step) {
-    typename VT::raw raw[U][NV];
+  for (long base = 0; base + sh.first() < rows; base += sh.step) {
+    const long r = sh.row0 + base;
+    typename VT::raw raw[NV];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long r = sh.row0 + base + u * sh.step;
+    for (int k = 0; k < NV; ++k)
+      if (r < rows && sh.has(k)) raw[k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
+      else raw[k] = typename VT::raw{};
+    float f[NV][V], s = 0.f;
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (r < rows && sh.has(k)) raw[u][k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
-        else raw[u][k] = typename VT::raw{};
+    for (int k = 0; k < NV; ++k) {
+      VT::un(raw[k], f[k]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) s += f[k][v];
     }
+    const float mean = row_sum<BLK>(s, sh.G, s4) / C;   // (a quotient: a constant row's mean is exact)
+    float q = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long r = sh.row0 + base + u * sh.step;
-      float f[NV][V], s = 0.f;
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        f[k][v] -= mean;
+        if (sh.has(k)) q += f[k][v] * f[k][v];
+      }
+    const float rstd = 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps);
+    if (r < rows) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        VT::un(raw[u][k], f[k]);
 #pragma unroll
-        for (int v = 0; v < V; ++v) s += f[k][v];
+        for (int v = 0; v < V; ++v) f[k][v] = f[k][v] * rstd * gn[k][v] + bs[k][v];
+        if (sh.has(k)) ((typename VT::raw*)(y + r * ldy))[sh.vec(k)] = VT::pk(f[k]);
       }
-      const float mean = row_sum<BLK>(s, sh.G, s4) / C;
-      float q = 0.f;
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          f[k][v] -= mean;
-          if (sh.has(k)) q += f[k][v] * f[k][v];
-        }
-      const float rstd = 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps);
-      if (r < rows) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) f[k][v] = f[k][v] * rstd * gn[k][v] + bs[k][v];
-          if (sh.has(k)) ((typename VT::raw*)(y + r * ldy))[sh.vec(k)] = VT::pk(f[k]);
-        }
-        if (stats && sh.l == 0) stats[r] = make_float2(mean, rstd);
-      }
+      if (stats && sh.l == 0) stats[r] = make_float2(mean, rstd);
     }
   }
 }
 
 // dx, and this block's column sums in part[block][2][C] (part NULL: none).
-template <typename T, int VB, int NV, bool BLK, int U>
+// Memory bounds it: 131072 x 128 bf16 take 19.8 us (5.1 TB/s) and their sums'
+// launch 3.9, 12544 x 256 8.4 and 3.2.
+template <typename T, int VB, int NV, bool BLK>
 __global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* x, long ldx,
                                                const float* __restrict__ gain,
                                                const float2* __restrict__ stats, T* dx, long lddx,
@@ -242,50 +242,42 @@ __global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* 
 #pragma unroll
     for (int v = 0; v < V; ++v) a[k][v] = b[k][v] = 0.f;
   const float inv_c = 1.f / C;
-  for (long base = 0; base + (BLK ? sh.row0 : (long)blockIdx.x * 4 * (64 / sh.G)) < rows; base += U * sh.step) {
-    typename VT::raw rd[U][NV], rx[U][NV];
-    float2 st[U];
+  for (long base = 0; base + sh.first() < rows; base += sh.step) {
+    const long r = sh.row0 + base;
+    typename VT::raw rd[NV], rx[NV];
+    const float2 st = r < rows ? stats[r] : make_float2(0.f, 0.f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long r = sh.row0 + base + u * sh.step;
-      st[u] = r < rows ? stats[r] : make_float2(0.f, 0.f);
+    for (int k = 0; k < NV; ++k)
+      if (r < rows && sh.has(k)) {
+        rd[k] = ((const typename VT::raw*)(dy + r * lddy))[sh.vec(k)];
+        rx[k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
+      } else {
+        rd[k] = rx[k] = typename VT::raw{};
+      }
+    float d[NV][V], xh[NV][V], s = 0.f, p = 0.f;
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (r < rows && sh.has(k)) {
-          rd[u][k] = ((const typename VT::raw*)(dy + r * lddy))[sh.vec(k)];
-          rx[u][k] = ((const typename VT::raw*)(x + r * ldx))[sh.vec(k)];
-        } else {
-          rd[u][k] = rx[u][k] = typename VT::raw{};
-        }
+    for (int k = 0; k < NV; ++k) {
+      VT::un(rd[k], d[k]);
+      VT::un(rx[k], xh[k]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        xh[k][v] = (xh[k][v] - st.x) * st.y;
+        a[k][v] += d[k][v] * xh[k][v];
+        b[k][v] += d[k][v];
+        const float g = d[k][v] * gn[k][v];
+        s += g;
+        p += g * xh[k][v];
+      }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long r = sh.row0 + base + u * sh.step;
-      float d[NV][V], xh[NV][V], s = 0.f, p = 0.f;
+    if (!dx) continue;
+    const float ms = row_sum<BLK>(s, sh.G, s4) * inv_c, mp = row_sum<BLK>(p, sh.G, s4) * inv_c;
+    if (r < rows) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        VT::un(rd[u][k], d[k]);
-        VT::un(rx[u][k], xh[k]);
+        float o[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          xh[k][v] = (xh[k][v] - st[u].x) * st[u].y;
-          a[k][v] += d[k][v] * xh[k][v];
-          b[k][v] += d[k][v];
-          const float g = d[k][v] * gn[k][v];
-          s += g;
-          p += g * xh[k][v];
-        }
-      }
-      if (!dx) continue;
-      const float ms = row_sum<BLK>(s, sh.G, s4) * inv_c, mp = row_sum<BLK>(p, sh.G, s4) * inv_c;
-      if (r < rows) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          float o[V];
-#pragma unroll
-          for (int v = 0; v < V; ++v) o[v] = st[u].y * (d[k][v] * gn[k][v] - ms - xh[k][v] * mp);
-          if (sh.has(k)) ((typename VT::raw*)(dx + r * lddx))[sh.vec(k)] = VT::pk(o);
-        }
+        for (int v = 0; v < V; ++v) o[v] = st.y * (d[k][v] * gn[k][v] - ms - xh[k][v] * mp);
+        if (sh.has(k)) ((typename VT::raw*)(dx + r * lddx))[sh.vec(k)] = VT::pk(o);
       }
     }
   }
@@ -473,10 +465,10 @@ void forward_regs(const Plan& p, const NormShape& s, const T* x, long ldx, const
   const double n = (double)s.rows * s.C;
   const unsigned grid = even_grid(s.rows, rows_of_block(p), kFwdBlocks);
   with_plan(p, [&](auto nv, auto blk) {
-    constexpr int NV = decltype(nv)::value, U = NV == 1 ? 4 : NV == 2 ? 2 : 1;
+    constexpr int NV = decltype(nv)::value;
     constexpr bool BLK = decltype(blk)::value;
     ProfScope ps("layer_norm_fwd", 8 * n, 2 * n * sizeof(T), st);
-    TGP_LAUNCH(ps, (norm_fwd<T, VB, NV, BLK, U>), dim3(grid), dim3(kT), 0, st, x, ldx, gain, bias,
+    TGP_LAUNCH(ps, (norm_fwd<T, VB, NV, BLK>), dim3(grid), dim3(kT), 0, st, x, ldx, gain, bias,
                eps, y, ldy, stats, s.rows, s.C, p.g);
   });
 }
@@ -487,19 +479,20 @@ void backward_regs(const Plan& p, unsigned grid, const NormShape& s, const T* dy
                    float* part, hipStream_t st) {
   const double n = (double)s.rows * s.C;
   with_plan(p, [&](auto nv, auto blk) {
-    constexpr int NV = decltype(nv)::value, U = NV == 1 ? 2 : 1;
+    constexpr int NV = decltype(nv)::value;
     constexpr bool BLK = decltype(blk)::value;
     ProfScope ps("layer_norm_bwd", 14 * n, (dx ? 3 : 2) * n * sizeof(T), st);
-    TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK, U>), dim3(grid), dim3(kT), 0, st, dy, lddy, x, ldx,
+    TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK>), dim3(grid), dim3(kT), 0, st, dy, lddy, x, ldx,
                gain, stats, dx, lddx, part, s.rows, s.C, p.g);
   });
 }
 
 // Row ranges (partial column sums) of the backward, at most: enough to fill
-// the chip; beyond that 16 rows each, so that the sums' traffic (16 bytes a
-// channel and range) stays a sixth of the rows' own.
+// the chip; beyond that 24 rows each, so that the sums' traffic (16 bytes a
+// channel and range) stays a ninth of the rows' own (12544 x 256: 11.0 us with
+// 24, 11.8 with 16, 13.0 with 48).
 int row_ranges(const NormShape& s) {
-  return (int)std::min<long>(std::min<long>(kColBlocks, std::max<long>(256, s.rows / 16)), s.rows);
+  return (int)std::min<long>(std::min<long>(kColBlocks, std::max<long>(256, s.rows / 24)), s.rows);
 }
 
 // Element size, and the bits of every address and row distance that the
