@@ -338,3 +338,37 @@ def test_micro_batches_add_up():
     torch.cuda.synchronize()
     dxr, dgr, dbr = ref.norm_backward(dy, xv.cpu(), gain, st[:, 0].cpu(), st[:, 1].cpu())
     assert ref.rel(dx, dxr) <= 1e-5 and ref.rel(dg, dgr) <= 1e-5 and ref.rel(db, dbr) <= 1e-5
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("c", [24, 1001])
+def test_rows_farther_apart_than_32_bits(c, dt):
+    """Rows whose byte offsets pass 2^32: three rows 1.2e9 elements apart in one buffer, in and out."""
+    say("layer norm, far rows", c, dt)
+    code, td = DT[dt]
+    ld = 1_200_000_008 if dt == "bf16" else 600_000_004
+    x, dy, gain, bias = _inputs(3, c, c)
+    buf = torch.empty(2 * ld + c + 8, dtype=td, device="cuda")
+    view = buf.as_strided((3, c), (ld, 1))
+    view.copy_(x)
+    want, _, st = _forward(x, gain, bias, dt, c, c)
+    g, b = gain.cuda(), bias.cuda()
+    y = torch.empty(3, c, dtype=td, device="cuda")
+    tgp.layer_norm_forward(3, c, code, buf.data_ptr(), ld, g.data_ptr(), b.data_ptr(), 1e-5, y.data_ptr(), c)
+    torch.cuda.synchronize()
+    assert torch.equal(y, _forward(x, gain, bias, dt, c, c)[1]) and torch.equal(view, want)
+    n = tgp.layer_norm_backward_workspace(3, c, code)
+    ws = torch.empty(n // 4 + 4, device="cuda")
+    d = dy.to(td).cuda()
+    got = []
+    for xp, xl in ((want, c), (buf, ld)):
+        dx, dg, db = torch.empty(3, c, dtype=td, device="cuda"), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+        tgp.layer_norm_backward(3, c, code, d.data_ptr(), c, xp.data_ptr(), xl, g.data_ptr(), st.data_ptr(),
+                                dx.data_ptr(), c, dg.data_ptr(), db.data_ptr(), True, ws.data_ptr(), n)
+        torch.cuda.synchronize()
+        got.append((dx, dg, db))
+    assert all(torch.equal(p, q) for p, q in zip(*got))
+    # and written there, in place
+    tgp.layer_norm_forward(3, c, code, buf.data_ptr(), ld, g.data_ptr(), b.data_ptr(), 1e-5, buf.data_ptr(), ld)
+    torch.cuda.synchronize()
+    assert torch.equal(view, y)

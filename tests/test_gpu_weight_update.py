@@ -279,3 +279,37 @@ def test_failed_launches_are_reported():
     with pytest.raises(tgp.TgpError):
         tgp.weight_step(tgp.step_tensors([(64, gd.data_ptr(), None, o.data_ptr(), 0.0)]), 0.0)
     tgp.debug_fail_launch(0)
+
+
+@pytest.mark.parametrize("r,c", [(4096, 131072), (131000, 4001)])
+def test_matrices_of_half_a_billion_values(r, c):
+    """Offsets that pass 32 bits.  A matrix of signs u v^T is one singular direction, whose value 1 one step
+    takes to a + b + c = 0.7010: every entry becomes its sign times 0.7010 / sqrt(r c), within bfloat16's
+    rounding and float16's of a few products (2^-8 + 2^-9)."""
+    say("muon", r, c)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    u = torch.randint(0, 2, (r, 1), device="cuda", generator=g, dtype=torch.int8) * 2 - 1
+    v = torch.randint(0, 2, (1, c), device="cuda", generator=g, dtype=torch.int8) * 2 - 1
+    grad = (u * v).float()
+    o = torch.empty(r, c, dtype=torch.bfloat16, device="cuda")
+    t = tgp.muon_tensors([(r, c, grad.data_ptr(), None, o.data_ptr())])
+    n = tgp.muon_workspace(t)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    tgp.muon_update(t, 0.0, False, 1, 0.0, ws.data_ptr(), n)
+    torch.cuda.synchronize()
+    want = sum(ref.NS) / math.sqrt(r * c)
+    off = (o.float() * grad / want - 1).abs().max().item()
+    assert off <= 2.0 ** -8 + 2.0 ** -9, off
+
+
+def test_weight_step_past_32_bits():
+    """Two billion values: more bytes than 32 bits count, more blocks than a launch takes."""
+    n = (1 << 31) + 4099
+    w = torch.ones(n, device="cuda")
+    o = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    o[-1], o[1 << 31] = 1.0, 2.0
+    tgp.weight_step(tgp.step_tensors([(n, w.data_ptr(), None, o.data_ptr(), 0.25)]), 0.0)
+    torch.cuda.synchronize()
+    assert w[-1].item() == 0.75 and w[1 << 31].item() == 0.5
+    w[-1] = w[1 << 31] = 0.875
+    assert bool((w == 0.875).all())
