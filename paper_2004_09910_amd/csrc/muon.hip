@@ -56,19 +56,31 @@ struct Mat {
   f16 *x[2], *s[3];    // X (mp x np, ping-pong), A, P and their products (mp x mp)
   float* d[3];         // their diagonals' rounding errors
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
-  int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;};
+  int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;
+  int two;             // takes two steps at a time
+};
 
 // The matrices of a list and, for each kind of launch, the first block of each
 // (and the number of blocks).  The first launch gets it as an argument and
 // leaves it in the workspace for the others: arguments lie in host memory,
 // which every block would have to reach for.
-enum { L_MOMENTUM, L_NORMALIZE, L_GRAM, L_SUM, L_SYM, L_APPLY, LAUNCHES };
+enum {
+  L_MOMENTUM, L_NORMALIZE, L_GRAM, L_SUM, L_SYM, L_APPLY,   // every matrix
+  L_GRAM1, L_SUM1, L_APPLY1,                                // those of one step at a time
+  L_SYM2,                                                   // those of two
+  LAUNCHES
+};
 struct Mats {
   int count;
   int blk0[LAUNCHES][kMaxMats + 1];
   Mat t[kMaxMats];
 };
 static_assert(sizeof(Mats) <= 3800, "kernel arguments");
+
+// An argument of a launch: for matrices of one step at a time, and of two.
+struct Each {
+  int v[2];
+};
 
 // Place of row i, column j of a matrix of mp rows.
 __device__ __forceinline__ long at(int mp, int i, int j) { return ((long)(j >> 5) * mp + i) * 32 + (j & 31); }
@@ -273,9 +285,12 @@ struct Tile {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const u32x4 rl = make_rsrc(L + (long)i0 * 32, 0x7fffffff);
-    const u32x4 rr = TR ? make_rsrc(R + (long)j0 * rrows, (rcols - j0) * rrows * 2)
-                        : make_rsrc(R + (long)j0 * 32, 0x7fffffff);
+    // what comes from a table in memory is the same in every lane
+    k0 = __builtin_amdgcn_readfirstlane(k0);
+    k1 = __builtin_amdgcn_readfirstlane(k1);
+    const u32x4 rl = uniform(make_rsrc(L + (long)i0 * 32, 0x7fffffff));
+    const u32x4 rr = uniform(TR ? make_rsrc(R + (long)j0 * rrows, (rcols - j0) * rrows * 2)
+                                : make_rsrc(R + (long)j0 * 32, 0x7fffffff));
     // byte offsets of this lane in its chunks of a stage (rows of chunks NW
     // apart agree in their swizzle, NW being even), and of the next stage
     static_assert(NW % 2 == 0, "pairs of chunks");
@@ -287,7 +302,8 @@ struct Tile {
     for (int u = 0; u < NR; ++u)
       vr[u] = TR ? ((wave >> 1) + u * (NW / 2)) * rrows * 64 + rrow * 64 + 16 * rswz(rrow, lane & 3)
                  : r16 * 64 + 16 * kswz(r16, lane & 3) + u * NW * 1024;
-    const int stl = lrows * 64, str = TR ? 2048 : rrows * 64;
+    const int stl = __builtin_amdgcn_readfirstlane(lrows * 64);
+    const int str = TR ? 2048 : __builtin_amdgcn_readfirstlane(rrows * 64);
     int sl = __builtin_amdgcn_readfirstlane(k0 * stl), sr = __builtin_amdgcn_readfirstlane(k0 * str);
     const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
     auto issue = [&](auto slot) __attribute__((always_inline)) {
@@ -371,6 +387,13 @@ struct Tile {
   }
 
  private:
+  // The same in every lane, in scalar registers.
+  __device__ __forceinline__ static u32x4 uniform(u32x4 v) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_readfirstlane(v[k]);
+    return v;
+  }
+
   // f(0), f(1), .. f(N - 1), as constants
   template <int N, typename F>
   __device__ __forceinline__ static void each(F f) {
@@ -530,21 +553,21 @@ __device__ __forceinline__ void upper(int b, int nt, int& r, int& c) {
 
 enum { GRAM, POLY, MUL };
 
-// Symmetric products, upper tiles only.  GRAM: s[0] = X X^T; where its sum is
-// split, the ranges' partial tiles go to t.part as the accumulators lie,
+// Symmetric products, upper tiles only.  GRAM: s[0] = x[a] x[a]^T; where its
+// sum is split, the ranges' partial tiles go to t.part as the accumulators lie,
 // [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
-// s[a].  MUL: s[c] = s[a] s[b], of matrices that commute.
+// s[0].  MUL: s[c] = s[a] s[b], of matrices that commute.
 template <int MODE, int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int a, int b, int c) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int launch, Each ea, int b, Each ec) {
   typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
   static_assert(TL::BM == TL::BN, "square tiles");
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = grouped(blockIdx.x, gridDim.x);
-  constexpr int LAUNCH = MODE == GRAM ? L_GRAM : L_SYM;
-  const int k = find(l, LAUNCH, blk);
+  const int k = find(l, launch, blk);
   const Mat& t = l->t[k];
+  const int a = MODE == POLY ? 0 : pickg(ea.v, t.two), c = pickg(ec.v, t.two);
   const int nt = t.mp / TL::BM, tiles = nt * (nt + 1) / 2;
-  const int q = blk - l->blk0[LAUNCH][k], sp = MODE == GRAM ? q / tiles : 0;
+  const int q = blk - l->blk0[launch][k], sp = MODE == GRAM ? q / tiles : 0;
   int ti, tj;
   upper(q - sp * tiles, nt, ti, tj);
   const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
@@ -609,13 +632,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
 // s[0] from the ranges' partial tiles, added in order: a wave takes one
 // fragment.
 template <int MT, int NT, int WM, int WN>
-__global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l) {
+__global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l, int launch) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * 2048];
-  const int k = find(l, L_SUM, blockIdx.x);
+  const int k = find(l, launch, blockIdx.x);
   const Mat& t = l->t[k];
   constexpr int BM = 32 * MT * WM, FR = WM * WN * MT * NT;
   const int nt = t.mp / BM, tiles = nt * (nt + 1) / 2;
-  const int f = (blockIdx.x - l->blk0[L_SUM][k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
+  const int f = (blockIdx.x - l->blk0[launch][k]) * 4 + (threadIdx.x >> 6), tile = f / FR, q = f % FR;
   const int lane = threadIdx.x & 63, wave = q / (MT * NT), i = q / NT % MT, j = q % NT;
   int ti, tj;
   upper(tile, nt, ti, tj);
@@ -654,13 +677,14 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
 
 // X' = s[p] X, or (last) the update itself.
 template <int MT, int NT, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int p, int from, int last) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last) {
   typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = grouped(blockIdx.x, gridDim.x);
-  const int k = find(l, L_APPLY, blk);
+  const int k = find(l, launch, blk);
   const Mat& t = l->t[k];
-  const int b = blk - l->blk0[L_APPLY][k], nt = t.mp / TL::BM;
+  const int p = pickg(ep.v, t.two), from = pickg(efrom.v, t.two);
+  const int b = blk - l->blk0[launch][k], nt = t.mp / TL::BM;
   const int i0 = b % nt * TL::BM, j0 = b / nt * TL::BN;
   const f16* x = gm(t.x[from]);
   const float* dp = gm(t.d[p]);
@@ -716,14 +740,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 constexpr int kSmallT = 512, kSmallX = 16384, kRow = 80;   // threads, most values of X, bytes of a row
 constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT;
 
+struct SmallLds {
+  unsigned char xs[kSmallX / 32 * kRow];               // X
+  unsigned char as[2 * 64 * kRow], pms[2 * 64 * kRow];   // A, P
+  float da[64], dp[64];                                // their diagonals' errors
+  double sh[8];
+};
+
 template <int MS>
-__global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
+__device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float mu, int nesterov, int steps,
+                                             float eps) {
   constexpr int Q = MS / 32, F = Q * Q;   // fragments of A's side and of A
-  __shared__ __attribute__((aligned(16))) unsigned char xs[kSmallX / 32 * kRow];
-  __shared__ __attribute__((aligned(16))) unsigned char as[Q * MS * kRow], pms[Q * MS * kRow];
-  __shared__ __attribute__((aligned(16))) float da[MS], dp[MS];
-  __shared__ double sh[8];
-  const Mat& t = l.t[blockIdx.x];
+  unsigned char *xs = lds.xs, *as = lds.as, *pms = lds.pms;
+  float *da = lds.da, *dp = lds.dp;
+  double* sh = lds.sh;
   const int ns = (t.n + 31) / 32 * 32, chunks = MS * ns / 8;
   const bool flip = t.rows > t.cols, vec = !flip && t.cols % 4 == 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -908,6 +938,13 @@ __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nest
   }
 }
 
+__global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
+  __shared__ __attribute__((aligned(16))) SmallLds lds;
+  const Mat& t = l.t[blockIdx.x];
+  if (t.m > 32) small_update<64>(lds, t, mu, nesterov, steps, eps);
+  else small_update<32>(lds, t, mu, nesterov, steps, eps);
+}
+
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kPad = 128;
 constexpr int kBlocks = 512;   // two a CU
@@ -927,14 +964,6 @@ bool small(const tgp_muon_tensor& d) {
   const long m = std::min(d.rows, d.cols), n = std::max(d.rows, d.cols);
   return m <= 64 && (m <= 32 ? 32 : 64) * ((n + 31) / 32 * 32) <= kSmallX;
 }
-// How a matrix is taken: whole by one block (of 32 or 64 rows), or by tiles,
-// one or two steps at a time.
-enum { WHOLE32, WHOLE64, SINGLES, PAIRS, KINDS };
-int kind_of(const tgp_muon_tensor& d) {
-  if (small(d)) return std::min(d.rows, d.cols) <= 32 ? WHOLE32 : WHOLE64;
-  return pairs(d) ? PAIRS : SINGLES;
-}
-
 void describe(const tgp_muon_tensor& d, Mat& t) {
   t = Mat{};
   t.grad = d.grad;
@@ -954,7 +983,7 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 // kRange stages at least (writing and reading back a partial tile takes the
 // time of 20 stages).  The ranges depend on the matrix alone, so that its
 // update does not depend on the others of the call.
-size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
+size_t lay_out(bool whole, int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
     char* p = ws + pos;
     pos += al256(bytes);
@@ -965,7 +994,8 @@ size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
     describe(*d[k], t);
-    if (kind == WHOLE32 || kind == WHOLE64) continue;
+    if (whole) continue;
+    t.two = pairs(*d[k]);
     t.mp = up(t.m);
     t.np = up(t.n);
     const long size = (long)t.rows * t.cols;
@@ -984,23 +1014,24 @@ size_t lay_out(int kind, int n, const tgp_muon_tensor* const* d, char* ws, size_
   return pos;
 }
 
-// Deals the matrices into lists of one kind each; within a list those of the
-// longest sums come first (stable), so that the short ones fill up its
-// launches' ends.  Calls go(kind, list of pointers, count).
+// Deals the matrices into lists, the small ones and the tiled ones apart;
+// within a list those of the longest sums come first (stable), so that the
+// short ones fill up its launches' ends.  Calls go(whether small, list of
+// pointers, count).
 template <typename F>
 void each_list(int n, const tgp_muon_tensor* t, F go) {
-  for (int kind = 0; kind < KINDS; ++kind) {
+  for (int kind = 0; kind < 2; ++kind) {
     const tgp_muon_tensor* list[kMaxMats];
     int count = 0;
     auto flush = [&]() {
       std::stable_sort(list, list + count, [](const tgp_muon_tensor* a, const tgp_muon_tensor* b) {
         return std::min(a->rows, a->cols) > std::min(b->rows, b->cols);
       });
-      if (count) go(kind, list, count);
+      if (count) go(kind == 0, list, count);
       count = 0;
     };
     for (int k = 0; k < n; ++k) {
-      if (kind_of(t[k]) != kind) continue;
+      if (small(t[k]) != (kind == 0)) continue;
       list[count++] = t + k;
       if (count == kMaxMats) flush();
     }
@@ -1020,23 +1051,19 @@ unsigned deal(Mats& l, int launch, F blocks) {
   return (unsigned)pos;
 }
 
-hipError_t update_small(const Mats& l, bool m64, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
+hipError_t update_small(const Mats& l, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
   double n = 0, flops = 0;
   for (int k = 0; k < l.count; ++k) {
     const double m = l.t[k].m;
     n += m * l.t[k].n;
     flops += steps * (3 * m * m * l.t[k].n + m * m * m);
   }
-  ProfScope ps(m64 ? "muon_small<64>" : "muon_small<32>", flops, (l.t[0].mom ? 14 : 6) * n, st);
-  if (m64)
-    TGP_LAUNCH(ps, muon_small<64>, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
-  else
-    TGP_LAUNCH(ps, muon_small<32>, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
+  ProfScope ps("muon_small", flops, 14 * n, st);
+  TGP_LAUNCH(ps, muon_small, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
   return launch_status();
 }
 
-hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, int steps, float eps,
-                       hipStream_t st) {
+hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
   double n = 0, gram = 0, cube = 0, cells = 0;
   long t192 = 0, t128 = 0, g128 = 0;   // tiles of P X, of X X^T
   for (int k = 0; k < l.count; ++k) {
@@ -1055,66 +1082,85 @@ hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, 
   // leaves CUs without one, 64 x 64 with twice the stages in flight.  The sums'
   // order is the same in all of them.
   const int ba = t192 >= kBlocks ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
-  const unsigned gm = deal(l, L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
-  const unsigned gn = deal(l, L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
-  const unsigned gg = deal(l, L_GRAM, [&](const Mat& t) { return uppers(t.mp / bg) * t.split; });
-  const unsigned gs = deal(l, L_SUM, [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; });
-  const unsigned gp = deal(l, L_SYM, [](const Mat& t) { return uppers(t.mp / 64); });
-  const unsigned ga = deal(l, L_APPLY, [&](const Mat& t) { return (t.mp / std::min(ba, 128)) * cdiv(t.np, ba); });
+  auto grams = [&](const Mat& t) { return uppers(t.mp / bg) * t.split; };
+  auto sums = [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; };
+  auto applies = [&](const Mat& t) { return (t.mp / std::min(ba, 128)) * cdiv(t.np, ba); };
+  auto syms = [](const Mat& t) { return uppers(t.mp / 64); };
+  unsigned grid[LAUNCHES];
+  grid[L_MOMENTUM] = deal(l, L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
+  grid[L_NORMALIZE] = deal(l, L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
+  grid[L_GRAM] = deal(l, L_GRAM, grams);
+  grid[L_SUM] = deal(l, L_SUM, sums);
+  grid[L_SYM] = deal(l, L_SYM, syms);
+  grid[L_APPLY] = deal(l, L_APPLY, applies);
+  grid[L_GRAM1] = deal(l, L_GRAM1, [&](const Mat& t) { return t.two ? 0 : grams(t); });
+  grid[L_SUM1] = deal(l, L_SUM1, [&](const Mat& t) { return t.two ? 0 : sums(t); });
+  grid[L_APPLY1] = deal(l, L_APPLY1, [&](const Mat& t) { return t.two ? 0 : applies(t); });
+  grid[L_SYM2] = deal(l, L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
+  const Mats* tb = table;
   {
     ProfScope ps("muon_momentum", 4 * n, 12 * n, st);
-    TGP_LAUNCH(ps, muon_momentum, dim3(gm), dim3(256), 0, st, l, table, mu, (int)nesterov);
+    TGP_LAUNCH(ps, muon_momentum, dim3(grid[L_MOMENTUM]), dim3(256), 0, st, l, table, mu, (int)nesterov);
   }
   {
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
-    TGP_LAUNCH(ps, muon_normalize, dim3(gn), dim3(256), 0, st, (const Mats*)table, mu, (int)nesterov, eps);
+    TGP_LAUNCH(ps, muon_normalize, dim3(grid[L_NORMALIZE]), dim3(256), 0, st, tb, mu, (int)nesterov, eps);
   }
-  auto poly = [&](int a, int c) {
-    ProfScope ps("muon_poly", cube, 4 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, (const Mats*)table, a, 0, c);
-  };
-  auto mul = [&](int a, int b, int c) {
-    ProfScope ps("muon_mul", cube, 6 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(gp), dim3(256), 0, st, (const Mats*)table, a, b, c);
-  };
-  int from = 0;
-  for (int s = 0; s < steps;) {
-    {
+  // the launches, each over the matrices of its table that have blocks in it
+  Each from{{0, 0}};   // which of its two buffers X is in
+  auto gram_of = [&](int lg, int ls) {
+    if (grid[lg]) {
       ProfScope ps("muon_gram", gram, 2 * n + 2 * cells, st);
       if (bg == 128)
-        TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(gg), dim3(256), 0, st, (const Mats*)table, from, 0, 0);
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
       else
-        TGP_LAUNCH(ps, (muon_sym<GRAM, 1, 1, 2, 2, 8>), dim3(gg), dim3(256), 0, st, (const Mats*)table, from, 0, 0);
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 1, 1, 2, 2, 8>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
     }
-    if (gs) {
+    if (grid[ls]) {
       ProfScope ps("muon_gram_sum", 0, 0, st);
-      if (bg == 128)
-        TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(gs), dim3(256), 0, st, (const Mats*)table);
-      else
-        TGP_LAUNCH(ps, (muon_gram_sum<1, 1, 2, 2>), dim3(gs), dim3(256), 0, st, (const Mats*)table);
+      if (bg == 128) TGP_LAUNCH(ps, (muon_gram_sum<2, 2, 2, 2>), dim3(grid[ls]), dim3(256), 0, st, tb, ls);
+      else TGP_LAUNCH(ps, (muon_gram_sum<1, 1, 2, 2>), dim3(grid[ls]), dim3(256), 0, st, tb, ls);
     }
-    poly(0, 1);
-    int p = 1;
-    if (two && s + 2 <= steps) {
-      mul(1, 0, 2);    // P A
-      mul(2, 1, 0);    // A' = P A P
-      poly(0, 2);      // P'
-      mul(2, 1, 0);    // P' P
-      p = 0;
-      ++s;
+  };
+  auto poly = [&](Each c) {
+    ProfScope ps("muon_poly", cube, 4 * cells, st);
+    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
+               (Each{{0, 0}}), 0, c);
+  };
+  auto mul = [&](int a, int b, int c) {
+    if (!grid[L_SYM2]) return;
+    ProfScope ps("muon_mul", cube, 6 * cells, st);
+    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
+               (Each{{a, a}}), b, (Each{{c, c}}));
+  };
+  auto apply = [&](int la, Each p, int last) {
+    if (!grid[la]) return;
+    ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
+    if (ba == 192)
+      TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+    else if (ba == 128)
+      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+    else
+      TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 8>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+  };
+  // Two steps a turn: what both kinds of matrices need is one launch for both,
+  // and a list of one kind has no launches of the other.
+  for (int s = 0; s < steps; s += 2) {
+    const bool turn = s + 2 <= steps;
+    gram_of(L_GRAM, L_SUM);
+    poly(Each{{1, 1}});
+    if (turn) {
+      mul(1, 0, 2);                          // P A
+      apply(L_APPLY1, Each{{1, 1}}, 0);
+      if (grid[L_APPLY1]) from.v[0] ^= 1;
+      mul(2, 1, 0);                          // A' = P A P
+      gram_of(L_GRAM1, L_SUM1);
+      poly(Each{{1, 2}});                    // P'
+      mul(2, 1, 0);                          // P' P
     }
-    ++s;
-    {
-      const int last = s == steps;
-      ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
-      if (ba == 192)
-        TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
-      else if (ba == 128)
-        TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
-      else
-        TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 8>), dim3(ga), dim3(256), 0, st, (const Mats*)table, p, from, last);
-    }
-    from ^= 1;
+    apply(L_APPLY, Each{{1, turn ? 0 : 1}}, s + 2 >= steps);
+    from.v[0] ^= 1;
+    from.v[1] ^= 1;
   }
   return launch_status();
 }
@@ -1124,8 +1170,8 @@ hipError_t update_list(Mats& l, Mats* table, bool two, float mu, bool nesterov, 
 size_t muon_bytes(int n, const tgp_muon_tensor* t) {
   size_t pos = 0;
   Mats l;
-  each_list(n, t, [&](int kind, const tgp_muon_tensor* const* d, int count) {
-    pos = lay_out(kind, count, d, nullptr, pos, l);
+  each_list(n, t, [&](bool whole, const tgp_muon_tensor* const* d, int count) {
+    pos = lay_out(whole, count, d, nullptr, pos, l);
   });
   return pos;
 }
@@ -1134,13 +1180,13 @@ hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov,
                        float eps, void* ws, hipStream_t st) {
   size_t pos = 0;
   hipError_t e = hipSuccess;
-  each_list(n, t, [&](int kind, const tgp_muon_tensor* const* d, int count) {
+  each_list(n, t, [&](bool whole, const tgp_muon_tensor* const* d, int count) {
     if (e != hipSuccess) return;
     Mats l;
     Mats* table = (Mats*)((char*)ws + pos);
-    pos = lay_out(kind, count, d, (char*)ws, pos, l);
-    e = kind == WHOLE32 || kind == WHOLE64 ? update_small(l, kind == WHOLE64, mu, nesterov, steps, eps, st)
-                                           : update_list(l, table, kind == PAIRS, mu, nesterov, steps, eps, st);
+    pos = lay_out(whole, count, d, (char*)ws, pos, l);
+    e = whole ? update_small(l, mu, nesterov, steps, eps, st)
+              : update_list(l, table, mu, nesterov, steps, eps, st);
   });
   return e;
 }
