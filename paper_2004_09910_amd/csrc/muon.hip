@@ -1097,6 +1097,11 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   grid[L_SUM1] = deal(l, L_SUM1, [&](const Mat& t) { return t.two ? 0 : sums(t); });
   grid[L_APPLY1] = deal(l, L_APPLY1, [&](const Mat& t) { return t.two ? 0 : applies(t); });
   grid[L_SYM2] = deal(l, L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
+  // The products of m x m matrices with up to two blocks a CU wait for their
+  // stages: six in flight, not four (one of 1024 x 4096 in all: 221 us, 238).
+  // With more blocks, six leave room for fewer of them (2048 x 18432: 1179 us,
+  // 1165 with four).
+  auto deep = [&](int launch) { return grid[launch] <= kBlocks; };
   const Mats* tb = table;
   {
     ProfScope ps("muon_momentum", 4 * n, 12 * n, st);
@@ -1124,14 +1129,22 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   };
   auto poly = [&](Each c) {
     ProfScope ps("muon_poly", cube, 4 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
-               (Each{{0, 0}}), 0, c);
+    if (deep(L_SYM))
+      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 6>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
+                 (Each{{0, 0}}), 0, c);
+    else
+      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
+                 (Each{{0, 0}}), 0, c);
   };
   auto mul = [&](int a, int b, int c) {
     if (!grid[L_SYM2]) return;
     ProfScope ps("muon_mul", cube, 6 * cells, st);
-    TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
-               (Each{{a, a}}), b, (Each{{c, c}}));
+    if (deep(L_SYM2))
+      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 6>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
+                 (Each{{a, a}}), b, (Each{{c, c}}));
+    else
+      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
+                 (Each{{a, a}}), b, (Each{{c, c}}));
   };
   auto apply = [&](int la, Each p, int last) {
     if (!grid[la]) return;
