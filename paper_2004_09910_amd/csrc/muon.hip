@@ -106,6 +106,30 @@ __device__ __forceinline__ float update_of(const Mat& t, long i, float mu, int n
   return nesterov ? g + mu * gm(t.mom)[i] : gm(t.mom)[i];
 }
 
+// The update at N x 4 values, each four from a multiple of four on and inside
+// (in[]), else zeros.  All loads at once, without a branch between them (where
+// there is no momentum, the gradient's again): taken one by one they left
+// 2048 x 18432 at 86 us.
+template <int N>
+__device__ __forceinline__ void update4(const Mat& t, const long (&at)[N], const bool (&in)[N], float mu, int nesterov,
+                                        float4 (&u)[N]) {
+  const float* gp = gm(t.grad);
+  const bool mom = gm(t.mom) != nullptr;
+  const float* mp = mom ? (const float*)gm(t.mom) : gp;
+  float4 m[N];
+#pragma unroll
+  for (int z = 0; z < N; ++z) u[z] = *(const float4*)(gp + (in[z] ? at[z] : 0));
+#pragma unroll
+  for (int z = 0; z < N; ++z) m[z] = *(const float4*)(mp + (in[z] ? at[z] : 0));
+  auto one = [&](bool in, float g, float m) {
+    return !in ? 0.f : !mom ? g : nesterov ? g + mu * m : m;
+  };
+#pragma unroll
+  for (int z = 0; z < N; ++z)
+    u[z] = make_float4(one(in[z], u[z].x, m[z].x), one(in[z], u[z].y, m[z].y), one(in[z], u[z].z, m[z].z),
+                       one(in[z], u[z].w, m[z].w));
+}
+
 // Sum over the block's 256 threads (the same value in all of them).
 __device__ __forceinline__ double block_sum(double s, double* sh) {
 #pragma unroll
@@ -177,10 +201,14 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
   const bool flip = t.rows > t.cols;
   double s = 0;
   for (int q = threadIdx.x; q < t.norm_blocks; q += 256) s += gm(t.norm)[q];
-  const double norm = sqrt(block_sum(s, sh)) + eps;
-  // a zero matrix stays zero; 1 / |U| may pass float32's range, so the product
-  // below is taken in float64
-  const double inv = norm > 0 || norm != norm ? kSX / norm : 0.0;
+  // the sums' barriers come after the loads of the first piece
+  double inv = 0;
+  auto scale = [&]() {
+    const double norm = sqrt(block_sum(s, sh)) + eps;
+    // a zero matrix stays zero; 1 / |U| may pass float32's range, so the
+    // product below is taken in float64
+    inv = norm > 0 || norm != norm ? kSX / norm : 0.0;
+  };
   auto put = [&](int i, int j, const float* f) {
     f16x8 h;
 #pragma unroll
@@ -191,15 +219,42 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
   for (int b = b0; b < b0 + t.norm_per; ++b) {
     if (flip) {
       const int nt = t.np / 64, i0 = b / nt * 64, j0 = b % nt * 64;
-      float u[16];
+      // four values of a row at once where their addresses allow it: 16 rows of
+      // the matrix a turn, else 4 (9216 x 1024: 25 us, 40)
+      if (t.cols % 4 == 0) {
+        float4 u[4];
+        const int c = i0 + threadIdx.x % 16 * 4;
+        long src[4];
+        bool in[4];
 #pragma unroll
-      for (int z = 0; z < 16; ++z) {
-        const int r = j0 + z * 4 + (threadIdx.x >> 6), c = i0 + (threadIdx.x & 63);
-        u[z] = r < t.rows && c < t.cols ? update_of(t, (long)r * t.cols + c, mu, nesterov) : 0.f;
+        for (int z = 0; z < 4; ++z) {
+          const int r = j0 + 16 * z + threadIdx.x / 16;
+          src[z] = (long)r * t.cols + c;
+          in[z] = r < t.rows && c < t.cols;
+        }
+        update4(t, src, in, mu, nesterov, u);
+        if (b == b0) scale();
+        __syncthreads();   // the previous piece has been read
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          float* to = &tile[16 * z + threadIdx.x / 16][threadIdx.x % 16 * 4];
+          to[0] = u[z].x;
+          to[1] = u[z].y;
+          to[2] = u[z].z;
+          to[3] = u[z].w;
+        }
+      } else {
+        float u[16];
+#pragma unroll
+        for (int z = 0; z < 16; ++z) {
+          const int r = j0 + z * 4 + (threadIdx.x >> 6), c = i0 + (threadIdx.x & 63);
+          u[z] = r < t.rows && c < t.cols ? update_of(t, (long)r * t.cols + c, mu, nesterov) : 0.f;
+        }
+        if (b == b0) scale();
+        __syncthreads();
+#pragma unroll
+        for (int z = 0; z < 16; ++z) tile[z * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = u[z];
       }
-      __syncthreads();   // the previous piece has been read
-#pragma unroll
-      for (int z = 0; z < 16; ++z) tile[z * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = u[z];
       __syncthreads();
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
@@ -211,31 +266,38 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
       }
       continue;
     }
-    const int nt = t.np / 128, i0 = b / nt * 32, j0 = b % nt * 128;
+    const int nt = t.np / 128, i0 = b / nt * 32 + threadIdx.x / 16, j = b % nt * 128 + threadIdx.x % 16 * 8;
+    float u[2][8];
+    if (t.cols % 4 == 0) {
+      float4 f[4];
+      long src[4];
+      bool in[4];
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const int i = i0 + 16 * z + threadIdx.x / 16, j = j0 + threadIdx.x % 16 * 8;
-      const long src = (long)i * t.cols + j;
-      float u[8];
-      if (i < t.rows && j + 8 <= t.cols && t.cols % 4 == 0) {
-        const float4 g0 = *(const float4*)(gm(t.grad) + src), g1 = *(const float4*)(gm(t.grad) + src + 4);
-        const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
-        if (gm(t.mom)) {
-          const float4 m0 = *(const float4*)(gm(t.mom) + src), m1 = *(const float4*)(gm(t.mom) + src + 4);
-          const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
-#pragma unroll
-          for (int v = 0; v < 8; ++v) u[v] = nesterov ? g[v] + mu * m[v] : m[v];
-        } else {
-#pragma unroll
-          for (int v = 0; v < 8; ++v) u[v] = g[v];
-        }
-      } else {
-#pragma unroll
-        for (int v = 0; v < 8; ++v)
-          u[v] = i < t.rows && j + v < t.cols ? update_of(t, src + v, mu, nesterov) : 0.f;
+      for (int z = 0; z < 4; ++z) {
+        const int i = i0 + z / 2 * 16, c = j + z % 2 * 4;
+        src[z] = (long)i * t.cols + c;
+        in[z] = i < t.rows && c < t.cols;
       }
-      put(i, j, u);
+      update4(t, src, in, mu, nesterov, f);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        u[z / 2][z % 2 * 4] = f[z].x;
+        u[z / 2][z % 2 * 4 + 1] = f[z].y;
+        u[z / 2][z % 2 * 4 + 2] = f[z].z;
+        u[z / 2][z % 2 * 4 + 3] = f[z].w;
+      }
+    } else {
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          const int i = i0 + 16 * z;
+          u[z][v] = i < t.rows && j + v < t.cols ? update_of(t, (long)i * t.cols + j + v, mu, nesterov) : 0.f;
+        }
     }
+    if (b == b0) scale();
+#pragma unroll
+    for (int z = 0; z < 2; ++z) put(i0 + 16 * z, j, u[z]);
   }
 }
 
@@ -1078,10 +1140,11 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   }
   // Columns of a tile of P X and X X^T.  P X on tiles of 128 x 192 takes a
   // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 158 us,
-  // 184); it is taken where the tiles make two blocks a CU.  Where 128 x 128
-  // leaves CUs without one, 64 x 64 with twice the stages in flight.  The sums'
-  // order is the same in all of them.
-  const int ba = t192 >= kBlocks ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
+  // 184; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken where
+  // its tiles make one block a CU.  Where 128 x 128 leaves CUs without one, 64 x
+  // 64 with twice the stages in flight.  The sums' order is the same in all of
+  // them.
+  const int ba = t192 >= 256 ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
   auto grams = [&](const Mat& t) { return uppers(t.mp / bg) * t.split; };
   auto sums = [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; };
   auto applies = [&](const Mat& t) { return (t.mp / std::min(ba, 128)) * cdiv(t.np, ba); };
