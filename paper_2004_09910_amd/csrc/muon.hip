@@ -190,6 +190,18 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float 
   if (threadIdx.x == 0) gm(t.norm)[b] = s;
 }
 
+// What U is multiplied by for X: kSX / norm, a factor that may pass float32's
+// range, as a power of two, which is exact, and the rest.  A zero matrix stays
+// zero.
+struct Scale {
+  float rest;
+  int two;
+  __device__ __forceinline__ explicit Scale(double norm) {
+    rest = (float)frexp(norm > 0 || norm != norm ? kSX / norm : 0.0, &two);
+  }
+  __device__ __forceinline__ float operator()(float u) const { return ldexpf(u, two) * rest; }
+};
+
 // X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
 // in the padding: a piece is 64 rows x 64 columns through LDS where the matrix
 // is transposed, else 32 rows x 128 columns.
@@ -202,17 +214,12 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
   double s = 0;
   for (int q = threadIdx.x; q < t.norm_blocks; q += 256) s += gm(t.norm)[q];
   // the sums' barriers come after the loads of the first piece
-  double inv = 0;
-  auto scale = [&]() {
-    const double norm = sqrt(block_sum(s, sh)) + eps;
-    // a zero matrix stays zero; 1 / |U| may pass float32's range, so the
-    // product below is taken in float64
-    inv = norm > 0 || norm != norm ? kSX / norm : 0.0;
-  };
+  Scale scale(0);
+  auto set_scale = [&]() { scale = Scale(sqrt(block_sum(s, sh)) + eps); };
   auto put = [&](int i, int j, const float* f) {
     f16x8 h;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(f[v] * inv);
+    for (int v = 0; v < 8; ++v) h[v] = (f16)scale(f[v]);
     *(f16x8*)(gm(t.x[0]) + at(t.mp, i, j)) = h;
   };
   const int b0 = (blockIdx.x - l->blk0[L_NORMALIZE][k]) * t.norm_per;
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
           in[z] = r < t.rows && c < t.cols;
         }
         update4(t, src, in, mu, nesterov, u);
-        if (b == b0) scale();
+        if (b == b0) set_scale();
         __syncthreads();   // the previous piece has been read
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
@@ -250,7 +257,7 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
           const int r = j0 + z * 4 + (threadIdx.x >> 6), c = i0 + (threadIdx.x & 63);
           u[z] = r < t.rows && c < t.cols ? update_of(t, (long)r * t.cols + c, mu, nesterov) : 0.f;
         }
-        if (b == b0) scale();
+        if (b == b0) set_scale();
         __syncthreads();
 #pragma unroll
         for (int z = 0; z < 16; ++z) tile[z * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = u[z];
@@ -295,7 +302,7 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
           u[z][v] = i < t.rows && j + v < t.cols ? update_of(t, (long)i * t.cols + j + v, mu, nesterov) : 0.f;
         }
     }
-    if (b == b0) scale();
+    if (b == b0) set_scale();
 #pragma unroll
     for (int z = 0; z < 2; ++z) put(i0 + 16 * z, j, u[z]);
   }
@@ -794,22 +801,30 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 
 // ------------------------------------------------- small matrices, whole
 
-// A matrix whose X fits in LDS: the whole update by one block of eight waves,
+// A matrix whose X fits in LDS: the whole update by one block of twelve waves,
 // X, A and P staying in LDS (panels of 32 columns, a row's 64 bytes 80 apart:
 // eight rows read at one chunk hit distinct banks).  MS: m rounded up to 32 or
-// 64.  What it does is bound by the latencies between its barriers, four a
-// step; five launches a step take five times as long.
-constexpr int kSmallT = 512, kSmallX = 16384, kRow = 80;   // threads, most values of X, bytes of a row
-constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT;
+// 64; RANGES: of A's sum, each one's a wave (or four).  What bounds it is one
+// CU's rate of loading and the latencies between its barriers, three a step:
+// five steps of 16 x 144 take 12.4 us, of 64 x 576 33, where four launches a
+// step take 89.  (Eight waves 36 us, sixteen 37.)
+constexpr int kSmallT = 768, kSmallX = 55296, kRow = 80;   // threads, most values of X, bytes of a row
+// chunks of 8 values of a thread, and those whose loads are in flight together
+constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT, kFlight = 2;
+// Columns from which on the one fragment's sum is dealt to five waves: 32 x
+// 1152 35.2 -> 29.8 us, 32 x 512 19.7 -> 18.9; two more barriers and 0.7 us for
+// the short ones.  Four fragments gain little from two ranges each (64 x 576
+// 32.9 -> 31.9, 64 x 256 20.1 -> 20.7) and take one.
+constexpr int kSmallLong = 512;
 
 struct SmallLds {
   unsigned char xs[kSmallX / 32 * kRow];               // X
   unsigned char as[2 * 64 * kRow], pms[2 * 64 * kRow];   // A, P
   float da[64], dp[64];                                // their diagonals' errors
-  double sh[8];
+  double sh[kSmallT / 64];
 };
 
-template <int MS>
+template <int MS, int RANGES>
 __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float mu, int nesterov, int steps,
                                              float eps) {
   constexpr int Q = MS / 32, F = Q * Q;   // fragments of A's side and of A
@@ -832,66 +847,73 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     }
     return c < chunks;
   };
-  float u[kSmallChunks][8], m[kSmallChunks][8];
-#pragma unroll
-  for (int z = 0; z < kSmallChunks; ++z) {
-    int i, j;
-#pragma unroll
-    for (int v = 0; v < 8; ++v) u[z][v] = m[z][v] = 0.f;
-    if (z * kSmallT >= chunks) break;
-    if (!place(z, i, j) || i >= t.m) continue;
-    if (vec && j + 8 <= t.n) {
-      const float4* g = (const float4*)(gm(t.grad) + i * t.cols + j);
-      const float4 g0 = g[0], g1 = g[1];
-      u[z][0] = g0.x; u[z][1] = g0.y; u[z][2] = g0.z; u[z][3] = g0.w;
-      u[z][4] = g1.x; u[z][5] = g1.y; u[z][6] = g1.z; u[z][7] = g1.w;
-      if (gm(t.mom)) {
-        const float4* q = (const float4*)(gm(t.mom) + i * t.cols + j);
-        const float4 m0 = q[0], m1 = q[1];
-        m[z][0] = m0.x; m[z][1] = m0.y; m[z][2] = m0.z; m[z][3] = m0.w;
-        m[z][4] = m1.x; m[z][5] = m1.y; m[z][6] = m1.z; m[z][7] = m1.w;
-      }
-    } else {
-#pragma unroll
-      for (int v = 0; v < 8; ++v)
-        if (j + v < t.n) {
-          const int e = flip ? (j + v) * t.cols + i : i * t.cols + j + v;
-          u[z][v] = gm(t.grad)[e];
-          if (gm(t.mom)) m[z][v] = gm(t.mom)[e];
-        }
-    }
-  }
+  float u[kSmallChunks][8];
   double sum = 0;
 #pragma unroll
-  for (int z = 0; z < kSmallChunks; ++z) {
-    int i, j;
-    if (z * kSmallT >= chunks) break;
-    if (!place(z, i, j) || i >= t.m) continue;
-    if (gm(t.mom)) {
+  for (int z0 = 0; z0 < kSmallChunks; z0 += kFlight) {
+    if (z0 * kSmallT >= chunks) break;
+    float m[kFlight][8];
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        m[z][v] = mu * m[z][v] + u[z][v];
-        u[z][v] = nesterov ? u[z][v] + mu * m[z][v] : m[z][v];
-      }
+    for (int z = z0; z < min(z0 + kFlight, kSmallChunks); ++z) {
+      int i, j;
+#pragma unroll
+      for (int v = 0; v < 8; ++v) u[z][v] = m[z - z0][v] = 0.f;
+      if (!place(z, i, j) || i >= t.m) continue;
       if (vec && j + 8 <= t.n) {
-        float4* q = (float4*)(gm(t.mom) + i * t.cols + j);
-        q[0] = make_float4(m[z][0], m[z][1], m[z][2], m[z][3]);
-        q[1] = make_float4(m[z][4], m[z][5], m[z][6], m[z][7]);
+        const float4* g = (const float4*)(gm(t.grad) + i * t.cols + j);
+        const float4 g0 = g[0], g1 = g[1];
+        u[z][0] = g0.x; u[z][1] = g0.y; u[z][2] = g0.z; u[z][3] = g0.w;
+        u[z][4] = g1.x; u[z][5] = g1.y; u[z][6] = g1.z; u[z][7] = g1.w;
+        if (gm(t.mom)) {
+          const float4* q = (const float4*)(gm(t.mom) + i * t.cols + j);
+          const float4 m0 = q[0], m1 = q[1];
+          float* to = m[z - z0];
+          to[0] = m0.x; to[1] = m0.y; to[2] = m0.z; to[3] = m0.w;
+          to[4] = m1.x; to[5] = m1.y; to[6] = m1.z; to[7] = m1.w;
+        }
       } else {
 #pragma unroll
         for (int v = 0; v < 8; ++v)
-          if (j + v < t.n) gm(t.mom)[flip ? (j + v) * t.cols + i : i * t.cols + j + v] = m[z][v];
+          if (j + v < t.n) {
+            const int e = flip ? (j + v) * t.cols + i : i * t.cols + j + v;
+            u[z][v] = gm(t.grad)[e];
+            if (gm(t.mom)) m[z - z0][v] = gm(t.mom)[e];
+          }
       }
     }
 #pragma unroll
-    for (int v = 0; v < 8; ++v) sum += (double)u[z][v] * u[z][v];
+    for (int z = z0; z < min(z0 + kFlight, kSmallChunks); ++z) {
+      int i, j;
+      if (!place(z, i, j) || i >= t.m) continue;
+      if (gm(t.mom)) {
+        float* q = m[z - z0];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          q[v] = mu * q[v] + u[z][v];
+          u[z][v] = nesterov ? u[z][v] + mu * q[v] : q[v];
+        }
+        if (vec && j + 8 <= t.n) {
+          float4* to = (float4*)(gm(t.mom) + i * t.cols + j);
+          to[0] = make_float4(q[0], q[1], q[2], q[3]);
+          to[1] = make_float4(q[4], q[5], q[6], q[7]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            if (j + v < t.n) gm(t.mom)[flip ? (j + v) * t.cols + i : i * t.cols + j + v] = q[v];
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < 8; ++v) sum += (double)u[z][v] * u[z][v];
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) sh[wave] = sum;
   __syncthreads();
-  const double norm = sqrt(((sh[0] + sh[1]) + (sh[2] + sh[3])) + ((sh[4] + sh[5]) + (sh[6] + sh[7]))) + eps;
-  const double inv = norm > 0 || norm != norm ? kSX / norm : 0.0;
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < kSmallT / 64; ++w) sum += sh[w];
+  const Scale scale(sqrt(sum) + eps);
 #pragma unroll
   for (int z = 0; z < kSmallChunks; ++z) {
     int i, j;
@@ -899,7 +921,7 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     if (!place(z, i, j)) continue;
     f16x8 h;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) h[v] = (f16)(float)(u[z][v] * inv);
+    for (int v = 0; v < 8; ++v) h[v] = (f16)scale(u[z][v]);
     *(f16x8*)(xs + ((j >> 5) * MS + i) * kRow + (j & 31) * 2) = h;
   }
   __syncthreads();
@@ -924,20 +946,41 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(b, j0 + fr, i0 + 16 * h + 8 * hi) = c; });
   };
   const int i0 = wave % F / Q * 32, j0 = wave % Q * 32;   // this wave's fragment of A and P
+  static_assert((RANGES - 1) * F * 4096 <= sizeof(lds.as) + sizeof(lds.pms) && RANGES * F <= kSmallT / 64,
+                "partial sums in A's and P's place");
+  const int range = wave / F;
   for (int s = 0; s < steps; ++s) {
-    // A = X X^T, the even and the odd panels' sums apart
+    // A = X X^T, the even and the odd panels' sums apart; a long sum in ranges
+    // of other waves, whose results lie where A and P will
     f32x4_t f[4];
-    if (wave < F) {
+    if (range < RANGES) {
       f32x16 acc = {}, odd = {};
-      for (int p = 0; p < ns / 32; p += 2) {
+      const int p1 = ns / 32 * (range + 1) / RANGES;
+      for (int p = ns / 32 * range / RANGES; p < p1; p += 2) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           acc = mfma(rows_of(xs, p, i0, kk), rows_of(xs, p, j0, kk), acc);
-          if (p + 1 < ns / 32) odd = mfma(rows_of(xs, p + 1, i0, kk), rows_of(xs, p + 1, j0, kk), odd);
+          if (p + 1 < p1) odd = mfma(rows_of(xs, p + 1, i0, kk), rows_of(xs, p + 1, j0, kk), odd);
         }
       }
 #pragma unroll
-      for (int g = 0; g < 4; ++g) f[g] = (part_of(acc, g) + part_of(odd, g)) * (1.f / (kSX * kSX));
+      for (int g = 0; g < 4; ++g) f[g] = part_of(acc, g) + part_of(odd, g);
+    }
+    if constexpr (RANGES > 1) {
+      f32x4_t* part = (f32x4_t*)as + wave % F * 256 + lane;
+      if (range > 0 && range < RANGES)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) part[((range - 1) * F * 4 + g) * 64] = f[g];
+      __syncthreads();
+      if (range == 0)
+        for (int q = 0; q < RANGES - 1; ++q)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) f[g] += part[(q * F * 4 + g) * 64];
+      __syncthreads();
+    }
+    if (wave < F) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) f[g] *= 1.f / (kSX * kSX);
       store(as, da, i0, j0, f);
     }
     // one wave reads what its other lanes wrote: LDS keeps a wave's order, and
@@ -965,7 +1008,7 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     }
     __syncthreads();
     // X = P X, a panel a wave and turn, in place
-    for (int pj = wave; pj < ns / 32; pj += 8) {
+    for (int pj = wave; pj < ns / 32; pj += kSmallT / 64) {
       f32x16 acc[Q] = {};
 #pragma unroll
       for (int p = 0; p < Q; ++p)
@@ -1003,8 +1046,9 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
 __global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
   __shared__ __attribute__((aligned(16))) SmallLds lds;
   const Mat& t = l.t[blockIdx.x];
-  if (t.m > 32) small_update<64>(lds, t, mu, nesterov, steps, eps);
-  else small_update<32>(lds, t, mu, nesterov, steps, eps);
+  if (t.m > 32) small_update<64, 1>(lds, t, mu, nesterov, steps, eps);
+  else if (t.n > kSmallLong) small_update<32, 5>(lds, t, mu, nesterov, steps, eps);
+  else small_update<32, 1>(lds, t, mu, nesterov, steps, eps);
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }

@@ -183,6 +183,25 @@ def test_muon_side_stream_and_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, m + o))
 
 
+@pytest.mark.parametrize("r,c", [(32, 512), (32, 513), (1728, 30), (31, 1729), (64, 864), (865, 64), (50, 860), (33, 863),
+                                 (16, 1616), (1616, 16)])
+def test_update_of_middling_matrices(r, c):
+    """On both sides of where one block does a matrix alone, and of where its waves share a sum."""
+    say("muon", r, c)
+    g, m = _grad(r, c, r + c), _grad(r, c, 2 * r + c)
+    for mom, steps in ((m, 5), (m, 2), (None, 5)):
+        (mg, o), = _muon([(g, mom)], steps=steps)
+        mw, ow = ref.muon(g, mom, 0.95, True, steps, 1e-7)
+        assert ref.rel(o, ow) <= UPDATE
+        assert mom is None or ref.rel(mg, mw) <= 2.0 ** -23
+    bad = g.clone()
+    bad[r // 2, c // 3] = float("nan")
+    (_, a), (_, b), (_, d) = _muon([(g, m), (bad, m), (g, m)])
+    assert bool(torch.isnan(b.float()).all()) and torch.equal(a, d)
+    (_, z), = _muon([(torch.zeros(r, c), None)])
+    assert bool((z == 0).all())
+
+
 SIZES = [0, 1, 3, 4, 7, 64, 1000, 1024, 1025, 40001, 300000]
 
 
