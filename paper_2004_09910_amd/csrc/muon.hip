@@ -47,6 +47,7 @@ constexpr float kSX = 2048.f, kSM = 1024.f;
 
 constexpr int kNormBlocks = 1024;  // most partial sums of |U|^2 of a matrix
 constexpr int kMaxMats = 20;       // matrices of one launch
+constexpr int kFirstT = 768;       // threads of the first launch's blocks
 
 struct Mat {
   const float* grad;
@@ -58,6 +59,9 @@ struct Mat {
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
   int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;
   int two;             // takes two steps at a time
+  // one block's: no blocks of the other launches, and nothing but the addresses
+  // and rows .. n set
+  __host__ __device__ bool whole() const { return norm_blocks == 0; }
 };
 
 // The matrices of a list and, for each kind of launch, the first block of each
@@ -130,6 +134,18 @@ __device__ __forceinline__ void update4(const Mat& t, const long (&at)[N], const
                        one(in[z], u[z].w, m[z].w));
 }
 
+// Sum over the first launch's threads (the same value in all of them).
+__device__ __forceinline__ double first_sum(double s, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0;
+#pragma unroll
+  for (int w = 0; w < kFirstT / 64; ++w) s += sh[w];
+  return s;
+}
+
 // Sum over the block's 256 threads (the same value in all of them).
 __device__ __forceinline__ double block_sum(double s, double* sh) {
 #pragma unroll
@@ -139,17 +155,19 @@ __device__ __forceinline__ double block_sum(double s, double* sh) {
   return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
+// Leaves the argument in the workspace, by one block.
+__device__ __forceinline__ void leave_table(const Mats& l, Mats* table) {
+  for (int i = threadIdx.x; i < (int)(sizeof(Mats) / 4); i += kFirstT) ((int*)table)[i] = ((const int*)&l)[i];
+}
+
 // M = mu M + G, and partial sums of U^2 (in float64: squares of float32 values
-// neither overflow nor vanish).  Purely a matter of memory: 16-byte accesses,
-// two of each tensor in flight a thread.
-__global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float mu, int nesterov) {
-  __shared__ double sh[4];
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < (int)(sizeof(Mats) / 4); i += 256) ((int*)table)[i] = ((const int*)&l)[i];
-  const int k = find(&l, L_MOMENTUM, blockIdx.x);
+// neither overflow nor vanish), block blk's of the launch.  Purely a matter of
+// memory: 16-byte accesses, two of each tensor in flight a thread.
+__device__ __forceinline__ void momentum(const Mats& l, int blk, float mu, int nesterov, double* sh) {
+  const int k = find(&l, L_MOMENTUM, blk);
   const Mat& t = l.t[k];
-  const int b = blockIdx.x - l.blk0[L_MOMENTUM][k];
-  const long N = (long)t.rows * t.cols, N4 = N / 4, step = (long)t.norm_blocks * 256;
+  const int b = blk - l.blk0[L_MOMENTUM][k];
+  const long N = (long)t.rows * t.cols, N4 = N / 4, step = (long)t.norm_blocks * kFirstT;
   const float4* g4 = (const float4*)gm(t.grad);
   float4* m4 = (float4*)gm(t.mom);
   double s = 0;
@@ -161,7 +179,7 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float 
     }
     s += (double)u * u;
   };
-  for (long i = (long)b * 256 + threadIdx.x; i < N4; i += 2 * step) {
+  for (long i = (long)b * kFirstT + threadIdx.x; i < N4; i += 2 * step) {
     const bool two = i + step < N4;
     float4 g[2], m[2];
     g[0] = g4[i];
@@ -186,8 +204,15 @@ __global__ __launch_bounds__(256) void muon_momentum(Mats l, Mats* table, float 
     one(gm(t.grad)[e], m);
     if (gm(t.mom)) gm(t.mom)[e] = m;
   }
-  s = block_sum(s, sh);
+  s = first_sum(s, sh);
   if (threadIdx.x == 0) gm(t.norm)[b] = s;
+}
+
+// The first launch of a list without matrices that one block does whole.
+__global__ __launch_bounds__(kFirstT) void muon_momentum(Mats l, Mats* table, float mu, int nesterov) {
+  __shared__ double sh[kFirstT / 64];
+  if (blockIdx.x == 0) leave_table(l, table);
+  momentum(l, blockIdx.x, mu, nesterov, sh);
 }
 
 // What U is multiplied by for X: kSX / norm, a factor that may pass float32's
@@ -804,40 +829,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 // A matrix whose X fits in LDS: the whole update by one block of twelve waves,
 // X, A and P staying in LDS (panels of 32 columns, a row's 64 bytes 80 apart:
 // eight rows read at one chunk hit distinct banks).  MS: m rounded up to 32 or
-// 64; RANGES: of A's sum, each one's a wave (or four).  What bounds it is one
-// CU's rate of loading and the latencies between its barriers, three a step:
-// five steps of 16 x 144 take 12.4 us, of 64 x 576 33, where four launches a
-// step take 89.  (Eight waves 36 us, sixteen 37.)
-constexpr int kSmallT = 768, kSmallX = 55296, kRow = 80;   // threads, most values of X, bytes of a row
+// 64.  What bounds it is one CU's rate of loading and the latencies between its
+// barriers, three a step: five steps of 16 x 144 take 12.4 us, of 64 x 256 20
+// (eight waves 20.5, sixteen 22.5), where four launches a step take 70 to 90.
+// LDS holds up to 55296 values, and a list of 64 x 576 alone would gain (89 us
+// as tiles, 33); among others such a block outlasts the launch it shares by
+// more than a few matrices more cost the tiles (9 matrices of all sorts with
+// one of 1144 x 9: 158 us, 177).
+constexpr int kSmallX = 16384, kRow = 80;   // most values of X, bytes of a row
 // chunks of 8 values of a thread, and those whose loads are in flight together
-constexpr int kSmallChunks = (kSmallX / 8 + kSmallT - 1) / kSmallT, kFlight = 2;
-// Columns from which on the one fragment's sum is dealt to five waves: 32 x
-// 1152 35.2 -> 29.8 us, 32 x 512 19.7 -> 18.9; two more barriers and 0.7 us for
-// the short ones.  Four fragments gain little from two ranges each (64 x 576
-// 32.9 -> 31.9, 64 x 256 20.1 -> 20.7) and take one.
-constexpr int kSmallLong = 512;
+constexpr int kSmallChunks = (kSmallX / 8 + kFirstT - 1) / kFirstT, kFlight = 2;
 
 struct SmallLds {
   unsigned char xs[kSmallX / 32 * kRow];               // X
   unsigned char as[2 * 64 * kRow], pms[2 * 64 * kRow];   // A, P
   float da[64], dp[64];                                // their diagonals' errors
-  double sh[kSmallT / 64];
+  double sh[kFirstT / 64];
 };
 
-template <int MS, int RANGES>
+template <int MS>
 __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float mu, int nesterov, int steps,
                                              float eps) {
   constexpr int Q = MS / 32, F = Q * Q;   // fragments of A's side and of A
   unsigned char *xs = lds.xs, *as = lds.as, *pms = lds.pms;
   float *da = lds.da, *dp = lds.dp;
-  double* sh = lds.sh;
   const int ns = (t.n + 31) / 32 * 32, chunks = MS * ns / 8;
   const bool flip = t.rows > t.cols, vec = !flip && t.cols % 4 == 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // U in registers: chunk z of this thread is 8 columns from j of row i
   auto place = [&](int z, int& i, int& j) {
-    const int c = z * kSmallT + tid;
+    const int c = z * kFirstT + tid;
     if (flip) {
       i = c % MS;
       j = c / MS * 8;
@@ -851,7 +873,7 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
   double sum = 0;
 #pragma unroll
   for (int z0 = 0; z0 < kSmallChunks; z0 += kFlight) {
-    if (z0 * kSmallT >= chunks) break;
+    if (z0 * kFirstT >= chunks) break;
     float m[kFlight][8];
 #pragma unroll
     for (int z = z0; z < min(z0 + kFlight, kSmallChunks); ++z) {
@@ -906,18 +928,11 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
       for (int v = 0; v < 8; ++v) sum += (double)u[z][v] * u[z][v];
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) sh[wave] = sum;
-  __syncthreads();
-  sum = 0;
-#pragma unroll
-  for (int w = 0; w < kSmallT / 64; ++w) sum += sh[w];
-  const Scale scale(sqrt(sum) + eps);
+  const Scale scale(sqrt(first_sum(sum, lds.sh)) + eps);
 #pragma unroll
   for (int z = 0; z < kSmallChunks; ++z) {
     int i, j;
-    if (z * kSmallT >= chunks) break;
+    if (z * kFirstT >= chunks) break;
     if (!place(z, i, j)) continue;
     f16x8 h;
 #pragma unroll
@@ -946,41 +961,20 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     put8(pk, [&](int h, u32x4 c) { *(u32x4*)four(b, j0 + fr, i0 + 16 * h + 8 * hi) = c; });
   };
   const int i0 = wave % F / Q * 32, j0 = wave % Q * 32;   // this wave's fragment of A and P
-  static_assert((RANGES - 1) * F * 4096 <= sizeof(lds.as) + sizeof(lds.pms) && RANGES * F <= kSmallT / 64,
-                "partial sums in A's and P's place");
-  const int range = wave / F;
   for (int s = 0; s < steps; ++s) {
-    // A = X X^T, the even and the odd panels' sums apart; a long sum in ranges
-    // of other waves, whose results lie where A and P will
+    // A = X X^T, the even and the odd panels' sums apart
     f32x4_t f[4];
-    if (range < RANGES) {
+    if (wave < F) {
       f32x16 acc = {}, odd = {};
-      const int p1 = ns / 32 * (range + 1) / RANGES;
-      for (int p = ns / 32 * range / RANGES; p < p1; p += 2) {
+      for (int p = 0; p < ns / 32; p += 2) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           acc = mfma(rows_of(xs, p, i0, kk), rows_of(xs, p, j0, kk), acc);
-          if (p + 1 < p1) odd = mfma(rows_of(xs, p + 1, i0, kk), rows_of(xs, p + 1, j0, kk), odd);
+          if (p + 1 < ns / 32) odd = mfma(rows_of(xs, p + 1, i0, kk), rows_of(xs, p + 1, j0, kk), odd);
         }
       }
 #pragma unroll
-      for (int g = 0; g < 4; ++g) f[g] = part_of(acc, g) + part_of(odd, g);
-    }
-    if constexpr (RANGES > 1) {
-      f32x4_t* part = (f32x4_t*)as + wave % F * 256 + lane;
-      if (range > 0 && range < RANGES)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) part[((range - 1) * F * 4 + g) * 64] = f[g];
-      __syncthreads();
-      if (range == 0)
-        for (int q = 0; q < RANGES - 1; ++q)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) f[g] += part[(q * F * 4 + g) * 64];
-      __syncthreads();
-    }
-    if (wave < F) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g) f[g] *= 1.f / (kSX * kSX);
+      for (int g = 0; g < 4; ++g) f[g] = (part_of(acc, g) + part_of(odd, g)) * (1.f / (kSX * kSX));
       store(as, da, i0, j0, f);
     }
     // one wave reads what its other lanes wrote: LDS keeps a wave's order, and
@@ -1008,7 +1002,7 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     }
     __syncthreads();
     // X = P X, a panel a wave and turn, in place
-    for (int pj = wave; pj < ns / 32; pj += kSmallT / 64) {
+    for (int pj = wave; pj < ns / 32; pj += kFirstT / 64) {
       f32x16 acc[Q] = {};
 #pragma unroll
       for (int p = 0; p < Q; ++p)
@@ -1043,12 +1037,20 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
   }
 }
 
-__global__ __launch_bounds__(kSmallT) void muon_small(Mats l, float mu, int nesterov, int steps, float eps) {
+// The first launch of a list with such matrices: a block each, while the other
+// blocks take the others' momentum.
+__global__ __launch_bounds__(kFirstT) void muon_whole(Mats l, Mats* table, int wholes, float mu, int nesterov, int steps,
+                                                      float eps) {
   __shared__ __attribute__((aligned(16))) SmallLds lds;
-  const Mat& t = l.t[blockIdx.x];
-  if (t.m > 32) small_update<64, 1>(lds, t, mu, nesterov, steps, eps);
-  else if (t.n > kSmallLong) small_update<32, 5>(lds, t, mu, nesterov, steps, eps);
-  else small_update<32, 1>(lds, t, mu, nesterov, steps, eps);
+  const int blk = blockIdx.x;
+  if (blk >= wholes) {
+    if (blk == wholes) leave_table(l, table);
+    momentum(l, blk - wholes, mu, nesterov, lds.sh);
+    return;
+  }
+  const Mat& t = l.t[l.count - wholes + blk];   // the last of the list
+  if (t.m > 32) small_update<64>(lds, t, mu, nesterov, steps, eps);
+  else small_update<32>(lds, t, mu, nesterov, steps, eps);
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -1065,7 +1067,7 @@ bool pairs(const tgp_muon_tensor& d) {
   return std::max(d.rows, d.cols) >= 4 * (long)std::min(d.rows, d.cols);
 }
 
-// Whether one block does the whole update (muon_small).
+// Whether one block does the whole update.
 bool small(const tgp_muon_tensor& d) {
   const long m = std::min(d.rows, d.cols), n = std::max(d.rows, d.cols);
   return m <= 64 && (m <= 32 ? 32 : 64) * ((n + 31) / 32 * 32) <= kSmallX;
@@ -1089,7 +1091,7 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 // kRange stages at least (writing and reading back a partial tile takes the
 // time of 20 stages).  The ranges depend on the matrix alone, so that its
 // update does not depend on the others of the call.
-size_t lay_out(bool whole, int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
+size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
     char* p = ws + pos;
     pos += al256(bytes);
@@ -1100,12 +1102,12 @@ size_t lay_out(bool whole, int n, const tgp_muon_tensor* const* d, char* ws, siz
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
     describe(*d[k], t);
-    if (whole) continue;
+    if (small(*d[k])) continue;
     t.two = pairs(*d[k]);
     t.mp = up(t.m);
     t.np = up(t.n);
     const long size = (long)t.rows * t.cols;
-    t.norm_blocks = (int)std::min<long>(kNormBlocks, cdiv(size, 4096));
+    t.norm_blocks = (int)std::min<long>(kNormBlocks, cdiv(size, 8 * kFirstT));
     t.norm_per = size >= 1 << 22 ? 4 : 1;   // where it is large, |U| is summed up by fewer blocks
     t.norm = (double*)take(kNormBlocks * sizeof(double));
     for (int z = 0; z < 2; ++z) t.x[z] = (f16*)take((size_t)t.mp * t.np * 2);
@@ -1120,29 +1122,28 @@ size_t lay_out(bool whole, int n, const tgp_muon_tensor* const* d, char* ws, siz
   return pos;
 }
 
-// Deals the matrices into lists, the small ones and the tiled ones apart;
-// within a list those of the longest sums come first (stable), so that the
-// short ones fill up its launches' ends.  Calls go(whether small, list of
+// Deals the matrices into lists of at most kMaxMats: the tiled ones, those of
+// the longest sums first (stable), so that the short ones fill up a launch's
+// end, and after them those that one block does whole.  Calls go(list of
 // pointers, count).
 template <typename F>
 void each_list(int n, const tgp_muon_tensor* t, F go) {
-  for (int kind = 0; kind < 2; ++kind) {
-    const tgp_muon_tensor* list[kMaxMats];
-    int count = 0;
-    auto flush = [&]() {
-      std::stable_sort(list, list + count, [](const tgp_muon_tensor* a, const tgp_muon_tensor* b) {
-        return std::min(a->rows, a->cols) > std::min(b->rows, b->cols);
-      });
-      if (count) go(kind == 0, list, count);
-      count = 0;
-    };
+  const tgp_muon_tensor* list[kMaxMats];
+  int count = 0;
+  auto flush = [&]() {
+    std::stable_sort(list, list + count, [](const tgp_muon_tensor* a, const tgp_muon_tensor* b) {
+      return small(*a) != small(*b) ? small(*b) : std::min(a->rows, a->cols) > std::min(b->rows, b->cols);
+    });
+    if (count) go(list, count);
+    count = 0;
+  };
+  for (int kind = 0; kind < 2; ++kind)
     for (int k = 0; k < n; ++k) {
-      if (small(t[k]) != (kind == 0)) continue;
+      if (small(t[k]) != (kind == 1)) continue;
       list[count++] = t + k;
       if (count == kMaxMats) flush();
     }
-    flush();
-  }
+  flush();
 }
 
 // Fills blk0 of a launch with blocks(t) of each matrix; returns the grid.
@@ -1157,27 +1158,24 @@ unsigned deal(Mats& l, int launch, F blocks) {
   return (unsigned)pos;
 }
 
-hipError_t update_small(const Mats& l, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
-  double n = 0, flops = 0;
-  for (int k = 0; k < l.count; ++k) {
-    const double m = l.t[k].m;
-    n += m * l.t[k].n;
-    flops += steps * (3 * m * m * l.t[k].n + m * m * m);
-  }
-  ProfScope ps("muon_small", flops, 14 * n, st);
-  TGP_LAUNCH(ps, muon_small, dim3(l.count), dim3(kSmallT), 0, st, l, mu, (int)nesterov, steps, eps);
-  return launch_status();
-}
-
 hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps, float eps, hipStream_t st) {
-  double n = 0, gram = 0, cube = 0, cells = 0;
+  double n = 0, gram = 0, cube = 0, cells = 0;   // of the tiled matrices
+  double wn = 0, wflops = 0;                     // of the others
   long t192 = 0, t128 = 0, g128 = 0;   // tiles of P X, of X X^T
+  int wholes = 0;
   for (int k = 0; k < l.count; ++k) {
     const Mat& t = l.t[k];
-    n += (double)t.rows * t.cols;
-    gram += (double)t.m * t.m * t.n;
-    cube += (double)t.m * t.m * t.m;
-    cells += (double)t.m * t.m;
+    const double m = t.m, mn = m * t.n;
+    if (t.whole()) {
+      ++wholes;
+      wn += mn;
+      wflops += steps * (3 * m * mn + m * m * m);
+      continue;
+    }
+    n += mn;
+    gram += m * mn;
+    cube += m * m * m;
+    cells += m * m;
     t192 += (long)(t.mp / 128) * cdiv(t.np, 192);
     t128 += (long)(t.mp / 128) * (t.np / 128);
     g128 += (long)uppers(t.mp / 128) * t.split;
@@ -1194,25 +1192,33 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   auto applies = [&](const Mat& t) { return (t.mp / std::min(ba, 128)) * cdiv(t.np, ba); };
   auto syms = [](const Mat& t) { return uppers(t.mp / 64); };
   unsigned grid[LAUNCHES];
-  grid[L_MOMENTUM] = deal(l, L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
-  grid[L_NORMALIZE] = deal(l, L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
-  grid[L_GRAM] = deal(l, L_GRAM, grams);
-  grid[L_SUM] = deal(l, L_SUM, sums);
-  grid[L_SYM] = deal(l, L_SYM, syms);
-  grid[L_APPLY] = deal(l, L_APPLY, applies);
-  grid[L_GRAM1] = deal(l, L_GRAM1, [&](const Mat& t) { return t.two ? 0 : grams(t); });
-  grid[L_SUM1] = deal(l, L_SUM1, [&](const Mat& t) { return t.two ? 0 : sums(t); });
-  grid[L_APPLY1] = deal(l, L_APPLY1, [&](const Mat& t) { return t.two ? 0 : applies(t); });
-  grid[L_SYM2] = deal(l, L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
+  auto tiled = [&](int launch, auto blocks) {
+    grid[launch] = deal(l, launch, [&](const Mat& t) { return t.whole() ? 0 : blocks(t); });
+  };
+  tiled(L_MOMENTUM, [](const Mat& t) { return t.norm_blocks; });
+  tiled(L_NORMALIZE, [](const Mat& t) { return t.mp * (t.np / 128) / 32 / t.norm_per; });
+  tiled(L_GRAM, grams);
+  tiled(L_SUM, sums);
+  tiled(L_SYM, syms);
+  tiled(L_APPLY, applies);
+  tiled(L_GRAM1, [&](const Mat& t) { return t.two ? 0 : grams(t); });
+  tiled(L_SUM1, [&](const Mat& t) { return t.two ? 0 : sums(t); });
+  tiled(L_APPLY1, [&](const Mat& t) { return t.two ? 0 : applies(t); });
+  tiled(L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
   // The products of m x m matrices with up to two blocks a CU wait for their
   // stages: six in flight, not four (one of 1024 x 4096 in all: 221 us, 238).
   // With more blocks, six leave room for fewer of them (2048 x 18432: 1179 us,
   // 1165 with four).
   auto deep = [&](int launch) { return grid[launch] <= kBlocks; };
   const Mats* tb = table;
-  {
+  if (wholes) {
+    ProfScope ps("muon_whole", wflops + 4 * n, 14 * wn + 12 * n, st);
+    TGP_LAUNCH(ps, muon_whole, dim3(wholes + grid[L_MOMENTUM]), dim3(kFirstT), 0, st, l, table, wholes, mu,
+               (int)nesterov, steps, eps);
+    if (!grid[L_MOMENTUM]) return launch_status();
+  } else {
     ProfScope ps("muon_momentum", 4 * n, 12 * n, st);
-    TGP_LAUNCH(ps, muon_momentum, dim3(grid[L_MOMENTUM]), dim3(256), 0, st, l, table, mu, (int)nesterov);
+    TGP_LAUNCH(ps, muon_momentum, dim3(grid[L_MOMENTUM]), dim3(kFirstT), 0, st, l, table, mu, (int)nesterov);
   }
   {
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
@@ -1290,8 +1296,8 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
 size_t muon_bytes(int n, const tgp_muon_tensor* t) {
   size_t pos = 0;
   Mats l;
-  each_list(n, t, [&](bool whole, const tgp_muon_tensor* const* d, int count) {
-    pos = lay_out(whole, count, d, nullptr, pos, l);
+  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count) {
+    pos = lay_out(count, d, nullptr, pos, l);
   });
   return pos;
 }
@@ -1300,13 +1306,12 @@ hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov,
                        float eps, void* ws, hipStream_t st) {
   size_t pos = 0;
   hipError_t e = hipSuccess;
-  each_list(n, t, [&](bool whole, const tgp_muon_tensor* const* d, int count) {
+  each_list(n, t, [&](const tgp_muon_tensor* const* d, int count) {
     if (e != hipSuccess) return;
     Mats l;
     Mats* table = (Mats*)((char*)ws + pos);
-    pos = lay_out(whole, count, d, (char*)ws, pos, l);
-    e = whole ? update_small(l, mu, nesterov, steps, eps, st)
-              : update_list(l, table, mu, nesterov, steps, eps, st);
+    pos = lay_out(count, d, (char*)ws, pos, l);
+    e = update_list(l, table, mu, nesterov, steps, eps, st);
   });
   return e;
 }
