@@ -6,7 +6,8 @@
 // Backward: with xhat = (x - mean) rstd and g = gain dy, dx = rstd (g -
 // mean(g) - xhat mean(g xhat)), and the column sums of dy xhat and dy.
 // Column sums are partial sums of row ranges, left in a workspace and added
-// up in a fixed order by a second launch.
+// up in a fixed order by a second launch; of few rows, blocks of their own
+// take them in the same launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,6 +21,7 @@ namespace {
 constexpr int kT = 256;          // threads of a block
 constexpr int kFwdBlocks = 2048; // most blocks of a forward launch
 constexpr int kColBlocks = 1024; // most row ranges of the column sums
+constexpr int kColFlight = 4;    // rows in flight of a lane that sums columns
 
 // Sum over the block's kT threads, the same value in every thread: a wave's
 // xor tree, then the waves' sums in order.
@@ -135,11 +137,12 @@ struct Share {
   static constexpr int V = VB / (int)sizeof(T);
   int l, G, nvec;
   long row0, step;   // first row of this lane, rows from one turn to the next
-  __device__ __forceinline__ Share(int C, int g) : G(BLK ? kT : g), nvec(C / V) {
+  // blocks: those of the launch that take rows
+  __device__ __forceinline__ Share(int C, int g, int blocks) : G(BLK ? kT : g), nvec(C / V) {
     const int per = BLK ? 1 : 64 / G, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     l = BLK ? threadIdx.x : lane & (G - 1);
     row0 = BLK ? blockIdx.x : ((long)blockIdx.x * 4 + wave) * per + lane / G;
-    step = (long)gridDim.x * (BLK ? 1 : 4 * per);
+    step = (long)blocks * (BLK ? 1 : 4 * per);
   }
   // first row of the block's first turn
   __device__ __forceinline__ long first() const { return BLK ? row0 : (long)blockIdx.x * 4 * (64 / G); }
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float
   typedef Share<T, VB, NV, BLK> SH;
   constexpr int V = SH::V;
   __shared__ float s4[4];
-  const SH sh(C, G);
+  const SH sh(C, G, gridDim.x);
   float gn[NV][V], bs[NV][V];
   sh.channels(gain, 1.f, gn);
   sh.channels(bias, 0.f, bs);
@@ -222,19 +225,84 @@ __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float
   }
 }
 
-// dx, and this block's column sums in part[block][2][C] (part NULL: none).
+// The whole column sums of four vectors of channels: 64 rows at a time, a
+// vector a lane, kColFlight rows a lane in flight.
+template <typename T, int VB>
+__device__ __forceinline__ void norm_cols(const T* dy, long lddy, const T* x, long ldx, const float2* stats,
+                                          long rows, int C, int blk, float* dgain, float* dbias, int overwrite) {
+  typedef Vec<T, VB> VT;
+  constexpr int V = VB / (int)sizeof(T);
+  __shared__ float sums[kT / 64][2 * V][4];
+  const int tid = threadIdx.x, q = blk * 4 + (tid & 3);
+  const bool has = q < C / V;
+  float a[V] = {}, b[V] = {};
+  for (long r0 = tid >> 2; r0 < rows; r0 += kColFlight * (kT / 4)) {
+    typename VT::raw rd[kColFlight], rx[kColFlight];
+    float2 st[kColFlight];
+#pragma unroll
+    for (int z = 0; z < kColFlight; ++z) {
+      const long r = r0 + z * (kT / 4);
+      rd[z] = rx[z] = typename VT::raw{};
+      st[z] = make_float2(0.f, 0.f);
+      if (!has || r >= rows) continue;
+      rd[z] = ((const typename VT::raw*)(dy + r * lddy))[q];
+      rx[z] = ((const typename VT::raw*)(x + r * ldx))[q];
+      st[z] = stats[r];
+    }
+#pragma unroll
+    for (int z = 0; z < kColFlight; ++z) {
+      float d[V], f[V];
+      VT::un(rd[z], d);
+      VT::un(rx[z], f);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        a[v] += d[v] * ((f[v] - st[z].x) * st[z].y);
+        b[v] += d[v];
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+#pragma unroll
+    for (int o = 4; o < 64; o <<= 1) {
+      a[v] += __shfl_xor(a[v], o);
+      b[v] += __shfl_xor(b[v], o);
+    }
+    if ((tid & 63) < 4) {
+      sums[tid >> 6][v][tid & 3] = a[v];
+      sums[tid >> 6][V + v][tid & 3] = b[v];
+    }
+  }
+  __syncthreads();
+  if (tid >= 8 * V) return;
+  const int l = tid & 3, e = tid >> 2;   // (lane, one of its 2 V sums)
+  const int c = (blk * 4 + l) * V + e % V;
+  if (c >= C) return;
+  const float s = (sums[0][e][l] + sums[1][e][l]) + (sums[2][e][l] + sums[3][e][l]);
+  float* to = (e < V ? dgain : dbias) + c;
+  *to = overwrite ? s : *to + s;
+}
+
+// dx, and the column sums: those of the block's rows in part[block][2][C]
+// (part NULL: none), or (DIRECT) the whole ones by the blocks after the
+// row_blocks that take rows.
 // Memory bounds it: 131072 x 128 bf16 take 19.8 us (5.1 TB/s) and their sums'
 // launch 3.9, 12544 x 256 8.4 and 3.2.
-template <typename T, int VB, int NV, bool BLK>
+template <typename T, int VB, int NV, bool BLK, bool DIRECT>
 __global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* x, long ldx,
                                                const float* __restrict__ gain,
                                                const float2* __restrict__ stats, T* dx, long lddx,
-                                               float* __restrict__ part, long rows, int C, int G) {
+                                               float* __restrict__ part, long rows, int C, int G,
+                                               int row_blocks, float* dgain, float* dbias, int overwrite) {
+  if (DIRECT && (int)blockIdx.x >= row_blocks) {
+    norm_cols<T, VB>(dy, lddy, x, ldx, stats, rows, C, blockIdx.x - row_blocks, dgain, dbias, overwrite);
+    return;
+  }
   typedef Vec<T, VB> VT;
   typedef Share<T, VB, NV, BLK> SH;
   constexpr int V = SH::V;
   __shared__ float s4[4];
-  const SH sh(C, G);
+  const SH sh(C, G, DIRECT ? row_blocks : gridDim.x);
   float gn[NV][V], a[NV][V], b[NV][V];
   sh.channels(gain, 1.f, gn);
 #pragma unroll
@@ -262,8 +330,10 @@ __global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* 
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         xh[k][v] = (xh[k][v] - st.x) * st.y;
-        a[k][v] += d[k][v] * xh[k][v];
-        b[k][v] += d[k][v];
+        if constexpr (!DIRECT) {
+          a[k][v] += d[k][v] * xh[k][v];
+          b[k][v] += d[k][v];
+        }
         const float g = d[k][v] * gn[k][v];
         s += g;
         p += g * xh[k][v];
@@ -281,7 +351,7 @@ __global__ __launch_bounds__(kT) void norm_bwd(const T* dy, long lddy, const T* 
       }
     }
   }
-  if (!part) return;
+  if (DIRECT || !part) return;
   float* out = part + (long)blockIdx.x * 2 * C;
   if constexpr (BLK) {
 #pragma unroll
@@ -474,16 +544,21 @@ void forward_regs(const Plan& p, const NormShape& s, const T* x, long ldx, const
 }
 
 template <typename T, int VB>
-void backward_regs(const Plan& p, unsigned grid, const NormShape& s, const T* dy, long lddy,
-                   const T* x, long ldx, const float* gain, const float2* stats, T* dx, long lddx,
-                   float* part, hipStream_t st) {
+void backward_regs(const Plan& p, bool direct, int row_blocks, int col_blocks, const NormShape& s, const T* dy,
+                   long lddy, const T* x, long ldx, const float* gain, const float2* stats, T* dx,
+                   long lddx, float* part, float* dgain, float* dbias, bool overwrite, hipStream_t st) {
   const double n = (double)s.rows * s.C;
   with_plan(p, [&](auto nv, auto blk) {
     constexpr int NV = decltype(nv)::value;
     constexpr bool BLK = decltype(blk)::value;
     ProfScope ps("layer_norm_bwd", 14 * n, (dx ? 3 : 2) * n * sizeof(T), st);
-    TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK>), dim3(grid), dim3(kT), 0, st, dy, lddy, x, ldx,
-               gain, stats, dx, lddx, part, s.rows, s.C, p.g);
+    if (direct)
+      TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK, true>), dim3(row_blocks + col_blocks), dim3(kT), 0, st, dy,
+                 lddy, x, ldx, gain, stats, dx, lddx, part, s.rows, s.C, p.g, row_blocks, dgain, dbias,
+                 (int)overwrite);
+    else
+      TGP_LAUNCH(ps, (norm_bwd<T, VB, NV, BLK, false>), dim3(row_blocks), dim3(kT), 0, st, dy, lddy, x, ldx,
+                 gain, stats, dx, lddx, part, s.rows, s.C, p.g, row_blocks, dgain, dbias, (int)overwrite);
   });
 }
 
@@ -494,6 +569,13 @@ void backward_regs(const Plan& p, unsigned grid, const NormShape& s, const T* dy
 int row_ranges(const NormShape& s) {
   return (int)std::min<long>(std::min<long>(kColBlocks, std::max<long>(256, s.rows / 24)), s.rows);
 }
+
+// Most rows whose column sums blocks of their own take, reading the rows once
+// more, in the one launch.  A launch less is worth more than the reading up to
+// there: 64 x 64 bf16 7.3 -> 3.8 us, 1024 x 128 7.3 -> 5.9, 1024 x 3848 21.4
+// -> 12.1 (2048 x 128 7.2, 9.0).  What bounds such a block is its CU's loads of
+// 64 bytes a row; eight rows in flight a lane take what four take.
+constexpr long kDirectRows = 1024;
 
 // Element size, and the bits of every address and row distance that the
 // widest vector has to divide.
@@ -537,15 +619,28 @@ hipError_t backward_t(const NormShape& s, const void* dy, long lddy, const void*
                          place<T>(dy, lddy) | place<T>(x, ldx) | (dx ? place<T>(dx, lddx) : 0));
   if (p.vb) {
     const int S = (int)even_grid(s.rows, rows_of_block(p), most);
-    auto regs = [&](auto vb) {
-      backward_regs<T, decltype(vb)::value>(p, (unsigned)S, s, (const T*)dy, lddy, (const T*)x, ldx,
-                                            gain, (const float2*)stats, (T*)dx, lddx,
-                                            dgain ? part : nullptr, st);
+    // the column sums: by blocks of their own, or of the rows' blocks
+    const bool direct = dgain && s.rows <= kDirectRows;
+    const int cols = direct ? cdiv((long)s.C * sizeof(T), 4 * p.vb) : 0;
+    auto launch = [&](int row_blocks, int col_blocks) {
+      auto regs = [&](auto vb) {
+        backward_regs<T, decltype(vb)::value>(p, direct, row_blocks, col_blocks, s, (const T*)dy, lddy, (const T*)x,
+                                              ldx, gain, (const float2*)stats, (T*)dx, lddx,
+                                              dgain && !direct ? part : nullptr, dgain, dbias, overwrite, st);
+      };
+      if (p.vb == 16) regs(std::integral_constant<int, 16>());
+      else if (p.vb == 4) regs(std::integral_constant<int, 4>());
+      else regs(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
     };
-    if (p.vb == 16) regs(std::integral_constant<int, 16>());
-    else if (p.vb == 4) regs(std::integral_constant<int, 4>());
-    else regs(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
-    if (dgain) sum_columns(S, s.C, part, dgain, dbias, overwrite, st);
+    if (!direct) {
+      launch(S, 0);
+      if (dgain) sum_columns(S, s.C, part, dgain, dbias, overwrite, st);
+    } else if (dx == dy || dx == x) {   // the columns' blocks read what the rows' would write over
+      launch(0, cols);
+      launch(S, 0);
+    } else {
+      launch(dx ? S : 0, cols);
+    }
     return launch_status();
   }
   if (dgain) {   // first: dx may be written over dy or x

@@ -133,6 +133,14 @@ def test_forward_and_backward(rows, c, dt):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,c", [(1023, 9), (1024, 72), (1024, 1002), (1025, 1), (1026, 7), (1030, 100), (1100, 255),
+                                    (1025, 513), (1025, 1000), (1031, 2056), (1025, 4096)])
+def test_rows_around_the_sums_by_columns(rows, c, dt):
+    """On both sides of where the gain's and bias's gradients are summed in the one launch."""
+    test_forward_and_backward(rows, c, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("c,ldx,ldy,offx,offy", [
     (64, 192, 64, 64, 0), (64, 64, 200, 0, 72), (100, 228, 100, 0, 0), (100, 101, 103, 1, 3),
     (24, 25, 24, 5, 0), (256, 260, 264, 4, 8), (1, 3, 2, 1, 1), (2050, 2051, 2050, 0, 1)])
