@@ -341,23 +341,25 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // The tile product of a block: WM x WN waves, each MT x NT fragments of 32 x
-// 32, over stages of 32 sum values in a ring of NS LDS slots.  L is BM rows
-// from row i0 on, contiguous in the sum, R BN rows from j0 on likewise; with
-// TR, R is the 32 sum rows of BN columns from j0 on, and its fragments are
-// gathered by transpose loads.  A slot holds 64-byte rows, whose 16-byte
-// chunks are XOR-swizzled.  With SWAP the accumulators hold the transposed
-// tile: a lane has column (row with SWAP) l % 32 of a fragment and rows
-// (columns) 8 (v / 4) + 4 (l / 32) + v % 4.
+// 32, over stages of U panels (32 sum values each) in a ring of NS LDS slots.
+// L is BM rows from row i0 on, contiguous in the sum, R BN rows from j0 on
+// likewise; with TR, R is the 32 sum rows of BN columns from j0 on, and its
+// fragments are gathered by transpose loads.  A slot holds 64-byte rows, whose
+// 16-byte chunks are XOR-swizzled.  With SWAP the accumulators hold the
+// transposed tile: a lane has column (row with SWAP) l % 32 of a fragment and
+// rows (columns) 8 (v / 4) + 4 (l / 32) + v % 4.
 //
 // A stage is visible to all waves one turn before it is multiplied, so that
 // its fragments are read while the stage before it is (a step of 16 ahead, the
 // 4 products of a 64 x 64 wave tile do not cover the reads: X X^T of 2048 x
-// 18432 109 us, 101 with a stage ahead).
-template <int MT, int NT, int WM, int WN, int NS, bool TR, bool SWAP>
+// 18432 109 us, 101 with a stage ahead).  With one fragment a wave a panel has
+// two products, less than a turn's barrier and reads take: two panels a stage
+// (18 of 256 x 256 100 -> 92 us, one of 1024 x 4096 210 -> 204).
+template <int MT, int NT, int WM, int WN, int NS, int U, bool TR, bool SWAP>
 struct Tile {
   static constexpr int NW = WM * WN, BM = 32 * MT * WM, BN = 32 * NT * WN;
   static constexpr int LCH = BM / 16, RCH = BN / 16;   // 1 KiB DMA chunks of a stage: 16 rows
-  static constexpr int CH = LCH + RCH, SB = CH * 1024, PER = CH / NW;
+  static constexpr int CH = LCH + RCH, SB = U * CH * 1024, PER = U * CH / NW;
   static_assert(LCH % NW == 0 && RCH % NW == 0 && NS * SB <= 160 * 1024, "whole DMA rounds, LDS ring");
   static_assert(NS >= 3, "a stage ahead");
 
@@ -401,18 +403,20 @@ struct Tile {
     int sl = __builtin_amdgcn_readfirstlane(k0 * stl), sr = __builtin_amdgcn_readfirstlane(k0 * str);
     const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
     auto issue = [&](auto slot) __attribute__((always_inline)) {
-      issue_stage<decltype(slot)::value * SB>(dst, vl, vr, rl, rr, sl, sr);
-      sl += stl;
-      sr += str;
+      each<U>([&](auto u) {
+        issue_panel<decltype(slot)::value * SB + decltype(u)::value * CH * 1024>(dst, vl, vr, rl, rr, sl, sr);
+        sl += stl;
+        sr += str;
+      });
     };
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{};
-    const int total = k1 - k0;
+    const int total = (k1 - k0) / U;
     // fragments of two stages in turn: those of the next are read while this
     // one's are multiplied
-    u32x4 a[2][2][MT], b[2][2][NT];
+    u32x4 a[2][2 * U][MT], b[2][2 * U][NT];
     const int fr = lane & 31;                                   // row of a fragment
     const int kb = 8 * (lane >> 5) + ((lane & 15) >> 2);        // (TR) row of the transpose load
     const int cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);   // (TR) its chunk
@@ -420,15 +424,15 @@ struct Tile {
     const int lb = LCH * 1024 + (TR ? wn * NT * 2048 + kb * 64 + rswz(kb, cb) * 16 + 8 * (lane & 1)
                                     : (wn * NT * 32 + fr) * 64 + kswz(fr, lane >> 5) * 16);
     auto load = [&](auto slot, int z) __attribute__((always_inline)) {
-      const unsigned char* s = ring + decltype(slot)::value * SB;
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
+      for (int h = 0; h < 2 * U; ++h) {
+        const unsigned char* s = ring + decltype(slot)::value * SB + h / 2 * CH * 1024;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[z][kk][i] = *(const u32x4*)(s + (la ^ (32 * kk)) + i * 2048);
+        for (int i = 0; i < MT; ++i) a[z][h][i] = *(const u32x4*)(s + (la ^ (32 * (h & 1))) + i * 2048);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          if constexpr (TR) b[z][kk][j] = frag_tr(s + lb + j * 2048 + kk * 1024, 64);
-          else b[z][kk][j] = *(const u32x4*)(s + (lb ^ (32 * kk)) + j * 2048);
+          if constexpr (TR) b[z][h][j] = frag_tr(s + lb + j * 2048 + (h & 1) * 1024, 64);
+          else b[z][h][j] = *(const u32x4*)(s + (lb ^ (32 * (h & 1))) + j * 2048);
         }
       }
     };
@@ -452,16 +456,16 @@ struct Tile {
       if (STEADY || idx + NS - 1 < total) issue(std::integral_constant<int, (Z + NS - 1) % NS>());
       if (STEADY || idx + 1 < total) load(std::integral_constant<int, (Z + 1) % NS>(), (Z + 1) % 2);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+      for (int h = 0; h < 2 * U; ++h)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            acc[i][j] = SWAP ? mfma(b[Z % 2][kk][j], a[Z % 2][kk][i], acc[i][j])
-                             : mfma(a[Z % 2][kk][i], b[Z % 2][kk][j], acc[i][j]);
+            acc[i][j] = SWAP ? mfma(b[Z % 2][h][j], a[Z % 2][h][i], acc[i][j])
+                             : mfma(a[Z % 2][h][i], b[Z % 2][h][j], acc[i][j]);
       // reads between the products
       if constexpr (STEADY) {
-        constexpr int MF = 2 * MT * NT, RD = 2 * (MT + (TR ? 2 : 1) * NT), PM = (RD + MF - 1) / MF;
+        constexpr int MF = 2 * U * MT * NT, RD = 2 * U * (MT + (TR ? 2 : 1) * NT), PM = (RD + MF - 1) / MF;
 #pragma unroll
         for (int m = 0; m < MF; ++m) {
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // a product
@@ -501,7 +505,7 @@ struct Tile {
   // L's at offsets vl + sl, then R's at vr + sr.  M0 holds the destination only
   // inside (as in dma16, one wait state between writing it and the load).
   template <int AT>
-  __device__ __forceinline__ static void issue_stage(unsigned dst, const int (&vl)[3], const int (&vr)[3],
+  __device__ __forceinline__ static void issue_panel(unsigned dst, const int (&vl)[3], const int (&vr)[3],
                                                      u32x4 rl, u32x4 rr, int sl, int sr) {
     unsigned saved;
 #define TGP_FIRST "s_mov_b32 %0, m0\n\ts_add_u32 m0, %1, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 "
@@ -651,9 +655,9 @@ enum { GRAM, POLY, MUL };
 // sum is split, the ranges' partial tiles go to t.part as the accumulators lie,
 // [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
 // s[0].  MUL: s[c] = s[a] s[b], of matrices that commute.
-template <int MODE, int MT, int NT, int WM, int WN, int NS>
+template <int MODE, int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int launch, Each ea, int b, Each ec) {
-  typedef Tile<MT, NT, WM, WN, NS, false, false> TL;
+  typedef Tile<MT, NT, WM, WN, NS, U, false, false> TL;
   static_assert(TL::BM == TL::BN, "square tiles");
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = grouped(blockIdx.x, gridDim.x);
@@ -665,8 +669,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
   int ti, tj;
   upper(q - sp * tiles, nt, ti, tj);
   const int i0 = ti * TL::BM, j0 = tj * TL::BN, nk = (MODE == GRAM ? t.np : t.mp) / 32;
-  const int k0 = MODE == GRAM ? (int)((long)nk * sp / t.split) : 0;
-  const int k1 = MODE == GRAM ? (int)((long)nk * (sp + 1) / t.split) : nk;
+  // ranges of whole pairs of panels
+  const int k0 = MODE == GRAM ? (int)(nk / 2L * sp / t.split) * 2 : 0;
+  const int k1 = MODE == GRAM ? (int)(nk / 2L * (sp + 1) / t.split) * 2 : nk;
   const f16* L = MODE == GRAM ? gm(t.x[a]) : gm(t.s[a]);
   const f16* R = MODE == MUL ? gm(t.s[b]) : L;
   const float* dl = gm(t.d[a]);
@@ -770,9 +775,9 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
 }
 
 // X' = s[p] X, or (last) the update itself.
-template <int MT, int NT, int WM, int WN, int NS>
+template <int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last) {
-  typedef Tile<MT, NT, WM, WN, NS, true, true> TL;
+  typedef Tile<MT, NT, WM, WN, NS, U, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = grouped(blockIdx.x, gridDim.x);
   const int k = find(l, launch, blk);
@@ -1184,8 +1189,7 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 158 us,
   // 184; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken where
   // its tiles make one block a CU.  Where 128 x 128 leaves CUs without one, 64 x
-  // 64 with twice the stages in flight.  The sums' order is the same in all of
-  // them.
+  // 64.  The sums' order is the same in all of them.
   const int ba = t192 >= 256 ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
   auto grams = [&](const Mat& t) { return uppers(t.mp / bg) * t.split; };
   auto sums = [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; };
@@ -1206,10 +1210,9 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   tiled(L_APPLY1, [&](const Mat& t) { return t.two ? 0 : applies(t); });
   tiled(L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
   // The products of m x m matrices with up to two blocks a CU wait for their
-  // stages: six in flight, not four (one of 1024 x 4096 in all: 221 us, 238).
-  // With more blocks, six leave room for fewer of them (2048 x 18432: 1179 us,
-  // 1165 with four).
-  auto deep = [&](int launch) { return grid[launch] <= kBlocks; };
+  // stages: two panels each.  With more blocks one panel, whose ring takes half
+  // the LDS, leaves room for more of them (2048 x 18432: 1122 us, 1160 with two).
+  auto few = [&](int launch) { return grid[launch] <= kBlocks; };
   const Mats* tb = table;
   if (wholes) {
     ProfScope ps("muon_whole", wflops + 4 * n, 14 * wn + 12 * n, st);
@@ -1230,9 +1233,9 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
     if (grid[lg]) {
       ProfScope ps("muon_gram", gram, 2 * n + 2 * cells, st);
       if (bg == 128)
-        TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 2, 2, 2, 2, 4, 1>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
       else
-        TGP_LAUNCH(ps, (muon_sym<GRAM, 1, 1, 2, 2, 8>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
+        TGP_LAUNCH(ps, (muon_sym<GRAM, 1, 1, 2, 2, 4, 2>), dim3(grid[lg]), dim3(256), 0, st, tb, lg, from, 0, (Each{{0, 0}}));
     }
     if (grid[ls]) {
       ProfScope ps("muon_gram_sum", 0, 0, st);
@@ -1242,32 +1245,32 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   };
   auto poly = [&](Each c) {
     ProfScope ps("muon_poly", cube, 4 * cells, st);
-    if (deep(L_SYM))
-      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 6>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
+    if (few(L_SYM))
+      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4, 2>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
                  (Each{{0, 0}}), 0, c);
     else
-      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
+      TGP_LAUNCH(ps, (muon_sym<POLY, 1, 1, 2, 2, 4, 1>), dim3(grid[L_SYM]), dim3(256), 0, st, tb, (int)L_SYM,
                  (Each{{0, 0}}), 0, c);
   };
   auto mul = [&](int a, int b, int c) {
     if (!grid[L_SYM2]) return;
     ProfScope ps("muon_mul", cube, 6 * cells, st);
-    if (deep(L_SYM2))
-      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 6>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
+    if (few(L_SYM2))
+      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4, 2>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
                  (Each{{a, a}}), b, (Each{{c, c}}));
     else
-      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
+      TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4, 1>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
                  (Each{{a, a}}), b, (Each{{c, c}}));
   };
   auto apply = [&](int la, Each p, int last) {
     if (!grid[la]) return;
     ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
     if (ba == 192)
-      TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
     else if (ba == 128)
-      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
     else
-      TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 8>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 4, 2>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
   };
   // Two steps a turn: what both kinds of matrices need is one launch for both,
   // and a list of one kind has no launches of the other.
