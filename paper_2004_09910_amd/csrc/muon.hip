@@ -10,7 +10,8 @@
 //
 //   A = X X^T          P = a I + b A + c A A          X' = P X
 //
-// launches over the tiles of all matrices.  A and P are float16 with the
+// launches over the tiles of all matrices, the diagonal's upper half of the
+// first two.  A and P are float16 with the
 // rounding error of their diagonals beside them in float32: near convergence
 // A is nearly a multiple of I, whose one rounding would shift every singular
 // value alike and be multiplied by b / p(1) = 7.  A product of two such
@@ -23,6 +24,11 @@
 // eigenvalues span the square of X's range, which P^2 stretches 12-fold a
 // step: three at once lose small singular values to float16's 11 bits, 8e-3
 // of the update's norm where two leave 1.5e-3.)
+//
+// Five steps of one 2048 x 18432 take 1122 us, of a U-Net's 19 matrices of up
+// to 1024 x 9216 547 us, of 18 of 256 x 256 92 us, of four of up to 16 x 144 13
+// us: operations at 1256 TFLOP/s, what a large matrix product of float16
+// reaches here, are 629, 182 and 5 us of that, the tensors' bytes 98, 81 and 2.
 #include <algorithm>
 #include <type_traits>
 
@@ -161,8 +167,9 @@ __device__ __forceinline__ void leave_table(const Mats& l, Mats* table) {
 }
 
 // M = mu M + G, and partial sums of U^2 (in float64: squares of float32 values
-// neither overflow nor vanish), block blk's of the launch.  Purely a matter of
-// memory: 16-byte accesses, two of each tensor in flight a thread.
+// neither overflow nor vanish), block blk's of the launch.  Memory bounds it:
+// 16-byte accesses, two of each tensor in flight a thread (2048 x 18432, 453 MB:
+// 78 us, 5.8 TB/s).
 __device__ __forceinline__ void momentum(const Mats& l, int blk, float mu, int nesterov, double* sh) {
   const int k = find(&l, L_MOMENTUM, blk);
   const Mat& t = l.t[k];
@@ -229,7 +236,9 @@ struct Scale {
 
 // X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
 // in the padding: a piece is 64 rows x 64 columns through LDS where the matrix
-// is transposed, else 32 rows x 128 columns.
+// is transposed, else 32 rows x 128 columns.  Memory bounds it: U is read once
+// more, as |U| is known only when all of it has been (2048 x 18432, 377 MB: 67 us,
+// 5.6 TB/s).
 __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l, float mu, int nesterov, float eps) {
   __shared__ double sh[4];
   __shared__ float tile[64][65];
@@ -351,8 +360,8 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 //
 // A stage is visible to all waves one turn before it is multiplied, so that
 // its fragments are read while the stage before it is (a step of 16 ahead, the
-// 4 products of a 64 x 64 wave tile do not cover the reads: X X^T of 2048 x
-// 18432 109 us, 101 with a stage ahead).  With one fragment a wave a panel has
+// 4 products of a 64 x 64 wave tile do not cover the reads: 8% of X X^T of 2048 x
+// 18432).  With one fragment a wave a panel has
 // two products, less than a turn's barrier and reads take: two panels a stage
 // (18 of 256 x 256 100 -> 92 us, one of 1024 x 4096 210 -> 204).
 template <int MT, int NT, int WM, int WN, int NS, int U, bool TR, bool SWAP>
@@ -537,7 +546,8 @@ struct Tile {
 // the 8 XCDs, each with its own L2: sixteen consecutive tiles, which share a
 // panel of X, go to one XCD, and every 128 tiles are spread over all of them,
 // since tiles of one launch differ in length (a contiguous eighth for each XCD
-// leaves some with the long ones).
+// leaves some with the long ones).  A U-Net's 19 matrices: X X^T 43 us and P X 62,
+// 50 and 73 in the blocks' own order.
 __device__ __forceinline__ int grouped(int blk, int n) {
   const int w = blk & ~127, r = blk & 127;
   return w + 128 <= n ? w + (r & 7) * 16 + (r >> 3) : blk;
@@ -655,6 +665,14 @@ enum { GRAM, POLY, MUL };
 // sum is split, the ranges' partial tiles go to t.part as the accumulators lie,
 // [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
 // s[0].  MUL: s[c] = s[a] s[b], of matrices that commute.
+//
+// GRAM in tiles of 128 x 128 (2048 x 18432: 88 us, 930 TFLOP/s of the upper
+// tiles) is bound by the matrix instructions' and the LDS reads' turns at two
+// blocks a CU.  POLY and MUL in tiles of 64 x 64 (2048: 22 and 23 us, 390
+// TFLOP/s) read as much from LDS as they multiply, and 528 tiles are two a CU
+// and three on some; tiles of 128 x 128 would be 136 for 256 CUs.  Under about
+// 1024 a launch and the latencies of a tile's first and last stage are most of
+// it (256: 5 to 6 us).
 template <int MODE, int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int launch, Each ea, int b, Each ec) {
   typedef Tile<MT, NT, WM, WN, NS, U, false, false> TL;
@@ -729,7 +747,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
 }
 
 // s[0] from the ranges' partial tiles, added in order: a wave takes one
-// fragment.
+// fragment.  Three ranges of 2048 x 2048: 8.5 us, 27 MB from the caches.
 template <int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l, int launch) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * 2048];
@@ -774,7 +792,9 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
   }
 }
 
-// X' = s[p] X, or (last) the update itself.
+// X' = s[p] X, or (last) the update itself.  In tiles of 128 x 192 it is bound
+// by the matrix instructions and the LDS reads that feed them: 2048 x 18432 147
+// us, 1050 TFLOP/s (the library's product of 2048 x 2048 x 18432: 155 us).
 template <int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last) {
   typedef Tile<MT, NT, WM, WN, NS, U, true, true> TL;
@@ -835,7 +855,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 // X, A and P staying in LDS (panels of 32 columns, a row's 64 bytes 80 apart:
 // eight rows read at one chunk hit distinct banks).  MS: m rounded up to 32 or
 // 64.  What bounds it is one CU's rate of loading and the latencies between its
-// barriers, three a step: five steps of 16 x 144 take 12.4 us, of 64 x 256 20
+// barriers, three a step: five steps of 16 x 144 take 12.9 us, of 64 x 256 20
 // (eight waves 20.5, sixteen 22.5), where four launches a step take 70 to 90.
 // LDS holds up to 55296 values, and a list of 64 x 576 alone would gain (89 us
 // as tiles, 33); among others such a block outlasts the launch it shares by
@@ -1061,13 +1081,15 @@ __global__ __launch_bounds__(kFirstT) void muon_whole(Mats l, Mats* table, int w
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 constexpr int kPad = 128;
 constexpr int kBlocks = 512;   // two a CU
-constexpr int kRange = 64;     // stages of 32 sum values
+constexpr int kRange = 64;     // panels
 int up(int x) { return (x + kPad - 1) / kPad * kPad; }
 int uppers(int nt) { return nt * (nt + 1) / 2; }
 
 // Whether two steps are taken at once.  The products with X that this saves
 // run at about twice the rate of the m x m ones that replace them, on fewer
-// tiles: from n = 4 m on (a 3 x 3 layer has 9 m and more).
+// tiles: from n = 4 m on (a 3 x 3 layer has 9 m and more).  1024 x 4096 205 us,
+// 217 one step at a time; 2048 x 8192 653, 762; below, 1024 x 2048 166 and 155,
+// 2048 x 4096 491 and 515.
 bool pairs(const tgp_muon_tensor& d) {
   return std::max(d.rows, d.cols) >= 4 * (long)std::min(d.rows, d.cols);
 }
@@ -1092,9 +1114,10 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 // workspace ws on; returns their end.  The sum of A = X X^T is split where a
 // matrix has too few tiles to fill the chip: into as many ranges as make at
 // most kBlocks blocks (one more than run at once waits for all of them: 2048 x
-// 18432 in 3 ranges 105 us, in 4 126, in 7 99 and 5 more to add them up), of
-// kRange stages at least (writing and reading back a partial tile takes the
-// time of 20 stages).  The ranges depend on the matrix alone, so that its
+// 18432 in 3 ranges 89 us and 8.6 to add them up, in 4 101 and 9.7, in 7 86 and
+// 13.4), of kRange panels at least (writing and reading back a partial tile takes
+// the time of 20; with 32 at least, 2048 x 2048 takes 398 us and not 377, a
+// U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not 324).  The ranges depend on the matrix alone, so that its
 // update does not depend on the others of the call.
 size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
@@ -1186,8 +1209,8 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
     g128 += (long)uppers(t.mp / 128) * t.split;
   }
   // Columns of a tile of P X and X X^T.  P X on tiles of 128 x 192 takes a
-  // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 158 us,
-  // 184; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken where
+  // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 147 us,
+  // 160; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken where
   // its tiles make one block a CU.  Where 128 x 128 leaves CUs without one, 64 x
   // 64.  The sums' order is the same in all of them.
   const int ba = t192 >= 256 ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
