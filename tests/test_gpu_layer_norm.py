@@ -141,6 +141,14 @@ def test_rows_around_the_sums_by_columns(rows, c, dt):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,c", [(9, 1025), (70, 1501), (33, 2049), (1100, 1501), (1026, 2047), (1030, 2502), (1025, 4095),
+                                    (6, 4098), (5, 4097), (3, 8190), (2, 8193)])
+def test_long_rows_of_narrow_accesses(rows, c, dt):
+    """Rows of more than 1024 accesses of 2 or 4 bytes, up to what registers hold and beyond."""
+    test_forward_and_backward(rows, c, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("c,ldx,ldy,offx,offy", [
     (64, 192, 64, 64, 0), (64, 64, 200, 0, 72), (100, 228, 100, 0, 0), (100, 101, 103, 1, 3),
     (24, 25, 24, 5, 0), (256, 260, 264, 4, 8), (1, 3, 2, 1, 1), (2050, 2051, 2050, 0, 1)])
