@@ -666,13 +666,13 @@ enum { GRAM, POLY, MUL };
 // [range][tile][wave][fragment][g][lane].  POLY: s[c] = a I + b A + c A A of A =
 // s[0].  MUL: s[c] = s[a] s[b], of matrices that commute.
 //
-// GRAM in tiles of 128 x 128 (2048 x 18432: 88 us, 930 TFLOP/s of the upper
-// tiles) is bound by the matrix instructions' and the LDS reads' turns at two
-// blocks a CU.  POLY and MUL in tiles of 64 x 64 (2048: 22 and 23 us, 390
-// TFLOP/s) read as much from LDS as they multiply, and 528 tiles are two a CU
-// and three on some; tiles of 128 x 128 would be 136 for 256 CUs.  Under about
-// 1024 a launch and the latencies of a tile's first and last stage are most of
-// it (256: 5 to 6 us).
+// GRAM in tiles of 128 x 128: 2048 x 18432 88 us, 930 TFLOP/s of the upper tiles;
+// 408 blocks of two a CU leave some CUs one, and the clock is at 2.0 GHz.  POLY
+// and MUL in tiles of 64 x 64 (2048: 22 and 23 us, 390 TFLOP/s) wait two thirds of
+// their waves' cycles for stages and barriers, with the matrix instructions and
+// LDS at a sixth each; 528 tiles are two a CU and three on some, and tiles of 128
+// x 128 would be 136 for 256 CUs.  Under about 1024 a launch and the latencies of
+// a tile's first and last stage are most of it (256: 5 to 6 us).
 template <int MODE, int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int launch, Each ea, int b, Each ec) {
   typedef Tile<MT, NT, WM, WN, NS, U, false, false> TL;
@@ -793,8 +793,9 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
 }
 
 // X' = s[p] X, or (last) the update itself.  In tiles of 128 x 192 it is bound
-// by the matrix instructions and the LDS reads that feed them: 2048 x 18432 147
-// us, 1050 TFLOP/s (the library's product of 2048 x 2048 x 18432: 155 us).
+// by the clock that the matrix instructions' power leaves, 1.7 GHz, 58% of whose
+// cycles they are busy: 2048 x 18432 147 us, 1050 TFLOP/s (the library's product
+// of 2048 x 2048 x 18432: 155 us).
 template <int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last) {
   typedef Tile<MT, NT, WM, WN, NS, U, true, true> TL;
