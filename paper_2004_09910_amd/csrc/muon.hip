@@ -1116,13 +1116,14 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 // matrix has too few tiles to fill the chip: into as many ranges as make at
 // most kBlocks blocks (one more than run at once waits for all of them: 2048 x
 // 18432 in 3 ranges 89 us and 8.6 to add them up, in 4 101 and 9.7, in 7 86 and
-// 13.4), of kRange panels at least (writing and reading back a partial tile takes
-// the time of 20; with 32 at least, 2048 x 2048 takes 398 us and not 377, a
-// U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not 324).  The ranges depend on the matrix alone, so that its
-// update does not depend on the others of the call.
+// 13.4), of kRange panels at least (writing and reading back a partial tile
+// takes the time of 20; with 32 at least, 2048 x 2048 takes 398 us and not 377,
+// a U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not 324).  The
+// ranges depend on the matrix alone, so that its update does not depend on the
+// others of the call.
 size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
   auto take = [&](size_t bytes) {
-    char* p = ws + pos;
+    char* p = ws ? ws + pos : nullptr;   // (none: only the size is asked for)
     pos += al256(bytes);
     return p;
   };
