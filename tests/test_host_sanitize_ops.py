@@ -7,13 +7,24 @@ with every launch skipped, so no GPU is needed.  Needs the in-tree build
 import concurrent.futures
 import glob
 import os
+import subprocess
 import tempfile
 
 import pytest
 
-from test_host_sanitize import CLANG, HIPCC, PKG, ROOT, SAN, _run
-
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PKG = os.path.join(ROOT, "paper_2004_09910_amd")
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CLANG = "/opt/rocm/llvm/bin/clang++"
+SAN = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+       "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer"]
 SOURCES = ["runtime.cpp", "prof.cpp", "train_ops.cpp", "layer_norm.hip", "muon.hip", "weight_step.hip"]
+
+
+def _run(cmd, **kw):
+    r = subprocess.run(cmd, capture_output=True, text=True, **kw)
+    assert r.returncode == 0, f"{' '.join(cmd)}\n{r.stdout[-3000:]}\n{r.stderr[-3000:]}"
+    return r
 
 
 def test_host_side_of_operators_under_asan_and_ubsan():
