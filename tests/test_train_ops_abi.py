@@ -83,8 +83,8 @@ def test_muon_refusals(kw, want):
 def test_muon_of_nothing_and_workspaces():
     assert _mu(tensors=[], ws=None, ws_bytes=0) == tgp.OK
     assert tgp.muon_workspace(tgp.muon_tensors([])) == 0
-    one = tgp.muon_workspace(tgp.muon_tensors([(128, 576, None, None, None)]))
-    two = tgp.muon_workspace(tgp.muon_tensors([(128, 576, None, None, None)] * 2))
+    one = tgp.muon_workspace(tgp.muon_tensors([(64, 576, None, None, None)]))
+    two = tgp.muon_workspace(tgp.muon_tensors([(64, 576, None, None, None)] * 2))
     assert 0 < one < two
     assert tgp.call_status("tgp_muon_workspace", 1, tgp.muon_tensors([(4, 4, P, P, P)]), None) == tgp.EINVAL
     v = ctypes.c_size_t()
