@@ -10,12 +10,12 @@
 //
 //   A = X X^T          P = a I + b A + c A A          X' = P X
 //
-// launches over the tiles of all matrices, the diagonal's upper half of the
-// first two.  A and P are float16 with the
-// rounding error of their diagonals beside them in float32: near convergence
-// A is nearly a multiple of I, whose one rounding would shift every singular
-// value alike and be multiplied by b / p(1) = 7.  A product of two such
-// matrices (L + dL)(R + dR), dL and dR diagonal, is taken as L R + dL R + L dR.
+// launches over the tiles of all matrices, of A and P the upper ones only.  A
+// and P are float16 with the rounding error of their diagonals beside them in
+// float32: near convergence A is nearly a multiple of I, whose one rounding
+// would shift every singular value alike and be multiplied by b / p(1) = 7.  A
+// product of two such matrices (L + dL)(R + dR), dL and dR diagonal, is taken as
+// L R + dL R + L dR.
 //
 // Two steps at once, for long matrices: X'' = P(A') P(A) X, and as P(A) and A
 // commute, A' = X' X'^T = P A P.  That replaces the first step's product with X
@@ -860,8 +860,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 // (eight waves 20.5, sixteen 22.5), where four launches a step take 70 to 90.
 // LDS holds up to 55296 values, and a list of 64 x 576 alone would gain (89 us
 // as tiles, 33); among others such a block outlasts the launch it shares by
-// more than a few matrices more cost the tiles (9 matrices of all sorts with
-// one of 1144 x 9: 158 us, 177).
+// more than a few matrices more cost the tiles (six matrices of all sorts with
+// one of 1144 x 9: 149 us, 177).
 constexpr int kSmallX = 16384, kRow = 80;   // most values of X, bytes of a row
 // chunks of 8 values of a thread, and those whose loads are in flight together
 constexpr int kSmallChunks = (kSmallX / 8 + kFirstT - 1) / kFirstT, kFlight = 2;
