@@ -356,7 +356,9 @@ tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap
  * channel slice of a wider tensor.  x and y have the type `dtype`; gain and
  * bias are float32 (NULL: ones, zeros).  stats, rows pairs of float32 (mean,
  * rstd), is what the backward reads; NULL where none will run.  Sums are
- * float32, the variance is that of the differences from the mean, and y is
+ * float32 or better, and the mean and the differences from it are corrected by
+ * the differences' own mean, so that a row's offset does not enter: a constant
+ * row gives the bias.  The variance is that of the differences, and y is
  * rounded once.  y may be x itself (ldy = ldx); other overlaps are not
  * allowed.  An infinity or NaN in a row makes that row NaN and no other.
  * Alignment: elements of x and y at multiples of their size, gain and bias at

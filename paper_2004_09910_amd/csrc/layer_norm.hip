@@ -2,7 +2,12 @@
 // tensor), forward and backward.
 //
 // Forward: mean and rstd = (var + eps)^-1/2 of each row, the variance taken
-// from the differences to the mean, y = gain (x - mean) rstd + bias.
+// from the differences to the mean, y = gain (x - mean) rstd + bias.  A float32
+// sum of C values around an offset is rounded at the size of the offset, and
+// its mean is off by that many times the spread of a row that varies little
+// (a constant row of 1000 values 12345.678 comes out 2e-3 lower, and y with
+// eps = 1e-5 at half a unit in every channel): the differences' own mean is
+// taken off them, and added to the mean.
 // Backward: with xhat = (x - mean) rstd and g = gain dy, dx = rstd (g -
 // mean(g) - xhat mean(g xhat)), and the column sums of dy xhat and dy.
 // Column sums are partial sums of row ranges, left in a workspace and added
@@ -25,7 +30,8 @@ constexpr int kColFlight = 4;    // rows in flight of a lane that sums columns
 
 // Sum over the block's kT threads, the same value in every thread: a wave's
 // xor tree, then the waves' sums in order.
-__device__ __forceinline__ float block_sum(float v, float* s4) {
+template <typename F>
+__device__ __forceinline__ F block_sum(F v, F* s4) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) s4[threadIdx.x >> 6] = v;
@@ -36,8 +42,10 @@ __device__ __forceinline__ float block_sum(float v, float* s4) {
 }
 
 // One block a row (rows dealt out over the grid), the row read once for each
-// of the mean, the variance and the result.  One value a lane and access: 2048 x
-// 20000 bf16 114 us, 1.4 TB/s of what has to be read and written.
+// of the mean, the variance and the result.  The mean is a float64 sum, exact
+// to float32, which costs less than a reading of the differences more.  One
+// value a lane and access: 2048 x 20000 bf16 105 us, 1.6 TB/s of what has to be
+// read and written.
 template <typename T>
 __global__ __launch_bounds__(kT) void norm_fwd_any(const T* __restrict__ x, long ldx,
                                                    const float* __restrict__ gain,
@@ -45,20 +53,23 @@ __global__ __launch_bounds__(kT) void norm_fwd_any(const T* __restrict__ x, long
                                                    T* y, long ldy, float2* __restrict__ stats,
                                                    long rows, int C) {
   __shared__ float s4[4];
+  __shared__ double d4[4];
   for (long r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* xr = x + r * ldx;
     T* yr = y + r * ldy;
-    float s = 0.f;
+    double s = 0;
     for (int c = threadIdx.x; c < C; c += kT) s += Elt<T>::ld(xr + c);
-    const float mean = block_sum(s, s4) / C;
+    s = block_sum(s, d4) / C;
+    // as a float32 and what that leaves out
+    const float mean = (float)s, rest = (float)(s - mean);
     float q = 0.f;
     for (int c = threadIdx.x; c < C; c += kT) {
-      const float d = Elt<T>::ld(xr + c) - mean;
+      const float d = Elt<T>::ld(xr + c) - mean - rest;
       q += d * d;
     }
     const float rstd = 1.f / sqrtf(block_sum(q, s4) / C + eps);
     for (int c = threadIdx.x; c < C; c += kT) {
-      float v = (Elt<T>::ld(xr + c) - mean) * rstd;
+      float v = (Elt<T>::ld(xr + c) - mean - rest) * rstd;
       if (gain) v *= gain[c];
       if (bias) v += bias[c];
       Elt<T>::st(yr + c, v);
@@ -173,10 +184,14 @@ struct Share {
   }
 };
 
-// Memory bounds it: 147456 x 64 bf16 take 9.5 us (4.1 TB/s of what has to be
-// read and written; a copy of that size, out of the caches, 4.7 us and a
-// launch), 144 x 1024 3.6.  One row a lane is on its way at a time: two or
-// four cost registers and waves, and come out slower (10.4 us).
+// Memory bounds it, and what comes between a row's loads and its stores: 147456
+// x 64 bf16 take 10.2 us (3.8 TB/s of what has to be read and written; a copy of
+// that size, out of the caches, 4.7 us and a launch), 0.8 of them for the
+// correction of the mean, 144 x 1024 3.7.  Taking the variance beside the
+// correction, as the squares' mean less the correction's square, saves nothing
+// of that.  One row a lane is on its way at a time: two or four cost registers
+// and waves, and come out slower (10.4 us, where one took 9.5 without the
+// correction).
 template <typename T, int VB, int NV, bool BLK>
 __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float* __restrict__ gain,
                                                const float* __restrict__ bias, float eps, T* y,
@@ -205,13 +220,24 @@ __global__ __launch_bounds__(kT) void norm_fwd(const T* x, long ldx, const float
 #pragma unroll
       for (int v = 0; v < V; ++v) s += f[k][v];
     }
-    const float mean = row_sum<BLK>(s, sh.G, s4) / C;   // (a quotient: a constant row's mean is exact)
-    float q = 0.f;
+    float mean = row_sum<BLK>(s, sh.G, s4) / C, e = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         f[k][v] -= mean;
+        if (sh.has(k)) e += f[k][v];
+      }
+    // what the differences leave of a mean: a constant row's are all one small
+    // multiple of its last place, whose sum and quotient are exact
+    e = row_sum<BLK>(e, sh.G, s4) / C;
+    mean += e;
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        f[k][v] -= e;
         if (sh.has(k)) q += f[k][v] * f[k][v];
       }
     const float rstd = 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps);
@@ -495,7 +521,7 @@ struct Plan {
 // leave the same (a row's vectors then lie side by side in one access).  A
 // row of more than 4 x 64 vectors takes a block, of more than 4 x 256 (16 x 256
 // of 2 or 4 bytes, whose values fit in as many registers) none: 8192 x 4095 bf16
-// forward 28 us, backward 77; by the kernels of any row 70 and 106.
+// forward 31 us, backward 77; by the kernels of any row 70 and 106.
 Plan plan_of(int dt, int C, uintptr_t bits) {
   const int esz = dt == TGP_BF16 ? 2 : 4;
   bits |= (uintptr_t)C * esz;

@@ -388,3 +388,37 @@ def test_rows_farther_apart_than_32_bits(c, dt):
     tgp.layer_norm_forward(3, c, code, buf.data_ptr(), ld, g.data_ptr(), b.data_ptr(), 1e-5, buf.data_ptr(), ld)
     torch.cuda.synchronize()
     assert torch.equal(view, y)
+
+
+def _narrow_rows(c, dt):
+    """Rows far from zero: constant ones, and ones whose values vary by little around them."""
+    g = torch.Generator().manual_seed(c)
+    vals = [12345.678, 1000.1, 100000.3, 0.1, -77777.77, 1e-6, 3.0]
+    x = torch.tensor(vals)[:, None].repeat(1, c)
+    spread = torch.tensor([2.0 ** -5, 2.0 ** -8, 1.0, 2.0 ** -22, 0.25, 2.0 ** -36, 2.0 ** -3])
+    return torch.cat((x, x + spread[:, None] * torch.randn(len(vals), c, generator=g))).to(DT[dt][1]), len(vals)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("c,ldx", [(5, 5), (64, 64), (101, 103), (640, 640), (1000, 1000), (1000, 1001), (2050, 2050),
+                                   (4099, 4099), (9000, 9000), (20001, 20001)])
+def test_rows_that_vary_little(c, ldx, dt):
+    """A constant row of any value is its bias and its own mean, exactly: the first mean is off by some units
+    of its last place, all differences are that many, and their sum (under 2^24 units) and quotient are exact.
+    Where values vary, x - mean is exact or off by 2^-24 of itself, and its mean by 64 x 2^-24 of the mean
+    magnitude of the differences, not of the values: EPS32 of the spread is asked of xhat and of rstd, and of
+    the saved mean one rounding, 2^-24 of itself, more."""
+    say("layer norm, narrow rows", c, ldx, dt)
+    x, n = _narrow_rows(c, dt)
+    _, _, gain, bias = _inputs(x.shape[0], c, c)
+    xv, yv, st = _forward(x, gain, bias, dt, ldx, c)
+    td = DT[dt][1]
+    assert torch.equal(yv[:n].cpu(), bias.to(td).expand(n, c))
+    assert torch.equal(st[:n, 0].cpu(), x[:n, 0].float())
+    y, mean, rstd = ref.norm_forward(xv.cpu(), gain, bias, 1e-5)
+    d = (xv.cpu().double() - mean[:, None]) * rstd[:, None]
+    slack = EPS32 * ((d.abs() + d.abs().mean(1, keepdim=True)) * gain.double().abs() + bias.double().abs())
+    assert _err(yv, y, slack, dt == "bf16") <= 1
+    off = (st[:, 0].cpu().double() - mean).abs()
+    assert bool((off <= 2.0 ** -24 * mean.abs() * 1.01 + EPS32 * d.abs().mean(1) / rstd).all())
+    assert float((st[:, 1].cpu().double() / rstd - 1).abs().max()) <= EPS32
