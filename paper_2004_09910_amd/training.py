@@ -28,22 +28,38 @@ from .harness import TORCH_DT, Session
 
 class NormPipeline(Session):
     """A Session (network, partitions, bound parameters) with a layer norm before
-    every partition and an optimiser."""
+    every partition and an optimiser.  A new partition (balance_by_time) takes
+    effect with the plan() that has to follow it: a norm whose boundary stays
+    keeps its values and its optimiser's states, the others start anew."""
 
     def __init__(self, net: specs.Net, dtype: int, n: int, eps: float = 1e-5, **kw):
         super().__init__(net, dtype, n=n, **kw)
         self.eps = eps
-        self.norms = []
-        for j in range(1, n + 1):
-            c = self.part_in_shape(j)[0]
-            self.norms.append({k: torch.full((c,), v, device=self.device) for k, v in
-                               (("gain", 1.0), ("bias", 0.0), ("dgain", 0.0), ("dbias", 0.0))})
+        self.norms, self.norm_at = [], []     # of each partition, and its first layer
         self._optimiser()
+        self._match_norms()
 
     # ------------------------------------------------------------- optimiser
 
+    def _match_norms(self):
+        """Norms for the network's present partition, and the list of what AdamW updates."""
+        self._set_bounds()
+        at = [lo for lo, _ in self.bounds]
+        old = dict(zip(self.norm_at, self.norms))
+        self.norms, self.norm_at = [], at
+        for j, lo in enumerate(at, 1):
+            c = self.part_in_shape(j)[0]
+            # gain, bias and AdamW's two states of each
+            self.norms.append(old.get(lo) or {
+                k: torch.full((c,), float(k == "gain"), device=self.device)
+                for k in ("gain", "bias", "dgain", "dbias", "gain_m", "gain_v", "bias_m", "bias_v")})
+        self.adam = tgp.adamw_tensors(self.vectors + [
+            (q[k].numel(), q[k].data_ptr(), None, q["d" + k].data_ptr(), q[k + "_m"].data_ptr(), q[k + "_v"].data_ptr())
+            for q in self.norms for k in ("gain", "bias")])
+
     def _optimiser(self, rate=0.02, weight_decay=0.01):
-        muon, step, adam = [], [], []
+        muon, step = [], []
+        self.vectors = []    # AdamW's tensors but the norms'
         self.state = []      # keeps the buffers behind the lists alive
 
         def zeros(like, dtype=torch.float32):
@@ -52,8 +68,8 @@ class NormPipeline(Session):
             return t
 
         def vector(w, w16, grad):
-            adam.append((w.numel(), w.data_ptr(), None if w16 is None else w16.data_ptr(),
-                         grad.data_ptr(), zeros(w).data_ptr(), zeros(w).data_ptr()))
+            self.vectors.append((w.numel(), w.data_ptr(), None if w16 is None else w16.data_ptr(),
+                                 grad.data_ptr(), zeros(w).data_ptr(), zeros(w).data_ptr()))
 
         for idx, p in self.params.items():
             w16 = p["w"] if self.dtype == BF16 else None
@@ -70,11 +86,7 @@ class NormPipeline(Session):
                              o.data_ptr(), rate * math.sqrt(max(1.0, rows / cols))))
             if p["b"] is not None:
                 vector(p["b"], None, p["db"])
-        for q in self.norms:
-            vector(q["gain"], None, q["dgain"])
-            vector(q["bias"], None, q["dbias"])
-        self.muon, self.step, self.adam = (tgp.muon_tensors(muon), tgp.step_tensors(step),
-                                           tgp.adamw_tensors(adam))
+        self.muon, self.step = tgp.muon_tensors(muon), tgp.step_tensors(step)
         self.decay = rate * weight_decay
         self.updates = 0
         self.muon_ws = torch.empty(max(tgp.muon_workspace(self.muon), 256), dtype=torch.uint8,
@@ -93,6 +105,7 @@ class NormPipeline(Session):
 
     def plan(self, B: int, m: int, mode: int, lanes: int = 1) -> int:
         need = super().plan(B, m, mode, lanes)
+        self._match_norms()
         dt = TORCH_DT[self.dtype]
 
         def buf(j):
@@ -112,6 +125,10 @@ class NormPipeline(Session):
         self.norm_ws = torch.empty(max(ws + [256]), dtype=torch.uint8, device=self.device)
         return need
 
+    def _planned(self):
+        if self.ws is None:
+            raise RuntimeError("plan() has to come first, again after a new partition or layer times")
+
     def _rows(self, t, i):
         """Micro-batch i of a full-batch tensor: address, pixels, channels."""
         per = t.shape[0] // self.m
@@ -120,6 +137,7 @@ class NormPipeline(Session):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """All F_{i,j}, each after its norm; returns the network's output (full batch)."""
+        self._planned()
         s = torch.cuda.current_stream().cuda_stream
         self.x = x
         for i in range(1, self.m + 1):
@@ -138,6 +156,7 @@ class NormPipeline(Session):
         """F' and B of every task in the order i = m..1, each followed by its
         norm's backward; the gradients are left in the accumulators, and the
         input's in dx (if given)."""
+        self._planned()
         s = torch.cuda.current_stream().cuda_stream
         for i in range(self.m, 0, -1):
             for j in range(self.n, 0, -1):

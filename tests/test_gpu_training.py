@@ -127,3 +127,28 @@ def test_bfloat16_weights_follow_their_masters():
     for p in sess.params.values():
         assert torch.equal(p["w"], p["master"].bfloat16())
     sess.close()
+
+
+def test_gradients_after_a_new_partition():
+    """balance_by_time between two steps, to more partitions: outputs and the norms' gradients are those of the
+    new partition's network (tolerance as above)."""
+    torch.manual_seed(3)
+    sess = NormPipeline(_net(), FP32, n=1, balance=[4])
+    sess.plan(8, 4, specs.CKPT_ALWAYS)
+    x, t = (torch.randn(8, 12, 12, 8, device="cuda") for _ in range(2))
+    sess.train_step(x, t)
+    for n in (4, 2):
+        sess.balance_by_time(2, n, specs.CKPT_ALWAYS)
+        sess.plan(8, 4, specs.CKPT_ALWAYS)
+        say("partition", sess.balance)
+        _, y64, x64, _, N = _reference(sess, x, t)
+        y = sess.forward(x)
+        dx = torch.empty_like(x)
+        sess.backward((y - t) * (2.0 / y.numel()), dx)
+        torch.cuda.synchronize()
+        assert ref.rel(y, y64.detach().permute(0, 2, 3, 1)) <= 1e-4
+        assert ref.rel(dx, x64.grad.permute(0, 2, 3, 1)) <= 1e-4
+        for q, (gain, bias) in zip(sess.norms, N):
+            assert ref.rel(q["dgain"], gain.grad) <= 1e-4 and ref.rel(q["dbias"], bias.grad) <= 1e-4
+        sess.update()
+    sess.close()
