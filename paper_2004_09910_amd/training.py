@@ -120,6 +120,7 @@ class NormPipeline(Session):
         self.stats = [torch.empty((t.numel() // t.shape[3], 2), device=self.device) for t in self.xn]
         self.out = [buf(j) for j in range(2, self.n + 1)]
         self.out.append(torch.empty((B, h, w, self.net.out_channels()), dtype=dt, device=self.device))
+        self.x = None     # the last forward's input
         ws = [tgp.layer_norm_backward_workspace(t.numel() // t.shape[3] // m, t.shape[3], self.dtype)
               for t in self.xn]
         self.norm_ws = torch.empty(max(ws + [256]), dtype=torch.uint8, device=self.device)
@@ -129,8 +130,17 @@ class NormPipeline(Session):
         if self.ws is None:
             raise RuntimeError("plan() has to come first, again after a new partition or layer times")
 
+    def _fits(self, name, t, like, raw=True):
+        """t as the plan has it: the shape of its buffer `like` and, where its address is taken (raw), the
+        type, layout and device."""
+        if t.shape != like.shape:
+            raise ValueError(f"{name} is {tuple(t.shape)}, the plan has {tuple(like.shape)} (NHWC)")
+        if raw and (t.dtype != like.dtype or t.device != like.device or not t.is_contiguous()):
+            raise ValueError(f"{name} is {t.dtype} on {t.device}, strides {t.stride()}; the plan has {like.dtype} on "
+                             f"{like.device}, contiguous")
+
     def _rows(self, t, i):
-        """Micro-batch i of a full-batch tensor: address, pixels, channels."""
+        """Micro-batch i of a full-batch tensor (or of its pixels): address, pixels, channels."""
         per = t.shape[0] // self.m
         part = t[(i - 1) * per:i * per]
         return part.data_ptr(), part.numel() // t.shape[-1], t.shape[-1]
@@ -138,6 +148,7 @@ class NormPipeline(Session):
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """All F_{i,j}, each after its norm; returns the network's output (full batch)."""
         self._planned()
+        self._fits("x", x, self.xn[0])
         s = torch.cuda.current_stream().cuda_stream
         self.x = x
         for i in range(1, self.m + 1):
@@ -157,6 +168,11 @@ class NormPipeline(Session):
         norm's backward; the gradients are left in the accumulators, and the
         input's in dx (if given)."""
         self._planned()
+        if self.x is None:
+            raise RuntimeError("forward() has to come first")
+        self._fits("dy", dy, self.out[-1])
+        if dx is not None:
+            self._fits("dx", dx, self.x)
         s = torch.cuda.current_stream().cuda_stream
         for i in range(self.m, 0, -1):
             for j in range(self.n, 0, -1):
@@ -175,7 +191,12 @@ class NormPipeline(Session):
                                         self.norm_ws.data_ptr(), self.norm_ws.numel(), s)
 
     def train_step(self, x: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
-        """Forward, mean squared error, backward, update; returns the loss (on the device)."""
+        """Forward, mean squared error, backward, update; returns the loss (on the device).
+        x, and what forward and backward take, are contiguous NHWC tensors of the planned batch in the
+        network's type; ValueError otherwise, before anything runs."""
+        self._planned()
+        self._fits("x", x, self.xn[0])
+        self._fits("target", target, self.out[-1], raw=False)
         y = self.forward(x)
         err = y.float() - target.float()
         self.backward((err * (2.0 / err.numel())).to(y.dtype))

@@ -105,3 +105,76 @@ def test_a_dropped_plan_is_not_run(monkeypatch, recorder):
             call()
     assert not recorder.calls
     sess.close()
+
+
+def _wrong(good):
+    """Tensors that are not the planned one: more and fewer samples, other extents, channels first, another type, a
+    slice of a wider tensor, another device."""
+    b, h, w, c = good.shape
+    return [torch.zeros(b + 2, h, w, c), torch.zeros(b - 2, h, w, c), torch.zeros(b, h + 1, w, c), torch.zeros(b, h, w, c + 1),
+            torch.zeros(b, c, h, w), torch.zeros(b, c, h, w).permute(0, 2, 3, 1), good.double(), good.bfloat16(),
+            torch.zeros(b, h, w, 2 * c)[..., :c], good.to("meta"), good[0]]
+
+
+def test_tensors_that_do_not_fit_the_plan(recorder):
+    """Refused before the first launch: the calls read raw addresses by the plan's sizes."""
+    net = Net("ends", (Layer(CONV3X3, 8, 16), Layer(CONV1X1, 16, 24, relu=False)), 8, 6, 10)
+    sess = NormPipeline(net, FP32, n=2, balance=[1, 1], device="cpu")
+    sess.plan(4, 2, CKPT_ALWAYS)
+    x, y = torch.zeros(4, 6, 10, 8), torch.zeros(4, 6, 10, 24)
+    for bad in _wrong(x):
+        with pytest.raises(ValueError, match="^x "):
+            sess.forward(bad)
+        with pytest.raises(ValueError, match="^x "):
+            sess.train_step(bad, y)
+    assert not recorder.calls
+    sess.forward(x)
+    recorder.calls.clear()
+    for bad in _wrong(y):
+        with pytest.raises(ValueError, match="^dy "):
+            sess.backward(bad)
+    for bad in _wrong(x):
+        with pytest.raises(ValueError, match="^dx "):
+            sess.backward(y, bad)
+    for shape in ((4, 6, 10, 1), (1, 6, 10, 24), (24,), (6, 6, 10, 24)):     # what torch would broadcast, or not
+        with pytest.raises(ValueError, match="^target "):
+            sess.train_step(x, torch.zeros(shape))
+    assert not recorder.calls
+    sess.backward(y, x.clone())
+    sess.train_step(x, y.bfloat16())
+    assert recorder.calls
+    sess.close()
+
+
+def test_backward_needs_its_forward(recorder):
+    """The plan's buffers hold nothing before the first forward."""
+    sess = NormPipeline(_net(), FP32, n=2, balance=[2, 2], device="cpu")
+    for _ in range(2):
+        sess.plan(4, 2, CKPT_ALWAYS)
+        x = torch.zeros(4, 6, 6, 8)
+        recorder.calls.clear()
+        with pytest.raises(RuntimeError):
+            sess.backward(x)
+        assert not recorder.calls
+        sess.forward(x)
+        sess.backward(x)
+    sess.close()
+
+
+def test_micro_batches_cover_the_buffers(recorder):
+    """The forward's rows of x, xn and statistics, of all micro-batches: each buffer once, from end to end."""
+    sess = NormPipeline(_net(), FP32, n=2, balance=[1, 3], device="cpu")
+    sess.plan(6, 3, CKPT_ALWAYS)
+    x = torch.zeros(6, 6, 6, 8)
+    sess.forward(x)
+    for j, src in ((1, x), (2, sess.out[0])):
+        c = src.shape[3]
+        calls = [a for name, a in recorder.calls if name == "layer_norm_forward" and a[1] == c]
+        assert len(calls) == 3
+        for t, place, each in ((src, 3, 4 * c), (sess.xn[j - 1], 8, 4 * c), (sess.stats[j - 1], 10, 8)):
+            at = t.data_ptr()
+            for a in calls:
+                assert a[place] == at
+                at += a[0] * each
+            assert at == t.data_ptr() + t.numel() * 4
+    sess.close()
