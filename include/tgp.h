@@ -351,7 +351,8 @@ tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap
  *   mean = sum_c x_c / C        rstd = 1 / sqrt(sum_c (x_c - mean)^2 / C + eps)
  *   y_c = gain_c (x_c - mean) rstd + bias_c
  *
- * rows pixels of C channels (rows = 0 is allowed; C >= 1).  Consecutive rows
+ * rows pixels of C channels (rows = 0 is allowed; C >= 1;
+ * EUNSUPPORTED where C is over 2^30).  Consecutive rows
  * of x and y are ldx and ldy elements apart (>= C), so that either may be a
  * channel slice of a wider tensor.  x and y have the type `dtype`; gain and
  * bias are float32 (NULL: ones, zeros).  stats, rows pairs of float32 (mean,

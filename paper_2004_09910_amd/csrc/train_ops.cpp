@@ -21,6 +21,8 @@ tgp_status check_norm(const char* who, int64_t rows, int C, int dtype) {
   // byte offsets stay far inside 64 bits, and row counts inside the kernels' 32-bit block maths
   if (rows > ((int64_t)1 << 40) / C)
     return fail(TGP_EINVAL, "%s: %lld x %d values are too many", who, (long long)rows, C);
+  // a block steps through a row's channels in 32 bits
+  if (C > 1 << 30) return fail(TGP_EUNSUPPORTED, "%s: rows of %d channels are too long", who, C);
   return TGP_OK;
 }
 

@@ -118,3 +118,22 @@ def test_adamw_refusals(kw):
     assert tgp.call_status("tgp_adamw_step", 1, tgp.adamw_tensors([a["t"]]), a["rate"], a["beta1"], a["beta2"],
                            a["eps"], a["decay"], a["step"], None) == tgp.EINVAL
     assert "adamw_step" in tgp.last_error()
+
+
+@pytest.fixture
+def no_launch():
+    """Every launch is skipped (and fails), so that calls whose checks pass end without touching a device."""
+    tgp.debug_fail_launch(1)
+    yield
+    tgp.debug_fail_launch(0)
+
+
+@pytest.mark.parametrize("c", [(1 << 30) + 1, (1 << 31) - 256, (1 << 31) - 1])
+def test_rows_longer_than_the_kernels_count(no_launch, c):
+    """The kernels step through a row's channels by a block's threads in 32 bits."""
+    for dtype in (tgp.BF16, tgp.FP32):
+        assert _fwd(rows=1, C=c, dtype=dtype, ldx=c, ldy=c) == tgp.EUNSUPPORTED
+        assert _bwd(rows=1, C=c, dtype=dtype, lddy=c, ldx=c, lddx=c, ws_bytes=1 << 60) == tgp.EUNSUPPORTED
+        v = ctypes.c_size_t()
+        assert tgp.call_status("tgp_layer_norm_backward_workspace", 1, c, dtype, ctypes.byref(v)) == tgp.EUNSUPPORTED
+    assert _fwd(rows=1, C=1 << 30, ldx=1 << 30, ldy=1 << 30, y=P + (1 << 40)) == tgp.EHIP     # as far as its launch
