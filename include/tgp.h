@@ -360,8 +360,8 @@ tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap
  * float32 or better, and the mean and the differences from it are corrected by
  * the differences' own mean, so that a row's offset does not enter: a constant
  * row gives the bias.  The variance is that of the differences, and y is
- * rounded once.  y may be x itself (ldy = ldx); other overlaps are not
- * allowed.  An infinity or NaN in a row makes that row NaN and no other.
+ * rounded once.  y may be x itself (ldy = ldx); other overlaps are
+ * refused (EINVAL).  An infinity or NaN in a row makes that row NaN and no other.
  * Alignment: elements of x and y at multiples of their size, gain and bias at
  * 4 bytes, stats at 8.  Pointers and row distances at multiples of 16 bytes
  * are read and written in 16-byte vectors.  EINVAL otherwise. */
@@ -375,7 +375,8 @@ tgp_status tgp_layer_norm_forward(int64_t rows, int C, int dtype, const void* x,
  *   dgain_c (+)= sum_rows dy_c xhat_c        dbias_c (+)= sum_rows dy_c
  *
  * dx (rows lddx apart; NULL where it is not wanted) has the type `dtype`, and
- * may be dy or x itself at the same row distance.  dgain and dbias are
+ * may be dy or x itself at the same row distance (other overlaps: EINVAL).
+ * dgain and dbias are
  * float32 accumulators like tgp_bind_params' (both set, or both NULL):
  * overwrite = 1 for a step's first micro-batch, 0 to add to them.  The sums
  * over rows run in an order fixed by (rows, C, dtype) and the alignment.

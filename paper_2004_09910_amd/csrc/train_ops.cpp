@@ -3,6 +3,8 @@
 #include "train_ops.h"
 
 #include <cmath>
+#include <cstdlib>
+#include <numeric>
 
 #include "error.h"
 #include "tgp.h"
@@ -35,6 +37,39 @@ tgp_status check_rows(const char* who, const char* name, const void* p, int64_t 
     return fail(TGP_EINVAL, "%s: rows of %s are %lld apart: too far", who, name, (long long)ld);
   if (!at(p, dtype == TGP_BF16 ? 2 : 4))
     return fail(TGP_EINVAL, "%s: %s (%p) is not aligned to its elements", who, name, p);
+  return TGP_OK;
+}
+
+// Whether rows of w bytes, la apart from a on, share bytes with rows lb apart
+// from b on.
+bool rows_meet(int64_t a, int64_t la, int64_t b, int64_t lb, int64_t rows, int64_t w) {
+  if (a + (rows - 1) * la + w <= b || b + (rows - 1) * lb + w <= a) return false;
+  // every distance of a row of b from one of a is that of a and b but for
+  // multiples of what divides both la and lb
+  const int64_t g = std::gcd(la, lb), d = ((b - a) % g + g) % g;
+  if (d >= w && g - d >= w) return false;
+  // row by row of a: the rows of b that start last at or before it and next
+  // (where those of very many rows do not keep clear as above, they meet)
+  if (la != lb && rows > 1 << 16) return true;
+  const int64_t step = la == lb ? 1 : rows;
+  for (int64_t i = 0; i < step; ++i) {
+    const int64_t at = a + i * la - b, k = (at >= 0 ? at : at - lb + 1) / lb;
+    for (int64_t j = k; j <= k + 1; ++j) {
+      // (of equal distances only the difference of the rows' numbers counts)
+      const bool there = la == lb ? std::abs(j) < rows : j >= 0 && j < rows;
+      if (there && std::abs(at - j * lb) < w) return true;
+    }
+  }
+  return false;
+}
+
+// `out` may lie on `in` row by row, and share nothing with it otherwise.
+tgp_status check_apart(const char* who, const char* out, const void* p, int64_t ldp, const char* in,
+                       const void* q, int64_t ldq, int64_t rows, int C, int dtype) {
+  if (p == q && (ldp == ldq || rows == 1)) return TGP_OK;
+  const int64_t e = dtype == TGP_BF16 ? 2 : 4;
+  if (rows_meet((int64_t)(uintptr_t)q, ldq * e, (int64_t)(uintptr_t)p, ldp * e, rows, C * e))
+    return fail(TGP_EINVAL, "%s: %s overlaps %s and is not %s itself at its row distance", who, out, in, in);
   return TGP_OK;
 }
 
@@ -87,6 +122,7 @@ tgp_status tgp_layer_norm_forward(int64_t rows, int C, int dtype, const void* x,
   if (rows == 0) return TGP_OK;
   TRY(check_rows(who, "x", x, ldx, C, dtype, rows));
   TRY(check_rows(who, "y", y, ldy, C, dtype, rows));
+  TRY(check_apart(who, "y", y, ldy, "x", x, ldx, rows, C, dtype));
   HIPCHK(tgpk::layer_norm_forward(dtype, {(long)rows, C}, x, ldx, gain, bias, eps, y, ldy, stats,
                                   (hipStream_t)stream),
          who);
@@ -117,7 +153,11 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
   if (rows > 0) {
     TRY(check_rows(who, "dy", dy, lddy, C, dtype, rows));
     TRY(check_rows(who, "x", x, ldx, C, dtype, rows));
-    if (dx) TRY(check_rows(who, "dx", dx, lddx, C, dtype, rows));
+    if (dx) {
+      TRY(check_rows(who, "dx", dx, lddx, C, dtype, rows));
+      TRY(check_apart(who, "dx", dx, lddx, "dy", dy, lddy, rows, C, dtype));
+      TRY(check_apart(who, "dx", dx, lddx, "x", x, ldx, rows, C, dtype));
+    }
     if (!stats) return fail(TGP_EINVAL, "%s: stats is NULL", who);
     const size_t need = dgain ? tgpk::layer_norm_partial_floats(dtype, {(long)rows, C}) * 4 : 0;
     if (need) {

@@ -137,3 +137,54 @@ def test_rows_longer_than_the_kernels_count(no_launch, c):
         v = ctypes.c_size_t()
         assert tgp.call_status("tgp_layer_norm_backward_workspace", 1, c, dtype, ctypes.byref(v)) == tgp.EUNSUPPORTED
     assert _fwd(rows=1, C=1 << 30, ldx=1 << 30, ldy=1 << 30, y=P + (1 << 40)) == tgp.EHIP     # as far as its launch
+
+
+# (offset in elements, row distance) of a tensor of 4 rows of 8 channels beside one at 0, 24: what shares elements
+# with it in another way than row by row, and what does not
+SHARED = [(0, 8), (0, 16), (0, 25), (0, 32), (1, 24), (7, 24), (-7, 24), (24, 24), (-24, 24), (31, 24), (72, 24), (-72, 24),
+          (24, 8), (8, 12), (12, 12), (-8, 16), (40, 16), (17, 25), (79, 8)]
+APART = [(0, 24), (8, 24), (16, 24), (-8, 24), (80, 8), (80, 24), (-32, 8), (-80, 24), (96, 24), (8, 48), (-16, 48),
+         (88, 24), (8, 25), (9, 24)]
+
+
+@pytest.mark.parametrize("dtype", [tgp.BF16, tgp.FP32])
+def test_tensors_that_overlap(no_launch, dtype):
+    """Sharing elements in another way than y (dx) lying on x (dy, x) row by row is refused: rows are
+    written while others are read.  Slices that lie between each other's rows are not."""
+    e = 2 if dtype == tgp.BF16 else 4
+
+    def elements(at, ld):
+        return {at + r * ld + c for r in range(4) for c in range(8)}
+
+    base = elements(0, 24)
+    assert all(elements(*t) & base for t in SHARED)
+    assert all(t == (0, 24) or not elements(*t) & base for t in APART)
+    for at, ld in SHARED + APART:
+        want = tgp.EHIP if (at, ld) in APART else tgp.EINVAL    # the launch, skipped here, or the refusal
+        p, far = P + at * e, P + (1 << 20)
+        for dst, src in (((p, ld), (P, 24)), ((P, 24), (p, ld))):
+            for status in (
+                    lambda: _fwd(dtype=dtype, x=src[0], ldx=src[1], y=dst[0], ldy=dst[1]),
+                    lambda: _bwd(dtype=dtype, dy=src[0], lddy=src[1], x=far, ldx=8, dx=dst[0], lddx=dst[1]),
+                    lambda: _bwd(dtype=dtype, dy=far, lddy=8, x=src[0], ldx=src[1], dx=dst[0], lddx=dst[1])):
+                tgp.debug_fail_launch(1)
+                assert status() == want, (at, ld, tgp.last_error())
+                assert want == tgp.EHIP or "overlap" in tgp.last_error()
+    tgp.debug_fail_launch(1)
+    assert _fwd(dtype=dtype, rows=1, x=P, ldx=8, y=P, ldy=24) == tgp.EHIP        # one row lies on itself
+    assert _fwd(dtype=dtype, rows=1, x=P, ldx=8, y=P + e, ldy=24) == tgp.EINVAL
+    # what is only read may overlap, and no dx is none
+    tgp.debug_fail_launch(1)
+    assert _bwd(dtype=dtype, dy=P + e, lddy=9, x=P, ldx=8, dx=P + (1 << 20)) == tgp.EHIP
+    tgp.debug_fail_launch(1)
+    assert _bwd(dtype=dtype, dy=P, lddy=9, x=P, ldx=8, dx=None, lddx=0) == tgp.EHIP
+
+
+def test_many_rows_that_overlap(no_launch):
+    """By row distances that many rows bring onto each other, and ones whose rows never meet."""
+    rows, e = 1 << 24, 2
+    assert _fwd(rows=rows, C=8, x=P, ldx=101, y=P + 50 * e, ldy=100) == tgp.EINVAL
+    assert _fwd(rows=rows, C=8, x=P, ldx=64, y=P + 16 * e, ldy=128) == tgp.EHIP
+    tgp.debug_fail_launch(1)
+    assert _fwd(rows=rows, C=8, x=P, ldx=64, y=P + 64 * rows * e, ldy=65) == tgp.EHIP
+    assert _fwd(rows=rows, C=8, x=P, ldx=64, y=P + (64 * rows - 65) * e, ldy=65) == tgp.EINVAL
