@@ -45,9 +45,9 @@ __device__ __forceinline__ F block_sum(F v, F* s4) {
 // of the mean, the variance and the result.  The mean is a float64 sum, exact
 // to float32, which costs less than a reading of the differences more.  One
 // value a lane and access: 2048 x 20000 bf16 105 us, 1.6 TB/s of what has to be
-// read and written.
+// read and written.  (y may be x: a thread reads a value before it writes it.)
 template <typename T>
-__global__ __launch_bounds__(kT) void norm_fwd_any(const T* __restrict__ x, long ldx,
+__global__ __launch_bounds__(kT) void norm_fwd_any(const T* x, long ldx,
                                                    const float* __restrict__ gain,
                                                    const float* __restrict__ bias, float eps,
                                                    T* y, long ldy, float2* __restrict__ stats,

@@ -422,3 +422,42 @@ def test_rows_that_vary_little(c, ldx, dt):
     off = (st[:, 0].cpu().double() - mean).abs()
     assert bool((off <= 2.0 ** -24 * mean.abs() * 1.01 + EPS32 * d.abs().mean(1) / rstd).all())
     assert float((st[:, 1].cpu().double() / rstd - 1).abs().max()) <= EPS32
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,c,ld", [
+    (1030, 64, 64), (3000, 64, 64), (3000, 8, 12), (1030, 100, 101), (1030, 1500, 1500), (3000, 1100, 1101),   # a wave's rows
+    (1030, 4096, 4096), (1100, 2049, 2051), (1030, 4095, 4095), (1030, 3000, 3001),                          # a block's
+    (50, 9000, 9000), (1030, 9000, 9000), (50, 4099, 4099), (1030, 4500, 4501)])                             # any row's
+def test_in_place_of_every_kernel(rows, c, ld, dt):
+    """y on x, dx on dy and dx on x: the bits of the calls with tensors of their own, by every kind of
+    kernel, and nothing between the rows touched."""
+    say("layer norm in place", rows, c, ld, dt)
+    code, td = DT[dt]
+    x, dy, gain, bias = _inputs(rows, c, rows + c)
+    xv, yv, st = _forward(x, gain, bias, dt, ld, ld)
+    g, b = gain.cuda(), bias.cuda()
+    buf, z = _rows(rows, c, ld, 0, td, x)
+    st2 = torch.empty_like(st)
+    tgp.layer_norm_forward(rows, c, code, z.data_ptr(), ld, g.data_ptr(), b.data_ptr(), 1e-5, z.data_ptr(), ld,
+                           st2.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(z, yv) and torch.equal(st2, st)
+    _untouched(buf, lambda k: k[:rows * ld].view(rows, ld)[:, :c].fill_(False), "y's neighbours")
+    n = tgp.layer_norm_backward_workspace(rows, c, code)
+    ws = torch.empty(n // 4 + 4, device="cuda")
+    got = []
+    for place in ("apart", "dy", "x"):
+        bufs = {"apart": _rows(rows, c, ld, 0, td), "dy": _rows(rows, c, ld, 0, td, dy), "x": _rows(rows, c, ld, 0, td, x)}
+        dx = bufs[place][1]
+        dg, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+        tgp.layer_norm_backward(rows, c, code, bufs["dy"][1].data_ptr(), ld, bufs["x"][1].data_ptr(), ld, g.data_ptr(),
+                                st.data_ptr(), dx.data_ptr(), ld, dg.data_ptr(), db.data_ptr(), True, ws.data_ptr(), n)
+        torch.cuda.synchronize()
+        _untouched(bufs[place][0], lambda k: k[:rows * ld].view(rows, ld)[:, :c].fill_(False), "dx's neighbours")
+        got.append((dx, dg, db))
+    dxr, dgr, dbr = ref.norm_backward(dy.to(td), xv.cpu(), gain, st[:, 0].cpu(), st[:, 1].cpu())
+    assert ref.rel(got[0][0], dxr) <= (2.0 ** -8 if dt == "bf16" else EPS32)
+    assert ref.rel(got[0][1], dgr) <= EPS32 and ref.rel(got[0][2], dbr) <= EPS32
+    for o in got[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(o, got[0]))
