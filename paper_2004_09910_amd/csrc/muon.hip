@@ -596,14 +596,18 @@ __device__ __forceinline__ float diagonal(const f32x4_t (&f)[4]) {
 __device__ __forceinline__ float lost(float v) { return v - (float)(f16)(v * kSM) * (1.f / kSM); }
 
 // Stores one 32 x 32 fragment of a symmetric matrix of mp rows at rows i0,
-// columns j0, and its mirror image where the tile does not hold it already:
-// eight consecutive rows of a column are eight columns of the mirror's row as
-// they are, and eight columns of a row come by way of `lds` (2 KiB of this
-// wave's).  value(g, i, j) is what elements 4 g .. 4 g + 3 (rows i .. i + 3,
-// column j) become.
+// columns j0, and its mirror image: eight consecutive rows of a column are
+// eight columns of the mirror's row as they are, and eight columns of a row come
+// by way of `lds` (2 KiB of this wave's).  value(g, i, j) is what elements 4 g ..
+// 4 g + 3 (rows i .. i + 3, column j) become.  What is stored is the upper half
+// and its mirror image in every place: of a tile on the diagonal the fragments
+// above it, and of a fragment on it the elements.  A product of two matrices
+// that commute but for rounding is symmetric but for rounding, and both halves as
+// computed cost half of the accuracy there (64 x 576 with 32 singular values
+// of 1 and 32 of 1 / 20: 8.3e-3 of the update's norm, 4.5e-3 so).
 template <typename F>
-__device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int j0, bool mirror,
-                                          unsigned char* lds, F value) {
+__device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int j0, unsigned char* lds, F value) {
+  if (i0 > j0) return;
   const int lane = threadIdx.x & 63, hi = lane >> 5, fr = lane & 31, j = j0 + fr;
   unsigned pk[8];
   f32x4_t f[4];
@@ -614,22 +618,34 @@ __device__ __forceinline__ void store_sym(f16* m, float* d, int mp, int i0, int 
     pk[2 * g + 1] = pack_f16(f[g][2] * kSM, f[g][3] * kSM);
     // rows of 64 bytes, chunks swizzled so that neither the writes nor the
     // transpose reads meet in a bank more than they must
-    if (mirror) *(uint2*)(lds + fr * 64 + (g ^ ((fr >> 2) & 3)) * 16 + 8 * hi) = make_uint2(pk[2 * g], pk[2 * g + 1]);
+    *(uint2*)(lds + fr * 64 + (g ^ ((fr >> 2) & 3)) * 16 + 8 * hi) = make_uint2(pk[2 * g], pk[2 * g + 1]);
   }
   if (i0 == j0 && diagonal_here()) d[j] = lost(diagonal(f));
-  put8(pk, [&](int h, u32x4 c) { *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * hi)) = c; });
-  if (mirror) {
-    const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  u32x4 down[2];   // columns 16 h + 8 hi .. of row j
+  put8(pk, [&](int h, u32x4 c) { down[h] = c; });
+  const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      uint2 v[2];
+  for (int h = 0; h < 2; ++h) {
+    uint2 v[2];
 #pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int row = 16 * kk + kb + 4 * z;
-        v[z] = lds_tr16(lds + row * 64 + (cb ^ ((row >> 2) & 3)) * 16 + 8 * (lane & 1));
-      }
-      *(u32x4*)(m + at(mp, i0 + fr, j0 + 16 * kk + 8 * hi)) = u32x4{v[0].x, v[0].y, v[1].x, v[1].y};
+    for (int z = 0; z < 2; ++z) {
+      const int row = 16 * h + kb + 4 * z;
+      v[z] = lds_tr16(lds + row * 64 + (cb ^ ((row >> 2) & 3)) * 16 + 8 * (lane & 1));
     }
+    u32x4 across = {v[0].x, v[0].y, v[1].x, v[1].y};   // those of row i0 + fr
+    if (i0 != j0) {
+      *(u32x4*)(m + at(mp, j, i0 + 16 * h + 8 * hi)) = down[h];
+    } else {
+      // the same row: its columns from the diagonal on are above it as they are,
+      // those before it as mirror images
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int c = 16 * h + 8 * hi + 2 * w;
+        const unsigned above = (fr <= c ? 0xffffu : 0u) | (fr <= c + 1 ? 0xffff0000u : 0u);
+        across[w] = (across[w] & above) | (down[h][w] & ~above);
+      }
+    }
+    *(u32x4*)(m + at(mp, i0 + fr, j0 + 16 * h + 8 * hi)) = across;
   }
 }
 
@@ -729,7 +745,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restri
         for (int g = 0; g < 4; ++g) part[64 * g] = part_of(acc, g);
         continue;
       }
-      store_sym(out, dout, t.mp, wi + 32 * i, wj + 32 * j, ti != tj, ring + wave * 2048,
+      store_sym(out, dout, t.mp, wi + 32 * i, wj + 32 * j, ring + wave * 2048,
                 [&](int g, int r, int c) {
         if constexpr (MODE == GRAM) {
           return part_of(acc, g) * (1.f / (kSX * kSX));
@@ -766,7 +782,7 @@ __global__ __launch_bounds__(256) void muon_gram_sum(const Mats* __restrict__ l,
 #pragma unroll
     for (int g = 0; g < 4; ++g) acc[g] += in[s * step + 64 * g];
   store_sym(gm(t.s[0]), gm(t.d[0]), t.mp, ti * BM + (wave / WN * MT + i) * 32, tj * BM + (wave % WN * NT + j) * 32,
-            ti != tj, lds + (threadIdx.x >> 6) * 2048,
+            lds + (threadIdx.x >> 6) * 2048,
             [&](int g, int, int) { return acc[g] * (1.f / (kSX * kSX)); });
 }
 

@@ -202,6 +202,23 @@ def test_update_of_middling_matrices(r, c):
     assert bool((z == 0).all())
 
 
+@pytest.mark.parametrize("r,c", [(64, 576), (64, 1100), (1100, 64), (128, 640), (256, 1100), (1100, 500)])
+def test_two_levels_of_singular_values(r, c):
+    """Half of the singular values 20 times the others, a span of 2^4.3: UPDATE, whatever tile an element lies in."""
+    say("muon, two levels", r, c)
+    gen = torch.Generator().manual_seed(r + c)
+    n = min(r, c)
+    u, v = (torch.linalg.qr(torch.randn(k, n, generator=gen, dtype=torch.float64))[0] for k in (r, c))
+    s = torch.where(torch.arange(n) < n // 2, 1.0, 0.05).double()
+    g = ((u * s) @ v.T).float()
+    for steps in (4, 5):
+        (_, o), = _muon([(g, None)], steps=steps)
+        _, ow = ref.muon(g, None, 0.95, True, steps, 1e-7)
+        e = ref.rel(o, ow)
+        say(steps, "%.1e" % e)
+        assert e <= UPDATE
+
+
 SIZES = [0, 1, 3, 4, 7, 64, 1000, 1024, 1025, 40001, 300000]
 
 
