@@ -17,6 +17,24 @@
 // product of two such matrices (L + dL)(R + dR), dL and dR diagonal, is taken as
 // L R + dL R + L dR.
 //
+// X itself is kept to 19 bits until two steps are left: what rounding it to
+// float16 leaves out lies beside it (xl), in 8 bits a value.  Rounding X adds
+// directions that U does not have at 2^-12 of it, and five steps multiply what is
+// near zero by a^5 = 485: alone, float16 would leave an update of a rank-one U
+// 0.14 of its norm off, of rank 8 0.035, of singular values that fall as 1 / k^2
+// 0.02.  Those directions see P(0) = a I, so P X = P Xh + a xl is all the second
+// part takes, one value at a time; in directions that U has, where P is less
+// than a, this turns X's right side by about 2^-12 and is not multiplied.  With
+// three steps left, when most singular values are near one and little
+// multiplying is to come, P's own diagonal stands for it: nearly p I for a U of
+// full rank, nearly a I for one of few directions.  Rounding A and P multiplies X
+// by I + E from the left, which turns the update by |E| whatever the singular
+// values.  Over spectra from flat to rank one, ranges of 2^14 and half of the
+// singular values zero, 0.3 to 7e-3 of the update's norm is left beside its
+// rounding to bfloat16, 1.7e-3.  xl costs two readings and two writings of a byte
+// a value: 18 of 256 x 256 92 -> 95 us, 2048 x 18432 1113 -> 1167, a U-Net's 19
+// matrices 544 -> 613 (with 16 bits a value 643).
+//
 // Two steps at once, for long matrices: X'' = P(A') P(A) X, and as P(A) and A
 // commute, A' = X' X'^T = P A P.  That replaces the first step's product with X
 // and the second's X X^T, 3 m^2 n operations, by four products of m x m
@@ -25,8 +43,8 @@
 // step: three at once lose small singular values to float16's 11 bits, 8e-3
 // of the update's norm where two leave 1.5e-3.)
 //
-// Five steps of one 2048 x 18432 take 1122 us, of a U-Net's 19 matrices of up
-// to 1024 x 9216 547 us, of 18 of 256 x 256 92 us, of four of up to 16 x 144 13
+// Five steps of one 2048 x 18432 take 1167 us, of a U-Net's 19 matrices of up
+// to 1024 x 9216 613 us, of 18 of 256 x 256 95 us, of four of up to 16 x 144 15
 // us: operations at 1256 TFLOP/s, what a large matrix product of float16
 // reaches here, are 629, 182 and 5 us of that, the tensors' bytes 98, 81 and 2.
 #include <algorithm>
@@ -60,7 +78,7 @@ struct Mat {
   float* mom;
   bf16_t* out;
   double* norm;        // partial sums of |U|^2
-  f16 *x[2], *s[3];    // X (mp x np, ping-pong), A, P and their products (mp x mp)
+  f16 *x[2], *s[3];    // X (mp x np, ping-pong; then xl, bytes), A, P and their products (mp x mp)
   float* d[3];         // their diagonals' rounding errors
   float* part;         // partial tiles of A, of `split` ranges of its sum (1: none)
   int rows, cols, m, n, mp, np, norm_blocks, norm_per, split;
@@ -68,6 +86,7 @@ struct Mat {
   // one block's: no blocks of the other launches, and nothing but the addresses
   // and rows .. n set
   __host__ __device__ bool whole() const { return norm_blocks == 0; }
+  __device__ unsigned char* xl() const { return (unsigned char*)(x[1] + (long)mp * np); }
 };
 
 // The matrices of a list and, for each kind of launch, the first block of each
@@ -91,6 +110,20 @@ static_assert(sizeof(Mats) <= 3800, "kernel arguments");
 struct Each {
   int v[2];
 };
+
+// What a product P X does about xl, likewise: the factor of xl (0: X has none;
+// P_DIAGONAL: P's diagonal), and whether X' gets one.
+constexpr float P_DIAGONAL = -1.f;
+struct EachLow {
+  float factor[2];
+  int out[2];
+};
+// An X with `left` steps to come, and its product of the next `take` of them.  The
+// rounding of an X with two steps left is multiplied by a^2 at most: 1.7e-3.
+__host__ __device__ __forceinline__ bool keeps_low(int left) { return left >= 3; }
+__host__ __device__ __forceinline__ float low_factor(int left, int take) {
+  return !keeps_low(left) ? 0.f : left == 3 ? P_DIAGONAL : take == 2 ? kA * kA : kA;
+}
 
 // Place of row i, column j of a matrix of mp rows.
 __device__ __forceinline__ long at(int mp, int i, int j) { return ((long)(j >> 5) * mp + i) * 32 + (j & 31); }
@@ -222,24 +255,50 @@ __global__ __launch_bounds__(kFirstT) void muon_momentum(Mats l, Mats* table, fl
   momentum(l, blockIdx.x, mu, nesterov, sh);
 }
 
+// What rounding four values to float16s of X leaves out, as a word of xl.  A
+// float32 has 13 bits of mantissa more than a float16: as integers the value and
+// its float16 are at most 2^12 apart (but near zero, under 2^-25 of |U|, where as
+// much as that is kept), of which the upper 8 bits of 13 are a byte.
+__device__ __forceinline__ unsigned low4(const float* v) {
+  unsigned w = 0;
+#pragma unroll
+  for (int z = 0; z < 4; ++z) {
+    const int off = __float_as_int(v[z]) - __float_as_int((float)(f16)v[z]);
+    w |= (unsigned)(min(max(off, -4096), 4095) + 4096) >> 5 << (8 * z);
+  }
+  return w;
+}
+// Value z of such a word beside the float16 h (the middle of what the byte
+// stands for).
+__device__ __forceinline__ float low_of(unsigned w, int z, float h) {
+  return __int_as_float(__float_as_int(h) + (int)((w >> (8 * z) & 255u) << 5) + (16 - 4096)) - h;
+}
+
 // What U is multiplied by for X: kSX / norm, a factor that may pass float32's
 // range, as a power of two, which is exact, and the rest.  A zero matrix stays
-// zero.
+// zero.  The product is a float32, out of the compiler's sight: taken together
+// with its rounding to float16 in one place and not in another, X and xl would
+// differ by a whole unit where it lies halfway between two.
 struct Scale {
   float rest;
   int two;
   __device__ __forceinline__ explicit Scale(double norm) {
     rest = (float)frexp(norm > 0 || norm != norm ? kSX / norm : 0.0, &two);
   }
-  __device__ __forceinline__ float operator()(float u) const { return ldexpf(u, two) * rest; }
+  __device__ __forceinline__ float operator()(float u) const {
+    float x = ldexpf(u, two) * rest;
+    asm("" : "+v"(x));
+    return x;
+  }
 };
 
 // X = U / (|U| + eps) as float16, norm_per pieces of 4096 values a block, zeros
 // in the padding: a piece is 64 rows x 64 columns through LDS where the matrix
 // is transposed, else 32 rows x 128 columns.  Memory bounds it: U is read once
-// more, as |U| is known only when all of it has been (2048 x 18432, 377 MB: 67 us,
-// 5.6 TB/s).
-__global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l, float mu, int nesterov, float eps) {
+// more, as |U| is known only when all of it has been (2048 x 18432, 415 MB: 78 us,
+// 5.3 TB/s).  keep: X gets its xl.
+__global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l, float mu, int nesterov, float eps,
+                                                      int keep) {
   __shared__ double sh[4];
   __shared__ float tile[64][65];
   const int k = find(l, L_NORMALIZE, blockIdx.x);
@@ -252,9 +311,14 @@ __global__ __launch_bounds__(256) void muon_normalize(const Mats* __restrict__ l
   auto set_scale = [&]() { scale = Scale(sqrt(block_sum(s, sh)) + eps); };
   auto put = [&](int i, int j, const float* f) {
     f16x8 h;
+    float x[8];
 #pragma unroll
-    for (int v = 0; v < 8; ++v) h[v] = (f16)scale(f[v]);
+    for (int v = 0; v < 8; ++v) {
+      x[v] = scale(f[v]);
+      h[v] = (f16)x[v];
+    }
     *(f16x8*)(gm(t.x[0]) + at(t.mp, i, j)) = h;
+    if (keep) *(uint2*)(gm(t.xl()) + at(t.mp, i, j)) = make_uint2(low4(x), low4(x + 4));
   };
   const int b0 = (blockIdx.x - l->blk0[L_NORMALIZE][k]) * t.norm_per;
   for (int b = b0; b < b0 + t.norm_per; ++b) {
@@ -567,10 +631,21 @@ __device__ __forceinline__ void put8(const unsigned (&pk)[8], F put) {
   }
 }
 
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned pack_f16(float a, float b) {
-  typedef f16 f16x2 __attribute__((ext_vector_type(2)));
   const f16x2 v = {(f16)a, (f16)b};
   return __builtin_bit_cast(unsigned, v);
+}
+
+// Words of groups 0, 2, 1, 3 of 8 columns (4 of them in lane l, 4 in lane l + 32)
+// to the words of 16 consecutive columns, 0 .. 15 in lane l and 16 .. 31 in lane
+// l + 32, and back.
+__device__ __forceinline__ u32x4 swap16(u32x4 v) {
+  // (a word's upper half of the wave changes places with the lower half of the
+  // word of the group two on)
+  const auto a = __builtin_amdgcn_permlane32_swap(v[0], v[1], false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(v[2], v[3], false, false);
+  return u32x4{a[0], a[1], b[0], b[1]};
 }
 
 __device__ __forceinline__ f32x4_t from_f16(const f16* p) {
@@ -811,9 +886,10 @@ __device__ __forceinline__ void store_update(const Mat& t, int r, int c0, const 
 // X' = s[p] X, or (last) the update itself.  In tiles of 128 x 192 it is bound
 // by the clock that the matrix instructions' power leaves, 1.7 GHz, 58% of whose
 // cycles they are busy: 2048 x 18432 147 us, 1050 TFLOP/s (the library's product
-// of 2048 x 2048 x 18432: 155 us).
+// of 2048 x 2048 x 18432: 155 us), and 163 where it reads and writes xl.
 template <int MT, int NT, int WM, int WN, int NS, int U>
-__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __restrict__ l, int launch, Each ep, Each efrom, int last,
+                                                              EachLow elow) {
   typedef Tile<MT, NT, WM, WN, NS, U, true, true> TL;
   __shared__ __attribute__((aligned(16))) unsigned char ring[NS * TL::SB];
   const int blk = grouped(blockIdx.x, gridDim.x);
@@ -828,6 +904,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
   // X's own elements of a wave with one fragment, on their way while the sum
   // runs; with more there are the others' products to hide them
   constexpr bool EARLY = MT * NT == 1;
+  const float factor = pickg(elow.factor, t.two);
+  const bool keep = pickg(elow.out, t.two);
+  unsigned char* xl = gm(t.xl());
   f32x4_t xe[4];
   if constexpr (EARLY) {
     const int r = i0 + wave / WN * 32 + (lane & 31), c0 = j0 + wave % WN * 32;
@@ -835,16 +914,28 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
     for (int g = 0; g < 4; ++g)
       xe[g] = c0 < t.np ? from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5))) : f32x4_t{};
   }
+  // xl of 16 columns of the lane's rows likewise
+  u32x4 le[MT][NT] = {};
+  if (factor != 0)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31), c0 = j0 + (wave % WN * NT + j) * 32;
+        if (c0 < t.np) le[i][j] = *(const u32x4*)(xl + at(t.mp, r, c0 + 16 * (lane >> 5)));
+      }
   TL tl;
   tl.run(ring, gm(t.s[p]), t.mp, i0, x, t.mp, t.np, j0, 0, t.mp / 32);
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int r = i0 + (wave / WN * MT + i) * 32 + (lane & 31);
     const float d = dp[r] * (1.f / kSX);
+    const float pl = (factor == P_DIAGONAL ? (float)gm(t.s[p])[at(t.mp, r, r)] * (1.f / kSM) + dp[r] : factor) * (1.f / kSX);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int c0 = j0 + (wave % WN * NT + j) * 32;
       if (c0 >= t.np) continue;
+      const u32x4 lv = swap16(le[i][j]);   // as the accumulators lie: a word of group 0, 2, 1, 3 of 8 columns
       const f32x16& acc = tl.acc[i][j];
       unsigned pk[8];
       float y[16];
@@ -852,13 +943,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
       for (int g = 0; g < 4; ++g) {
         const f32x4_t xv = EARLY ? xe[g] : from_f16(x + at(t.mp, r, c0 + 8 * g + 4 * (lane >> 5)));
 #pragma unroll
-        for (int z = 0; z < 4; ++z) y[4 * g + z] = acc[4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
+        for (int z = 0; z < 4; ++z)
+          y[4 * g + z] = acc[4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
+        if (factor != 0)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[4 * g + z] += pl * low_of(lv[g >> 1 | (g & 1) << 1], z, xv[z]);
       }
       if (!last) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) pk[g] = pack_f16(y[2 * g] * kSX, y[2 * g + 1] * kSX);
         f16* out = gm(t.x[from ^ 1]);
         put8(pk, [&](int h, u32x4 c) { *(u32x4*)(out + at(t.mp, r, c0 + 16 * h + 8 * (lane >> 5))) = c; });
+        if (keep) {   // in place: what this wave has read
+#pragma unroll
+          for (int v = 0; v < 16; ++v) y[v] *= kSX;
+          *(u32x4*)(xl + at(t.mp, r, c0 + 16 * (lane >> 5))) =
+              swap16(u32x4{low4(y), low4(y + 8), low4(y + 4), low4(y + 12)});
+        }
       } else {
         store_update(t, r, c0, y);
       }
@@ -889,6 +990,7 @@ struct SmallLds {
   double sh[kFirstT / 64];
 };
 
+// xl is in registers, where each wave needs it.
 template <int MS>
 __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float mu, int nesterov, int steps,
                                              float eps) {
@@ -971,19 +1073,44 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     }
   }
   const Scale scale(sqrt(first_sum(sum, lds.sh)) + eps);
+  auto put_x = [&](auto part) {
 #pragma unroll
-  for (int z = 0; z < kSmallChunks; ++z) {
-    int i, j;
-    if (z * kFirstT >= chunks) break;
-    if (!place(z, i, j)) continue;
-    f16x8 h;
+    for (int z = 0; z < kSmallChunks; ++z) {
+      int i, j;
+      if (z * kFirstT >= chunks) break;
+      if (!place(z, i, j)) continue;
+      f16x8 h;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) h[v] = (f16)scale(u[z][v]);
-    *(f16x8*)(xs + ((j >> 5) * MS + i) * kRow + (j & 31) * 2) = h;
-  }
-  __syncthreads();
-
+      for (int v = 0; v < 8; ++v) h[v] = (f16)part(scale(u[z][v]));
+      *(f16x8*)(xs + ((j >> 5) * MS + i) * kRow + (j & 31) * 2) = h;
+    }
+    __syncthreads();
+  };
   const int fr = lane & 31, hi = lane >> 5;
+  // xl of this wave's panels (wave, wave + 12, ..), as the products' accumulators
+  // lie: by way of X's place in LDS
+  constexpr int kPanels = (kSmallX / MS / 32 + kFirstT / 64 - 1) / (kFirstT / 64);
+  // (there as float16)
+  constexpr float kSL = 2048.f;
+  auto low = [](float v) { return (v - (float)(f16)v) * kSL; };
+  unsigned xl[kPanels][Q][8];
+  if (keeps_low(steps)) {
+    put_x(low);
+#pragma unroll
+    for (int k = 0; k < kPanels; ++k)
+#pragma unroll
+      for (int i = 0; i < Q; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int pj = min(wave + k * (kFirstT / 64), ns / 32 - 1);
+          const uint2 v = *(const uint2*)(xs + (pj * MS + 32 * i + fr) * kRow + 16 * g + 8 * hi);
+          xl[k][i][2 * g] = v.x;
+          xl[k][i][2 * g + 1] = v.y;
+        }
+    __syncthreads();
+  }
+  put_x([](float v) { return v; });
+
   const int kb = 8 * hi + ((lane & 15) >> 2), cb = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   // fragment of 32 rows from r0 on, sum values 16 kk .. of panel p
   auto rows_of = [&](const unsigned char* b, int p, int r0, int kk) {
@@ -1044,7 +1171,11 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
     }
     __syncthreads();
     // X = P X, a panel a wave and turn, in place
-    for (int pj = wave; pj < ns / 32; pj += kFirstT / 64) {
+    const float factor = low_factor(steps - s, 1);
+#pragma unroll
+    for (int k = 0; k < kPanels; ++k) {
+      const int pj = wave + k * (kFirstT / 64);
+      if (pj >= ns / 32) break;
       f32x16 acc[Q] = {};
 #pragma unroll
       for (int p = 0; p < Q; ++p)
@@ -1064,6 +1195,16 @@ __device__ __forceinline__ void small_update(SmallLds& lds, const Mat& t, float 
           const f32x4_t xv = from_f16((const f16*)four(xs, r, 32 * pj + 8 * g + 4 * hi));
 #pragma unroll
           for (int z = 0; z < 4; ++z) y[4 * g + z] = acc[i][4 * g + z] * (1.f / (kSM * kSX)) + d * xv[z];
+        }
+        if (factor != 0) {
+          const float p = factor == P_DIAGONAL ? (float)*(const f16*)four(pms, r, r) * (1.f / kSM) + dp[r] : factor;
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            const f16x2 v = __builtin_bit_cast(f16x2, xl[k][i][g]);
+            y[2 * g] += p * (1.f / (kSX * kSL)) * (float)v[0];
+            y[2 * g + 1] += p * (1.f / (kSX * kSL)) * (float)v[1];
+            xl[k][i][g] = pack_f16(low(y[2 * g] * kSX), low(y[2 * g + 1] * kSX));
+          }
         }
         if (s + 1 < steps) {
           unsigned pk[8];
@@ -1157,6 +1298,7 @@ size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mat
     t.norm_per = size >= 1 << 22 ? 4 : 1;   // where it is large, |U| is summed up by fewer blocks
     t.norm = (double*)take(kNormBlocks * sizeof(double));
     for (int z = 0; z < 2; ++z) t.x[z] = (f16*)take((size_t)t.mp * t.np * 2);
+    take((size_t)t.mp * t.np);   // xl, after x[1] (whose size is a multiple of 256)
     for (int z = 0; z < 3; ++z) {
       t.s[z] = (f16*)take((size_t)t.mp * t.mp * 2);
       t.d[z] = (float*)take((size_t)t.mp * 4);
@@ -1266,7 +1408,8 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   }
   {
     ProfScope ps("muon_normalize", 2 * n, 10 * n, st);
-    TGP_LAUNCH(ps, muon_normalize, dim3(grid[L_NORMALIZE]), dim3(256), 0, st, tb, mu, (int)nesterov, eps);
+    TGP_LAUNCH(ps, muon_normalize, dim3(grid[L_NORMALIZE]), dim3(256), 0, st, tb, mu, (int)nesterov, eps,
+               (int)keeps_low(steps));
   }
   // the launches, each over the matrices of its table that have blocks in it
   Each from{{0, 0}};   // which of its two buffers X is in
@@ -1303,15 +1446,15 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
       TGP_LAUNCH(ps, (muon_sym<MUL, 1, 1, 2, 2, 4, 1>), dim3(grid[L_SYM2]), dim3(256), 0, st, tb, (int)L_SYM2,
                  (Each{{a, a}}), b, (Each{{c, c}}));
   };
-  auto apply = [&](int la, Each p, int last) {
+  auto apply = [&](int la, Each p, int last, EachLow low) {
     if (!grid[la]) return;
     ProfScope ps("muon_apply", 2 * gram, 4 * n + 2 * cells, st);
     if (ba == 192)
-      TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<2, 3, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last, low);
     else if (ba == 128)
-      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<2, 2, 2, 2, 4, 1>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last, low);
     else
-      TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 4, 2>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last);
+      TGP_LAUNCH(ps, (muon_apply<1, 1, 2, 2, 4, 2>), dim3(grid[la]), dim3(256), 0, st, tb, la, p, from, last, low);
   };
   // Two steps a turn: what both kinds of matrices need is one launch for both,
   // and a list of one kind has no launches of the other.
@@ -1321,14 +1464,16 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
     poly(Each{{1, 1}});
     if (turn) {
       mul(1, 0, 2);                          // P A
-      apply(L_APPLY1, Each{{1, 1}}, 0);
+      apply(L_APPLY1, Each{{1, 1}}, 0, EachLow{{low_factor(steps - s, 1), 0.f}, {keeps_low(steps - s - 1), 0}});
       if (grid[L_APPLY1]) from.v[0] ^= 1;
       mul(2, 1, 0);                          // A' = P A P
       gram_of(L_GRAM1, L_SUM1);
       poly(Each{{1, 2}});                    // P'
       mul(2, 1, 0);                          // P' P
     }
-    apply(L_APPLY, Each{{1, turn ? 0 : 1}}, s + 2 >= steps);
+    const int end = std::min(s + 2, steps), keep = keeps_low(steps - end);
+    apply(L_APPLY, Each{{1, turn ? 0 : 1}}, end == steps,
+          EachLow{{low_factor(steps - end + 1, 1), low_factor(steps - s, end - s)}, {keep, keep}});
     from.v[0] ^= 1;
     from.v[1] ^= 1;
   }

@@ -349,3 +349,67 @@ def test_weight_step_past_32_bits():
     assert w[-1].item() == 0.75 and w[1 << 31].item() == 0.5
     w[-1] = w[1 << 31] = 0.875
     assert bool((w == 0.875).all())
+
+
+# Of matrices whose singular values are anything, what is left (as parts of the update's norm): bfloat16's rounding
+# of the result, 2^-9 / sqrt(3) x 1.5 = 1.7e-3; float16's of the products' left operands, which turns X by at most
+# |E P^-1| a product, E being 2^-12 / sqrt(3) of P's entries: 1.4e-4 x a^2 / 0.68 = 2.4e-3 for two steps at once, twice;
+# of X where two steps are left, times their a^2 in directions that U lacks: 1.4e-4 x 11.9 = 1.7e-3; and of X before
+# that, where P's diagonal stands for P (three steps left): half of 1.4e-4 x a^3 = 2.9e-3 at most.  In quadrature 5.1e-3;
+# the sum of the largest two and half the others, 8e-3, is asked.
+ANY_SPECTRUM = 8e-3
+
+
+def _spectrum(kind, m, n, gen):
+    """A matrix of m x n with the singular values that `kind` names, in random directions."""
+    def ortho(k):
+        return torch.linalg.qr(torch.randn(k, min(k, min(m, n)), generator=gen, dtype=torch.float64))[0]
+
+    r = min(m, n)
+    k = torch.arange(r, dtype=torch.float64)
+    if kind == "cells":     # four rows at a time are one direction
+        g = torch.zeros(m, n, dtype=torch.float64)
+        for i in range(0, m, 4):
+            g[i:i + 4] = torch.randn(min(4, m - i), 1, generator=gen, dtype=torch.float64) @ torch.randn(
+                1, n, generator=gen, dtype=torch.float64)
+        return g.float()
+    if kind == "rows":      # half of the rows are zero
+        g = torch.randn(m, n, generator=gen)
+        g[::2] = 0
+        return g
+    s = {"flat": k * 0 + 1, "squares": (k + 1) ** -2, "decades": 10.0 ** (-4 * k / max(r - 1, 1)),
+         "2^9": 2.0 ** (-9 * k / max(r - 1, 1)), "2^11": 2.0 ** (-11 * k / max(r - 1, 1)),
+         "2^14": 2.0 ** (-14 * k / max(r - 1, 1)), "one of 2000": torch.where(k == 0, 2000.0, 1.0).double(),
+         "rank 1": (k < 1).double(), "rank 8": (k < 8).double(), "half rank": (k < (r + 1) // 2).double()}[kind]
+    return ((ortho(m) * s) @ ortho(n).T).float()
+
+
+@pytest.mark.parametrize("kind", ["flat", "squares", "decades", "2^9", "2^11", "2^14", "one of 2000", "rank 1", "rank 8",
+                                  "half rank", "cells", "rows"])
+def test_any_spectrum(kind):
+    """By one block (up to 64 rows), by tiles one step at a time and two, whole and transposed, and a list of all."""
+    shapes = [(16, 144), (30, 32), (64, 256), (64, 64), (200, 60), (256, 256), (300, 500), (64, 576), (130, 700),
+              (256, 2304), (1152, 128)]
+    gen = torch.Generator().manual_seed(len(kind) * 7 + ord(kind[0]))
+    mats = [(_spectrum(kind, r, c, gen), None) for r, c in shapes]
+    got = _muon(mats)
+    for (g, _), (_, o), (r, c) in zip(mats, got, shapes):
+        _, ow = ref.muon(g, None, 0.95, True, 5, 1e-7)
+        e = ref.rel(o, ow)
+        say(kind, r, c, "%.1e" % e)
+        assert e <= ANY_SPECTRUM
+
+
+@pytest.mark.parametrize("steps", [3, 4, 6, 7])
+@pytest.mark.parametrize("kind", ["squares", "rank 1", "half rank", "flat"])
+def test_any_spectrum_of_other_steps(kind, steps):
+    """As above; with each step beyond five what X's rounding left out is multiplied by a or a^2 once more where P is
+    near one, which turns X by up to 1.4e-4 x a^2: twice the tolerance."""
+    gen = torch.Generator().manual_seed(steps)
+    shapes = [(24, 200), (64, 200), (250, 250), (128, 640), (640, 128)]
+    mats = [(_spectrum(kind, r, c, gen), None) for r, c in shapes]
+    for (g, _), (_, o), (r, c) in zip(mats, _muon(mats, steps=steps), shapes):
+        _, ow = ref.muon(g, None, 0.95, True, steps, 1e-7)
+        e = ref.rel(o, ow)
+        say(kind, r, c, steps, "%.1e" % e)
+        assert e <= ANY_SPECTRUM * (1 if steps < 6 else 2)
