@@ -413,3 +413,60 @@ def test_any_spectrum_of_other_steps(kind, steps):
         e = ref.rel(o, ow)
         say(kind, r, c, steps, "%.1e" % e)
         assert e <= ANY_SPECTRUM * (1 if steps < 6 else 2)
+
+
+def _muon64(grad, momentum, steps):
+    """The definition in 64 bits on the device (plain products; contiguous operands)."""
+    m = 0.95 * momentum.double() + grad.double()
+    u = grad.double() + 0.95 * m
+    x = u.T.contiguous() if u.shape[0] > u.shape[1] else u
+    x = x / (torch.linalg.vector_norm(x) + 1e-7)
+    for _ in range(steps):
+        a = x @ x.T.contiguous()
+        x = ref.NS[0] * x + (ref.NS[1] * a + ref.NS[2] * (a @ a)) @ x
+    return m, (x.T if u.shape[0] > u.shape[1] else x)
+
+
+@pytest.mark.parametrize("shapes", [
+    # P X in tiles of 128 columns, two steps at a time and one
+    [(1024, 4096)], [(1024, 2600), (700, 2000)], [(2048, 2048)],
+    # P in more blocks than two a CU
+    [(2500, 2100)],
+    # P X in tiles of 192 columns, X X^T in ranges of tiles of 64 x 64 or (2048 x 18432) 128 x 128
+    [(1024, 9216)], [(9216, 1024)], [(2048, 18432)],
+    # X X^T whole in tiles of 128 x 128, P X one step at a time in tiles of 192; all sorts in one list
+    [(4096, 4100), (300, 5000), (40, 40), (1000, 1001)],
+], ids=lambda s: "+".join("%dx%d" % t for t in s))
+@pytest.mark.parametrize("strong", [8, 0])
+def test_large_matrices(shapes, strong):
+    """Every kind of tile with all five steps: eight strong directions in noise (UPDATE), and of rank 8
+    (ANY_SPECTRUM)."""
+    say("muon, large", shapes, strong)
+    g = torch.Generator(device="cuda").manual_seed(len(shapes) + strong)
+
+    def grad(r, c):
+        d = min(8, r, c)
+        t = torch.randn(r, d, device="cuda", generator=g) @ torch.randn(d, c, device="cuda", generator=g) / math.sqrt(8)
+        return 1e-3 * (t + torch.randn(r, c, device="cuda", generator=g) if strong else t)
+
+    grads, moms = [grad(r, c) for r, c in shapes], [5 * grad(r, c) for r, c in shapes]
+    if not strong:
+        moms = [-2 * t for t in grads]      # the same eight directions
+    news = [t.clone() for t in moms]
+    out = [torch.empty(r, c, dtype=torch.bfloat16, device="cuda") for r, c in shapes]
+    t = tgp.muon_tensors([(r, c, a.data_ptr(), b.data_ptr(), o.data_ptr())
+                          for (r, c), a, b, o in zip(shapes, grads, news, out)])
+    n = tgp.muon_workspace(t)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for steps in (5, 2):
+        for a, b in zip(news, moms):
+            a.copy_(b)
+        tgp.muon_update(t, 0.95, True, steps, 1e-7, ws.data_ptr(), n)
+        torch.cuda.synchronize()
+        for a, b, m, o in zip(grads, moms, news, out):
+            mw, ow = _muon64(a, b, steps)
+            e = float(torch.linalg.vector_norm(o.double() - ow) / torch.linalg.vector_norm(ow))
+            say(tuple(a.shape), steps, "%.1e" % e)
+            assert float(torch.linalg.vector_norm(m.double() - mw) / torch.linalg.vector_norm(mw)) <= 2.0 ** -22
+            assert e <= (UPDATE if strong else ANY_SPECTRUM)
+            del mw, ow
