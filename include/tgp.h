@@ -416,7 +416,9 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * steps >= 1; 1 <= rows, cols, and rows x cols (each rounded up to a multiple
  * of 128) < 2^30 (EUNSUPPORTED beyond).  grad, momentum and update at
  * multiples of 16 bytes; ws at a multiple of 256, of at least the size that
- * tgp_muon_workspace returns for the same shapes (ENOSPACE if smaller).
+ * tgp_muon_workspace returns for the same shapes (ENOSPACE if smaller).  More
+ * than 20 matrices are taken 20 at a time, one sequence of launches after the
+ * other in the same workspace.
  * `t` is read on the host before the call returns. */
 typedef struct {
   int32_t rows, cols;

@@ -1268,8 +1268,8 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
   t.n = std::max(t.rows, t.cols);
 }
 
-// Describes n (at most kMaxMats) matrices laid out from byte `pos` of the
-// workspace ws on; returns their end.  The sum of A = X X^T is split where a
+// Describes n (at most kMaxMats) matrices laid out in the workspace ws (NULL:
+// only the size is asked for); returns its bytes.  The sum of A = X X^T is split where a
 // matrix has too few tiles to fill the chip: into as many ranges as make at
 // most kBlocks blocks (one more than run at once waits for all of them: 2048 x
 // 18432 in 3 ranges 89 us and 8.6 to add them up, in 4 101 and 9.7, in 7 86 and
@@ -1278,14 +1278,15 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 // a U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not 324).  The
 // ranges depend on the matrix alone, so that its update does not depend on the
 // others of the call.
-size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, size_t pos, Mats& l) {
+size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, Mats& l) {
+  size_t pos = 0;
   auto take = [&](size_t bytes) {
-    char* p = ws ? ws + pos : nullptr;   // (none: only the size is asked for)
+    char* p = ws ? ws + pos : nullptr;
     pos += al256(bytes);
     return p;
   };
   l.count = n;
-  take(sizeof(Mats));   // the launches' table
+  take(sizeof(Mats));   // the launches' table, first
   for (int k = 0; k < n; ++k) {
     Mat& t = l.t[k];
     describe(*d[k], t);
@@ -1482,25 +1483,25 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
 
 }  // namespace
 
+// The lists of one call run one after the other on its stream, and share the
+// workspace.
 size_t muon_bytes(int n, const tgp_muon_tensor* t) {
-  size_t pos = 0;
+  size_t most = 0;
   Mats l;
   each_list(n, t, [&](const tgp_muon_tensor* const* d, int count) {
-    pos = lay_out(count, d, nullptr, pos, l);
+    most = std::max(most, lay_out(count, d, nullptr, l));
   });
-  return pos;
+  return most;
 }
 
 hipError_t muon_update(int n, const tgp_muon_tensor* t, float mu, bool nesterov, int steps,
                        float eps, void* ws, hipStream_t st) {
-  size_t pos = 0;
   hipError_t e = hipSuccess;
   each_list(n, t, [&](const tgp_muon_tensor* const* d, int count) {
     if (e != hipSuccess) return;
     Mats l;
-    Mats* table = (Mats*)((char*)ws + pos);
-    pos = lay_out(count, d, (char*)ws, pos, l);
-    e = update_list(l, table, mu, nesterov, steps, eps, st);
+    lay_out(count, d, (char*)ws, l);
+    e = update_list(l, (Mats*)ws, mu, nesterov, steps, eps, st);
   });
   return e;
 }

@@ -470,3 +470,17 @@ def test_large_matrices(shapes, strong):
             assert float(torch.linalg.vector_norm(m.double() - mw) / torch.linalg.vector_norm(mw)) <= 2.0 ** -22
             assert e <= (UPDATE if strong else ANY_SPECTRUM)
             del mw, ow
+
+
+def test_long_lists_share_their_workspace():
+    """More tiled matrices than a list takes, of sizes that lie differently in each list's workspace, with
+    whole ones among them: every matrix as by itself, twice over in one workspace."""
+    shapes = [(128, 300), (300, 128), (64, 700), (260, 520), (16, 144), (130, 130), (90, 200), (500, 65), (64, 64)] * 6
+    mats = [(_grad(r, c, k, scale=10.0 ** -(k % 5)), _grad(r, c, k + 100)) for k, (r, c) in enumerate(shapes)]
+    got = _muon(mats)
+    again = _muon(mats, ws_fill=0)
+    for k, (a, b) in enumerate(zip(got, again)):
+        assert torch.equal(a[1], b[1]) and torch.equal(a[0], b[0]), k
+    for k in range(0, len(mats), 5):
+        (mom, o), = _muon([mats[k]])
+        assert torch.equal(o, got[k][1]) and torch.equal(mom, got[k][0]), k

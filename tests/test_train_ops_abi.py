@@ -188,3 +188,16 @@ def test_many_rows_that_overlap(no_launch):
     tgp.debug_fail_launch(1)
     assert _fwd(rows=rows, C=8, x=P, ldx=64, y=P + 64 * rows * e, ldy=65) == tgp.EHIP
     assert _fwd(rows=rows, C=8, x=P, ldx=64, y=P + (64 * rows - 65) * e, ldy=65) == tgp.EINVAL
+
+
+def test_muon_workspace_of_long_lists():
+    """Lists that run one after the other share their workspace: no more than the largest asks for."""
+    def need(n, r, c):
+        return tgp.muon_workspace(tgp.muon_tensors([(r, c, None, None, None)] * n))
+
+    for r, c in ((2048, 18432), (128, 1152), (300, 70)):
+        most = need(20, r, c)
+        assert need(1, r, c) < need(10, r, c) < most
+        assert all(need(n, r, c) == most for n in (21, 40, 41, 100))
+    mixed = tgp.muon_tensors([(2048, 4096, None, None, None)] * 30 + [(64, 576, None, None, None)] * 5)
+    assert tgp.muon_workspace(mixed) == need(20, 2048, 4096)
