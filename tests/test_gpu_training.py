@@ -152,3 +152,95 @@ def test_gradients_after_a_new_partition():
             assert ref.rel(q["dgain"], gain.grad) <= 1e-4 and ref.rel(q["dbias"], bias.grad) <= 1e-4
         sess.update()
     sess.close()
+
+
+def _reference_skips(sess, x, gout):
+    """As _reference, of a network with pools and skips, from the output's gradient: output, input, layers'
+    (weight, bias) and norms, with their gradients."""
+    P, N, skips = {}, [], {}
+    for idx, p in sess.params.items():
+        L = sess.net.layers[idx]
+        w = p["w"].double().cpu()
+        w = w.reshape(L.cout, 1, 3, 3) if L.kind == DWCONV3X3 else w.permute(0, 3, 1, 2).contiguous()
+        P[idx] = (w.requires_grad_(), None if p["b"] is None else p["b"].double().cpu().requires_grad_())
+    for q in sess.norms:
+        N.append(tuple(q[k].double().cpu().requires_grad_() for k in ("gain", "bias")))
+    xin = x.double().cpu().permute(0, 3, 1, 2).contiguous().requires_grad_()
+    h = xin
+    for (lo, hi), (gain, bias) in zip(sess.bounds, N):
+        mean = h.mean(1, keepdim=True)
+        var = (h - mean).square().mean(1, keepdim=True)
+        h = (h - mean) / torch.sqrt(var + sess.eps) * gain[:, None, None] + bias[:, None, None]
+        for idx in range(lo, hi):
+            L = sess.net.layers[idx]
+            if L.prologue == specs.PRO_MAXPOOL2:
+                h = F.max_pool2d(h, 2)
+            elif L.prologue == specs.PRO_UPCAT2:
+                h = torch.cat((F.interpolate(h, scale_factor=2, mode="nearest"), skips[L.pop_id]), 1)
+            h = F.conv2d(h, P[idx][0], P[idx][1], padding=0 if L.kind == CONV1X1 else 1,
+                         groups=L.cout if L.kind == DWCONV3X3 else 1)
+            h = h.relu() if L.relu else h
+            if L.stash_id >= 0:
+                skips[L.stash_id] = h
+    h.backward(gout.double().cpu().permute(0, 3, 1, 2))
+    return h, xin, P, N
+
+
+def _compare_skips(sess, x, dy, tol):
+    h, xin, P, N = _reference_skips(sess, x, dy)
+    y = sess.forward(x)
+    dx = torch.empty_like(x)
+    sess.backward(dy, dx)
+    torch.cuda.synchronize()
+    assert ref.rel(y, h.detach().permute(0, 2, 3, 1)) <= tol
+    assert ref.rel(dx, xin.grad.permute(0, 2, 3, 1)) <= tol
+    for idx, (w, b) in P.items():
+        L = sess.net.layers[idx]
+        want = w.grad.reshape(L.cout, 9) if L.kind == DWCONV3X3 else w.grad.permute(0, 2, 3, 1)
+        assert ref.rel(sess.params[idx]["dw"], want) <= tol, idx
+        if b is not None:
+            assert ref.rel(sess.params[idx]["db"], b.grad) <= tol, idx
+    for q, (gain, bias) in zip(sess.norms, N):
+        assert ref.rel(q["dgain"], gain.grad) <= tol and ref.rel(q["dbias"], bias.grad) <= tol
+
+
+def _skip_net():
+    return Net("norm-unet", (Layer(CONV3X3, 8, 16, stash_id=0),
+                             Layer(CONV3X3, 16, 24, prologue=specs.PRO_MAXPOOL2),
+                             Layer(CONV3X3, 24, 24),
+                             Layer(CONV3X3, 40, 16, prologue=specs.PRO_UPCAT2, pop_id=0),
+                             Layer(CONV1X1, 16, 8, relu=False)), 8, 12, 12)
+
+
+@pytest.mark.parametrize("mode", [specs.CKPT_ALWAYS, specs.CKPT_NEVER])
+@pytest.mark.parametrize("balance", [[1, 2, 2], [2, 2, 1], [3, 2]])
+def test_gradients_of_a_network_with_skips(balance, mode):
+    """A small U-Net in float32, its skip within a partition, across one and from a partition's last layer:
+    1e-4 of each gradient's norm, as above."""
+    say("normalised U-Net", balance, mode)
+    torch.manual_seed(4)
+    sess = NormPipeline(_skip_net(), FP32, n=len(balance), balance=balance)
+    for q in sess.norms:
+        q["gain"].copy_(1 + 0.2 * torch.randn_like(q["gain"]))
+        q["bias"].copy_(0.2 * torch.randn_like(q["bias"]))
+    sess.plan(8, 4, mode)
+    x, dy = torch.randn(8, 12, 12, 8, device="cuda"), 1e-3 * torch.randn(8, 12, 12, 8, device="cuda")
+    _compare_skips(sess, x, dy, 1e-4)
+    sess.close()
+
+
+def test_bfloat16_gradients():
+    """Layers without ReLU, so that no decision hangs on a rounding: each of some ten tensors between x and dx (outputs,
+    norms, gradients of both) is rounded to bfloat16, 2^-9 / sqrt(3) x 1.5 of its norm a time, and a gradient sees up to twenty
+    of them: 20^1/2 x 1.7e-3 = 7.6e-3; twice that is asked."""
+    torch.manual_seed(5)
+    sess = NormPipeline(Net("norm-chain", (Layer(CONV3X3, 16, 32, relu=False), Layer(DWCONV3X3, 32, 32, relu=False, bias=False),
+                                           Layer(CONV1X1, 32, 24, relu=False), Layer(CONV3X3, 24, 16, relu=False)), 16, 12, 12),
+                        BF16, n=3, balance=[1, 2, 1])
+    for q in sess.norms:
+        q["gain"].copy_(1 + 0.2 * torch.randn_like(q["gain"]))
+        q["bias"].copy_(0.2 * torch.randn_like(q["bias"]))
+    sess.plan(8, 4, specs.CKPT_ALWAYS)
+    x, dy = torch.randn(8, 12, 12, 16, device="cuda").bfloat16(), (1e-3 * torch.randn(8, 12, 12, 16, device="cuda")).bfloat16()
+    _compare_skips(sess, x, dy, 1.5e-2)
+    sess.close()
