@@ -359,7 +359,7 @@ tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap
  * rstd), is what the backward reads; NULL where none will run.  Sums are
  * float32 or better, and the mean and the differences from it are corrected by
  * the differences' own mean, so that a row's offset does not enter: a constant
- * row gives the bias.  The variance is that of the differences, and y is
+ * row gives the bias (eps > 0).  The variance is that of the differences, and y is
  * rounded once.  y may be x itself (ldy = ldx); other overlaps are
  * refused (EINVAL).  An infinity or NaN in a row makes that row NaN and no other.
  * Alignment: elements of x and y at multiples of their size, gain and bias at

@@ -973,12 +973,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void muon_apply(const Mats* __rest
 // X, A and P staying in LDS (panels of 32 columns, a row's 64 bytes 80 apart:
 // eight rows read at one chunk hit distinct banks).  MS: m rounded up to 32 or
 // 64.  What bounds it is one CU's rate of loading and the latencies between its
-// barriers, three a step: five steps of 16 x 144 take 12.9 us, of 64 x 256 20
-// (eight waves 20.5, sixteen 22.5), where four launches a step take 70 to 90.
-// LDS holds up to 55296 values, and a list of 64 x 576 alone would gain (89 us
-// as tiles, 33); among others such a block outlasts the launch it shares by
-// more than a few matrices more cost the tiles (six matrices of all sorts with
-// one of 1144 x 9: 149 us, 177).
+// barriers, three a step: five steps of 16 x 144 take 14.8 us, of 64 x 256 24
+// (without xl 12.9 and 20; there eight waves 20.5, sixteen 22.5), where four
+// launches a step take 70 to 90.  LDS could hold an X of 55296 values.  A list of
+// 64 x 576 alone took 33 us so, and 89 as tiles; but among other matrices such a
+// block runs on after the launch that it shares, for longer than tiles take for
+// one matrix more (six matrices of all sorts, one of them 1144 x 9: 177 us so,
+// 149 as tiles).
 constexpr int kSmallX = 16384, kRow = 80;   // most values of X, bytes of a row
 // chunks of 8 values of a thread, and those whose loads are in flight together
 constexpr int kSmallChunks = (kSmallX / 8 + kFirstT - 1) / kFirstT, kFlight = 2;
@@ -1245,9 +1246,9 @@ int uppers(int nt) { return nt * (nt + 1) / 2; }
 
 // Whether two steps are taken at once.  The products with X that this saves
 // run at about twice the rate of the m x m ones that replace them, on fewer
-// tiles: from n = 4 m on (a 3 x 3 layer has 9 m and more).  1024 x 4096 205 us,
-// 217 one step at a time; 2048 x 8192 653, 762; below, 1024 x 2048 166 and 155,
-// 2048 x 4096 491 and 515.
+// tiles: from n = 4 m on (a 3 x 3 layer has 9 m and more).  1024 x 4096 224 us,
+// 244 one step at a time; 2048 x 8192 740, 876.  At n = 2 m it depends on m: 1024 x
+// 2048 174 and 165, 2048 x 4096 552 and 588.
 bool pairs(const tgp_muon_tensor& d) {
   return std::max(d.rows, d.cols) >= 4 * (long)std::min(d.rows, d.cols);
 }
@@ -1269,15 +1270,15 @@ void describe(const tgp_muon_tensor& d, Mat& t) {
 }
 
 // Describes n (at most kMaxMats) matrices laid out in the workspace ws (NULL:
-// only the size is asked for); returns its bytes.  The sum of A = X X^T is split where a
-// matrix has too few tiles to fill the chip: into as many ranges as make at
-// most kBlocks blocks (one more than run at once waits for all of them: 2048 x
+// only the size is asked for); returns its bytes.  The sum of A = X X^T is split
+// where a matrix has too few tiles to fill the chip: into as many ranges as make
+// at most kBlocks blocks (one more than run at once waits for all of them: 2048 x
 // 18432 in 3 ranges 89 us and 8.6 to add them up, in 4 101 and 9.7, in 7 86 and
 // 13.4), of kRange panels at least (writing and reading back a partial tile
-// takes the time of 20; with 32 at least, 2048 x 2048 takes 398 us and not 377,
-// a U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not 324).  The
-// ranges depend on the matrix alone, so that its update does not depend on the
-// others of the call.
+// takes the time of 20; with 32 at least, before X had its xl, 2048 x 2048 took 398
+// us and not 377, a U-Net's 19 matrices 635 and not 610, 1024 x 9216 318 and not
+// 324).  The ranges depend on the matrix alone, so that its update does not
+// depend on the others of the call.
 size_t lay_out(int n, const tgp_muon_tensor* const* d, char* ws, Mats& l) {
   size_t pos = 0;
   auto take = [&](size_t bytes) {
@@ -1370,10 +1371,12 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
     g128 += (long)uppers(t.mp / 128) * t.split;
   }
   // Columns of a tile of P X and X X^T.  P X on tiles of 128 x 192 takes a
-  // sixth less from the caches and LDS than on 128 x 128 (2048 x 18432: 147 us,
-  // 160; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken where
-  // its tiles make one block a CU.  Where 128 x 128 leaves CUs without one, 64 x
-  // 64.  The sums' order is the same in all of them.
+  // sixth less from the caches and LDS than on 128 x 128 (without xl 2048 x 18432:
+  // 147 us, 160; 1024 x 9216, one and a half blocks a CU: 27.9, 29.5); it is taken
+  // where its tiles make one block a CU.  (Where n is no multiple of 192 it
+  // multiplies zeros, which this does not weigh: 20 of 512 x 640 285 us, and 267
+  // in tiles of 128; 6 of 1024 x 1024 391 and 366.)  Where 128 x 128 leaves CUs
+  // without one, 64 x 64.  The sums' order is the same in all of them.
   const int ba = t192 >= 256 ? 192 : t128 >= 256 ? 128 : 64, bg = g128 >= 256 ? 128 : 64;
   auto grams = [&](const Mat& t) { return uppers(t.mp / bg) * t.split; };
   auto sums = [&](const Mat& t) { return t.split > 1 ? uppers(t.mp / bg) * (bg / 64) * (bg / 64) : 0; };
@@ -1395,7 +1398,8 @@ hipError_t update_list(Mats& l, Mats* table, float mu, bool nesterov, int steps,
   tiled(L_SYM2, [&](const Mat& t) { return t.two ? syms(t) : 0; });
   // The products of m x m matrices with up to two blocks a CU wait for their
   // stages: two panels each.  With more blocks one panel, whose ring takes half
-  // the LDS, leaves room for more of them (2048 x 18432: 1122 us, 1160 with two).
+  // the LDS, leaves room for more of them (2048 x 18432 without xl: 1122 us, 1160
+  // with two).
   auto few = [&](int launch) { return grid[launch] <= kBlocks; };
   const Mats* tb = table;
   if (wholes) {
