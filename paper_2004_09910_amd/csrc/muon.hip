@@ -761,8 +761,9 @@ enum { GRAM, POLY, MUL };
 // 408 blocks of two a CU leave some CUs one, and the clock is at 2.0 GHz.  POLY
 // and MUL in tiles of 64 x 64 (2048: 22 and 23 us, 390 TFLOP/s) wait two thirds of
 // their waves' cycles for stages and barriers, with the matrix instructions and
-// LDS at a sixth each; 528 tiles are two a CU and three on some, and tiles of 128
-// x 128 would be 136 for 256 CUs.  Under about 1024 a launch and the latencies of
+// LDS at a sixth each; 528 tiles are two a CU and three on some.  Tiles of 128 x
+// 128 would be 136 for 256 CUs: slower before the stage loop was as it is, and not
+// measured since.  Under about 1024 a launch and the latencies of
 // a tile's first and last stage are most of it (256: 5 to 6 us).
 template <int MODE, int MT, int NT, int WM, int WN, int NS, int U>
 __global__ __launch_bounds__(64 * WM * WN, 2) void muon_sym(const Mats* __restrict__ l, int launch, Each ea, int b, Each ec) {
