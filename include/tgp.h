@@ -336,8 +336,9 @@ tgp_status tgp_pipeline_step_static(tgp_net* net, const void* x, const void* tar
 tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap, int* count);
 
 /* ------------------------------------------------------------------------
- * Layer normalisation and the weights' update: what a training program does
- * between stage calls and after the last accumulation of a step.
+ * Layer normalisation, gated and residual blocks, and the weights' update: what
+ * a training program does between stage calls and after the last accumulation of
+ * a step.
  *
  * These calls keep no state of their own: tensors, statistics and workspaces
  * are the caller's, every argument check runs on the host before anything is
@@ -390,6 +391,142 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
                                    const float* stats, void* dx, int64_t lddx, float* dgain,
                                    float* dbias, int overwrite, void* ws, size_t ws_bytes,
                                    void* stream);
+
+/* A gated feed-forward block over the channels of each pixel (no value
+ * crosses a pixel, so a micro-batched run's gradients equal the full batch's):
+ *
+ *   g = x Wg^T + bg      u = x Wu^T + bu      h = act(g) u      y = h Wd^T + bd
+ *
+ * act: TGP_ACT_SILU g / (1 + exp(-g)), or TGP_ACT_GELU g (1 + erf(g / sqrt 2)) / 2.
+ * rows pixels (0 is allowed) of cin channels become cout; Wg and Wu are hidden x
+ * cin, Wd cout x hidden, dense, of the type `dtype` (1x1 convolutions' weights as
+ * tgp_bind_params takes them); biases float32 (NULL: zeros).  Consecutive rows of
+ * x and y are ldx and ldy elements apart.  Products run on bfloat16 matrix
+ * instructions with float32 sums.  TGP_BF16: h is rounded to bfloat16 before the
+ * last product, y once more.  TGP_FP32: every factor is split into three
+ * bfloat16s, of whose nine products the six largest are summed, which keeps
+ * float32's accuracy.  A factor that is infinite or NaN makes what is summed with
+ * it NaN or infinite, and nothing else.
+ *
+ * The backward starts from x and dy alone (g, u and h are computed again, with
+ * the forward's bits, as a stage's F' does):
+ *
+ *   dh = dy Wd      dg = dh u act'(g)      du = dh act(g)
+ *   dx = dg Wg + du Wu      dWg (+)= dg^T x      dWu (+)= du^T x      dWd (+)= dy^T h
+ *   dbg (+)= sum_rows dg      dbu (+)= sum_rows du      dbd (+)= sum_rows dy
+ *
+ * Gradients of the weights and biases are float32 accumulators like
+ * tgp_bind_params' (each may be NULL: not wanted; grads NULL: none): overwrite =
+ * 1 for a step's first micro-batch, 0 to add to them.  dx NULL: not wanted.  dx
+ * may be dy or x itself at the same row distance and width; y and dx may not
+ * overlap x or dy otherwise (EINVAL).  Of a TGP_BF16 network dg, du and h enter
+ * dx rounded to bfloat16, and the weights' gradients as two bfloat16s each (16
+ * bits; 3e-6 of the gradient's norm).
+ * rows = 0 leaves the accumulators as they are, or zeroes them (overwrite).
+ * Sums over rows run in an order fixed by the shape, rows and alignment.
+ *
+ * ws: device memory of at least what tgp_gated_workspace returns for the call
+ * (backward 0 or 1), at a multiple of 256 bytes; ENOSPACE if smaller.  Nothing
+ * in it needs to start at zero, and nothing is kept in it between calls.
+ * Alignment: elements of x, y, dy, dx and weights at multiples of their size,
+ * biases and gradients at 4 bytes.  Tensors of a TGP_BF16 network whose address,
+ * rows and row distances are multiples of 16 bytes are read as they are, others
+ * copied into ws first.  EINVAL for a bad shape, pointer or overlap;
+ * EUNSUPPORTED where cin, hidden or cout is over 2^20, a matrix has 2^30 values
+ * or more, or there are 2^31 rows or more. */
+typedef enum { TGP_ACT_SILU = 0, TGP_ACT_GELU = 1 } tgp_act;
+typedef struct {
+  int32_t cin, hidden, cout;
+  int32_t dtype;   /* tgp_dtype */
+  int32_t act;     /* tgp_act */
+} tgp_gated_shape;
+typedef struct {
+  const void *gate, *up, *down;
+  const float *b_gate, *b_up, *b_down;
+} tgp_gated_weights;
+typedef struct {
+  float *gate, *up, *down;
+  float *b_gate, *b_up, *b_down;
+} tgp_gated_grads;
+tgp_status tgp_gated_workspace(const tgp_gated_shape* shape, int64_t rows, int backward,
+                               size_t* bytes);
+tgp_status tgp_gated_forward(const tgp_gated_shape* shape, int64_t rows,
+                             const tgp_gated_weights* weights, const void* x, int64_t ldx, void* y,
+                             int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+tgp_status tgp_gated_backward(const tgp_gated_shape* shape, int64_t rows,
+                              const tgp_gated_weights* weights, const void* dy, int64_t lddy,
+                              const void* x, int64_t ldx, void* dx, int64_t lddx,
+                              const tgp_gated_grads* grads, int overwrite, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* What stands between two blocks of a residual stream: the norm after the one,
+ * its gate and scale, the sum, and the norm before the other, in one pass.
+ *
+ *   n = post_gain (f - mean_f) rstd_f + post_bias   (post = 1; n = f otherwise)
+ *   out = r + scale gate n
+ *   z = pre_gain (out - mean_out) rstd_out + pre_bias
+ *
+ * over rows pixels of C channels (rows = 0 is allowed), with mean and rstd as
+ * tgp_layer_norm_forward has them.  r: the stream; f: the block's output; gate:
+ * a row of C values for every `group` consecutive pixels (group = 1: every
+ * pixel; the pixels of an image: every image; rows is a multiple of group), or
+ * NULL for ones; scale, gains and biases float32 over C (NULL: ones, zeros).  z
+ * NULL: no norm follows.  r, f, gate, out and z have the type `dtype`; their rows
+ * are ld* elements apart.  z is the norm of the sum before its rounding to out.
+ * stats: rows x 4 float32 (mean_f, rstd_f, mean_out, rstd_out; zeros where there
+ * is no such norm), which the backward reads; NULL where none will run.
+ *
+ * Backward, with fhat and ohat the normalised f and out (out as stored):
+ *
+ *   G = dout + rstd_out (a - mean(a) - ohat mean(a ohat)),   a = pre_gain dz
+ *   dr = G      dn = scale gate G      dgate = sum_group scale G n
+ *   df = rstd_f (b - mean(b) - fhat mean(b fhat)),   b = post_gain dn   (or dn)
+ *   dscale (+)= sum_rows G gate n
+ *   dpost_gain (+)= sum_rows dn fhat      dpost_bias (+)= sum_rows dn
+ *   dpre_gain (+)= sum_rows dz ohat       dpre_bias (+)= sum_rows dz
+ *
+ * dz NULL: no norm follows; dout NULL: nothing but it reads the stream (not
+ * both).  dgate (rows of C values as the gate's; NULL: not wanted) is written,
+ * the sums over rows are float32 accumulators (each may be NULL; grads NULL:
+ * none; overwrite as above).  Sums over rows run in an order fixed by the shape
+ * and alignment.  They need ws, of at least the bytes that
+ * tgp_residual_norm_backward_workspace returns, at a multiple of 16 (ENOSPACE if
+ * smaller; it may be NULL where that is 0).
+ *
+ * An output may be an input itself at the same row distance (of the gates: where
+ * group = 1); any other overlap of an output with an input or output is refused
+ * (EINVAL).  An infinity or NaN in a row of r or f makes that row NaN and no
+ * other; in the backward it reaches its row of dr and df and the sums it is in.
+ * Alignment as of tgp_layer_norm_forward, stats at 16 bytes.  EUNSUPPORTED where
+ * C is over 32768. */
+typedef struct {
+  int64_t rows;
+  int64_t group;   /* pixels that share a row of the gate; not read without one */
+  int32_t C;
+  int32_t dtype;   /* tgp_dtype */
+  int32_t post;    /* 0/1 */
+  float eps;
+} tgp_residual_shape;
+typedef struct {
+  const float *scale, *post_gain, *post_bias, *pre_gain, *pre_bias;
+} tgp_residual_params;
+typedef struct {
+  float *scale, *post_gain, *post_bias, *pre_gain, *pre_bias;
+} tgp_residual_grads;
+tgp_status tgp_residual_norm_forward(const tgp_residual_shape* shape,
+                                     const tgp_residual_params* params, const void* r, int64_t ldr,
+                                     const void* f, int64_t ldf, const void* gate, int64_t ldgate,
+                                     void* out, int64_t ldout, void* z, int64_t ldz, float* stats,
+                                     void* stream);
+tgp_status tgp_residual_norm_backward_workspace(const tgp_residual_shape* shape, size_t* bytes);
+tgp_status tgp_residual_norm_backward(const tgp_residual_shape* shape,
+                                      const tgp_residual_params* params, const void* dz,
+                                      int64_t lddz, const void* dout, int64_t lddout,
+                                      const void* out, int64_t ldout, const void* f, int64_t ldf,
+                                      const void* gate, int64_t ldgate, const float* stats,
+                                      void* dr, int64_t lddr, void* df, int64_t lddf, void* dgate,
+                                      int64_t lddgate, const tgp_residual_grads* grads,
+                                      int overwrite, void* ws, size_t ws_bytes, void* stream);
 
 /* Orthogonalised updates of weight matrices (the Muon rule): for each of n
  * matrices of rows x cols float32 values (a convolution's cout x (kh kw cin),
@@ -466,6 +603,55 @@ typedef struct {
 } tgp_adamw_tensor;
 tgp_status tgp_adamw_step(int n, const tgp_adamw_tensor* t, float rate, float beta1, float beta2,
                           float eps, float decay, int64_t step, void* stream);
+
+/* AdamW with states in 8 bits, for n tensors of count values each: two bytes a
+ * value in place of eight.
+ *
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - decay) - rate (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *   w16 = bfloat16(w)
+ *
+ * from the m and v that are kept, with m and root = sqrt(v) then rounded to 8
+ * bits: a float of 4 exponent and 3 mantissa bits (OCP E4M3: sign, exponent bias
+ * 7, subnormals, 0x7f for NaN) times a power of two that each TGP_ADAMW8_BLOCK
+ * consecutive values share.  exps holds two bytes a block, for m and for root: 0
+ * where all values are zero, else e = 127 + floor(log2(largest magnitude)), 1 at
+ * least, and a code c stands for E4M3(c) 2^(e - 134).  Zeroed states are zeros.
+ * A value between two codes goes to the one or the other, in proportion, by 16
+ * bits of a hash of (seed, the tensor's place in the list, the value's index):
+ * the mean over seeds is the value itself, so that a state whose change in a step
+ * is less than a code's distance still moves.  A seed of its own for each step
+ * (say, its number) is the caller's part.  A root that is not zero stays so
+ * (the smallest code), so that no step is m / eps.  m, v and the roundings are
+ * computed in float64, the weight's step in float32.  A value whose m or v is
+ * infinite or NaN gets the NaN code and does not count for its block.
+ *
+ * With L(x) and H(x) the low and high 32 bits of a number, and all sums and
+ * products mod 2^32,
+ *
+ *   mix(x): x ^= x >> 16; x *= 0x9e3779b1; x ^= x >> 15; x *= 0xbb67ae85; x ^= x >> 16
+ *   key = mix(L(seed) ^ mix(H(seed) + mix(place + 1)))
+ *   bits = mix(L(index) ^ (key + 0x9e3779b1 H(index)))
+ *
+ * m takes the low 16 of them, root the high 16: a value at the share p of the way
+ * to the next code goes there where p + (bits + 1/2) / 2^16 >= 1.
+ *
+ * w, w16 (may be NULL), grad, m and root at multiples of 16 bytes, exps (2
+ * ceil(count / TGP_ADAMW8_BLOCK) bytes) at 2.  0 <= beta1, beta2 < 1; step counts
+ * from 1.  `t` is read on the host before the call returns. */
+#define TGP_ADAMW8_BLOCK 128
+typedef struct {
+  int64_t count;
+  float* w;
+  void* w16;
+  const float* grad;
+  uint8_t* m;
+  uint8_t* root;
+  uint8_t* exps;
+} tgp_adamw8_tensor;
+tgp_status tgp_adamw8_step(int n, const tgp_adamw8_tensor* t, float rate, double beta1,
+                           double beta2, float eps, float decay, int64_t step, uint64_t seed,
+                           void* stream);
 
 /* Measurement hooks (outside the method).  While enabled on the calling
  * thread, each kernel launch is bracketed by two HIP events on its stream.

@@ -33,6 +33,8 @@ _lib = ctypes.CDLL(LIB_PATH)
 OK, EINVAL, ESTATE, ENOSPACE, EHIP, EUNSUPPORTED = range(6)
 STATUS_NAMES = {0: "OK", 1: "EINVAL", 2: "ESTATE", 3: "ENOSPACE", 4: "EHIP", 5: "EUNSUPPORTED"}
 BF16, FP32 = 0, 1
+ACT_SILU, ACT_GELU = 0, 1
+ADAMW8_BLOCK = 128    # values of 8-bit states that share a power of two
 CKPT_ALWAYS, CKPT_EXCEPT_LAST, CKPT_NEVER = 0, 1, 2
 OP_FORWARD, OP_RECOMPUTE, OP_BACKWARD, OP_ACCUMULATE, OP_LOSS = range(5)
 
@@ -64,11 +66,45 @@ class AdamwTensor(ctypes.Structure):
                 ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p)]
 
 
+class GatedShape(ctypes.Structure):
+    _fields_ = [("cin", ctypes.c_int32), ("hidden", ctypes.c_int32), ("cout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class GatedWeights(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("gate", "up", "down", "b_gate", "b_up", "b_down")]
+
+
+class GatedGrads(ctypes.Structure):
+    _fields_ = list(GatedWeights._fields_)
+
+
+class ResidualShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("group", ctypes.c_int64), ("C", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("post", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class ResidualParams(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("scale", "post_gain", "post_bias", "pre_gain", "pre_bias")]
+
+
+class ResidualGrads(ctypes.Structure):
+    _fields_ = list(ResidualParams._fields_)
+
+
+class Adamw8Tensor(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("w", ctypes.c_void_p), ("w16", ctypes.c_void_p),
+                ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("root", ctypes.c_void_p),
+                ("exps", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _L = ctypes.c_int64
 _F = ctypes.c_float
+_D = ctypes.c_double
 _Z = ctypes.c_size_t
+_R = [_P, _L]    # a tensor's address and row distance
 _SIG = {
     "tgp_net_create": [ctypes.POINTER(Layer), _I, _I, _I, _I, _I, ctypes.POINTER(_P)],
     "tgp_layer_flops": [_P, _I, ctypes.POINTER(ctypes.c_int64)],
@@ -101,6 +137,15 @@ _SIG = {
     "tgp_muon_update": [_I, ctypes.POINTER(MuonTensor), _F, _I, _I, _F, _P, _Z, _P],
     "tgp_weight_step": [_I, ctypes.POINTER(StepTensor), _F, _P],
     "tgp_adamw_step": [_I, ctypes.POINTER(AdamwTensor), _F, _F, _F, _F, _F, _L, _P],
+    "tgp_gated_workspace": [ctypes.POINTER(GatedShape), _L, _I, ctypes.POINTER(_Z)],
+    "tgp_gated_forward": [ctypes.POINTER(GatedShape), _L, ctypes.POINTER(GatedWeights)] + 2 * _R + [_P, _Z, _P],
+    "tgp_gated_backward": [ctypes.POINTER(GatedShape), _L, ctypes.POINTER(GatedWeights)] + 3 * _R +
+                          [ctypes.POINTER(GatedGrads), _I, _P, _Z, _P],
+    "tgp_residual_norm_forward": [ctypes.POINTER(ResidualShape), ctypes.POINTER(ResidualParams)] + 5 * _R + [_P, _P],
+    "tgp_residual_norm_backward_workspace": [ctypes.POINTER(ResidualShape), ctypes.POINTER(_Z)],
+    "tgp_residual_norm_backward": [ctypes.POINTER(ResidualShape), ctypes.POINTER(ResidualParams)] + 5 * _R + [_P] +
+                                  3 * _R + [ctypes.POINTER(ResidualGrads), _I, _P, _Z, _P],
+    "tgp_adamw8_step": [_I, ctypes.POINTER(Adamw8Tensor), _F, _D, _D, _F, _F, _L, ctypes.c_uint64, _P],
     "tgp_balance_by_time": [_P, _P, ctypes.c_size_t, _I, _I, ctypes.POINTER(_I),
                             ctypes.POINTER(ctypes.c_float), _P],
 }
@@ -353,6 +398,86 @@ def layer_norm_backward(rows: int, C: int, dtype: int, dy: int, lddy: int, x: in
            "tgp_layer_norm_backward")
 
 
+def gated_shape(cin: int, hidden: int, cout: int, dtype: int, act: int) -> GatedShape:
+    """A gated block's channels, type and activation (ACT_SILU, ACT_GELU)."""
+    return GatedShape(cin, hidden, cout, dtype, act)
+
+
+def gated_weights(gate: int, up: int, down: int, b_gate: Optional[int] = None, b_up: Optional[int] = None,
+                  b_down: Optional[int] = None) -> GatedWeights:
+    """Addresses of the matrices (hidden x cin twice, cout x hidden) and float32 biases."""
+    return GatedWeights(gate, up, down, b_gate, b_up, b_down)
+
+
+def gated_grads(gate: Optional[int], up: Optional[int], down: Optional[int], b_gate: Optional[int] = None,
+                b_up: Optional[int] = None, b_down: Optional[int] = None) -> GatedGrads:
+    """Addresses of their float32 accumulators (None: not wanted)."""
+    return GatedGrads(gate, up, down, b_gate, b_up, b_down)
+
+
+def gated_workspace(shape: GatedShape, rows: int, backward: bool) -> int:
+    v = ctypes.c_size_t()
+    _check(_lib.tgp_gated_workspace(shape, rows, int(backward), ctypes.byref(v)), "tgp_gated_workspace")
+    return v.value
+
+
+def gated_forward(shape: GatedShape, rows: int, weights: GatedWeights, x: int, ldx: int, y: int, ldy: int,
+                  ws: Optional[int], ws_bytes: int, stream: int = 0) -> None:
+    """y = (act(x Wg^T + bg) * (x Wu^T + bu)) Wd^T + bd over the channels of `rows` pixels."""
+    _check(_lib.tgp_gated_forward(shape, rows, weights, x, ldx, y, ldy, ws, ws_bytes, stream), "tgp_gated_forward")
+
+
+def gated_backward(shape: GatedShape, rows: int, weights: GatedWeights, dy: int, lddy: int, x: int, ldx: int,
+                   dx: Optional[int], lddx: int, grads: Optional[GatedGrads], overwrite: bool, ws: Optional[int],
+                   ws_bytes: int, stream: int = 0) -> None:
+    """dx (None: not wanted), and the weights' gradients into (overwrite) or added to `grads`."""
+    _check(_lib.tgp_gated_backward(shape, rows, weights, dy, lddy, x, ldx, dx, lddx, grads, int(overwrite), ws,
+                                   ws_bytes, stream), "tgp_gated_backward")
+
+
+def residual_shape(rows: int, C: int, dtype: int, group: int = 0, post: bool = True, eps: float = 1e-5) -> ResidualShape:
+    """Pixels and channels of a residual stream; group: pixels that share a row of the gate; post: whether the
+    block's output is normalised."""
+    return ResidualShape(rows, group, C, dtype, int(post), eps)
+
+
+def residual_params(scale: Optional[int] = None, post_gain: Optional[int] = None, post_bias: Optional[int] = None,
+                    pre_gain: Optional[int] = None, pre_bias: Optional[int] = None) -> ResidualParams:
+    """Addresses of the float32 vectors over channels (None: ones, zeros)."""
+    return ResidualParams(scale, post_gain, post_bias, pre_gain, pre_bias)
+
+
+def residual_grads(scale: Optional[int] = None, post_gain: Optional[int] = None, post_bias: Optional[int] = None,
+                   pre_gain: Optional[int] = None, pre_bias: Optional[int] = None) -> ResidualGrads:
+    """Addresses of their float32 accumulators (None: not wanted)."""
+    return ResidualGrads(scale, post_gain, post_bias, pre_gain, pre_bias)
+
+
+def residual_norm_forward(shape: ResidualShape, params: ResidualParams, r: int, ldr: int, f: int, ldf: int,
+                          gate: Optional[int], ldgate: int, out: int, ldout: int, z: Optional[int], ldz: int,
+                          stats: Optional[int] = None, stream: int = 0) -> None:
+    """out = r + scale gate norm(f) and z = norm(out); stats (rows x 4 float32) for the backward."""
+    _check(_lib.tgp_residual_norm_forward(shape, params, r, ldr, f, ldf, gate, ldgate, out, ldout, z, ldz, stats,
+                                          stream), "tgp_residual_norm_forward")
+
+
+def residual_norm_backward_workspace(shape: ResidualShape) -> int:
+    v = ctypes.c_size_t()
+    _check(_lib.tgp_residual_norm_backward_workspace(shape, ctypes.byref(v)), "tgp_residual_norm_backward_workspace")
+    return v.value
+
+
+def residual_norm_backward(shape: ResidualShape, params: ResidualParams, dz: Optional[int], lddz: int,
+                           dout: Optional[int], lddout: int, out: Optional[int], ldout: int, f: int, ldf: int,
+                           gate: Optional[int], ldgate: int, stats: int, dr: int, lddr: int, df: int, lddf: int,
+                           dgate: Optional[int], lddgate: int, grads: Optional[ResidualGrads], overwrite: bool,
+                           ws: Optional[int], ws_bytes: int, stream: int = 0) -> None:
+    """dr, df and dgate, and the vectors' gradients into (overwrite) or added to `grads`."""
+    _check(_lib.tgp_residual_norm_backward(shape, params, dz, lddz, dout, lddout, out, ldout, f, ldf, gate, ldgate,
+                                           stats, dr, lddr, df, lddf, dgate, lddgate, grads, int(overwrite), ws,
+                                           ws_bytes, stream), "tgp_residual_norm_backward")
+
+
 def _descriptors(cls, rows):
     rows = list(rows)
     return (cls * len(rows))(*[cls(*r) for r in rows])
@@ -398,6 +523,20 @@ def adamw_step(tensors, rate: float, beta1: float, beta2: float, eps: float, dec
     """AdamW's step number `step` (from 1) for every tensor of adamw_tensors()."""
     _check(_lib.tgp_adamw_step(len(tensors), tensors, rate, beta1, beta2, eps, decay, step,
                                stream), "tgp_adamw_step")
+
+
+def adamw8_tensors(tensors: Sequence[Tuple]):
+    """The list that adamw8_step takes, of (count, w, w16 or None, grad, m, root, exps) for each tensor: m and root
+    hold a byte a value, exps two bytes for every ADAMW8_BLOCK of them."""
+    return _descriptors(Adamw8Tensor, tensors)
+
+
+def adamw8_step(tensors, rate: float, beta1: float, beta2: float, eps: float, decay: float, step: int, seed: int,
+                stream: int = 0) -> None:
+    """AdamW's step number `step` (from 1) with 8-bit states for every tensor of adamw8_tensors(); seed: of the
+    states' rounding, another for each step."""
+    _check(_lib.tgp_adamw8_step(len(tensors), tensors, rate, beta1, beta2, eps, decay, step, seed, stream),
+           "tgp_adamw8_step")
 
 
 def profile_enable(enable: bool) -> None:
