@@ -3,8 +3,8 @@
 Tolerances, fixed before the first run, as 2-norms relative to the result's.
 BF16: a stored bfloat16 is off by 2^-8 of itself at most; y has two such
 roundings (h and its own), dx two (dg or du and its own): 2 x 2^-8 plus FP32.
-The weights' gradients take dg, du and h as two bfloat16s, off by 2^-16 at
-most: 2^-16 + FP32; the biases' are float32 sums of what the factors give: FP32.
+The weights' and biases' gradients take dg, du and h as two bfloat16s, off by
+2^-16 at most: 2^-16 + FP32.
 FP32 = 5e-6: a product of three-part factors leaves out 3 x 2^-24 of a term, a
 float32 sum of K terms in random order some sqrt(K) 2^-24 (K up to 5000 here: 4e-6)
 of its terms' 2-norm, which random signs make the result's.
@@ -18,7 +18,7 @@ from gpu_util import say
 
 pytestmark = pytest.mark.gpu
 FP32 = 5e-6
-TOL = {"bf16": {"y": 2 * 2.0 ** -8 + FP32, "dx": 2 * 2.0 ** -8 + FP32, "w": 2.0 ** -16 + FP32, "b": FP32},
+TOL = {"bf16": {"y": 2 * 2.0 ** -8 + FP32, "dx": 2 * 2.0 ** -8 + FP32, "w": 2.0 ** -16 + FP32, "b": 2.0 ** -16 + FP32},
        "fp32": {"y": FP32, "dx": FP32, "w": FP32, "b": FP32}}
 DT = {"bf16": (tgp.BF16, torch.bfloat16), "fp32": (tgp.FP32, torch.float32)}
 NAMES = ("gate", "up", "down", "b_gate", "b_up", "b_down")
@@ -123,7 +123,9 @@ SHAPES = [(1, 1, 1, 1), (1, 8, 8, 8), (2, 3, 5, 7), (1, 256, 1024, 256), (5, 64,
           (17, 72, 96, 40), (31, 128, 64, 128), (32, 64, 520, 1000), (33, 40, 24, 56), (64, 64, 64, 64), (65, 65, 65, 65),
           (100, 16, 1000, 8), (127, 32, 128, 160), (128, 128, 128, 128), (129, 136, 264, 24), (144, 512, 1024, 512),
           (200, 1, 300, 1), (257, 200, 56, 72), (300, 513, 100, 257), (1000, 64, 256, 64), (1001, 24, 40, 24),
-          (2049, 128, 72, 136), (4100, 8, 16, 8), (5000, 61, 33, 45)]
+          (2049, 128, 72, 136), (4100, 8, 16, 8), (5000, 61, 33, 45),
+          (17000, 136, 264, 136), (17001, 129, 257, 100),    # large tiles, odd ends
+          (9001, 64, 2000, 72)]                              # (float32) pixels in three parts
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
