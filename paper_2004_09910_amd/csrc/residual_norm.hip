@@ -18,24 +18,11 @@
 
 #include "common.h"
 #include "prof.h"
+#include "row_regs.h"
 #include "train_ops.h"
 
 namespace tgpk {
 namespace {
-
-constexpr int kT = 256;   // threads of a block
-
-// Sum over the block's kT threads, the same value in every thread.
-template <typename F>
-__device__ __forceinline__ F block_sum(F v, F* s4) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) s4[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-  __syncthreads();
-  return v;
-}
 
 // Mean and rstd of the row in LDS.
 __device__ __forceinline__ float2 row_stats(const float* row, int C, float eps, float* s4, double* d4, float* rest) {
@@ -181,24 +168,381 @@ __global__ __launch_bounds__(kT) void res_bwd_any(const T* dz, long lddz, const 
   }
 }
 
+// ------------------------------------------------- rows held in registers
+
+// Row sums divided by C, of the values that the lane has.
+template <typename SH, bool BLK, int NV, int V>
+__device__ __forceinline__ float mean_of(const SH& sh, const float (&f)[NV][V], int C, float* s4) {
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) s += sh.has(k) ? f[k][v] : 0.f;
+  return row_sum<BLK>(s, sh.G, s4) / C;
+}
+
+// f less its mean, and the row's mean and rstd: the differences' own mean is taken
+// off them and added to the mean, as the layer norm does.
+template <typename SH, bool BLK, int NV, int V>
+__device__ __forceinline__ float2 centre(const SH& sh, float (&f)[NV][V], int C, float eps, float* s4) {
+  float mean = mean_of<SH, BLK, NV, V>(sh, f, C, s4);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[k][v] -= mean;
+  const float e = mean_of<SH, BLK, NV, V>(sh, f, C, s4);
+  float q = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      f[k][v] -= e;
+      if (sh.has(k)) q += f[k][v] * f[k][v];
+    }
+  return make_float2(mean + e, 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps));
+}
+
+template <typename VT, typename SH, typename T, int NV, int V>
+__device__ __forceinline__ void load_row(const SH& sh, const T* p, bool in, float (&f)[NV][V]) {
+  typename VT::raw raw[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (in && sh.has(k)) raw[k] = ((const typename VT::mem*)p)[sh.vec(k)];
+    else raw[k] = typename VT::raw{};
+#pragma unroll
+  for (int k = 0; k < NV; ++k) VT::un(raw[k], f[k]);
+}
+template <typename VT, typename SH, typename T, int NV, int V>
+__device__ __forceinline__ void store_row(const SH& sh, T* p, const float (&f)[NV][V]) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (sh.has(k)) ((typename VT::mem*)p)[sh.vec(k)] = (typename VT::mem)VT::pk(f[k]);
+}
+
+struct FwdArgs {
+  const void *r, *f, *gate;
+  void *out, *z;
+  long ldr, ldf, ldgate, ldout, ldz, rows;
+  unsigned group;
+  Vectors w;
+  float eps;
+  float4* stats;
+  int C, G;
+};
+
+// A row's values stay in registers from their loads to both results.
+template <typename T, int VB, int NV, bool BLK, bool POST>
+__global__ __launch_bounds__(kT) void res_fwd(FwdArgs a) {
+  typedef Vec<T, VB> VT;
+  typedef Share<T, VB, NV, BLK> SH;
+  constexpr int V = SH::V;
+  __shared__ float s4[4];
+  const SH sh(a.C, a.G, gridDim.x);
+  // scale (post_gain fhat + post_bias) as one gain and one bias
+  float pg[NV][V], pb[NV][V], ng[NV][V], nb[NV][V];
+  sh.channels(a.w.scale, 1.f, pg);
+  if constexpr (POST) {
+    float t[NV][V];
+    sh.channels(a.w.post_bias, 0.f, pb);
+    sh.channels(a.w.post_gain, 1.f, t);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        pb[k][v] *= pg[k][v];
+        pg[k][v] *= t[k][v];
+      }
+  }
+  sh.channels(a.w.pre_gain, 1.f, ng);
+  sh.channels(a.w.pre_bias, 0.f, nb);
+  // the trip count is the same for every lane of the block (block_sum meets a barrier)
+  for (long base = 0; base + sh.first() < a.rows; base += sh.step) {
+    const long p = sh.row0 + base;
+    const bool in = p < a.rows;
+    float x[NV][V], r[NV][V], q[NV][V];
+    load_row<VT>(sh, (const T*)a.f + p * a.ldf, in, x);
+    load_row<VT>(sh, (const T*)a.r + p * a.ldr, in, r);
+    if (a.gate) {
+      const long g = a.group == 1 ? p : a.rows <= 0xffffffffl ? (long)((unsigned)p / a.group) : p / a.group;
+      load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, in, q);
+    }
+    float2 st = make_float2(0.f, 0.f), so = st;
+    if constexpr (POST) st = centre<SH, BLK>(sh, x, a.C, a.eps, s4);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float n = POST ? x[k][v] * st.y * pg[k][v] + pb[k][v] : x[k][v] * pg[k][v];
+        if (a.gate) n *= q[k][v];
+        x[k][v] = r[k][v] + n;
+      }
+    if (in) store_row<VT>(sh, (T*)a.out + p * a.ldout, x);
+    if (a.z) {
+      so = centre<SH, BLK>(sh, x, a.C, a.eps, s4);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[k][v] = x[k][v] * so.y * ng[k][v] + nb[k][v];
+      if (in) store_row<VT>(sh, (T*)a.z + p * a.ldz, x);
+    }
+    if (in && a.stats && sh.l == 0) a.stats[p] = make_float4(st.x, st.y, so.x, so.y);
+  }
+}
+
+// Which pixels a block takes.  Ranges: `ranges` blocks for each of the groups of
+// pixels that share a gate (one group of all pixels where none do), `per` pixels
+// each.  Whole: whole groups by a wave (a block, where a row is a block's), side
+// by side in parts of `part` lanes' rows (a power of two) where they are small.
+struct BwdArgs {
+  const void *dz, *dout, *out, *f, *gate;
+  void *dr, *df, *dgate;
+  long lddz, lddout, ldout, ldf, ldgate, lddr, lddf, lddgate, rows, group, per;
+  Vectors w;
+  const float4* stats;
+  float* part;   // [block][4][C]: dz ohat, dz, S1, S2 (ranges of a shared gate: U1, U2)
+  int C, G, ranges, slots;
+  int shared;    // a gate for several pixels
+};
+
+template <typename T, int VB, int NV, bool BLK, bool POST, bool WHOLE>
+__global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
+  typedef Vec<T, VB> VT;
+  typedef Share<T, VB, NV, BLK> SH;
+  constexpr int V = SH::V;
+  __shared__ float s4[4];
+  const SH sh(a.C, a.G, gridDim.x);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rpw = BLK ? 1 : 64 / sh.G, rl = BLK ? 0 : lane / sh.G;   // rows of a wave, this lane's
+  float pg[NV][V], pb[NV][V], ng[NV][V];   // scale post_gain, scale post_bias, pre_gain
+  sh.channels(a.w.scale, 1.f, pg);
+  if constexpr (POST) {
+    float t[NV][V];
+    sh.channels(a.w.post_bias, 0.f, pb);
+    sh.channels(a.w.post_gain, 1.f, t);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        pb[k][v] *= pg[k][v];
+        pg[k][v] *= t[k][v];
+      }
+  }
+  sh.channels(a.w.pre_gain, 1.f, ng);
+  float sum[4][NV][V];
+#pragma unroll
+  for (int z = 0; z < 4; ++z)
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum[z][k][v] = 0.f;
+  const float inv_c = 1.f / a.C;
+  float q[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) q[k][v] = 1.f;
+
+  // one row's gradients; u1 and u2 take G fhat and G
+  auto row = [&](long p, bool in, float (&u1)[NV][V], float (&u2)[NV][V]) __attribute__((always_inline)) {
+    float G[NV][V], x[NV][V];
+    const float4 st = in ? a.stats[p] : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.dout) load_row<VT>(sh, (const T*)a.dout + p * a.lddout, in, G);
+    load_row<VT>(sh, (const T*)a.f + p * a.ldf, in, x);
+    if (a.gate && !a.shared) load_row<VT>(sh, (const T*)a.gate + p * a.ldgate, in, q);
+    if (a.dz) {
+      float d[NV][V], o[NV][V], s = 0.f, t = 0.f;
+      load_row<VT>(sh, (const T*)a.dz + p * a.lddz, in, d);
+      load_row<VT>(sh, (const T*)a.out + p * a.ldout, in, o);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          o[k][v] = (o[k][v] - st.z) * st.w;
+          sum[0][k][v] += d[k][v] * o[k][v];
+          sum[1][k][v] += d[k][v];
+          d[k][v] *= ng[k][v];
+          if (sh.has(k)) {
+            s += d[k][v];
+            t += d[k][v] * o[k][v];
+          }
+        }
+      s = row_sum<BLK>(s, sh.G, s4) * inv_c;
+      t = row_sum<BLK>(t, sh.G, s4) * inv_c;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float n = st.w * (d[k][v] - s - o[k][v] * t);
+          G[k][v] = a.dout ? G[k][v] + n : n;
+        }
+    }
+    float b[NV][V], s = 0.f, t = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if constexpr (POST) x[k][v] = (x[k][v] - st.x) * st.y;
+        const float g = a.shared ? G[k][v] : G[k][v] * q[k][v];
+        u1[k][v] += g * x[k][v];
+        u2[k][v] += g;
+        b[k][v] = G[k][v] * q[k][v] * pg[k][v];
+        if (POST && sh.has(k)) {
+          s += b[k][v];
+          t += b[k][v] * x[k][v];
+        }
+      }
+    if constexpr (POST) {
+      s = row_sum<BLK>(s, sh.G, s4) * inv_c;
+      t = row_sum<BLK>(t, sh.G, s4) * inv_c;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[k][v] = st.y * (b[k][v] - s - x[k][v] * t);
+    }
+    if (!in) return;
+    store_row<VT>(sh, (T*)a.dr + p * a.lddr, G);
+    store_row<VT>(sh, (T*)a.df + p * a.lddf, b);
+    if (a.dgate && !a.shared) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) G[k][v] *= POST ? x[k][v] * pg[k][v] + pb[k][v] : x[k][v] * pg[k][v];
+      store_row<VT>(sh, (T*)a.dgate + p * a.lddgate, G);
+    }
+  };
+
+  // trip counts are the same for every lane of a block whose rows are the block's
+  if constexpr (!WHOLE) {
+    const long g = blockIdx.x / (unsigned)a.ranges;
+    const long lo = g * a.group + (blockIdx.x - g * a.ranges) * a.per, hi = min(lo + a.per, (g + 1) * a.group);
+    if (a.shared) load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, true, q);
+    const int turn = BLK ? 1 : 4 * rpw;
+    for (long p0 = lo; p0 < hi; p0 += turn) {
+      const long p = p0 + (BLK ? 0 : wave * rpw + rl);
+      row(p, p < hi, sum[2], sum[3]);
+    }
+  } else {
+    const int part = rpw / a.slots, slot = rl / part, first = rl - slot * part;
+    const long groups = a.rows / a.group, step = (long)gridDim.x * (BLK ? 1 : 4 * a.slots);
+    for (long g0 = BLK ? blockIdx.x : ((long)blockIdx.x * 4 + wave) * a.slots; g0 < groups; g0 += step) {
+      const long g = g0 + slot;
+      const bool there = g < groups;
+      float u1[NV][V], u2[NV][V];
+      load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, there, q);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) u1[k][v] = u2[k][v] = 0.f;
+      for (long t = 0; t < a.group; t += part) row(g * a.group + t + first, there && t + first < a.group, u1, u2);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if constexpr (!BLK)
+            for (int o = sh.G; o < sh.G * part; o <<= 1) {
+              u1[k][v] += __shfl_xor(u1[k][v], o);
+              u2[k][v] += __shfl_xor(u2[k][v], o);
+            }
+          // every lane of the group has the sums: the first row's takes them on
+          sum[2][k][v] += first ? 0.f : q[k][v] * u1[k][v];
+          sum[3][k][v] += first ? 0.f : q[k][v] * u2[k][v];
+          u1[k][v] = POST ? pg[k][v] * u1[k][v] + pb[k][v] * u2[k][v] : pg[k][v] * u1[k][v];
+        }
+      if (a.dgate && there && first == 0) store_row<VT>(sh, (T*)a.dgate + g * a.lddgate, u1);
+    }
+  }
+  if (!a.part) return;
+  float* to = a.part + (long)blockIdx.x * 4 * a.C;
+  if constexpr (BLK) {
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (sh.has(k))
+#pragma unroll
+          for (int v = 0; v < V; ++v) to[(long)z * a.C + sh.vec(k) * V + v] = sum[z][k][v];
+  } else {
+    // the wave's rows, then the four waves' sums in order
+    __shared__ float ws[3][NV * V][64];
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      if (z) __syncthreads();
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          for (int o = sh.G; o < 64; o <<= 1) sum[z][k][v] += __shfl_xor(sum[z][k][v], o);
+          if (wave > 0) ws[wave - 1][k * V + v][lane] = sum[z][k][v];
+        }
+      __syncthreads();
+      if (wave == 0 && lane < sh.G)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (sh.has(k))
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              const int e = k * V + v;
+              to[(long)z * a.C + sh.vec(k) * V + v] = ((sum[z][k][v] + ws[0][e][lane]) + ws[1][e][lane]) + ws[2][e][lane];
+            }
+    }
+  }
+}
+
+// The gates' gradients from the ranges' partial sums, and S1 and S2 of each gate in
+// the place of U1 and U2 of its first range: 64 channels of a gate a block.
+template <typename T>
+__global__ __launch_bounds__(kT) void res_join(float* part, int ranges, const T* gate, long ldgate, Vectors w, int post,
+                                               T* dgate, long lddgate, int C) {
+  __shared__ float sh[3][4][64];
+  const int l = threadIdx.x & 63, k = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
+  float* at = part + (long)blockIdx.y * ranges * 4 * C + c;
+  float s[4] = {};
+  if (c < C)
+#pragma unroll 4
+    for (int b = k; b < ranges; b += 4)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) s[z] += at[((long)b * 4 + z) * C];
+  if (k)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) sh[k - 1][z][l] = s[z];
+  __syncthreads();
+  if (k || c >= C) return;
+#pragma unroll
+  for (int z = 0; z < 4; ++z) s[z] = ((s[z] + sh[0][z][l]) + sh[1][z][l]) + sh[2][z][l];
+  const float g = Elt<T>::ld(gate + blockIdx.y * ldgate + c);
+  at[0] = s[0];
+  at[C] = s[1];
+  at[2L * C] = g * s[2];
+  at[3L * C] = g * s[3];
+  if (!dgate) return;
+  const float n = post ? at_or(w.post_gain, c, 1.f) * s[2] + at_or(w.post_bias, c, 0.f) * s[3] : s[2];
+  Elt<T>::st(dgate + blockIdx.y * lddgate + c, at_or(w.scale, c, 1.f) * n);
+}
+
 // The vectors' gradients from the partial sums of S blocks, `stride` sums of C a
-// block: sixteen columns a block, sixteen threads a column.
-__global__ __launch_bounds__(256) void res_sums(const float* part, int S, int stride, Vectors w, int post,
-                                                tgp_residual_grads g, int overwrite, int C) {
-  __shared__ float sh[4][16][17];
+// block: sixteen columns a block, 64 threads a column.
+__global__ __launch_bounds__(1024) void res_sums(const float* part, int S, int stride, Vectors w, int post,
+                                                 tgp_residual_grads g, int overwrite, int C) {
+  __shared__ float sh[4][64][17];
   const int l = threadIdx.x & 15, k = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
   float s[4] = {};
   if (c < C)
-    for (int b = k; b < S; b += 16)
+#pragma unroll 4
+    for (int b = k; b < S; b += 64)
 #pragma unroll
       for (int z = 0; z < 4; ++z) s[z] += part[((long)b * stride + z) * C + c];
 #pragma unroll
   for (int z = 0; z < 4; ++z) sh[z][k][l] = s[z];
   __syncthreads();
+  for (int o = 32; o > 0; o >>= 1) {
+    if (k < o)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) sh[z][k][l] += sh[z][k + o][l];
+    __syncthreads();
+  }
   if (k || c >= C) return;
 #pragma unroll
-  for (int z = 0; z < 4; ++z)
-    for (int i = 1; i < 16; ++i) s[z] += sh[z][i][l];
+  for (int z = 0; z < 4; ++z) s[z] = sh[z][0][l];
   auto put = [&](float* p, float v) {
     if (p) p[c] = overwrite ? v : p[c] + v;
   };
@@ -210,44 +554,177 @@ __global__ __launch_bounds__(256) void res_sums(const float* part, int S, int st
   put(g.scale, post ? at_or(w.post_gain, c, 1.f) * s[2] + at_or(w.post_bias, c, 0.f) * s[3] : s[2]);
 }
 
+// ------------------------------------------------- plans
+
 Vectors vectors(const tgp_residual_params& p) {
   return {p.scale, p.post_gain, p.post_bias, p.pre_gain, p.pre_bias};
 }
 
+constexpr int kFwdBlocks = 2048;   // most blocks of a forward launch
+constexpr int kBlocks = 1024;      // most ranges of a backward one
 constexpr int kAnyBlocks = 512;
 
 bool any_sum(const tgp_residual_grads& g) {
   return g.scale || g.post_gain || g.post_bias || g.pre_gain || g.pre_bias;
 }
 
+// How registers hold a row: vb bytes an access, nv of them a lane, g lanes a row (0:
+// the block); vb = 0: not at all.
+struct Plan {
+  int vb, nv, g;
+};
+
+// The widest accesses that every row's start and length allow, at most `most` values a
+// lane; then the lanes that leave fewest idle, more lanes where two leave the same.
+Plan plan_of(int esz, int C, uintptr_t bits, int most) {
+  bits |= (uintptr_t)C * esz;
+  const int vb = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2, nvec = C * esz / vb, top = most * esz / vb;
+  Plan best{vb, 0, 64};
+  int room = 1 << 30;
+  for (int g = 64; g >= 1; g >>= 1) {
+    const int nv = cdiv(nvec, g);
+    if (nv > std::min(4, top)) break;
+    if (nv * g < room) room = nv * g, best = {vb, nv, g};
+  }
+  if (best.nv) return best;
+  const int nv = cdiv(nvec, kT);
+  if (nv > top) return {0, 0, 0};
+  return {vb, nv <= 4 ? nv : nv <= 8 ? 8 : 16, 0};
+}
+
+// Calls f(VB, NV, BLK as constants); MOST: values a lane.
+template <int ESZ, int MOST, typename F>
+void with_plan(const Plan& p, F f) {
+  auto nv = [&](auto vb, auto blk) {
+    constexpr int TOP = MOST * ESZ / decltype(vb)::value;
+    constexpr bool BLK = decltype(blk)::value;
+    auto go = [&](auto n) {
+      if constexpr (decltype(n)::value <= TOP && (BLK || decltype(n)::value <= 4)) f(vb, n, blk);
+    };
+    switch (p.nv) {
+      case 1: return go(std::integral_constant<int, 1>());
+      case 2: return go(std::integral_constant<int, 2>());
+      case 3: return go(std::integral_constant<int, 3>());
+      case 4: return go(std::integral_constant<int, 4>());
+      case 8: return go(std::integral_constant<int, 8>());
+      default: return go(std::integral_constant<int, 16>());
+    }
+  };
+  auto vec = [&](auto blk) {
+    if (p.vb == 16) nv(std::integral_constant<int, 16>(), blk);
+    else if (p.vb == 4) nv(std::integral_constant<int, 4>(), blk);
+    else if constexpr (ESZ == 2) nv(std::integral_constant<int, 2>(), blk);
+  };
+  if (p.g) vec(std::false_type());
+  else vec(std::true_type());
+}
+
+// f(whether there is a post norm, as a constant)
+template <typename F>
+void with_post(int post, F f) {
+  if (post) f(std::true_type());
+  else f(std::false_type());
+}
+
+// The bits of a tensor's address and row distance that the widest access has to divide.
+template <typename T>
+uintptr_t place(const Rows& r) { return r.p ? (uintptr_t)r.p | (uintptr_t)r.ld * sizeof(T) : 0; }
+
+constexpr int kFwdValues = 32, kBwdValues = 16;   // of a row, a lane
+
 template <typename T>
 hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
   const double n = (double)a.s.rows * a.s.C;
-  ProfScope ps("residual_norm_fwd_any", 20 * n, 4 * n * sizeof(T), st);
-  TGP_LAUNCH(ps, res_fwd_any<T>, dim3((unsigned)std::min<long>(a.s.rows, 2048)), dim3(kT),
-             a.s.C * sizeof(float), st, (const T*)a.r.p, a.r.ld, (const T*)a.f.p, a.f.ld, (const T*)a.gate.p,
-             a.gate.ld, (long)a.s.group, vectors(a.w), a.s.eps, a.s.post, (T*)a.out.p, a.out.ld, (T*)a.z.p, a.z.ld,
-             (float4*)a.stats, (long)a.s.rows, a.s.C);
+  const Plan p = plan_of(sizeof(T), a.s.C, place<T>(a.r) | place<T>(a.f) | place<T>(a.gate) | place<T>(a.out) | place<T>(a.z),
+                         kFwdValues);
+  if (!p.vb || (a.gate.p && a.s.group > 0x7fffffff)) {
+    ProfScope ps("residual_norm_fwd_any", 20 * n, 4 * n * sizeof(T), st);
+    TGP_LAUNCH(ps, res_fwd_any<T>, dim3((unsigned)std::min<long>(a.s.rows, 2048)), dim3(kT),
+               a.s.C * sizeof(float), st, (const T*)a.r.p, a.r.ld, (const T*)a.f.p, a.f.ld, (const T*)a.gate.p,
+               a.gate.ld, (long)a.s.group, vectors(a.w), a.s.eps, a.s.post, (T*)a.out.p, a.out.ld, (T*)a.z.p, a.z.ld,
+               (float4*)a.stats, (long)a.s.rows, a.s.C);
+    return launch_status();
+  }
+  const FwdArgs k{a.r.p, a.f.p, a.gate.p, a.out.p, a.z.p, a.r.ld, a.f.ld, a.gate.ld, a.out.ld, a.z.ld, (long)a.s.rows,
+                  (unsigned)a.s.group, vectors(a.w), a.s.eps, (float4*)a.stats, a.s.C, p.g};
+  const unsigned grid = even_grid(a.s.rows, p.g == 0 ? 1 : 4 * (64 / p.g), kFwdBlocks);
+  with_post(a.s.post, [&](auto post) {
+    with_plan<sizeof(T), kFwdValues>(p, [&](auto vb, auto nv, auto blk) {
+      constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
+      constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
+      ProfScope ps("residual_norm_fwd", 20 * n, (a.z.p ? 4 : 3) * n * sizeof(T), st);
+      TGP_LAUNCH(ps, (res_fwd<T, VB, NV, BLK, POST>), dim3(grid), dim3(kT), 0, st, k);
+    });
+  });
   return launch_status();
 }
 
 template <typename T>
 hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   const double n = (double)a.s.rows * a.s.C;
-  const long group = a.gate.p ? (long)a.s.group : 1;
-  const int S = (int)std::min<long>(kAnyBlocks, a.s.rows / group);
-  {
-    ProfScope ps("residual_norm_bwd_any", 40 * n, 6 * n * sizeof(T), st);
-    TGP_LAUNCH(ps, res_bwd_any<T>, dim3(S), dim3(kT), a.s.C * sizeof(float), st, (const T*)a.dz.p, a.dz.ld,
-               (const T*)a.dout.p, a.dout.ld, (const T*)a.out.p, a.out.ld, (const T*)a.f.p, a.f.ld,
-               (const T*)a.gate.p, a.gate.ld, group, vectors(a.w), a.s.post, (const float4*)a.stats, (T*)a.dr.p,
-               a.dr.ld, (T*)a.df.p, a.df.ld, (T*)a.dgate.p, a.dgate.ld, a.part, (long)a.s.rows, a.s.C);
-  }
-  if (any_sum(a.g)) {
+  const long rows = a.s.rows, group = a.gate.p ? (long)a.s.group : 1;
+  const bool sums = any_sum(a.g), shared = group > 1;
+  const Plan p = plan_of(sizeof(T), a.s.C,
+                         place<T>(a.dz) | place<T>(a.dout) | (a.dz.p ? place<T>(a.out) : 0) | place<T>(a.f) | place<T>(a.gate) |
+                             place<T>(a.dr) | place<T>(a.df) | place<T>(a.dgate),
+                         kBwdValues);
+  auto add_up = [&](int S, int stride) {
     ProfScope ps("residual_norm_sums", 4.0 * S * a.s.C, 16.0 * S * a.s.C, st);
-    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(256), 0, st, a.part, S, 6, vectors(a.w), a.s.post, a.g,
+    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(1024), 0, st, a.part, S, stride, vectors(a.w), a.s.post, a.g,
                (int)a.overwrite, a.s.C);
+  };
+  if (!p.vb) {
+    const int S = (int)std::min<long>(kAnyBlocks, rows / group);
+    {
+      ProfScope ps("residual_norm_bwd_any", 40 * n, 6 * n * sizeof(T), st);
+      TGP_LAUNCH(ps, res_bwd_any<T>, dim3(S), dim3(kT), a.s.C * sizeof(float), st, (const T*)a.dz.p, a.dz.ld,
+                 (const T*)a.dout.p, a.dout.ld, (const T*)a.out.p, a.out.ld, (const T*)a.f.p, a.f.ld,
+                 (const T*)a.gate.p, a.gate.ld, group, vectors(a.w), a.s.post, (const float4*)a.stats, (T*)a.dr.p,
+                 a.dr.ld, (T*)a.df.p, a.df.ld, (T*)a.dgate.p, a.dgate.ld, a.part, rows, a.s.C);
+    }
+    if (sums) add_up(S, 6);
+    return launch_status();
   }
+  BwdArgs k{a.dz.p, a.dout.p, a.out.p, a.f.p, a.gate.p, a.dr.p, a.df.p, a.dgate.p, a.dz.ld, a.dout.ld, a.out.ld, a.f.ld,
+            a.gate.ld, a.dr.ld, a.df.ld, a.dgate.ld, rows, shared ? group : rows, 0, vectors(a.w), (const float4*)a.stats,
+            nullptr, a.s.C, p.g, 1, 1, shared};
+  const int rpw = p.g ? 64 / p.g : 1, turn = p.g ? 4 * rpw : 1;
+  const long groups = rows / k.group;
+  // blocks that fill the chip, of 24 rows where there are many (each leaves 16 bytes a channel)
+  const long most = std::min<long>(kBlocks, std::max<long>(256, rows / 24));
+  // whole groups where a wave (block) each fills the chip, or takes one in one turn
+  const bool whole = shared && (groups >= (p.g ? 1024 : 512) || k.group <= rpw);
+  unsigned grid;
+  if (whole) {
+    int part = 1;
+    while (part < k.group && part < rpw) part <<= 1;
+    k.slots = rpw / part;
+    grid = even_grid(groups, p.g ? 4 * k.slots : 1, most);
+  } else {
+    const long want = std::max<long>(1, most / groups);
+    k.per = (k.group + want - 1) / want;
+    k.per = (k.per + turn - 1) / turn * turn;
+    k.ranges = (int)((k.group + k.per - 1) / k.per);
+    grid = (unsigned)(groups * k.ranges);
+  }
+  const bool join = shared && !whole && (sums || a.dgate.p);
+  if (sums || join) k.part = a.part;
+  with_post(a.s.post, [&](auto post) {
+    with_plan<sizeof(T), kBwdValues>(p, [&](auto vb, auto nv, auto blk) {
+      constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
+      constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
+      ProfScope ps("residual_norm_bwd", 40 * n, (3 + (a.dout.p ? 1 : 0) + (a.dz.p ? 2 : 0)) * n * sizeof(T), st);
+      if (whole) TGP_LAUNCH(ps, (res_bwd<T, VB, NV, BLK, POST, true>), dim3(grid), dim3(kT), 0, st, k);
+      else TGP_LAUNCH(ps, (res_bwd<T, VB, NV, BLK, POST, false>), dim3(grid), dim3(kT), 0, st, k);
+    });
+  });
+  if (join) {
+    ProfScope ps("residual_norm_gates", 4.0 * grid * a.s.C, 16.0 * grid * a.s.C, st);
+    TGP_LAUNCH(ps, res_join<T>, dim3(cdiv(a.s.C, 64), (unsigned)groups), dim3(kT), 0, st, a.part, k.ranges,
+               (const T*)a.gate.p, a.gate.ld, vectors(a.w), a.s.post, (T*)a.dgate.p, a.dgate.ld, a.s.C);
+  }
+  if (sums && join) add_up((int)groups, 4 * k.ranges);
+  else if (sums) add_up((int)grid, 4);
   return launch_status();
 }
 
@@ -258,14 +735,14 @@ hipError_t residual_norm_forward(const ResidualForward& a, hipStream_t st) {
 }
 
 size_t residual_norm_partial_floats(const tgp_residual_shape& s) {
-  return 6 * (size_t)std::min<long>(kAnyBlocks, s.rows) * s.C;
+  return (size_t)std::max<long>(6 * std::min<long>(kAnyBlocks, s.rows), 4 * std::min<long>(kBlocks, s.rows)) * s.C;
 }
 
 hipError_t residual_norm_backward(const ResidualBackward& a, hipStream_t st) {
   if (a.s.rows == 0) {
     if (!any_sum(a.g) || !a.overwrite) return hipSuccess;
     ProfScope ps("residual_norm_zero", 0, 20.0 * a.s.C, st);
-    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(256), 0, st, nullptr, 0, 4, Vectors{}, 0, a.g, 1, a.s.C);
+    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(1024), 0, st, nullptr, 0, 4, Vectors{}, 0, a.g, 1, a.s.C);
     return launch_status();
   }
   return a.s.dtype == TGP_BF16 ? backward_t<bf16_t>(a, st) : backward_t<float>(a, st);
