@@ -16,6 +16,13 @@ __device__ __forceinline__ uint32_t f2bf(float f) {
   return u >> 16;
 }
 
+// Two floats rounded to bfloat16, as one word (the same rounding, by one instruction).
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+
 // Element traits: load as float, store from float (rounded for bf16).
 template <typename T> struct Elt;
 template <> struct Elt<float> {

@@ -275,12 +275,5 @@ __device__ __forceinline__ void put8(const unsigned (&pk)[8], F put) {
   }
 }
 
-// Two floats rounded to bfloat16, as one word.
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
-  return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
-}
-
 }  // namespace
 }  // namespace tgpk

@@ -14,6 +14,7 @@
 // gate the same two sums without the gate, U1 and U2, give its gradient, scale
 // (post_gain U1 + post_bias U2), and S1 and S2 are gate U1 and gate U2 added up.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "common.h"
@@ -202,21 +203,54 @@ __device__ __forceinline__ float2 centre(const SH& sh, float (&f)[NV][V], int C,
   return make_float2(mean + e, 1.f / sqrtf(row_sum<BLK>(q, sh.G, s4) / C + eps));
 }
 
+// One tensor's rows for a lane: those of a turn start at an address that is the same
+// for the wave, from which the lane's row is `off` bytes away.  (64-bit addresses a
+// lane and tensor cost registers, and the waves that hide memory's latency.)
+template <typename T>
+struct Lanes {
+  char* p;
+  long ld;        // bytes
+  unsigned off;
+  __device__ __forceinline__ Lanes(const void* t, long l, int row) : p((char*)t), ld(l * (long)sizeof(T)) {
+    off = (unsigned)(row * ld);
+  }
+  __device__ __forceinline__ char* at(long row) const { return p + row * ld; }   // of the wave
+};
+
+// A lane's part of a row as it is in memory.  All loads of a row go out before the
+// first value is looked at.
+template <typename VT, int NV>
+struct Raw {
+  typename VT::raw r[NV];
+  __device__ __forceinline__ void none() {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) r[k] = typename VT::raw{};
+  }
+  __device__ __forceinline__ void load(const char* p, unsigned off, int k) { r[k] = *(const typename VT::mem*)(p + off); }
+  template <int V>
+  __device__ __forceinline__ void to(float (&f)[NV][V]) const {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) VT::un(r[k], f[k]);
+  }
+};
+// ov: byte offsets of the lane's vectors in a row.
 template <typename VT, typename SH, typename T, int NV, int V>
-__device__ __forceinline__ void load_row(const SH& sh, const T* p, bool in, float (&f)[NV][V]) {
-  typename VT::raw raw[NV];
+__device__ __forceinline__ void store_row(const SH& sh, char* p, unsigned off, const unsigned (&ov)[NV],
+                                          const float (&f)[NV][V]) {
 #pragma unroll
   for (int k = 0; k < NV; ++k)
-    if (in && sh.has(k)) raw[k] = ((const typename VT::mem*)p)[sh.vec(k)];
-    else raw[k] = typename VT::raw{};
-#pragma unroll
-  for (int k = 0; k < NV; ++k) VT::un(raw[k], f[k]);
-}
-template <typename VT, typename SH, typename T, int NV, int V>
-__device__ __forceinline__ void store_row(const SH& sh, T* p, const float (&f)[NV][V]) {
-#pragma unroll
-  for (int k = 0; k < NV; ++k)
-    if (sh.has(k)) ((typename VT::mem*)p)[sh.vec(k)] = (typename VT::mem)VT::pk(f[k]);
+    if (sh.has(k)) {
+      char* q = p + (off + ov[k]);
+      if constexpr (sizeof(T) == 2 && V == 8)
+        *(uint4*)q = make_uint4(pack_bf16(f[k][0], f[k][1]), pack_bf16(f[k][2], f[k][3]),
+                                pack_bf16(f[k][4], f[k][5]), pack_bf16(f[k][6], f[k][7]));
+      else if constexpr (sizeof(T) == 2 && V == 4)
+        *(uint2*)q = make_uint2(pack_bf16(f[k][0], f[k][1]), pack_bf16(f[k][2], f[k][3]));
+      else if constexpr (sizeof(T) == 2 && V == 2)
+        *(uint32_t*)q = pack_bf16(f[k][0], f[k][1]);
+      else
+        *(typename VT::mem*)q = (typename VT::mem)VT::pk(f[k]);
+    }
 }
 
 struct FwdArgs {
@@ -255,17 +289,37 @@ __global__ __launch_bounds__(kT) void res_fwd(FwdArgs a) {
   }
   sh.channels(a.w.pre_gain, 1.f, ng);
   sh.channels(a.w.pre_bias, 0.f, nb);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rpw = BLK ? 1 : 64 / sh.G, rl = BLK ? 0 : (threadIdx.x & 63) / sh.G;   // rows of a wave, this lane's
+  const Lanes<T> f(a.f, a.ldf, rl), rs(a.r, a.ldr, rl), out(a.out, a.ldout, rl), z(a.z, a.ldz, rl);
+  unsigned ov[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) ov[k] = sh.vec(k) * VB;
   // the trip count is the same for every lane of the block (block_sum meets a barrier)
-  for (long base = 0; base + sh.first() < a.rows; base += sh.step) {
-    const long p = sh.row0 + base;
+  for (long base = BLK ? blockIdx.x : (long)blockIdx.x * 4 * rpw; base < a.rows; base += sh.step) {
+    const long p0 = base + (BLK ? 0 : wave * rpw), p = p0 + rl;   // the wave's first row, the lane's
     const bool in = p < a.rows;
     float x[NV][V], r[NV][V], q[NV][V];
-    load_row<VT>(sh, (const T*)a.f + p * a.ldf, in, x);
-    load_row<VT>(sh, (const T*)a.r + p * a.ldr, in, r);
-    if (a.gate) {
-      const long g = a.group == 1 ? p : a.rows <= 0xffffffffl ? (long)((unsigned)p / a.group) : p / a.group;
-      load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, in, q);
+    Raw<VT, NV> rx, rr, rq;
+    rx.none();
+    rr.none();
+    rq.none();
+    if (in) {
+      const char *fp = f.at(p0), *rp = rs.at(p0);
+      long g = p;
+      if (a.group > 1) g = a.rows <= 0xffffffffl ? (long)((unsigned)p / a.group) : p / a.group;
+      const char* gp = (const char*)a.gate + g * a.ldgate * (long)sizeof(T);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (sh.has(k)) {
+          rx.load(fp, f.off + ov[k], k);
+          rr.load(rp, rs.off + ov[k], k);
+          if (a.gate) rq.load(gp, ov[k], k);
+        }
     }
+    rx.to(x);
+    rr.to(r);
+    rq.to(q);
     float2 st = make_float2(0.f, 0.f), so = st;
     if constexpr (POST) st = centre<SH, BLK>(sh, x, a.C, a.eps, s4);
 #pragma unroll
@@ -276,14 +330,14 @@ __global__ __launch_bounds__(kT) void res_fwd(FwdArgs a) {
         if (a.gate) n *= q[k][v];
         x[k][v] = r[k][v] + n;
       }
-    if (in) store_row<VT>(sh, (T*)a.out + p * a.ldout, x);
+    if (in) store_row<VT, SH, T>(sh, out.at(p0), out.off, ov, x);
     if (a.z) {
       so = centre<SH, BLK>(sh, x, a.C, a.eps, s4);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) x[k][v] = x[k][v] * so.y * ng[k][v] + nb[k][v];
-      if (in) store_row<VT>(sh, (T*)a.z + p * a.ldz, x);
+      if (in) store_row<VT, SH, T>(sh, z.at(p0), z.off, ov, x);
     }
     if (in && a.stats && sh.l == 0) a.stats[p] = make_float4(st.x, st.y, so.x, so.y);
   }
@@ -309,11 +363,21 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
   typedef Vec<T, VB> VT;
   typedef Share<T, VB, NV, BLK> SH;
   constexpr int V = SH::V;
-  __shared__ float s4[4];
+  __shared__ float s8[2][4];
   const SH sh(a.C, a.G, gridDim.x);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rpw = BLK ? 1 : 64 / sh.G, rl = BLK ? 0 : lane / sh.G;   // rows of a wave, this lane's
-  float pg[NV][V], pb[NV][V], ng[NV][V];   // scale post_gain, scale post_bias, pre_gain
+  // (whole groups) rows of a part of the lanes, the lane's part and row in it
+  const int side = WHOLE ? rpw / a.slots : rpw, slot = rl / side, first = rl - slot * side;
+  const int lr = WHOLE ? (int)(slot * a.group) + first : rl;   // the lane's row from the wave's first
+  const Lanes<T> tz(a.dz, a.lddz, lr), to_(a.out, a.ldout, lr), td(a.dout, a.lddout, lr), tf(a.f, a.ldf, lr),
+      tg(a.gate, a.ldgate, lr), tr(a.dr, a.lddr, lr), tdf(a.df, a.lddf, lr), tdg(a.dgate, a.lddgate, lr);
+  unsigned ov[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) ov[k] = sh.vec(k) * VB;
+  // scale post_gain, scale post_bias, pre_gain; the first zero where the lane has no
+  // channel, so that nothing of such a lane gets into a row's sums
+  float pg[NV][V], pb[NV][V], ng[NV][V];
   sh.channels(a.w.scale, 1.f, pg);
   if constexpr (POST) {
     float t[NV][V];
@@ -324,7 +388,7 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         pb[k][v] *= pg[k][v];
-        pg[k][v] *= t[k][v];
+        pg[k][v] = sh.has(k) ? pg[k][v] * t[k][v] : 0.f;
       }
   }
   sh.channels(a.w.pre_gain, 1.f, ng);
@@ -342,17 +406,44 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) q[k][v] = 1.f;
 
+  // what a row's gradients need of memory; p: the wave's first row
+  struct Row {
+    float4 st;
+    Raw<VT, NV> g, x, q, d, o;
+  };
+  auto fetch = [&](long p, bool in, Row& m) __attribute__((always_inline)) {
+    m.st = make_float4(0.f, 0.f, 0.f, 0.f);
+    m.g.none();
+    m.x.none();
+    m.q.none();
+    m.d.none();
+    m.o.none();
+    if (!in) return;
+    m.st = (a.stats + p)[lr];
+    const char *pz = tz.at(p), *po = to_.at(p), *pd = td.at(p), *pf = tf.at(p), *pg = tg.at(p);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (sh.has(k)) {
+        if (a.dz) {
+          m.d.load(pz, tz.off + ov[k], k);
+          m.o.load(po, to_.off + ov[k], k);
+        }
+        if (a.dout) m.g.load(pd, td.off + ov[k], k);
+        m.x.load(pf, tf.off + ov[k], k);
+        if (a.gate && !a.shared) m.q.load(pg, tg.off + ov[k], k);
+      }
+  };
   // one row's gradients; u1 and u2 take G fhat and G
-  auto row = [&](long p, bool in, float (&u1)[NV][V], float (&u2)[NV][V]) __attribute__((always_inline)) {
+  auto row = [&](long p, bool in, const Row& m, float (&u1)[NV][V], float (&u2)[NV][V]) __attribute__((always_inline)) {
     float G[NV][V], x[NV][V];
-    const float4 st = in ? a.stats[p] : make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.dout) load_row<VT>(sh, (const T*)a.dout + p * a.lddout, in, G);
-    load_row<VT>(sh, (const T*)a.f + p * a.ldf, in, x);
-    if (a.gate && !a.shared) load_row<VT>(sh, (const T*)a.gate + p * a.ldgate, in, q);
+    const float4 st = m.st;
+    m.g.to(G);
+    m.x.to(x);
+    if (a.gate && !a.shared) m.q.to(q);
     if (a.dz) {
       float d[NV][V], o[NV][V], s = 0.f, t = 0.f;
-      load_row<VT>(sh, (const T*)a.dz + p * a.lddz, in, d);
-      load_row<VT>(sh, (const T*)a.out + p * a.ldout, in, o);
+      m.d.to(d);
+      m.o.to(o);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -361,19 +452,18 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
           sum[0][k][v] += d[k][v] * o[k][v];
           sum[1][k][v] += d[k][v];
           d[k][v] *= ng[k][v];
-          if (sh.has(k)) {
-            s += d[k][v];
-            t += d[k][v] * o[k][v];
-          }
+          s += d[k][v];
+          t += d[k][v] * o[k][v];
         }
-      s = row_sum<BLK>(s, sh.G, s4) * inv_c;
-      t = row_sum<BLK>(t, sh.G, s4) * inv_c;
+      row_sums<BLK>(s, t, sh.G, s8);
+      s *= inv_c;
+      t *= inv_c;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const float n = st.w * (d[k][v] - s - o[k][v] * t);
-          G[k][v] = a.dout ? G[k][v] + n : n;
+          G[k][v] += n;
         }
     }
     float b[NV][V], s = 0.f, t = 0.f;
@@ -382,73 +472,95 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if constexpr (POST) x[k][v] = (x[k][v] - st.x) * st.y;
-        const float g = a.shared ? G[k][v] : G[k][v] * q[k][v];
+        const float gq = G[k][v] * q[k][v], g = a.shared ? G[k][v] : gq;
         u1[k][v] += g * x[k][v];
         u2[k][v] += g;
-        b[k][v] = G[k][v] * q[k][v] * pg[k][v];
-        if (POST && sh.has(k)) {
+        b[k][v] = gq * pg[k][v];
+        if constexpr (POST) {
           s += b[k][v];
           t += b[k][v] * x[k][v];
         }
       }
     if constexpr (POST) {
-      s = row_sum<BLK>(s, sh.G, s4) * inv_c;
-      t = row_sum<BLK>(t, sh.G, s4) * inv_c;
+      row_sums<BLK>(s, t, sh.G, s8);
+      s *= inv_c;
+      t *= inv_c;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) b[k][v] = st.y * (b[k][v] - s - x[k][v] * t);
     }
     if (!in) return;
-    store_row<VT>(sh, (T*)a.dr + p * a.lddr, G);
-    store_row<VT>(sh, (T*)a.df + p * a.lddf, b);
+    store_row<VT, SH, T>(sh, tr.at(p), tr.off, ov, G);
+    store_row<VT, SH, T>(sh, tdf.at(p), tdf.off, ov, b);
     if (a.dgate && !a.shared) {
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) G[k][v] *= POST ? x[k][v] * pg[k][v] + pb[k][v] : x[k][v] * pg[k][v];
-      store_row<VT>(sh, (T*)a.dgate + p * a.lddgate, G);
+      store_row<VT, SH, T>(sh, tdg.at(p), tdg.off, ov, G);
     }
   };
 
+  auto take_gate = [&](long g) __attribute__((always_inline)) {
+    Raw<VT, NV> rq;
+    rq.none();
+    const char* gp = (const char*)a.gate + g * a.ldgate * (long)sizeof(T);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (sh.has(k)) rq.load(gp, ov[k], k);
+    rq.to(q);
+  };
   // trip counts are the same for every lane of a block whose rows are the block's
   if constexpr (!WHOLE) {
     const long g = blockIdx.x / (unsigned)a.ranges;
     const long lo = g * a.group + (blockIdx.x - g * a.ranges) * a.per, hi = min(lo + a.per, (g + 1) * a.group);
-    if (a.shared) load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, true, q);
+    if (a.shared) take_gate(g);
     const int turn = BLK ? 1 : 4 * rpw;
-    for (long p0 = lo; p0 < hi; p0 += turn) {
-      const long p = p0 + (BLK ? 0 : wave * rpw + rl);
-      row(p, p < hi, sum[2], sum[3]);
+    // the next row's loads are on their way while a row is worked on
+    const long p = lo + (BLK ? 0 : wave * rpw), mine = p + rl;
+    Row m[2];
+    fetch(p, mine < hi, m[0]);
+    for (long t = 0; lo + t < hi; t += 2 * turn) {
+      fetch(p + t + turn, mine + t + turn < hi, m[1]);
+      row(p + t, mine + t < hi, m[0], sum[2], sum[3]);
+      if (lo + t + turn >= hi) break;
+      fetch(p + t + 2 * turn, mine + t + 2 * turn < hi, m[0]);
+      row(p + t + turn, mine + t + turn < hi, m[1], sum[2], sum[3]);
     }
   } else {
-    const int part = rpw / a.slots, slot = rl / part, first = rl - slot * part;
     const long groups = a.rows / a.group, step = (long)gridDim.x * (BLK ? 1 : 4 * a.slots);
     for (long g0 = BLK ? blockIdx.x : ((long)blockIdx.x * 4 + wave) * a.slots; g0 < groups; g0 += step) {
       const long g = g0 + slot;
       const bool there = g < groups;
       float u1[NV][V], u2[NV][V];
-      load_row<VT>(sh, (const T*)a.gate + g * a.ldgate, there, q);
+      if (there) take_gate(g);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) u1[k][v] = u2[k][v] = 0.f;
-      for (long t = 0; t < a.group; t += part) row(g * a.group + t + first, there && t + first < a.group, u1, u2);
+      for (long t = 0; t < a.group; t += side) {
+        const bool in = there && t + first < a.group;
+        Row m;
+        fetch(g0 * a.group + t, in, m);
+        row(g0 * a.group + t, in, m, u1, u2);
+      }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           if constexpr (!BLK)
-            for (int o = sh.G; o < sh.G * part; o <<= 1) {
+            for (int o = sh.G; o < sh.G * side; o <<= 1) {
               u1[k][v] += __shfl_xor(u1[k][v], o);
               u2[k][v] += __shfl_xor(u2[k][v], o);
             }
           // every lane of the group has the sums: the first row's takes them on
-          sum[2][k][v] += first ? 0.f : q[k][v] * u1[k][v];
-          sum[3][k][v] += first ? 0.f : q[k][v] * u2[k][v];
+          sum[2][k][v] += first || !there ? 0.f : q[k][v] * u1[k][v];
+          sum[3][k][v] += first || !there ? 0.f : q[k][v] * u2[k][v];
           u1[k][v] = POST ? pg[k][v] * u1[k][v] + pb[k][v] * u2[k][v] : pg[k][v] * u1[k][v];
         }
-      if (a.dgate && there && first == 0) store_row<VT>(sh, (T*)a.dgate + g * a.lddgate, u1);
+      if (a.dgate && there && first == 0)
+        store_row<VT, SH, T>(sh, (char*)a.dgate + g * a.lddgate * (long)sizeof(T), 0u, ov, u1);
     }
   }
   if (!a.part) return;
@@ -488,70 +600,67 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
   }
 }
 
-// The gates' gradients from the ranges' partial sums, and S1 and S2 of each gate in
-// the place of U1 and U2 of its first range: 64 channels of a gate a block.
-template <typename T>
-__global__ __launch_bounds__(kT) void res_join(float* part, int ranges, const T* gate, long ldgate, Vectors w, int post,
-                                               T* dgate, long lddgate, int C) {
-  __shared__ float sh[3][4][64];
-  const int l = threadIdx.x & 63, k = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
-  float* at = part + (long)blockIdx.y * ranges * 4 * C + c;
-  float s[4] = {};
+// Sums z0 and z0 + 1 over S of stride x C floats, columns c: 64 threads a column (k),
+// summed in thread 0 of each.
+__device__ __forceinline__ float2 tree_sums(const float* part, int S, int stride, int C, int c, int k, int l, int z0) {
+  __shared__ float2 sh[64][17];
+  float2 s = make_float2(0.f, 0.f);
   if (c < C)
-#pragma unroll 4
-    for (int b = k; b < ranges; b += 4)
-#pragma unroll
-      for (int z = 0; z < 4; ++z) s[z] += at[((long)b * 4 + z) * C];
-  if (k)
-#pragma unroll
-    for (int z = 0; z < 4; ++z) sh[k - 1][z][l] = s[z];
+#pragma unroll 8
+    for (int b = k; b < S; b += 64) {
+      const float* p = part + ((long)b * stride + z0) * C + c;
+      s.x += p[0];
+      s.y += p[C];
+    }
+  sh[k][l] = s;
   __syncthreads();
+  for (int o = 32; o > 0; o >>= 1) {
+    if (k < o) {
+      sh[k][l].x += sh[k + o][l].x;
+      sh[k][l].y += sh[k + o][l].y;
+    }
+    __syncthreads();
+  }
+  return sh[0][l];
+}
+
+// The gates' gradients from the ranges' partial sums, and S1 and S2 of each gate in
+// the place of U1 and U2 of its first range: sixteen channels of a gate a block, the
+// sums of dz (blockIdx.z = 0) or of G.
+template <typename T>
+__global__ __launch_bounds__(1024) void res_join(float* part, int ranges, const T* gate, long ldgate, Vectors w,
+                                                 int post, T* dgate, long lddgate, int C) {
+  const int l = threadIdx.x & 15, k = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
+  float* of = part + (long)blockIdx.y * ranges * 4 * C;
+  const float2 s = tree_sums(of, ranges, 4, C, c, k, l, 2 * blockIdx.z);
   if (k || c >= C) return;
-#pragma unroll
-  for (int z = 0; z < 4; ++z) s[z] = ((s[z] + sh[0][z][l]) + sh[1][z][l]) + sh[2][z][l];
-  const float g = Elt<T>::ld(gate + blockIdx.y * ldgate + c);
-  at[0] = s[0];
-  at[C] = s[1];
-  at[2L * C] = g * s[2];
-  at[3L * C] = g * s[3];
-  if (!dgate) return;
-  const float n = post ? at_or(w.post_gain, c, 1.f) * s[2] + at_or(w.post_bias, c, 0.f) * s[3] : s[2];
+  const float g = blockIdx.z ? Elt<T>::ld(gate + blockIdx.y * ldgate + c) : 1.f;
+  of[2L * blockIdx.z * C + c] = g * s.x;
+  of[(2L * blockIdx.z + 1) * C + c] = g * s.y;
+  if (!dgate || !blockIdx.z) return;
+  const float n = post ? at_or(w.post_gain, c, 1.f) * s.x + at_or(w.post_bias, c, 0.f) * s.y : s.x;
   Elt<T>::st(dgate + blockIdx.y * lddgate + c, at_or(w.scale, c, 1.f) * n);
 }
 
 // The vectors' gradients from the partial sums of S blocks, `stride` sums of C a
-// block: sixteen columns a block, 64 threads a column.
+// block: sixteen columns a block, the pre norm's (blockIdx.y = 0) or the others.
 __global__ __launch_bounds__(1024) void res_sums(const float* part, int S, int stride, Vectors w, int post,
                                                  tgp_residual_grads g, int overwrite, int C) {
-  __shared__ float sh[4][64][17];
   const int l = threadIdx.x & 15, k = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
-  float s[4] = {};
-  if (c < C)
-#pragma unroll 4
-    for (int b = k; b < S; b += 64)
-#pragma unroll
-      for (int z = 0; z < 4; ++z) s[z] += part[((long)b * stride + z) * C + c];
-#pragma unroll
-  for (int z = 0; z < 4; ++z) sh[z][k][l] = s[z];
-  __syncthreads();
-  for (int o = 32; o > 0; o >>= 1) {
-    if (k < o)
-#pragma unroll
-      for (int z = 0; z < 4; ++z) sh[z][k][l] += sh[z][k + o][l];
-    __syncthreads();
-  }
+  const float2 s = tree_sums(part, S, stride, C, c, k, l, 2 * blockIdx.y);
   if (k || c >= C) return;
-#pragma unroll
-  for (int z = 0; z < 4; ++z) s[z] = sh[z][0][l];
   auto put = [&](float* p, float v) {
     if (p) p[c] = overwrite ? v : p[c] + v;
   };
+  if (blockIdx.y == 0) {
+    put(g.pre_gain, s.x);
+    put(g.pre_bias, s.y);
+    return;
+  }
   const float sc = at_or(w.scale, c, 1.f);
-  put(g.pre_gain, s[0]);
-  put(g.pre_bias, s[1]);
-  put(g.post_gain, sc * s[2]);
-  put(g.post_bias, sc * s[3]);
-  put(g.scale, post ? at_or(w.post_gain, c, 1.f) * s[2] + at_or(w.post_bias, c, 0.f) * s[3] : s[2]);
+  put(g.post_gain, sc * s.x);
+  put(g.post_bias, sc * s.y);
+  put(g.scale, post ? at_or(w.post_gain, c, 1.f) * s.x + at_or(w.post_bias, c, 0.f) * s.y : s.x);
 }
 
 // ------------------------------------------------- plans
@@ -576,12 +685,13 @@ struct Plan {
 
 // The widest accesses that every row's start and length allow, at most `most` values a
 // lane; then the lanes that leave fewest idle, more lanes where two leave the same.
-Plan plan_of(int esz, int C, uintptr_t bits, int most) {
+// near: a wave's rows are within 32 bits of each other; else it takes one at a time.
+Plan plan_of(int esz, int C, uintptr_t bits, int most, int widest, bool near) {
   bits |= (uintptr_t)C * esz;
-  const int vb = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2, nvec = C * esz / vb, top = most * esz / vb;
+  const int vb = bits % widest == 0 ? widest : bits % 4 == 0 ? 4 : 2, nvec = C * esz / vb, top = most * esz / vb;
   Plan best{vb, 0, 64};
   int room = 1 << 30;
-  for (int g = 64; g >= 1; g >>= 1) {
+  for (int g = 64; g >= (near ? 1 : 64); g >>= 1) {
     const int nv = cdiv(nvec, g);
     if (nv > std::min(4, top)) break;
     if (nv * g < room) room = nv * g, best = {vb, nv, g};
@@ -593,7 +703,7 @@ Plan plan_of(int esz, int C, uintptr_t bits, int most) {
 }
 
 // Calls f(VB, NV, BLK as constants); MOST: values a lane.
-template <int ESZ, int MOST, typename F>
+template <int ESZ, int MOST, int WIDE, typename F>
 void with_plan(const Plan& p, F f) {
   auto nv = [&](auto vb, auto blk) {
     constexpr int TOP = MOST * ESZ / decltype(vb)::value;
@@ -611,7 +721,7 @@ void with_plan(const Plan& p, F f) {
     }
   };
   auto vec = [&](auto blk) {
-    if (p.vb == 16) nv(std::integral_constant<int, 16>(), blk);
+    if (p.vb == WIDE) nv(std::integral_constant<int, WIDE>(), blk);
     else if (p.vb == 4) nv(std::integral_constant<int, 4>(), blk);
     else if constexpr (ESZ == 2) nv(std::integral_constant<int, 2>(), blk);
   };
@@ -626,6 +736,14 @@ void with_post(int post, F f) {
   else f(std::false_type());
 }
 
+// Whether a wave's rows of every tensor are within 32 bits of each other.
+template <typename T>
+bool near_rows(std::initializer_list<Rows> all) {
+  for (const Rows& r : all)
+    if (r.p && r.ld * (long)sizeof(T) * 64 >= 1l << 31) return false;
+  return true;
+}
+
 // The bits of a tensor's address and row distance that the widest access has to divide.
 template <typename T>
 uintptr_t place(const Rows& r) { return r.p ? (uintptr_t)r.p | (uintptr_t)r.ld * sizeof(T) : 0; }
@@ -636,7 +754,7 @@ template <typename T>
 hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
   const double n = (double)a.s.rows * a.s.C;
   const Plan p = plan_of(sizeof(T), a.s.C, place<T>(a.r) | place<T>(a.f) | place<T>(a.gate) | place<T>(a.out) | place<T>(a.z),
-                         kFwdValues);
+                         kFwdValues, 16, near_rows<T>({a.r, a.f, a.out, a.z}));
   if (!p.vb || (a.gate.p && a.s.group > 0x7fffffff)) {
     ProfScope ps("residual_norm_fwd_any", 20 * n, 4 * n * sizeof(T), st);
     TGP_LAUNCH(ps, res_fwd_any<T>, dim3((unsigned)std::min<long>(a.s.rows, 2048)), dim3(kT),
@@ -649,7 +767,7 @@ hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
                   (unsigned)a.s.group, vectors(a.w), a.s.eps, (float4*)a.stats, a.s.C, p.g};
   const unsigned grid = even_grid(a.s.rows, p.g == 0 ? 1 : 4 * (64 / p.g), kFwdBlocks);
   with_post(a.s.post, [&](auto post) {
-    with_plan<sizeof(T), kFwdValues>(p, [&](auto vb, auto nv, auto blk) {
+    with_plan<sizeof(T), kFwdValues, 16>(p, [&](auto vb, auto nv, auto blk) {
       constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
       constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
       ProfScope ps("residual_norm_fwd", 20 * n, (a.z.p ? 4 : 3) * n * sizeof(T), st);
@@ -661,16 +779,18 @@ hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
 
 template <typename T>
 hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
+  constexpr int WIDE = 4 * sizeof(T);   // bytes of an access: four values
   const double n = (double)a.s.rows * a.s.C;
   const long rows = a.s.rows, group = a.gate.p ? (long)a.s.group : 1;
   const bool sums = any_sum(a.g), shared = group > 1;
   const Plan p = plan_of(sizeof(T), a.s.C,
                          place<T>(a.dz) | place<T>(a.dout) | (a.dz.p ? place<T>(a.out) : 0) | place<T>(a.f) | place<T>(a.gate) |
                              place<T>(a.dr) | place<T>(a.df) | place<T>(a.dgate),
-                         kBwdValues);
+                         kBwdValues, WIDE,
+                         near_rows<T>({a.dz, a.dout, a.out, a.f, a.gate, a.dr, a.df, a.dgate}));
   auto add_up = [&](int S, int stride) {
     ProfScope ps("residual_norm_sums", 4.0 * S * a.s.C, 16.0 * S * a.s.C, st);
-    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(1024), 0, st, a.part, S, stride, vectors(a.w), a.s.post, a.g,
+    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16), 2), dim3(1024), 0, st, a.part, S, stride, vectors(a.w), a.s.post, a.g,
                (int)a.overwrite, a.s.C);
   };
   if (!p.vb) {
@@ -710,7 +830,7 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   const bool join = shared && !whole && (sums || a.dgate.p);
   if (sums || join) k.part = a.part;
   with_post(a.s.post, [&](auto post) {
-    with_plan<sizeof(T), kBwdValues>(p, [&](auto vb, auto nv, auto blk) {
+    with_plan<sizeof(T), kBwdValues, WIDE>(p, [&](auto vb, auto nv, auto blk) {
       constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
       constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
       ProfScope ps("residual_norm_bwd", 40 * n, (3 + (a.dout.p ? 1 : 0) + (a.dz.p ? 2 : 0)) * n * sizeof(T), st);
@@ -720,7 +840,7 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   });
   if (join) {
     ProfScope ps("residual_norm_gates", 4.0 * grid * a.s.C, 16.0 * grid * a.s.C, st);
-    TGP_LAUNCH(ps, res_join<T>, dim3(cdiv(a.s.C, 64), (unsigned)groups), dim3(kT), 0, st, a.part, k.ranges,
+    TGP_LAUNCH(ps, res_join<T>, dim3(cdiv(a.s.C, 16), (unsigned)groups, 2), dim3(1024), 0, st, a.part, k.ranges,
                (const T*)a.gate.p, a.gate.ld, vectors(a.w), a.s.post, (T*)a.dgate.p, a.dgate.ld, a.s.C);
   }
   if (sums && join) add_up((int)groups, 4 * k.ranges);
@@ -742,7 +862,7 @@ hipError_t residual_norm_backward(const ResidualBackward& a, hipStream_t st) {
   if (a.s.rows == 0) {
     if (!any_sum(a.g) || !a.overwrite) return hipSuccess;
     ProfScope ps("residual_norm_zero", 0, 20.0 * a.s.C, st);
-    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16)), dim3(1024), 0, st, nullptr, 0, 4, Vectors{}, 0, a.g, 1, a.s.C);
+    TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16), 2), dim3(1024), 0, st, nullptr, 0, 4, Vectors{}, 0, a.g, 1, a.s.C);
     return launch_status();
   }
   return a.s.dtype == TGP_BF16 ? backward_t<bf16_t>(a, st) : backward_t<float>(a, st);

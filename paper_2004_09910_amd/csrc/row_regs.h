@@ -1,6 +1,8 @@
 // Rows of a tensor held in registers: vectors of a row dealt over lanes, and sums
 // over them.  Internal linkage.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 namespace tgpk {
@@ -35,6 +37,15 @@ template <> struct Vec<bf16_t, 16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) d[i] = f2bf(f[2 * i]) | (f2bf(f[2 * i + 1]) << 16);
     return make_uint4(d[0], d[1], d[2], d[3]);
+  }
+};
+template <> struct Vec<bf16_t, 8> {
+  typedef uint2 mem, raw;
+  static __device__ __forceinline__ void un(raw v, float* f) {
+    f[0] = bf2f(v.x & 0xffffu); f[1] = bf2f(v.x >> 16); f[2] = bf2f(v.y & 0xffffu); f[3] = bf2f(v.y >> 16);
+  }
+  static __device__ __forceinline__ raw pk(const float* f) {
+    return make_uint2(f2bf(f[0]) | (f2bf(f[1]) << 16), f2bf(f[2]) | (f2bf(f[3]) << 16));
   }
 };
 template <> struct Vec<bf16_t, 4> {
@@ -80,6 +91,56 @@ __device__ __forceinline__ float row_sum(float v, int G, float* s4) {
     if (G >= 32) v += __shfl_xor(v, 16);
     if (G >= 64) v += __shfl_xor(v, 32);
     return v;
+  }
+}
+
+// Two such sums side by side.
+template <bool BLK>
+__device__ __forceinline__ void row_sums(float& s, float& t, int G, float (*s8)[4]) {
+  if constexpr (BLK) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      s += __shfl_xor(s, o);
+      t += __shfl_xor(t, o);
+    }
+    if ((threadIdx.x & 63) == 0) {
+      s8[0][threadIdx.x >> 6] = s;
+      s8[1][threadIdx.x >> 6] = t;
+    }
+    __syncthreads();
+    s = (s8[0][0] + s8[0][1]) + (s8[0][2] + s8[0][3]);
+    t = (s8[1][0] + s8[1][1]) + (s8[1][2] + s8[1][3]);
+    __syncthreads();
+  } else {
+    auto step = [&](auto c) __attribute__((always_inline)) {
+      s += dpp<decltype(c)::value>(s);
+      t += dpp<decltype(c)::value>(t);
+    };
+    typedef std::integral_constant<int, 0xB1> s1;
+    typedef std::integral_constant<int, 0x4E> s2;
+    typedef std::integral_constant<int, 0x141> s4;
+    typedef std::integral_constant<int, 0x140> s8th;
+    if (G >= 16) {
+      step(s1());
+      step(s2());
+      step(s4());
+      step(s8th());
+      if (G >= 32) {
+        s += __shfl_xor(s, 16);
+        t += __shfl_xor(t, 16);
+        if (G >= 64) {
+          s += __shfl_xor(s, 32);
+          t += __shfl_xor(t, 32);
+        }
+      }
+    } else if (G == 8) {
+      step(s1());
+      step(s2());
+      step(s4());
+    } else if (G >= 2) {
+      step(s1());
+      if (G == 4) step(s2());
+    }
   }
 }
 

@@ -366,7 +366,8 @@ def test_side_stream_and_graph(rows, c, group):
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("c", [24, 1001])
 def test_rows_farther_apart_than_32_bits(c, dt):
-    """Rows whose byte offsets pass 2^32: three rows of the stream 1.2e9 elements apart, updated in place."""
+    """Rows whose byte offsets pass 2^32: three rows of the stream 1.2e9 elements apart, updated in place.  A wave
+    takes such rows one at a time, which adds in another order: each side is off by EPS32 and a rounding."""
     say("residual norm, far rows", c, dt)
     ld = 1_200_000_008 if dt == "bf16" else 600_000_004
     a = Run(3, c, dt, 1)
@@ -379,7 +380,11 @@ def test_rows_farther_apart_than_32_bits(c, dt):
     tgp.residual_norm_forward(a.shape, a.params, buf.data_ptr(), ld, a.f.data_ptr(), c, a.gate.data_ptr(), c, buf.data_ptr(),
                               ld, z.data_ptr(), c, st.data_ptr())
     torch.cuda.synchronize()
-    assert torch.equal(far, want[0]) and torch.equal(z, want[1]) and torch.equal(st, want[2])
+    tol = 2 * ((2.0 ** -8 if dt == "bf16" else 0) + EPS32)
+    assert ref.rel(far, want[0].cpu().double()) <= tol and ref.rel(z, want[1].cpu().double()) <= tol
+    assert ref.rel(st, want[2].cpu().double()) <= 2 * EPS32
+    far.copy_(want[0])
+    st.copy_(want[2])
     n = tgp.residual_norm_backward_workspace(a.shape)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     df, dg = torch.empty(3, c, dtype=a.td, device="cuda"), torch.empty(3, c, dtype=a.td, device="cuda")
@@ -388,5 +393,5 @@ def test_rows_farther_apart_than_32_bits(c, dt):
                                a.f.data_ptr(), c, a.gate.data_ptr(), c, st.data_ptr(), buf.data_ptr(), ld, df.data_ptr(), c,
                                dg.data_ptr(), c, tgp.residual_grads(*[t.data_ptr() for t in grads]), True, ws.data_ptr(), n)
     torch.cuda.synchronize()
-    assert torch.equal(far, back["dr"]) and torch.equal(df, back["df"]) and torch.equal(dg, back["dgate"])
-    assert all(torch.equal(t, back[k]) for t, k in zip(grads, VEC))
+    for t, k in zip([far, df, dg] + grads, ("dr", "df", "dgate") + VEC):
+        assert ref.rel(t, back[k].cpu().double()) <= (tol if t.dtype == torch.bfloat16 else 2 * EPS32), k
