@@ -245,6 +245,45 @@ struct OutArgs {
   int tm, tn;
 };
 
+// Sixteen values of a lane's fragment, with the bias, as T to row r and columns from c
+// on of y.
+template <typename T>
+__device__ __forceinline__ void put_out(const f32x16_t& acc, const float (&b)[16], T* y, bool in, int c, int n, int vec) {
+  const int lane = threadIdx.x & 63;
+  float v[16];
+#pragma unroll
+  for (int z = 0; z < 16; ++z) v[z] = acc[z] + b[z];
+  if constexpr (sizeof(T) == 2) {
+    unsigned pk[8];
+#pragma unroll
+    for (int z = 0; z < 8; ++z) pk[z] = pack_bf16(v[2 * z], v[2 * z + 1]);
+    put8(pk, [&](int h, u32x4 u) {
+      const int at = c + 16 * h + 8 * (lane >> 5);
+      if (!in) return;
+      if (vec && at + 8 <= n) {
+        *(u32x4*)(y + at) = u;
+      } else {
+#pragma unroll
+        for (int z = 0; z < 8; ++z)
+          if (at + z < n) y[at + z] = (bf16_t)(u[z / 2] >> (16 * (z & 1)));
+      }
+    });
+  } else {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int at = c + 8 * g + 4 * (lane >> 5);
+      if (!in) continue;
+      if (vec && at + 4 <= n) {
+        *(float4*)(y + at) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+      } else {
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+          if (at + z < n) y[at + z] = v[4 * g + z];
+      }
+    }
+  }
+}
+
 template <typename PR, typename T>
 __global__ __launch_bounds__(PR::T, 2) void out_k(OutArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
@@ -262,40 +301,401 @@ __global__ __launch_bounds__(PR::T, 2) void out_k(OutArgs a) {
 #pragma unroll
     for (int i = 0; i < PR::MT; ++i) {
       const long r = i0 + (wave / PR::WN * PR::MT + i) * 32 + (lane & 31);
-      T* y = (T*)a.y + r * a.ldy;
+      put_out<T>(p.acc[0][i][j], b, (T*)a.y + r * a.ldy, r < a.rows, c, a.n, a.vec);
+    }
+  }
+}
+
+// ------------------------------------------------- narrow blocks in one launch
+
+struct NarrowArgs {
+  const bf16_t *x[kMaxParts], *w[2][kMaxParts], *wd[kMaxParts];
+  long lda, ldb, ldwd;
+  int rows, cin, hidden, cout;
+  const float *bg, *bu, *bd;
+  void* y;
+  long ldy;
+  int vec;
+};
+
+// The 32 biases from column c on (the same for the wave), by scalar loads: vector loads
+// would wait behind the ring's.  Lane l's sixteen, as in a fragment.  (Columns from n on
+// get some bias: what becomes of them meets zeros.)
+__device__ __forceinline__ void wave_biases(const float* b, int c, int n, float (&v)[16]) {
+  typedef const __attribute__((address_space(4))) float* uniform_p;
+  const bool hi = (threadIdx.x & 63) >= 32;
+  float s[32];
+#pragma unroll
+  for (int z = 0; z < 32; ++z) s[z] = 0.f;
+  if (b) {
+    const uniform_p p = (uniform_p)(unsigned long)b;
+    if (c + 32 <= n) {
+#pragma unroll
+      for (int z = 0; z < 32; ++z) s[z] = p[c + z];
+    } else {
+#pragma unroll
+      for (int z = 0; z < 32; ++z) s[z] = p[min(c + z, n - 1)];
+    }
+  }
+#pragma unroll
+  for (int z = 0; z < 16; ++z) v[z] = hi ? s[8 * (z / 4) + 4 + z % 4] : s[8 * (z / 4) + z % 4];
+}
+
+// y of 64 pixels, 32 NW hidden channels at a time: a wave has 64 pixels x 32 channels of
+// g and u, and leaves their h in LDS, the next product's left factor; nothing of the
+// hidden channels goes to memory.  The pixels' fragments (KSX stages of 64 channels,
+// P parts) stay in registers.  The ring's stages are all of one size and hold one
+// matrix's part: first the pixels', then 64 channels of Wg or Wu for the tile's hidden
+// channels, or of Wd for 32 CG output channels, KG = NW / CG ranges of 64 hidden
+// channels at once, by as many groups of waves, whose sums meet at the end.
+//
+// A turn multiplies a stage's fragments, and between its products reads the next
+// stage's and sends one load of the stage NS ahead after the other: a CU takes a KiB
+// of such loads in 19 clocks (55 bytes a clock, of rows of 128 bytes or more; half of
+// that of rows of 64), and a wave that sends four at once waits that long.  12544 x
+// 256, 1024 hidden channels: 58 us with the loads before the products.
+template <int P, int KSX, int NW, int CG, int ACT, typename T>
+__global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void narrow_k(NarrowArgs a) {
+  // from three stages of 64 channels on the pixels stay in LDS, which leaves the ring
+  // less, and the fragments of one are in registers: all of them spill
+  constexpr bool XL = P == 1 && KSX >= 3;
+  constexpr int XK = XL ? 1 : KSX;   // stages of pixels in registers
+  constexpr int NS = XL ? 3 : P == 1 ? 4 : 6, BK = 64, BH = 32 * NW, KG = NW / CG, H = BK / 16, L = 4;
+  typedef Feed<BH, BK, false, NW> FW;
+  typedef Feed<64, BK, false, 2> FH;   // (its layout)
+  constexpr int SLOT = FW::BYTES, HB = FH::BYTES, DUAL = 2 * P * KSX, SPT = DUAL + P * CG / 2;
+  static_assert(FW::LOADS == L && H == L && KSX * HB <= SLOT && P < NS, "a load between the products of a step");
+  __shared__ __align__(1024) unsigned char ring[NS * SLOT + P * (BH / 64) * HB + XL * SLOT];
+  static_assert(sizeof(ring) <= 160 * 1024 && NS * SLOT >= NW * 8192, "LDS");
+  unsigned char* const hs = ring + NS * SLOT;   // [part][64 channels], as stages of 64 rows
+  unsigned char* const xs = XL ? hs + P * (BH / 64) * HB : ring;   // the pixels, [64 channels][64 rows]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i0 = blockIdx.x * 64;
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
+  const int tiles = (a.hidden + BH - 1) / BH;
+  const long ldw = a.ldb * 2, ldd = a.ldwd * 2;
+  // the lane's chunks: of Wg and Wu, and of Wd (LDS row r is output channel r % (32 CG), of
+  // range r / (32 CG))
+  int vw[L], vd[L], kd[L];
+#pragma unroll
+  for (int u = 0; u < L; ++u) {
+    const int r = (wave + u * NW) * 8 + lane / 8, q = (lane % 8) ^ FW::swz(r), row = r % (32 * CG);
+    vw[u] = (int)(r * ldw) + q * 16;
+    kd[u] = 64 * (r / (32 * CG)) + q * 8;
+    vd[u] = row < a.cout ? (int)(row * ldd) + kd[u] * 2 : kOob;
+  }
+  const int kq = kd[0] & 63;   // (the same in all: swz sees the wave's parity alone)
+  auto desc = [&](unsigned long p, long bytes) __attribute__((always_inline)) {
+    return u32x4{(unsigned)p, (unsigned)(p >> 32) & 0xffffu, (unsigned)max(0l, min(bytes, 0x7fffffffl)), 0x00020000u};
+  };
+  // load u of stage `step` of tile t, into slot (beyond the last tile: zeros)
+  auto load = [&](auto stepc, int t, int slot, auto uc) __attribute__((always_inline)) {
+    constexpr int step = decltype(stepc)::value, u = decltype(uc)::value;
+    const unsigned d = lds + slot * SLOT + u * NW * 1024;
+    int v[1];
+    if constexpr (step < DUAL) {
+      constexpr int k = step / (2 * P), m = step & 1, j = P - 1 - step / 2 % P;
+      // rows from `hidden` on are past the matrix's end
+      const long at = t * (BH * ldw) + k * BK * 2;
+      v[0] = k < KSX - 1 || kq < a.cin - k * BK ? vw[u] : kOob;
+      dma_n<1, 0>(desc((unsigned long)a.w[m][j] + at, (long)a.hidden * ldw - at), d, v);
+    } else {
+      constexpr int o = (step - DUAL) / P, j = P - 1 - (step - DUAL) % P;
+      const int at = t * BH + o * (64 * KG);
+      v[0] = kd[u] < a.hidden - at ? vd[u] : kOob;
+      dma_n<1, 0>(desc((unsigned long)(a.wd[j] + at), t < tiles ? 0x7fffffff : 0), d, v);
+    }
+  };
+  auto stage = [&](auto stepc, int t, int slot) __attribute__((always_inline)) {
+    each<L>([&](auto u) { load(stepc, t, slot, u); });
+  };
+  // the pixels, part p in slot p: [64 channels][64 rows]
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    int v[L];
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      const int c8 = wave + u * NW, row = (c8 % 8) * 8 + lane / 8, k = c8 / 8, q = (lane % 8) ^ FH::swz(row);
+      v[u] = k < KSX && row < a.rows - i0 && k * BK + q * 8 < a.cin ? (int)(row * a.lda * 2) + k * BK * 2 + q * 16 : kOob;
+    }
+    const unsigned d = lds + (unsigned)(xs - ring) + p * SLOT;
+    dma_n<L, NW * 1024>(desc((unsigned long)(a.x[p] + (long)i0 * a.lda), 0x7fffffff), d, v);
+  }
+  // (in the first slots, where they do not stay)
+  constexpr int S0 = XL ? 0 : P;   // the first stage's slot
+  each<NS - S0>([&](auto z) {
+    constexpr int n = decltype(z)::value;
+    stage(std::integral_constant<int, n % SPT>(), n / SPT, S0 + n);
+  });
+  wait_vmcnt<(NS - S0) * L>();
+  ring_barrier();
+  u32x4 x[P][XK][H][2];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int k = 0; k < XK; ++k)
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[p][k][h][i] = FH::frag(xs + p * SLOT + k * HB, FH::place(32 * i), h);
+  if constexpr (!XL) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ring_barrier();
+    each<P>([&](auto z) {
+      constexpr int n = NS - P + decltype(z)::value;
+      stage(std::integral_constant<int, n % SPT>(), n / SPT, decltype(z)::value);
+    });
+  }
+  const int pb = FW::place(wave * 32);
+  u32x4 b[H];   // the fragments of the stage to be multiplied
+  int slot = S0;
+  wait_vmcnt<(NS - 1) * L>();
+  ring_barrier();
+#pragma unroll
+  for (int h = 0; h < H; ++h) b[h] = FW::frag(ring + slot * SLOT, pb, h);
+  // Stage `step` of tile t: mul(h) are the products of step h.  At the barrier the next
+  // stage has landed, and every wave has this one's fragments: its slot is free.
+  auto turn = [&](auto stepc, int t, auto mul) __attribute__((always_inline)) {
+    constexpr int step = decltype(stepc)::value, ahead = step + NS;
+    wait_vmcnt<(NS - 2) * L>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // b, and h where this wave has just written it
+    ring_barrier();
+    const int next = slot + 1 == NS ? 0 : slot + 1;
+    each<H>([&](auto hc) {
+      constexpr int h = decltype(hc)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      mul(h);
+      b[h] = FW::frag(ring + next * SLOT, pb, h);
+      load(std::integral_constant<int, ahead % SPT>(), t + ahead / SPT, slot, hc);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    slot = next;
+  };
+  f32x16_t y[2] = {};
+  for (int ht = 0; ht < tiles; ++ht) {
+    f32x16_t g[2], u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) g[i] = u[i] = f32x16_t{};
+    each<DUAL>([&](auto sc) {
+      constexpr int step = decltype(sc)::value, k = step / (2 * P), j = P - 1 - step / 2 % P;
+      turn(sc, ht, [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = P - 1 - j; p >= 0; --p)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if constexpr (step & 1) u[i] = mfma32(as_bf16x8(b[h]), as_bf16x8(x[p][XL ? 0 : k][h][i]), u[i]);
+            else g[i] = mfma32(as_bf16x8(b[h]), as_bf16x8(x[p][XL ? 0 : k][h][i]), g[i]);
+            if constexpr (XL && step & 1) x[0][0][h][i] = FH::frag(xs + (k + 1) % KSX * HB, FH::place(32 * i), h);
+          }
+      });
+    });
+    const int c = ht * BH + wave * 32;
+    float bg[16], bu[16];
+    wave_biases(a.bg, c, a.hidden, bg);
+    wave_biases(a.bu, c, a.hidden, bu);
+    // (every wave has met a barrier since the last product read h)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       float v[16];
 #pragma unroll
-      for (int z = 0; z < 16; ++z) v[z] = p.acc[0][i][j][z] + b[z];
-      if constexpr (sizeof(T) == 2) {
+      for (int z = 0; z < 16; ++z) {
+        float act, slope;
+        act_of<ACT>(g[i][z] + bg[z], &act, &slope);
+        v[z] = act * (u[i][z] + bu[z]);
+      }
+      const int row = 32 * i + (lane & 31);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
         unsigned pk[8];
 #pragma unroll
         for (int z = 0; z < 8; ++z) pk[z] = pack_bf16(v[2 * z], v[2 * z + 1]);
-        put8(pk, [&](int h, u32x4 u) {
-          const int at = c + 16 * h + 8 * (lane >> 5);
-          if (r >= a.rows) return;
-          if (a.vec && at + 8 <= a.n) {
-            *(u32x4*)(y + at) = u;
-          } else {
-#pragma unroll
-            for (int z = 0; z < 8; ++z)
-              if (at + z < a.n) y[at + z] = (bf16_t)(u[z / 2] >> (16 * (z & 1)));
-          }
+        put8(pk, [&](int h, u32x4 w) {
+          const int q = (wave & 1) * 4 + 2 * h + (lane >> 5);
+          *(u32x4*)(hs + (p * (BH / 64) + (wave >> 1)) * HB + row * 128 + ((q ^ FH::swz(row)) << 4)) = w;
         });
-      } else {
+        if (p + 1 < P)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int at = c + 8 * g + 4 * (lane >> 5);
-          if (r >= a.rows) continue;
-          if (a.vec && at + 4 <= a.n) {
-            *(float4*)(y + at) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
-          } else {
-#pragma unroll
-            for (int z = 0; z < 4; ++z)
-              if (at + z < a.n) y[at + z] = v[4 * g + z];
+          for (int z = 0; z < 16; ++z) {
+            const float hi = z & 1 ? __uint_as_float(pk[z / 2] & 0xffff0000u) : __uint_as_float(pk[z / 2] << 16);
+            v[z] = (__float_as_uint(hi) & 0x7f800000u) == 0x7f800000u ? 0.f : v[z] - hi;
           }
-        }
       }
     }
+    u32x4 hf[P][H][2];
+    each<P * CG / 2>([&](auto sc) {
+      constexpr int s = decltype(sc)::value, o = s / P, j = P - 1 - s % P;
+      turn(std::integral_constant<int, DUAL + s>(), ht, [&](int h) __attribute__((always_inline)) {
+        if (h == 0 && j == P - 1) {
+#pragma unroll
+          for (int z = 0; z < H; ++z)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                hf[p][z][i] = FH::frag(hs + (p * (BH / 64) + o * KG + wave / CG) * HB, FH::place(32 * i), z);
+        }
+#pragma unroll
+        for (int p = P - 1 - j; p >= 0; --p)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) y[i] = mfma32(as_bf16x8(b[h]), as_bf16x8(hf[p][h][i]), y[i]);
+      });
+    });
+  }
+  wait_vmcnt<0>();
+  if constexpr (KG > 1) {   // the groups' sums, in order
+    ring_barrier();         // nothing is on its way into the ring, and nothing read from it
+    float* red = (float*)ring;   // [wave][i][value][lane]
+    if (wave >= CG)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int z = 0; z < 16; ++z) red[((wave * 2 + i) * 16 + z) * 64 + lane] = y[i][z];
+    __syncthreads();
+    if (wave >= CG) return;
+#pragma unroll
+    for (int k = 1; k < KG; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int z = 0; z < 16; ++z) y[i][z] += red[(((wave + k * CG) * 2 + i) * 16 + z) * 64 + lane];
+  }
+  const int c = wave % CG * 32;
+  float bd[16];
+  biases(a.bd, c, a.cout, bd);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const long r = i0 + 32 * i + (lane & 31);
+    put_out<T>(y[i], bd, (T*)a.y + r * a.ldy, r < a.rows, c, a.cout, a.vec);
+  }
+}
+
+// ------------------------------------------------- few pixels
+
+// Eight values from k on of a row of n, as P bfloat16 fragments; `in`: whether the
+// row is there; vec: rows lie at multiples of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int k, int n, bool in, int vec, float (&v)[8]) {
+  if (in && vec && k + 8 <= n) {
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 w = *(const u32x4*)(row + k);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) v[z] = bf2f(z & 1 ? w[z / 2] >> 16 : w[z / 2] & 0xffffu);
+    } else {
+      const float4 a = *(const float4*)(row + k), b = *(const float4*)(row + k + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int z = 0; z < 8; ++z) v[z] = in && k + z < n ? Elt<T>::ld(row + k + z) : 0.f;
+  }
+}
+template <typename T>
+struct Frag {
+  static constexpr int P = sizeof(T) == 2 ? 1 : 3;
+  u32x4 p[P];
+  __device__ __forceinline__ void set(float (&v)[8]) {
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+#pragma unroll
+      for (int z = 0; z < 4; ++z) p[q][z] = pack_bf16(v[2 * z], v[2 * z + 1]);
+      if (q + 1 < P)
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+          const float hi = z & 1 ? __uint_as_float(p[q][z / 2] & 0xffff0000u) : __uint_as_float(p[q][z / 2] << 16);
+          v[z] = (__float_as_uint(hi) & 0x7f800000u) == 0x7f800000u ? 0.f : v[z] - hi;
+        }
+    }
+  }
+  // c + this fragment's rows times b's
+  __device__ __forceinline__ f32x16_t times(const Frag& b, f32x16_t c) const {
+    if constexpr (P == 3) {
+      c = mfma32(as_bf16x8(p[2]), as_bf16x8(b.p[0]), c);
+      c = mfma32(as_bf16x8(p[1]), as_bf16x8(b.p[1]), c);
+      c = mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[2]), c);
+      c = mfma32(as_bf16x8(p[1]), as_bf16x8(b.p[0]), c);
+      c = mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[1]), c);
+    }
+    return mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[0]), c);
+  }
+};
+
+struct FewArgs {
+  const void *x, *w[2];
+  const float* b[2];
+  void* y;
+  long ldx, ldw, ldy;
+  int rows, k, n, vx, vw;
+};
+
+// Up to 32 MF pixels: 32 channels of the result a block, NW waves that share the sum;
+// M matrices (two: h, else y).  Weights are read once, straight into fragments, by as
+// many blocks as there are, and that is what bounds it.
+template <typename T, int M, int MF, int NW, int ACT>
+__global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
+  constexpr int U = M == 2 ? 2 : 4;   // steps of 16 whose loads go out together
+  __shared__ float red[NW][M * MF][16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j0 = blockIdx.x * 32, col = j0 + (lane & 31), per = ((a.k + NW - 1) / NW + 15) / 16 * 16;
+  const int k1 = min(a.k, (wave + 1) * per);
+  f32x16_t acc[M][MF];
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[m][f] = f32x16_t{};
+  for (int k0 = wave * per; k0 < k1; k0 += 16 * U) {
+    float vw[U][M][8], vx[U][MF][8];
+#pragma unroll
+    for (int s = 0; s < U; ++s) {
+      const int k = k0 + 16 * s + 8 * (lane >> 5);
+#pragma unroll
+      for (int m = 0; m < M; ++m) load8((const T*)a.w[m] + col * a.ldw, k, k1, col < a.n, a.vw, vw[s][m]);
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
+        const int r = 32 * f + (lane & 31);
+        load8((const T*)a.x + r * a.ldx, k, k1, r < a.rows, a.vx, vx[s][f]);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < U; ++s) {
+      Frag<T> w[M], x;
+#pragma unroll
+      for (int m = 0; m < M; ++m) w[m].set(vw[s][m]);
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
+        x.set(vx[s][f]);
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[m][f] = w[m].times(x, acc[m][f]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) red[wave][m * MF + f][v][lane] = acc[m][f][v];
+  __syncthreads();
+  // a thread has columns n of pixel r: fragment value 4 (n / 8) + n % 4 of lane r % 32 +
+  // 32 (n / 4 % 2), summed over the waves in order
+  for (int e = threadIdx.x; e < 32 * 32 * MF; e += 64 * NW) {
+    const int n = e & 31, r = e >> 5, f = r >> 5;
+    if (r >= a.rows || j0 + n >= a.n) continue;
+    const int v = 4 * (n >> 3) + (n & 3), l = (r & 31) + 32 * ((n >> 2) & 1);
+    float s[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      s[m] = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) s[m] += red[w][m * MF + f][v][l];
+      if (a.b[m]) s[m] += a.b[m][j0 + n];
+    }
+    if constexpr (M == 2) {
+      float act, slope;
+      act_of<ACT>(s[0], &act, &slope);
+      s[0] = act * s[1];
+    }
+    Elt<T>::st((T*)a.y + r * a.ldy + j0 + n, s[0]);
   }
 }
 
@@ -588,11 +988,78 @@ void with_act(int act, F f) {
   else f(std::integral_constant<int, TGP_ACT_GELU>());
 }
 
+bool at16(const void* p, long ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
+
+constexpr int kFewRows = 64;
+
+// Whether one launch takes a forward pass whole: what its registers and LDS hold.
+bool narrow(const tgp_gated_shape& s, long rows) {
+  const int most = s.dtype == TGP_BF16 ? 256 : 128;
+  return s.cin <= most && s.cout <= most && (rows > kFewRows || s.hidden <= 256);
+}
+
+template <int P, int ACT, typename T>
+void launch_narrow(const NarrowArgs& a, hipStream_t st) {
+  ProfScope ps("gated_narrow", 2.0 * a.rows * a.hidden * (2 * a.cin + a.cout) * (P == 1 ? 1 : 6),
+               2.0 * a.rows * (a.cin + a.cout), st);
+  auto go = [&](auto ksx, auto nw, auto cg) {
+    constexpr int KSX = decltype(ksx)::value, NW = decltype(nw)::value, CG = decltype(cg)::value;
+    TGP_LAUNCH(ps, (narrow_k<P, KSX, NW, CG, ACT, T>), dim3(cdiv(a.rows, 64)), dim3(64 * NW), 0, st, a);
+  };
+  typedef std::integral_constant<int, 2> two;
+  typedef std::integral_constant<int, 4> four;
+  typedef std::integral_constant<int, 8> eight;
+  const int k = cdiv(a.cin, 64);
+  // up to 128 channels four waves a block, of bfloat16 two blocks a CU: one's first loads
+  // and activations beside the other's products (147456 x 64, 256 hidden channels: 65 us
+  // with eight waves)
+  auto cols = [&](auto ksx) {
+    if (a.cout <= 64) go(ksx, four(), two());
+    else go(ksx, four(), four());
+  };
+  if constexpr (P == 1) {
+    auto wide = [&](auto ksx) {
+      if (a.cout <= 64) go(ksx, eight(), two());
+      else if (a.cout <= 128) go(ksx, eight(), four());
+      else go(ksx, eight(), eight());
+    };
+    if (k == 4) return wide(std::integral_constant<int, 4>());
+    if (k == 3) return wide(std::integral_constant<int, 3>());
+    if (a.cout > 128) return k == 1 ? go(std::integral_constant<int, 1>(), eight(), eight()) : go(two(), eight(), eight());
+  }
+  if (k == 1) cols(std::integral_constant<int, 1>());
+  else cols(two());
+}
+
+template <typename T>
+hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, T* h, long ldh, hipStream_t st) {
+  const tgp_gated_shape& s = g.s;
+  const int rows = (int)g.rows, e = sizeof(T);
+  const FewArgs a{x, {g.w.gate, g.w.up}, {g.w.b_gate, g.w.b_up}, h, ldx, s.cin, ldh, rows, s.cin, s.hidden,
+                  at16(x, ldx, e), at16(g.w.gate, s.cin, e) && at16(g.w.up, s.cin, e)};
+  const FewArgs o{h, {g.w.down, nullptr}, {g.w.b_down, nullptr}, y, ldh, s.hidden, ldy, rows, s.hidden, s.cout,
+                  at16(h, ldh, e), at16(g.w.down, s.hidden, e)};
+  auto go = [&](auto mf) {
+    constexpr int MF = decltype(mf)::value;
+    with_act(s.act, [&](auto act) {
+      ProfScope ps("gated_few_hidden", 4.0 * rows * s.cin * s.hidden, 2.0 * e * s.cin * s.hidden, st);
+      TGP_LAUNCH(ps, (few_k<T, 2, MF, 4, decltype(act)::value>), dim3(cdiv(s.hidden, 32)), dim3(256), 0, st, a);
+    });
+    ProfScope ps("gated_few_out", 2.0 * rows * s.cout * s.hidden, (double)e * s.cout * s.hidden, st);
+    TGP_LAUNCH(ps, (few_k<T, 1, MF, 8, 0>), dim3(cdiv(s.cout, 32)), dim3(512), 0, st, o);
+  };
+  if (rows <= 32) go(std::integral_constant<int, 1>());
+  else go(std::integral_constant<int, 2>());
+  return launch_status();
+}
+
 template <typename T>
 hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void* ws, hipStream_t st) {
   constexpr int P = sizeof(T) == 2 ? 1 : 3;
   const tgp_gated_shape& s = g.s;
   Call c{g, plan_of(s, g.rows, false), (char*)ws, st};
+  if (g.rows <= kFewRows && !narrow(s, g.rows))
+    return forward_few<T>(g, x, ldx, y, ldy, (T*)((char*)ws + c.p.h), c.p.hidp, st);
   const Matrix wg = c.operand(g.w.gate, s.cin, s.hidden, s.cin, c.p.wg, s.hidden);
   const Matrix wu = c.operand(g.w.up, s.cin, s.hidden, s.cin, c.p.wu, s.hidden);
   const Matrix wd = c.operand(g.w.down, s.hidden, s.cout, s.hidden, c.p.wd, s.cout);
@@ -602,6 +1069,14 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
     const Matrix xm = c.operand(x + r0 * ldx, ldx, rows, s.cin, c.p.x, c.p.chunk);
     if (hipError_t e = c.flush(); e != hipSuccess) return e;
     HiddenArgs a = hidden_args(c, xm, wg, wu, rows);
+    if (narrow(s, g.rows)) {
+      const NarrowArgs n{{xm.part[0], xm.part[1], xm.part[2]},
+                         {{wg.part[0], wg.part[1], wg.part[2]}, {wu.part[0], wu.part[1], wu.part[2]}},
+                         {wd.part[0], wd.part[1], wd.part[2]}, xm.ld, wg.ld, wd.ld, (int)rows, s.cin, s.hidden,
+                         s.cout, a.bg, a.bu, g.w.b_down, y + r0 * ldy, ldy, at16(y + r0 * ldy, ldy, sizeof(T))};
+      with_act(s.act, [&](auto act) { launch_narrow<P, decltype(act)::value, T>(n, st); });
+      continue;
+    }
     a.h = h;
     auto hidden = [&](auto pr, auto act) {
       typedef decltype(pr) PR;
@@ -624,7 +1099,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
     o.bias = g.w.b_down;
     o.y = y + r0 * ldy;
     o.ldy = ldy;
-    o.vec = ((uintptr_t)o.y & 15) == 0 && ldy * sizeof(T) % 16 == 0;
+    o.vec = at16(o.y, ldy, sizeof(T));
     if (fills(rows, s.cout)) launch_out<OutL, T>("gated_out", o, st);
     else launch_out<OutS, T>("gated_out", o, st);
   }
@@ -738,7 +1213,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       o.n = s.cin;
       o.y = dx + r0 * lddx;
       o.ldy = lddx;
-      o.vec = ((uintptr_t)o.y & 15) == 0 && lddx * sizeof(T) % 16 == 0;
+      o.vec = at16(o.y, lddx, sizeof(T));
       if (fills(rows, s.cin)) launch_out<DxL, T>("gated_dx", o, st);
       else launch_out<DxS, T>("gated_dx", o, st);
     }

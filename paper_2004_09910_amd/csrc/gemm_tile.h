@@ -220,26 +220,33 @@ struct Product {
     for (int idx = 0; idx < total; ++idx) {
       wait_stages<NS, LPS>(min(NS - 2, total - 1 - idx));
       ring_barrier();
-      if (idx + NS - 1 < total) issue(slot == 0 ? NS - 1 : slot - 1);
       const unsigned char* st = ring + slot * SLOT;
+      // all of the stage's fragments first: read one by one before their products, each
+      // waits for LDS (half of the time); the next stage's loads go out while they come
+      u32x4 a[BK / 16][MT], b[BK / 16][NB][NT];
 #pragma unroll
       for (int h = 0; h < BK / 16; ++h) {
-        u32x4 a[MT], b[NB][NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[i] = FA::frag(st, pa[i], h);
+        for (int i = 0; i < MT; ++i) a[h][i] = FA::frag(st, pa[i], h);
 #pragma unroll
         for (int q = 0; q < NB; ++q)
 #pragma unroll
-          for (int j = 0; j < NT; ++j) b[q][j] = FB::frag(st + q * FB::BYTES, pb[j], h);
+          for (int j = 0; j < NT; ++j) b[h][q][j] = FB::frag(st + q * FB::BYTES, pb[j], h);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (idx + NS - 1 < total) issue(slot == 0 ? NS - 1 : slot - 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int h = 0; h < BK / 16; ++h) {
 #pragma unroll
         for (int q = 0; q < NB; ++q)
 #pragma unroll
           for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-              acc[q][i][j] = mfma32(as_bf16x8(b[q][j]), as_bf16x8(a[i]), acc[q][i][j]);
+              acc[q][i][j] = mfma32(as_bf16x8(b[h][q][j]), as_bf16x8(a[h][i]), acc[q][i][j]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) extra(a[i], i, pair);
+        for (int i = 0; i < MT; ++i) extra(a[h][i], i, pair);
       }
       if (--more == 0) {
         more = per;
