@@ -159,7 +159,7 @@ __device__ __forceinline__ void biases(const float* b, int c, int n, float (&v)[
 
 // h of a tile.  P: parts of a factor.
 template <typename PR, int ACT, int P>
-__global__ __launch_bounds__(PR::T, 2) void hidden_k(HiddenArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void hidden_k(HiddenArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
   int ti, tj;
   tile_of(xcd_remap(blockIdx.x, gridDim.x), a.tm, a.tn, &ti, &tj);
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(PR::T, 2) void hidden_k(HiddenArgs a) {
 // h, dg and du of a tile, each in P parts (one, and no h, where no weight's gradient
 // is wanted).
 template <typename PR, typename PD, int ACT, int P, bool GRADS>
-__global__ __launch_bounds__(PR::T, 2) void back_k(HiddenArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void back_k(HiddenArgs a) {
   static_assert(PR::BM == PD::BM && PR::BN == PD::BN && PR::MT == PD::MT && PR::WN == PD::WN, "one tile");
   __shared__ __align__(1024) unsigned char ring[PR::LDS > PD::LDS ? PR::LDS : PD::LDS];
   int ti, tj;
@@ -243,6 +243,8 @@ struct OutArgs {
   long ldy;
   int vec;   // 16-byte pieces of y's rows lie at multiples of 16
   int tm, tn;
+  float* part;   // the ranges' sums, rows of ldp floats
+  int ldp, per;
 };
 
 // Sixteen values of a lane's fragment, with the bias, as T to row r and columns from c
@@ -284,26 +286,51 @@ __device__ __forceinline__ void put_out(const f32x16_t& acc, const float (&b)[16
   }
 }
 
-template <typename PR, typename T>
-__global__ __launch_bounds__(PR::T, 2) void out_k(OutArgs a) {
+// SPLIT: ranges of `per` of the sum, each into rows of its own at part.
+template <typename PR, typename T, bool SPLIT>
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void out_k(OutArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
+  const int tiles = a.tm * a.tn, blk = xcd_remap(blockIdx.x, gridDim.x), q = SPLIT ? blk / tiles : 0;
+  const int k0 = SPLIT ? q * a.per : 0, k1 = SPLIT ? min(a.k, k0 + a.per) : a.k;
   int ti, tj;
-  tile_of(xcd_remap(blockIdx.x, gridDim.x), a.tm, a.tn, &ti, &tj);
+  tile_of(blk - q * tiles, a.tm, a.tn, &ti, &tj);
   const int i0 = ti * PR::BM, j0 = tj * PR::BN, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   PR p;
   p.zero();
-  p.run(ring, a.s, a.lda, a.ldb, a.rows, a.n, i0, j0, 0, a.k, [](u32x4, int, int) {});
+  p.run(ring, a.s, a.lda, a.ldb, a.rows, a.n, i0, j0, k0, k1, [](u32x4, int, int) {});
 #pragma unroll
   for (int j = 0; j < PR::NT; ++j) {
     const int c = j0 + (wave % PR::WN * PR::NT + j) * 32;
     float b[16];
-    biases(a.bias, c, a.n, b);
+    biases(SPLIT ? nullptr : a.bias, c, a.n, b);
 #pragma unroll
     for (int i = 0; i < PR::MT; ++i) {
       const long r = i0 + (wave / PR::WN * PR::MT + i) * 32 + (lane & 31);
-      put_out<T>(p.acc[0][i][j], b, (T*)a.y + r * a.ldy, r < a.rows, c, a.n, a.vec);
+      if constexpr (SPLIT)
+        put_out<float>(p.acc[0][i][j], b, a.part + ((long)q * a.rows + r) * a.ldp, r < a.rows, c, a.ldp, 1);
+      else
+        put_out<T>(p.acc[0][i][j], b, (T*)a.y + r * a.ldy, r < a.rows, c, a.n, a.vec);
     }
   }
+}
+
+// y = the ranges' sums, in order, + bias; four columns a thread.
+template <typename T>
+__global__ __launch_bounds__(kT) void join_k(OutArgs a, int ranges) {
+  const int per = a.ldp / 4, e = blockIdx.x * kT + threadIdx.x, r = e / per, c = (e - r * per) * 4;
+  if (r >= a.rows) return;
+  const float* p = a.part + (long)r * a.ldp + c;
+  float4 s = *(const float4*)p;
+#pragma unroll 4
+  for (int q = 1; q < ranges; ++q) {
+    const float4 v = *(const float4*)(p + (long)q * a.rows * a.ldp);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const float v[4] = {s.x, s.y, s.z, s.w};
+  T* y = (T*)a.y + r * a.ldy + c;
+#pragma unroll
+  for (int z = 0; z < 4; ++z)
+    if (c + z < a.n) Elt<T>::st(y + z, v[z] + (a.bias ? a.bias[c + z] : 0.f));
 }
 
 // ------------------------------------------------- narrow blocks in one launch
@@ -571,30 +598,51 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void narrow_k(NarrowArgs a
 
 // ------------------------------------------------- few pixels
 
-// Eight values from k on of a row of n, as P bfloat16 fragments; `in`: whether the
-// row is there; vec: rows lie at multiples of 16 bytes.
+// Eight values from k on of a row of n as they are in memory; `in`: whether the row is
+// there; vec: rows lie at multiples of 16 bytes.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int k, int n, bool in, int vec, float (&v)[8]) {
-  if (in && vec && k + 8 <= n) {
-    if constexpr (sizeof(T) == 2) {
-      const u32x4 w = *(const u32x4*)(row + k);
-#pragma unroll
-      for (int z = 0; z < 8; ++z) v[z] = bf2f(z & 1 ? w[z / 2] >> 16 : w[z / 2] & 0xffffu);
+struct Eight;
+template <>
+struct Eight<bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t* row, int k, int n, bool in, int vec) {
+    if (in && vec && k + 8 <= n) {
+      w = *(const u32x4*)(row + k);
     } else {
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const unsigned lo = in && k + 2 * z < n ? row[k + 2 * z] : 0u, hi = in && k + 2 * z + 1 < n ? row[k + 2 * z + 1] : 0u;
+        w[z] = lo | hi << 16;
+      }
+    }
+  }
+};
+template <>
+struct Eight<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* row, int k, int n, bool in, int vec) {
+    if (in && vec && k + 8 <= n) {
       const float4 a = *(const float4*)(row + k), b = *(const float4*)(row + k + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
       v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-  } else {
+    } else {
 #pragma unroll
-    for (int z = 0; z < 8; ++z) v[z] = in && k + z < n ? Elt<T>::ld(row + k + z) : 0.f;
+      for (int z = 0; z < 8; ++z) v[z] = in && k + z < n ? row[k + z] : 0.f;
+    }
   }
-}
+};
 template <typename T>
 struct Frag {
   static constexpr int P = sizeof(T) == 2 ? 1 : 3;
   u32x4 p[P];
-  __device__ __forceinline__ void set(float (&v)[8]) {
+  __device__ __forceinline__ void set(const Eight<T>& e) {
+    if constexpr (P == 1) p[0] = e.w;
+    else split(e.v);
+  }
+  __device__ __forceinline__ void split(const float (&f)[8]) {
+    float v[8];
+#pragma unroll
+    for (int z = 0; z < 8; ++z) v[z] = f[z];
 #pragma unroll
     for (int q = 0; q < P; ++q) {
 #pragma unroll
@@ -626,17 +674,21 @@ struct FewArgs {
   void* y;
   long ldx, ldw, ldy;
   int rows, k, n, vx, vw;
+  int cw;   // channels of a block
 };
 
-// Up to 32 MF pixels: 32 channels of the result a block, NW waves that share the sum;
-// M matrices (two: h, else y).  Weights are read once, straight into fragments, by as
-// many blocks as there are, and that is what bounds it.
+// Up to 32 MF pixels: cw channels of the result a block, NW waves that share the sum; M
+// matrices (two: h, else y).  Weights are read once, straight into fragments, and what
+// bounds it is how many of their loads are on their way at a time: as many waves as a
+// block has, and blocks of fewer channels (the other rows of their fragments are zeros)
+// where 32 each leave CUs without one.
 template <typename T, int M, int MF, int NW, int ACT>
 __global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
-  constexpr int U = M == 2 ? 2 : 4;   // steps of 16 whose loads go out together
+  constexpr int U = M == 1 && MF == 1 && sizeof(T) == 2 ? 8 : 4;   // steps of 16 whose loads go out together
   __shared__ float red[NW][M * MF][16][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int j0 = blockIdx.x * 32, col = j0 + (lane & 31), per = ((a.k + NW - 1) / NW + 15) / 16 * 16;
+  const int j0 = blockIdx.x * a.cw, col = j0 + (lane & 31), per = ((a.k + NW - 1) / NW + 15) / 16 * 16;
+  const bool here = (lane & 31) < a.cw && col < a.n;
   const int k1 = min(a.k, (wave + 1) * per);
   f32x16_t acc[M][MF];
 #pragma unroll
@@ -644,16 +696,16 @@ __global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
 #pragma unroll
     for (int f = 0; f < MF; ++f) acc[m][f] = f32x16_t{};
   for (int k0 = wave * per; k0 < k1; k0 += 16 * U) {
-    float vw[U][M][8], vx[U][MF][8];
+    Eight<T> vw[U][M], vx[U][MF];
 #pragma unroll
     for (int s = 0; s < U; ++s) {
       const int k = k0 + 16 * s + 8 * (lane >> 5);
 #pragma unroll
-      for (int m = 0; m < M; ++m) load8((const T*)a.w[m] + col * a.ldw, k, k1, col < a.n, a.vw, vw[s][m]);
+      for (int m = 0; m < M; ++m) vw[s][m].load((const T*)a.w[m] + col * a.ldw, k, k1, here, a.vw);
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         const int r = 32 * f + (lane & 31);
-        load8((const T*)a.x + r * a.ldx, k, k1, r < a.rows, a.vx, vx[s][f]);
+        vx[s][f].load((const T*)a.x + r * a.ldx, k, k1, r < a.rows, a.vx);
       }
     }
 #pragma unroll
@@ -680,7 +732,7 @@ __global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
   // 32 (n / 4 % 2), summed over the waves in order
   for (int e = threadIdx.x; e < 32 * 32 * MF; e += 64 * NW) {
     const int n = e & 31, r = e >> 5, f = r >> 5;
-    if (r >= a.rows || j0 + n >= a.n) continue;
+    if (r >= a.rows || n >= a.cw || j0 + n >= a.n) continue;
     const int v = 4 * (n >> 3) + (n & 3), l = (r & 31) + 32 * ((n >> 2) & 1);
     float s[M];
 #pragma unroll
@@ -703,22 +755,24 @@ __global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
 
 // One matrix's gradient, a^T b over the pixels: m columns of a, n of b; partial sums
 // of range q at part + q stride (rows of ldp floats), column sums of a at cols +
-// q stride.
+// q stride.  Of one range these are the gradients themselves (null: none), and are
+// added to with `add`.
 struct OuterJob {
   Segs<1> s;
   long lda, ldb;
-  int m, n, ldp, tm, tn, blk0;
+  int m, n, ldp, tm, tn, blk0, vec;   // vec: rows at part lie at multiples of 16 bytes
   int sums;   // the pairs, a bit each, whose a's go into the column sums: every part once
   float *part, *cols;
 };
 struct OuterArgs {
   OuterJob j[3];
   int n, rows, per;    // jobs, pixels, pixels of a range (a multiple of the stage)
+  int add;
   long stride;
 };
 
 template <typename PR>
-__global__ __launch_bounds__(PR::T, 2) void outer_k(OuterArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void outer_k(OuterArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
   int k = 0;
@@ -742,15 +796,31 @@ __global__ __launch_bounds__(PR::T, 2) void outer_k(OuterArgs a) {
   for (int i = 0; i < PR::MT; ++i) {
     const int r = i0 + (wave / PR::WN * PR::MT + i) * 32 + (lane & 31);
     if (r >= J.m) continue;
-    if (sums && lane < 32) J.cols[q * a.stride + r] = ones[i][0];
+    if (sums && lane < 32) {
+      float* to = J.cols + q * a.stride + r;
+      *to = a.add ? *to + ones[i][0] : ones[i][0];
+    }
+    if (!J.part) continue;
+    float* to = J.part + q * a.stride + (long)r * J.ldp;
 #pragma unroll
     for (int j = 0; j < PR::NT; ++j) {
-      float* to = J.part + q * a.stride + (long)r * J.ldp;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int at = j0 + (wave % PR::WN * PR::NT + j) * 32 + 8 * g + 4 * (lane >> 5);
         const f32x16_t& v = p.acc[0][i][j];
-        if (at < J.ldp) *(float4*)(to + at) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+        if (J.vec) {
+          if (at >= J.ldp) continue;
+          float4 f = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+          if (a.add) {
+            const float4 o = *(const float4*)(to + at);
+            f = make_float4(o.x + f.x, o.y + f.y, o.z + f.z, o.w + f.w);
+          }
+          *(float4*)(to + at) = f;
+        } else {
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+            if (at + z < J.n) to[at + z] = a.add ? to[at + z] + v[4 * g + z] : v[4 * g + z];
+        }
       }
     }
   }
@@ -815,16 +885,21 @@ __global__ void zero_k(float* p, long n) {
 
 // ------------------------------------------------- plans
 
-// Large and small tiles of each launch.
-typedef Product<2, 2, 2, 2, 32, 3, false, false, 2> HidL;
+// Large and small tiles of each launch; the large ones of y and dx with a deep ring, a
+// block a CU, and with a shallow one, two.
+typedef Product<2, 2, 4, 2, 64, 2, false, false, 2> HidL;
 typedef Product<1, 1, 2, 2, 64, 3, false, false, 2> HidS;
-typedef Product<2, 2, 2, 2, 32, 3, false, true, 1> DhL;
+typedef Product<2, 1, 2, 4, 64, 3, false, false, 2> BackL;
+typedef Product<2, 1, 2, 4, 64, 3, false, true, 1> DhL;
 typedef Product<1, 1, 2, 2, 64, 3, false, true, 1> DhS;
-typedef Product<2, 2, 2, 2, 64, 2, false, false, 1> OutL;
+typedef Product<2, 2, 2, 2, 64, 4, false, false, 1> OutL;
+typedef Product<2, 2, 2, 2, 64, 2, false, false, 1> OutL2;
 typedef Product<1, 1, 2, 2, 64, 4, false, false, 1> OutS;
-typedef Product<2, 2, 2, 2, 64, 2, false, true, 1> DxL;
+typedef Product<2, 2, 2, 2, 64, 4, false, true, 1> DxL;
+typedef Product<2, 2, 2, 2, 64, 2, false, true, 1> DxL2;
 typedef Product<1, 1, 2, 2, 64, 4, false, true, 1> DxS;
-typedef Product<2, 2, 2, 2, 64, 2, true, true, 1> OuterL;
+typedef Product<2, 4, 4, 2, 32, 4, true, true, 1> OuterX;
+typedef Product<2, 2, 2, 2, 32, 4, true, true, 1> OuterL;
 typedef Product<1, 1, 2, 2, 64, 4, true, true, 1> OuterS;
 
 constexpr long kFill = 256;   // tiles that fill the chip
@@ -834,13 +909,31 @@ struct Plan {
   int parts, low;        // of a factor; of h, dg and du (backward)
   long cinp, hidp, coutp;
   long chunk;            // pixels at a time
-  bool small_outer;
+  int wide;              // the weights' gradients' tiles
   int ranges, per;       // of the pixels of a chunk, at most
   long stride;           // floats of a range's partial sums
-  size_t x, dy, wg, wu, wd, h, dg, du, part, bytes;   // offsets
+  size_t x, dy, wg, wu, wd, h, dg, du, part, join, bytes;   // offsets
 };
 
 int ranges_of(long rows, int per) { return (int)((rows + per - 1) / per); }
+
+// A long sum for few tiles of 64 x 64: ranges of `per` of its k values, four stages each
+// at least, that the tiles' blocks fill the chip with; their partial sums are joined by a
+// launch of its own (144 x 1024, k 4096: 20.6 us as 48 blocks).
+struct Split {
+  int n, per;
+};
+Split split_of(long rows, long cols, int k, int pairs) {
+  const long tiles = cdiv(rows, 64) * (long)cdiv(cols, 64), stages = (k + 63) / 64;
+  const long want = std::min<long>(kFill / tiles, stages * pairs / 4);
+  if (want < 2) return {1, k};
+  const int per = (int)round_up((k + want - 1) / want, 64);
+  return {(k + per - 1) / per, per};
+}
+size_t split_bytes(long rows, long cols, int k, int pairs) {
+  const Split d = split_of(rows, cols, k, pairs);
+  return d.n > 1 ? (size_t)4 * d.n * rows * round_up(cols, 4) : 0;
+}
 
 Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   Plan p{};
@@ -874,16 +967,24 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
     p.du = take((size_t)2 * p.low * p.chunk * p.hidp);
     auto tiles = [&](long t) { return 2 * cdiv(s.hidden, t) * (long)cdiv(s.cin, t) + cdiv(s.cout, t) * (long)cdiv(s.hidden, t); };
     const long large = tiles(128);
-    p.small_outer = large * std::max<long>(1, p.chunk / 512) < kFill;
-    const long n = p.small_outer ? tiles(64) : large;
-    // ranges of four stages at least, as many as fill the chip twice
-    const long want = std::max<long>(1, std::min<long>(2 * kFill / n, p.chunk / 256));
+    // as large as leave enough of them, with the ranges' help, and are not mostly padding
+    const long x = tiles(256), runs = std::max<long>(1, p.chunk / 512);
+    p.wide = 8 * 4 * x <= 9 * large && 4 * x * runs >= 3 * kFill ? 256 : large * runs >= kFill ? 128 : 64;
+    const long n = tiles(p.wide), fill = p.wide == 256 ? kFill : 2 * kFill;
+    // ranges of four stages at least, as many as fill the chip; one where the tiles do
+    const long want = 4 * n >= 3 * kFill ? 1 : std::max<long>(1, std::min<long>(fill / n, p.chunk / 256));
     p.per = (int)round_up((p.chunk + want - 1) / want, 64);
     p.ranges = ranges_of(p.chunk, p.per);
     p.stride = 2 * (long)s.hidden * round_up(s.cin, 4) + (long)s.cout * round_up(s.hidden, 4) +
                2 * round_up(s.hidden, 4) + round_up(s.cout, 4);
-    p.part = take((size_t)4 * p.stride * p.ranges);
+    p.part = take(p.ranges > 1 ? (size_t)4 * p.stride * p.ranges : 0);
   }
+  const long rest = p.chunk ? rows % p.chunk : 0;
+  auto room = [&](long r) {
+    const int n = p.parts == 1 ? 1 : 6;
+    return !r ? 0 : backward ? split_bytes(r, s.cin, s.hidden, 2 * n) : split_bytes(r, s.cout, s.hidden, n);
+  };
+  p.join = take(std::max(room(p.chunk), room(rest)));
   p.bytes = at;
   return p;
 }
@@ -958,7 +1059,30 @@ void launch_out(const char* name, OutArgs a, hipStream_t st) {
   a.tm = cdiv(a.rows, PR::BM);
   a.tn = cdiv(a.n, PR::BN);
   ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * (a.k + a.n), st);
-  TGP_LAUNCH(ps, (out_k<PR, T>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
+  TGP_LAUNCH(ps, (out_k<PR, T, false>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
+}
+
+// y or dx, by the number of tiles: more than a block a CU (two shallow rings, 147456 x 64
+// of 256: 12.4 us, a deep one 16.0), one (4096 x 1024 of 4096: 50.5 us, shallow 59),
+// less, much less.
+template <typename PRL2, typename PRL, typename PRS, typename T>
+void launch_sum(const char* name, const char* name_join, OutArgs a, void* join, hipStream_t st) {
+  const long tiles = (long)cdiv(a.rows, 128) * cdiv(a.n, 128);
+  if (tiles > kFill) return launch_out<PRL2, T>(name, a, st);
+  if (tiles == kFill) return launch_out<PRL, T>(name, a, st);
+  const Split d = split_of(a.rows, a.n, a.k, a.s.n);
+  if (d.n == 1) return launch_out<PRS, T>(name, a, st);
+  a.part = (float*)join;
+  a.ldp = (int)round_up(a.n, 4);
+  a.per = d.per;
+  a.tm = cdiv(a.rows, PRS::BM);
+  a.tn = cdiv(a.n, PRS::BN);
+  {
+    ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * a.k + 4.0 * d.n * a.rows * a.n, st);
+    TGP_LAUNCH(ps, (out_k<PRS, T, true>), dim3((unsigned)a.tm * a.tn * d.n), dim3(PRS::T), 0, st, a);
+  }
+  ProfScope ps(name_join, 0, (4.0 * d.n + 2) * a.rows * a.n, st);
+  TGP_LAUNCH(ps, join_k<T>, dim3((unsigned)cdiv((long)a.rows * (a.ldp / 4), kT)), dim3(kT), 0, st, a, d.n);
 }
 
 HiddenArgs hidden_args(const Call& c, const Matrix& x, const Matrix& wg, const Matrix& wu, long rows) {
@@ -1035,18 +1159,19 @@ template <typename T>
 hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, T* h, long ldh, hipStream_t st) {
   const tgp_gated_shape& s = g.s;
   const int rows = (int)g.rows, e = sizeof(T);
+  auto width = [](int n) { return n >= 32 * 256 ? 32 : n >= 16 * 256 ? 16 : n >= 8 * 128 ? 8 : 4; };
   const FewArgs a{x, {g.w.gate, g.w.up}, {g.w.b_gate, g.w.b_up}, h, ldx, s.cin, ldh, rows, s.cin, s.hidden,
-                  at16(x, ldx, e), at16(g.w.gate, s.cin, e) && at16(g.w.up, s.cin, e)};
+                  at16(x, ldx, e), at16(g.w.gate, s.cin, e) && at16(g.w.up, s.cin, e), width(s.hidden)};
   const FewArgs o{h, {g.w.down, nullptr}, {g.w.b_down, nullptr}, y, ldh, s.hidden, ldy, rows, s.hidden, s.cout,
-                  at16(h, ldh, e), at16(g.w.down, s.hidden, e)};
+                  at16(h, ldh, e), at16(g.w.down, s.hidden, e), width(s.cout)};
   auto go = [&](auto mf) {
-    constexpr int MF = decltype(mf)::value;
+    constexpr int MF = decltype(mf)::value, NO = MF * sizeof(T) == 8 ? 8 : 16;   // (registers)
     with_act(s.act, [&](auto act) {
       ProfScope ps("gated_few_hidden", 4.0 * rows * s.cin * s.hidden, 2.0 * e * s.cin * s.hidden, st);
-      TGP_LAUNCH(ps, (few_k<T, 2, MF, 4, decltype(act)::value>), dim3(cdiv(s.hidden, 32)), dim3(256), 0, st, a);
+      TGP_LAUNCH(ps, (few_k<T, 2, MF, 8, decltype(act)::value>), dim3(cdiv(s.hidden, a.cw)), dim3(512), 0, st, a);
     });
     ProfScope ps("gated_few_out", 2.0 * rows * s.cout * s.hidden, (double)e * s.cout * s.hidden, st);
-    TGP_LAUNCH(ps, (few_k<T, 1, MF, 8, 0>), dim3(cdiv(s.cout, 32)), dim3(512), 0, st, o);
+    TGP_LAUNCH(ps, (few_k<T, 1, MF, NO, 0>), dim3(cdiv(s.cout, o.cw)), dim3(64 * NO), 0, st, o);
   };
   if (rows <= 32) go(std::integral_constant<int, 1>());
   else go(std::integral_constant<int, 2>());
@@ -1100,8 +1225,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
     o.y = y + r0 * ldy;
     o.ldy = ldy;
     o.vec = at16(o.y, ldy, sizeof(T));
-    if (fills(rows, s.cout)) launch_out<OutL, T>("gated_out", o, st);
-    else launch_out<OutS, T>("gated_out", o, st);
+    launch_sum<OutL2, OutL, OutS, T>("gated_out", "gated_out_join", o, (char*)ws + c.p.join, st);
   }
   return launch_status();
 }
@@ -1141,8 +1265,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
     };
     with_act(s.act, [&](auto act) {
       if (fills(rows, s.hidden)) {
-        if (grads) back(HidL(), DhL(), act, std::true_type());
-        else back(HidL(), DhL(), act, std::false_type());
+        if (grads) back(BackL(), DhL(), act, std::true_type());
+        else back(BackL(), DhL(), act, std::false_type());
       } else {
         if (grads) back(HidS(), DhS(), act, std::true_type());
         else back(HidS(), DhS(), act, std::false_type());
@@ -1159,7 +1283,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       m.add = !overwrite || r0 > 0;
       float* at = (float*)((char*)ws + p.part);
       int blocks = 0;
-      const int wide = p.small_outer ? OuterS::BM : OuterL::BM;
+      const bool direct = p.ranges == 1;
+      o.add = direct && m.add;
       auto job = [&](const Matrix& u, int nu, int rows_w, const Matrix& v, int nv, int cols_w, float* w, float* b) {
         const int ldp = (int)round_up(cols_w, 4);
         if (w || b) {
@@ -1170,14 +1295,22 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
           J.m = rows_w;
           J.n = cols_w;
           J.ldp = ldp;
-          J.tm = cdiv(rows_w, wide);
-          J.tn = w ? cdiv(cols_w, wide) : 1;   // the column sums alone: the first columns
+          J.tm = cdiv(rows_w, p.wide);
+          J.tn = w ? cdiv(cols_w, p.wide) : 1;   // the column sums alone: the first columns
           J.blk0 = blocks;
           int bit = 0;
           pairs(nu, nv, [&](int, int k) { J.sums |= (b && k == 0) << bit++; });
           J.part = at;
           J.cols = at + (long)rows_w * ldp;
+          J.vec = 1;
           blocks += J.tm * J.tn * m.ranges;
+          if (direct) {
+            J.part = w;
+            J.cols = b;
+            J.ldp = cols_w;
+            J.vec = at16(w, cols_w, 4);
+            return;
+          }
           if (w) m.j[m.jobs++] = {J.part, w, rows_w, cols_w, ldp, 0};
           if (b) m.j[m.jobs++] = {J.cols, b, 1, rows_w, (int)round_up(rows_w, 4), 0};
         }
@@ -1188,18 +1321,21 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       job(dym, P, s.cout, h, L, s.hidden, gr.down, gr.b_down);
       {
         ProfScope ps("gated_outer", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * o.j[0].s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
-        if (p.small_outer) TGP_LAUNCH(ps, outer_k<OuterS>, dim3((unsigned)blocks), dim3(OuterS::T), 0, st, o);
-        else TGP_LAUNCH(ps, outer_k<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
+        if (p.wide == 64) TGP_LAUNCH(ps, outer_k<OuterS>, dim3((unsigned)blocks), dim3(OuterS::T), 0, st, o);
+        else if (p.wide == 128) TGP_LAUNCH(ps, outer_k<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
+        else TGP_LAUNCH(ps, outer_k<OuterX>, dim3((unsigned)blocks), dim3(OuterX::T), 0, st, o);
       }
-      const bool deep = m.ranges >= 8;
-      int sb = 0;
-      for (int k = 0; k < m.jobs; ++k) {
-        m.j[k].blk0 = sb;
-        sb += cdiv((long)m.j[k].rows * (m.j[k].ldp / 4), deep ? 64 : 256);
+      if (!direct) {
+        const bool deep = m.ranges >= 8;
+        int sb = 0;
+        for (int k = 0; k < m.jobs; ++k) {
+          m.j[k].blk0 = sb;
+          sb += cdiv((long)m.j[k].rows * (m.j[k].ldp / 4), deep ? 64 : 256);
+        }
+        ProfScope ps("gated_sum", 0, 4.0 * m.ranges * p.stride, st);
+        if (deep) TGP_LAUNCH(ps, sum_k<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
+        else TGP_LAUNCH(ps, sum_k<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
       }
-      ProfScope ps("gated_sum", 0, 4.0 * m.ranges * p.stride, st);
-      if (deep) TGP_LAUNCH(ps, sum_k<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
-      else TGP_LAUNCH(ps, sum_k<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
     }
     if (dx) {   // last: it may be written over x or dy
       OutArgs o{};
@@ -1214,8 +1350,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       o.y = dx + r0 * lddx;
       o.ldy = lddx;
       o.vec = at16(o.y, lddx, sizeof(T));
-      if (fills(rows, s.cin)) launch_out<DxL, T>("gated_dx", o, st);
-      else launch_out<DxS, T>("gated_dx", o, st);
+      launch_sum<DxL2, DxL, DxS, T>("gated_dx", "gated_dx_join", o, (char*)ws + p.join, st);
     }
   }
   return launch_status();

@@ -71,7 +71,7 @@ struct Feed {
 
   // Chunk q of LDS row `row` lies at chunk q ^ swz(row).
   __device__ __forceinline__ static int swz(int row) {
-    if constexpr (!KS) return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+    if constexpr (!KS) return BK == 64 ? (row & 2) << 1 | (row >> 2 & 3) : (row >> 2) & 3;
     else if constexpr (R >= 128) return (row & 3) << 2;
     else if constexpr (R == 64) return ((row >> 1) & 1) << 2;
     else return 0;
@@ -100,26 +100,25 @@ struct Feed {
     at = (unsigned long)hi << 32 | lo;
   }
 
-  // The next stage into LDS at dst (of the wave: + 1024 wave); left: values of the
-  // sum from its first on.
-  __device__ __forceinline__ void issue(unsigned dst, int left) {
-    u32x4 r{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+  // The next stage: left, values of the sum from its first on.  Its loads u = 0 .. LOADS - 1
+  // go to LDS from dst on (of the wave: + 1024 wave).
+  u32x4 rsrc;
+  bool in;     // the lane's chunks are inside the sum (not KS)
+  __device__ __forceinline__ void next(int left) {
+    rsrc = u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
     if constexpr (KS) {
-      if (left < BK) r[2] = (unsigned)(left * (int)ldb);
-      r[2] = __builtin_amdgcn_readfirstlane(r[2]);
-      dma_n<LOADS, NW * 1024>(r, dst, vo);
+      if (left < BK) rsrc[2] = (unsigned)(left * (int)ldb);
+      rsrc[2] = __builtin_amdgcn_readfirstlane(rsrc[2]);
       at += (unsigned long)(BK * ldb);
     } else {
-      if (left >= BK) {
-        dma_n<LOADS, NW * 1024>(r, dst, vo);
-      } else {
-        int v[LOADS];
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) v[u] = kq < left ? vo[u] : kOob;
-        dma_n<LOADS, NW * 1024>(r, dst, v);
-      }
+      in = kq < left;
       at += BK * 2;
     }
+  }
+  template <int U>
+  __device__ __forceinline__ void load(unsigned dst) const {
+    const int v[1] = {KS || in ? vo[U] : kOob};
+    dma_n<1, 0>(rsrc, dst + U * NW * 1024, v);
   }
 
   // Byte offset of this lane's part of the fragment of rows f .. f + 31, and (KS) of
@@ -190,22 +189,31 @@ struct Product {
     for (int b = 0; b < NB; ++b) fb[b].init(ldb, n - j0);
     const int per = (k1 - k0 + BK - 1) / BK, total = per * s.n;
     const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
-    int seg = 0, left = k1 - k0;
+    int seg = 0, left = k1 - k0;   // of the next stage to be sent for
     auto seek = [&]() {
       fa.seek(s.a[seg], i0, k0);
 #pragma unroll
       for (int b = 0; b < NB; ++b) fb[b].seek(s.b[seg][b], j0, k0);
     };
     seek();
-    auto issue = [&](int slot) __attribute__((always_inline)) {
-      const unsigned d = lds + slot * SLOT;
-      fa.issue(d, left);
+    auto next = [&]() __attribute__((always_inline)) {
+      fa.next(left);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) fb[b].issue(d + FA::BYTES + b * FB::BYTES, left);
+      for (int b = 0; b < NB; ++b) fb[b].next(left);
       left -= BK;
       if (left <= 0 && ++seg < s.n) {
         left = k1 - k0;
         seek();
+      }
+    };
+    auto load = [&](auto uc, int slot) __attribute__((always_inline)) {   // load u of its LPS
+      constexpr int u = decltype(uc)::value;
+      const unsigned d = lds + slot * SLOT;
+      if constexpr (u < FA::LOADS) {
+        fa.template load<u>(d);
+      } else {
+        constexpr int v = u - FA::LOADS, b = v / FB::LOADS;
+        fb[b].template load<v % FB::LOADS>(d + FA::BYTES + b * FB::BYTES);
       }
     };
     int pa[MT], pb[NT];
@@ -214,30 +222,42 @@ struct Product {
 #pragma unroll
     for (int j = 0; j < NT; ++j) pb[j] = FA::BYTES + FB::place((wn * NT + j) * 32);
 #pragma unroll
-    for (int k = 0; k < NS - 1; ++k)
-      if (k < total) issue(k);
-    int slot = 0, pair = 0, more = per;
-    for (int idx = 0; idx < total; ++idx) {
-      wait_stages<NS, LPS>(min(NS - 2, total - 1 - idx));
-      ring_barrier();
-      const unsigned char* st = ring + slot * SLOT;
-      // all of the stage's fragments first: read one by one before their products, each
-      // waits for LDS (half of the time); the next stage's loads go out while they come
-      u32x4 a[BK / 16][MT], b[BK / 16][NB][NT];
-#pragma unroll
-      for (int h = 0; h < BK / 16; ++h) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) a[h][i] = FA::frag(st, pa[i], h);
-#pragma unroll
-        for (int q = 0; q < NB; ++q)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) b[h][q][j] = FB::frag(st + q * FB::BYTES, pb[j], h);
+    for (int k = 0; k < NS; ++k)
+      if (k < total) {
+        next();
+        each<LPS>([&](auto u) { load(u, k); });
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (idx + NS - 1 < total) issue(slot == 0 ? NS - 1 : slot - 1);
-      __builtin_amdgcn_sched_barrier(0);
+    // the fragments of the stage to be multiplied
+    constexpr int H = BK / 16;
+    u32x4 a[H][MT], b[H][NB][NT];
+    auto read = [&](int h, const unsigned char* st) __attribute__((always_inline)) {
 #pragma unroll
-      for (int h = 0; h < BK / 16; ++h) {
+      for (int i = 0; i < MT; ++i) a[h][i] = FA::frag(st, pa[i], h);
+#pragma unroll
+      for (int q = 0; q < NB; ++q)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[h][q][j] = FB::frag(st + q * FB::BYTES, pb[j], h);
+    };
+    wait_stages<NS + 1, LPS>(min(NS - 1, total - 1));
+    ring_barrier();
+#pragma unroll
+    for (int h = 0; h < H; ++h) read(h, ring);
+    int slot = 0, pair = 0, more = per;
+    // A turn multiplies a stage and, between its products, reads the next one's fragments
+    // in their place and sends the loads of the stage NS ahead: at its barrier the next
+    // stage has landed, and every wave has this one's fragments, so that its slot is free.
+    // (Reads and loads before the products: a wave waits for LDS, and for its loads to be
+    // taken, a KiB in 19 clocks; 12544 x 256 through 1024 hidden channels 58 us and 33.)
+    for (int idx = 0; idx < total; ++idx) {
+      wait_stages<NS, LPS>(max(0, min(NS - 2, total - 2 - idx)));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      ring_barrier();
+      const int nslot = slot + 1 == NS ? 0 : slot + 1;
+      const bool send = idx + NS < total;
+      if (send) next();
+      each<H>([&](auto hc) {
+        constexpr int h = decltype(hc)::value;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int q = 0; q < NB; ++q)
 #pragma unroll
@@ -247,15 +267,17 @@ struct Product {
               acc[q][i][j] = mfma32(as_bf16x8(b[h][q][j]), as_bf16x8(a[h][i]), acc[q][i][j]);
 #pragma unroll
         for (int i = 0; i < MT; ++i) extra(a[h][i], i, pair);
-      }
+        read(h, ring + nslot * SLOT);
+        if (send) each<(h + 1) * LPS / H - h * LPS / H>([&](auto u) {
+          load(std::integral_constant<int, h * LPS / H + decltype(u)::value>(), slot);
+        });
+      });
+      __builtin_amdgcn_sched_barrier(0);
       if (--more == 0) {
         more = per;
         ++pair;
       }
-      // the slot is written over once every wave has met the next barrier: its
-      // fragments have been read by then if their products are before it
-      __builtin_amdgcn_sched_barrier(0);
-      slot = slot + 1 == NS ? 0 : slot + 1;
+      slot = nslot;
     }
   }
 };
