@@ -6,7 +6,10 @@
 // values a thread, the 16 threads of a block of 128 agree on its exponents.  What
 // decides a rounding is computed in float64: a value next to the border between
 // two codes then goes the same way whatever the order of operations, and squares
-// of float32 gradients neither overflow nor vanish.
+// of float32 gradients neither overflow nor vanish.  Memory bounds it as long as those
+// operations are few: codes from a float64's upper half, a root of one step (31.4 million
+// values with the copy 114 us, 5.0 TB/s; with sqrt, scaled copies for the codes and
+// tails that index registers 135 us).
 #include <algorithm>
 
 #include "common.h"
@@ -38,8 +41,16 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 
 // 2^k as a float64, -1023 < k < 1024.
 __device__ __forceinline__ double pow2(int k) { return __longlong_as_double((long long)(k + 1023) << 52); }
-// floor(log2(v)) of a normal v > 0 (very small otherwise).
-__device__ __forceinline__ int log2_of(double v) { return (int)((__double_as_longlong(v) >> 52) & 0x7ff) - 1023; }
+// The upper half of |v|: its exponent + 1023 from bit 20 on, 20 bits of its fraction below.
+__device__ __forceinline__ int upper(double v) { return (int)(__double_as_longlong(v) >> 32) & 0x7fffffff; }
+constexpr int kInf = 0x7ff00000;   // of what is not finite, at least
+
+// sqrt(v) to float64's precision, v 0 or more and a normal number: a start good to 2^-22,
+// and the third-order step of 1 / sqrt(1 - d).  Not finite: NaN.
+__device__ __forceinline__ double root_of(double v) {
+  const double y = __builtin_amdgcn_rsq(v), r = v * y, d = fma(-r, y, 1.0);
+  return v == 0 ? 0 : fma(r * d, fma(0.375, d, 0.5), r);
+}
 
 // Largest of the 16 lanes that share a block.
 __device__ __forceinline__ int max16(int v) {
@@ -48,15 +59,24 @@ __device__ __forceinline__ int max16(int v) {
   return v;
 }
 
-// The code of |v| for a block of exponent byte e; r: 16 random bits.
-__device__ __forceinline__ uint32_t encode(double v, int e, uint32_t r) {
-  const double t = fabs(v) * pow2(134 - e);
-  const int k = max(log2_of(t), -6);
-  return ((k + 6) << 3) + (uint32_t)(t * pow2(3 - k) + (r + 0.5) * 0x1p-16);
-}
+// The codes of a block of exponent byte e.  A code's exponent and three bits of fraction
+// lie on top of a float64's, and the next 17 bits of the upper half are how far a value
+// lies between two codes: 16 random bits r and a half are added there, and what carries
+// over rounds up.  The least normal code added to what lies below it has codes' equal
+// steps there too.
+struct Coder {
+  double least;
+  int top, off;
+  __device__ __forceinline__ explicit Coder(int e) : least(pow2(e - 140)), top((e - 140 + 1023) << 20), off(8 * (e - 140 + 1022)) {}
+  __device__ __forceinline__ uint32_t of(double v, uint32_t r) const {
+    const bool low = upper(v) < top;
+    const double s = fabs(v) + least;
+    return (((uint32_t)(low ? upper(s) : upper(v)) + 2 * r + 1) >> 17) - (low ? off + 8 : off);
+  }
+};
 
 struct AdamK {
-  double beta1, beta2;
+  double beta1, beta2, gain1, gain2;   // gain: 1 - beta
   float rate, eps, keep, c1, rc2;
 };
 
@@ -79,32 +99,38 @@ __global__ __launch_bounds__(kT) void adamw8_k(List l, AdamK a) {
     *(float4*)w = *(const float4*)(t.w + i);
     *(float4*)(w + 4) = *(const float4*)(t.w + i + 4);
   } else {
-    for (int z = 0; z < n; ++z) {
+#pragma unroll
+    for (int z = 0; z < 8; ++z) {
+      if (z >= n) continue;
       g[z] = t.grad[i + z];
       w[z] = t.w[i + z];
       m8 |= (uint64_t)t.m[i + z] << (8 * z);
       r8 |= (uint64_t)t.root[i + z] << (8 * z);
     }
   }
-  const double sm = pow2((int)(ex & 255) - 134), sr = pow2((int)(ex >> 8) - 134);
+  // (squares of codes are exact in float32)
+  const double sr = pow2((int)(ex >> 8) - 134);
+  const double km = a.beta1 * pow2((int)(ex & 255) - 134), kr = a.beta2 * (sr * sr);
   double m[8], r[8];
-  int em = -4096, er = -4096;
+  int em = 0, er = 0;
 #pragma unroll
   for (int z = 0; z < 8; ++z) {
-    const double mo = __builtin_amdgcn_cvt_f32_fp8((int)(m8 >> (8 * z)) & 255, 0) * sm;
-    const double ro = __builtin_amdgcn_cvt_f32_fp8((int)(r8 >> (8 * z)) & 255, 0) * sr;
+    const float mo = __builtin_amdgcn_cvt_f32_fp8((int)(m8 >> (8 * z)) & 255, 0);
+    const float ro = __builtin_amdgcn_cvt_f32_fp8((int)(r8 >> (8 * z)) & 255, 0);
     const double gz = g[z];
-    m[z] = a.beta1 * mo + (1 - a.beta1) * gz;
-    r[z] = sqrt(a.beta2 * (ro * ro) + (1 - a.beta2) * (gz * gz));
+    m[z] = fma((double)mo, km, a.gain1 * gz);
+    r[z] = root_of(fma((double)(ro * ro), kr, a.gain2 * (gz * gz)));
     w[z] = w[z] * a.keep - a.rate * (((float)m[z] * a.c1) / ((float)r[z] * a.rc2 + a.eps));
-    if (m[z] != 0 && isfinite(m[z])) em = max(em, log2_of(fabs(m[z])));
-    if (r[z] != 0 && isfinite(r[z])) er = max(er, log2_of(r[z]));
+    const int um = upper(m[z]), ur = upper(r[z]);
+    em = max(em, um < kInf ? um : 0);
+    er = max(er, ur < kInf ? ur : 0);
   }
   em = max16(em);
   er = max16(er);
   // 0: nothing but zeros
-  em = em == -4096 ? 0 : min(max(em + 127, 1), 254);
-  er = er == -4096 ? 0 : min(max(er + 127, 1), 254);
+  em = em == 0 ? 0 : min(max((em >> 20) - 896, 1), 254);
+  er = er == 0 ? 0 : min(max((er >> 20) - 896, 1), 254);
+  const Coder cm8(em), cr8(er);
   const uint64_t at = (uint64_t)l.first[k] * kPer + i;
   const uint32_t key = l.key[k] + 0x9e3779b1u * (uint32_t)(at >> 32);
   uint64_t mn = 0, rn = 0;
@@ -112,8 +138,8 @@ __global__ __launch_bounds__(kT) void adamw8_k(List l, AdamK a) {
   for (int z = 0; z < 8; ++z) {
     const uint32_t bits = mix((uint32_t)(at + z) ^ key);
     uint32_t cm = 0x7f, cr = 0x7f;
-    if (isfinite(m[z])) cm = encode(m[z], em, bits & 0xffff) | (signbit(m[z]) ? 0x80 : 0);
-    if (isfinite(r[z])) cr = r[z] > 0 ? max(encode(r[z], er, bits >> 16), 1u) : 0;
+    if (upper(m[z]) < kInf) cm = cm8.of(m[z], bits & 0xffff) | ((uint32_t)(__double_as_longlong(m[z]) >> 56) & 0x80);
+    if (upper(r[z]) < kInf) cr = upper(r[z]) > 0 ? max(cr8.of(r[z], bits >> 16), 1u) : 0;
     mn |= (uint64_t)cm << (8 * z);
     rn |= (uint64_t)cr << (8 * z);
   }
@@ -127,11 +153,13 @@ __global__ __launch_bounds__(kT) void adamw8_k(List l, AdamK a) {
     if (w16) {
       uint32_t d[4];
 #pragma unroll
-      for (int z = 0; z < 4; ++z) d[z] = f2bf(w[2 * z]) | (f2bf(w[2 * z + 1]) << 16);
+      for (int z = 0; z < 4; ++z) d[z] = pack_bf16(w[2 * z], w[2 * z + 1]);
       *(uint4*)(w16 + i) = make_uint4(d[0], d[1], d[2], d[3]);
     }
   } else {
-    for (int z = 0; z < n; ++z) {
+#pragma unroll
+    for (int z = 0; z < 8; ++z) {
+      if (z >= n) continue;
       t.m[i + z] = (uint8_t)(mn >> (8 * z));
       t.root[i + z] = (uint8_t)(rn >> (8 * z));
       t.w[i + z] = w[z];
@@ -145,7 +173,7 @@ __global__ __launch_bounds__(kT) void adamw8_k(List l, AdamK a) {
 hipError_t adamw8_step(int n, const tgp_adamw8_tensor* t, float rate, double beta1, double beta2,
                        float eps, float decay, float c1, float rc2, uint64_t seed, hipStream_t st) {
   constexpr int kMost = 1 << 20;   // blocks of a launch
-  const AdamK a{beta1, beta2, rate, eps, 1.f - decay, c1, rc2};
+  const AdamK a{beta1, beta2, 1 - beta1, 1 - beta2, rate, eps, 1.f - decay, c1, rc2};
   List l;
   l.count = 0;
   int blocks = 0;
