@@ -545,15 +545,19 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
         fetch(g0 * a.group + t, in, m);
         row(g0 * a.group + t, in, m, u1, u2);
       }
+      if constexpr (!BLK)
+        for (int o = sh.G; o < sh.G * side; o <<= 1)
+#pragma unroll
+          for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              u1[k][v] += __shfl_xor(u1[k][v], o);
+              u2[k][v] += __shfl_xor(u2[k][v], o);
+            }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          if constexpr (!BLK)
-            for (int o = sh.G; o < sh.G * side; o <<= 1) {
-              u1[k][v] += __shfl_xor(u1[k][v], o);
-              u2[k][v] += __shfl_xor(u2[k][v], o);
-            }
           // every lane of the group has the sums: the first row's takes them on
           sum[2][k][v] += first || !there ? 0.f : q[k][v] * u1[k][v];
           sum[3][k][v] += first || !there ? 0.f : q[k][v] * u2[k][v];
@@ -578,14 +582,18 @@ __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
     __shared__ float ws[3][NV * V][64];
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
+      // (all values of a step together: one waits for LDS as long as twelve)
+      for (int o = sh.G; o < 64; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int v = 0; v < V; ++v) sum[z][k][v] += __shfl_xor(sum[z][k][v], o);
       if (z) __syncthreads();
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          for (int o = sh.G; o < 64; o <<= 1) sum[z][k][v] += __shfl_xor(sum[z][k][v], o);
+        for (int v = 0; v < V; ++v)
           if (wave > 0) ws[wave - 1][k * V + v][lane] = sum[z][k][v];
-        }
       __syncthreads();
       if (wave == 0 && lane < sh.G)
 #pragma unroll
@@ -625,15 +633,31 @@ __device__ __forceinline__ float2 tree_sums(const float* part, int S, int stride
 }
 
 // The gates' gradients from the ranges' partial sums, and S1 and S2 of each gate in
-// the place of U1 and U2 of its first range: sixteen channels of a gate a block, the
-// sums of dz (blockIdx.z = 0) or of G.
-template <typename T>
-__global__ __launch_bounds__(1024) void res_join(float* part, int ranges, const T* gate, long ldgate, Vectors w,
+// the place of U1 and U2 of its first range: the sums of dz (blockIdx.z = 0) or of G.
+// MANY ranges: sixteen channels of a gate a block; else a thread a channel (35 gates of
+// 2528 channels and five ranges: 33.9 us with 64 threads).
+template <typename T, bool MANY>
+__global__ __launch_bounds__(MANY ? 1024 : 256) void res_join(float* part, int ranges, const T* gate, long ldgate, Vectors w,
                                                  int post, T* dgate, long lddgate, int C) {
-  const int l = threadIdx.x & 15, k = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
   float* of = part + (long)blockIdx.y * ranges * 4 * C;
-  const float2 s = tree_sums(of, ranges, 4, C, c, k, l, 2 * blockIdx.z);
-  if (k || c >= C) return;
+  float2 s;
+  int c;
+  if constexpr (MANY) {
+    const int l = threadIdx.x & 15, k = threadIdx.x >> 4;
+    c = blockIdx.x * 16 + l;
+    s = tree_sums(of, ranges, 4, C, c, k, l, 2 * blockIdx.z);
+    if (k || c >= C) return;
+  } else {
+    c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= C) return;
+    s = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int b = 0; b < ranges; ++b) {
+      const float* p = of + (4L * b + 2 * blockIdx.z) * C + c;
+      s.x += p[0];
+      s.y += p[C];
+    }
+  }
   const float g = blockIdx.z ? Elt<T>::ld(gate + blockIdx.y * ldgate + c) : 1.f;
   of[2L * blockIdx.z * C + c] = g * s.x;
   of[(2L * blockIdx.z + 1) * C + c] = g * s.y;
@@ -810,8 +834,9 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
             nullptr, a.s.C, p.g, 1, 1, shared};
   const int rpw = p.g ? 64 / p.g : 1, turn = p.g ? 4 * rpw : 1;
   const long groups = rows / k.group;
-  // blocks that fill the chip, of 24 rows where there are many (each leaves 16 bytes a channel)
-  const long most = std::min<long>(kBlocks, std::max<long>(256, rows / 24));
+  // blocks that fill the chip, of 24 rows where there are many (each leaves 16 bytes a
+  // channel); of eight where a block takes a row at a time and waits for it
+  const long most = std::min<long>(kBlocks, std::max<long>(256, rows / (p.g ? 24 : 8)));
   // whole groups where a wave (block) each fills the chip, or takes one in one turn
   const bool whole = shared && (groups >= (p.g ? 1024 : 512) || k.group <= rpw);
   unsigned grid;
@@ -840,8 +865,14 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   });
   if (join) {
     ProfScope ps("residual_norm_gates", 4.0 * grid * a.s.C, 16.0 * grid * a.s.C, st);
-    TGP_LAUNCH(ps, res_join<T>, dim3(cdiv(a.s.C, 16), (unsigned)groups, 2), dim3(1024), 0, st, a.part, k.ranges,
-               (const T*)a.gate.p, a.gate.ld, vectors(a.w), a.s.post, (T*)a.dgate.p, a.dgate.ld, a.s.C);
+    auto go = [&](auto many) {
+      constexpr bool MANY = decltype(many)::value;
+      TGP_LAUNCH(ps, (res_join<T, MANY>), dim3(cdiv(a.s.C, MANY ? 16 : 256), (unsigned)groups, 2), dim3(MANY ? 1024 : 256),
+                 0, st, a.part, k.ranges, (const T*)a.gate.p, a.gate.ld, vectors(a.w), a.s.post, (T*)a.dgate.p,
+                 a.dgate.ld, a.s.C);
+    };
+    if (k.ranges > 16) go(std::true_type());
+    else go(std::false_type());
   }
   if (sums && join) add_up((int)groups, 4 * k.ranges);
   else if (sums) add_up((int)grid, 4);
