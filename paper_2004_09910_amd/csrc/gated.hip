@@ -826,6 +826,249 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
   }
 }
 
+// Where a range's sums of a weight go: rows of ldp floats at part, its bias's at cols
+// (null: not wanted), as an OuterJob's.
+struct Sink {
+  float *part, *cols;
+  int ldp, n, vec;
+};
+
+struct SlimArgs {
+  const bf16_t *x, *dy, *wg, *wu, *wd;
+  long ldx, lddy, ldw, ldwd;
+  int rows, per, cin, hidden, cout;
+  const float *bg, *bu;
+  Sink to[3];        // Wg, Wu, Wd
+  long stride;
+  int add;
+  bf16_t* dx;
+  long lddx;
+  int vec;
+};
+
+// Everything of a backward pass through at most 64 channels, 256 hidden and 64 again,
+// of bfloat16: a block takes `per` pixels, 64 at a time, and nothing of the hidden
+// channels goes to memory.  A wave has 32 hidden channels; g, u and dh lie in its
+// registers with a lane a hidden channel and pixels one after the other, which is how
+// the weights' gradients' products over pixels take h, dg and du, with the rows of x and
+// dy read from LDS in the order that those have (values j of a lane are pixels 4 (l / 32)
+// + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
+// For dx, dg and du go through LDS, rows of hidden channels beside the weights' rows.
+// What bounds it are the activations and the splitting in two parts, some 60 operations
+// a value of the hidden channels.
+template <int ACT, bool GRADS>
+__global__ __launch_bounds__(512, 2) void slim_k(SlimArgs a) {
+  typedef Feed<64, 64, false, 2> F;   // (its layout: rows of 64 values)
+  constexpr int TILE = 8192, WS = 32768;
+  __shared__ __align__(1024) unsigned char lds[4 * WS + 4 * TILE];
+  unsigned char *const wgs = lds, *const wus = lds + WS, *const dgs = lds + 2 * WS, *const dus = lds + 3 * WS,
+                *const xs = lds + 4 * WS;   // [slot][x, dy]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int lo = blockIdx.x * a.per, hi = min(a.rows, lo + a.per);
+  const unsigned base = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(lds) + wave * 1024);
+  auto desc = [&](const bf16_t* p) __attribute__((always_inline)) {
+    const unsigned long at = (unsigned long)p;
+    return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+  };
+  auto meet = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ring_barrier();
+  };
+  // 64 pixels of x and dy, a KiB a wave each
+  const int row = wave * 8 + lane / 8, q = (lane % 8) ^ F::swz(row);
+  auto send = [&](int i0, int slot) __attribute__((always_inline)) {
+    const int vx[1] = {row < hi - i0 && q * 8 < a.cin ? (int)(row * a.ldx * 2) + q * 16 : kOob};
+    const int vy[1] = {row < hi - i0 && q * 8 < a.cout ? (int)(row * a.lddy * 2) + q * 16 : kOob};
+    dma_n<1, 0>(desc(a.x + i0 * a.ldx), base + 4 * WS + slot * 2 * TILE, vx);
+    dma_n<1, 0>(desc(a.dy + i0 * a.lddy), base + 4 * WS + slot * 2 * TILE + TILE, vy);
+  };
+  {
+    int v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = (wave + 8 * u) * 8 + lane / 8, c = (lane % 8) ^ F::swz(r);
+      v[u] = r < a.hidden && c * 8 < a.cin ? (int)(r * a.ldw * 2) + c * 16 : kOob;
+    }
+    dma_n<4, 8192>(desc(a.wg), base, v);
+    dma_n<4, 8192>(desc(a.wu), base + WS, v);
+  }
+  send(lo, 0);
+  const int hid = 32 * wave + (lane & 31);   // the lane's hidden channel
+  const float bg = a.bg && hid < a.hidden ? a.bg[hid] : 0.f, bu = a.bu && hid < a.hidden ? a.bu[hid] : 0.f;
+  u32x4 wd[4];   // a row of Wd^T
+#pragma unroll
+  for (int h = 0; h < 4; ++h)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      const int c = 16 * h + 8 * half + 2 * z;
+      const unsigned e = hid < a.hidden && c < a.cout ? a.wd[c * a.ldwd + hid] : 0u;
+      const unsigned f = hid < a.hidden && c + 1 < a.cout ? a.wd[(c + 1) * a.ldwd + hid] : 0u;
+      wd[h][z] = e | f << 16;
+    }
+  // reads by columns: rows r0 and r0 + 8 of sixteen, 8 bytes of this lane's part
+  const int r0 = 4 * half + ((lane & 15) >> 2), q0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int at0 = r0 * 128 + ((q0 ^ F::swz(r0)) << 4) + 8 * (lane & 1);
+  const int at8 = (r0 + 8) * 128 + ((q0 ^ F::swz(r0 + 8)) << 4) + 8 * (lane & 1);
+  auto column = [&](const unsigned char* s, int f) __attribute__((always_inline)) {   // f: columns 32 f on
+    const uint2 e = lds_tr16(s + (at0 ^ (64 * f))), g = lds_tr16(s + (at8 ^ (64 * f)));
+    return u32x4{e.x, e.y, g.x, g.y};
+  };
+  f32x16_t sg[2], su[2], sd[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) sg[f] = su[f] = sd[f] = f32x16_t{};
+  float bsg = 0.f, bsu = 0.f, bsd = 0.f;
+  int slot = 0;
+  for (int i0 = lo; i0 < hi; i0 += 64, slot ^= 1) {
+    wait_vmcnt<0>();
+    meet();
+    if (i0 + 64 < hi) send(i0 + 64, slot ^ 1);
+    const unsigned char *const xt = xs + slot * 2 * TILE, *const yt = xt + TILE;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      __builtin_amdgcn_sched_barrier(0);   // one fragment's values at a time: registers
+      f32x16_t g{}, u{}, d{};
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const u32x4 x = F::frag(xt, F::place(32 * i), h), y = F::frag(yt, F::place(32 * i), h);
+        g = mfma32(as_bf16x8(x), as_bf16x8(F::frag(wgs, F::place(32 * wave), h)), g);
+        u = mfma32(as_bf16x8(x), as_bf16x8(F::frag(wus, F::place(32 * wave), h)), u);
+        d = mfma32(as_bf16x8(y), as_bf16x8(wd[h]), d);
+      }
+      const int left = hi - i0 - 32 * i - 4 * half;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float act, slope;
+        act_of<ACT>(g[v] + bg, &act, &slope);
+        const float up = u[v] + bu, dh = d[v];
+        const bool in = 8 * (v / 4) + v % 4 < left;   // (a bias may be infinite)
+        g[v] = in ? dh * up * slope : 0.f;
+        u[v] = in ? dh * act : 0.f;
+        d[v] = in ? act * up : 0.f;
+        bsg += g[v];
+        bsu += u[v];
+      }
+      // 16 pixels' parts of dg, du and h, and their products
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int s16 = (2 * i + k) * 2048;
+        u32x4 part[3][2];
+#pragma unroll
+        for (int m = 0; m < 3; ++m)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const f32x16_t& w = m == 0 ? g : m == 1 ? u : d;
+            const float e = w[8 * k + 2 * z], f = w[8 * k + 2 * z + 1];
+            const unsigned p = pack_bf16(e, f);
+            part[m][0][z] = p;
+            const float he = __uint_as_float(p << 16), hf = __uint_as_float(p & 0xffff0000u);
+            const bool ie = (p & 0x7f80u) == 0x7f80u, jf = (p & 0x7f800000u) == 0x7f800000u;
+            part[m][1][z] = pack_bf16(ie ? 0.f : e - he, jf ? 0.f : f - hf);
+          }
+        if (a.dx) {
+          // pixels 8 (2 k) + 4 half on, and 8 (2 k + 1) + 4 half on
+          const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 4 * i + 2 * k;
+          *(uint2*)(dgs + to + ((c ^ sw) << 4)) = make_uint2(part[0][0][0], part[0][0][1]);
+          *(uint2*)(dgs + to + (((c + 1) ^ sw) << 4)) = make_uint2(part[0][0][2], part[0][0][3]);
+          *(uint2*)(dus + to + ((c ^ sw) << 4)) = make_uint2(part[1][0][0], part[1][0][1]);
+          *(uint2*)(dus + to + (((c + 1) ^ sw) << 4)) = make_uint2(part[1][0][2], part[1][0][3]);
+        }
+        if constexpr (GRADS)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const u32x4 x = column(xt + s16, f), y = column(yt + s16, f);
+#pragma unroll
+          for (int w = 1; w >= 0; --w) {
+            sg[f] = mfma32(as_bf16x8(x), as_bf16x8(part[0][w]), sg[f]);
+            su[f] = mfma32(as_bf16x8(x), as_bf16x8(part[1][w]), su[f]);
+            sd[f] = mfma32(as_bf16x8(part[2][w]), as_bf16x8(y), sd[f]);
+          }
+        }
+      }
+    }
+    // column sums of dy: eight pixels a wave
+    if constexpr (GRADS)
+#pragma unroll
+    for (int z = 0; z < 8; ++z) {
+      const int r = 8 * wave + z;
+      bsd += bf2f(*(const bf16_t*)(yt + r * 128 + (((lane >> 3) ^ F::swz(r)) << 4) + 2 * (lane & 7)));
+    }
+    meet();
+    if (!a.dx) continue;
+    // a fragment of dx a wave, of dg Wg (waves 0 to 3) or du Wu
+    const int pf = wave >> 1 & 1, cf = wave & 1;
+    const unsigned char *const ds = wave < 4 ? dgs : dus, *const ws = wave < 4 ? wgs : wus;
+    f32x16_t o{};
+#pragma unroll 2
+    for (int h = 0; h < 16; ++h)
+      o = mfma32(as_bf16x8(column(ws + h * 2048, cf)), as_bf16x8(column(ds + h * 2048, pf)), o);
+    meet();
+    float* const half2 = (float*)dgs + (wave & 3) * 1024 + lane;
+    if (wave >= 4)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) half2[v * 64] = o[v];
+    meet();
+    if (wave < 4) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[v] += half2[v * 64];
+      const float none[16] = {};
+      const int r = i0 + 32 * pf + (lane & 31);
+      put_out<bf16_t>(o, none, a.dx + r * a.lddx, r < hi, 32 * cf, a.cin, a.vec);
+    }
+  }
+  if constexpr (!GRADS) return;
+  // the sums: rows of hidden channels (of Wd's: of cout), a lane each
+  const long off = blockIdx.x * a.stride;
+  auto put4 = [&](const Sink& t, int r, int c, float4 v) __attribute__((always_inline)) {
+    float* to = t.part + off + (long)r * t.ldp + c;
+    if (t.vec) {
+      if (c >= t.ldp) return;
+      if (a.add) {
+        const float4 e = *(const float4*)to;
+        v = make_float4(e.x + v.x, e.y + v.y, e.z + v.z, e.w + v.w);
+      }
+      *(float4*)to = v;
+    } else {
+      const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        if (c + z < t.n) to[z] = a.add ? to[z] + w[z] : w[z];
+    }
+  };
+  auto put_col = [&](const Sink& t, int r, int n, float v) __attribute__((always_inline)) {
+    if (!t.cols || r >= n) return;
+    float* to = t.cols + off + r;
+    *to = a.add ? *to + v : v;
+  };
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = 32 * f + 8 * g + 4 * half, r = 32 * f + (lane & 31), ch = 32 * wave + 8 * g + 4 * half;
+      if (a.to[0].part && hid < a.hidden)
+        put4(a.to[0], hid, c, make_float4(sg[f][4 * g], sg[f][4 * g + 1], sg[f][4 * g + 2], sg[f][4 * g + 3]));
+      if (a.to[1].part && hid < a.hidden)
+        put4(a.to[1], hid, c, make_float4(su[f][4 * g], su[f][4 * g + 1], su[f][4 * g + 2], su[f][4 * g + 3]));
+      if (a.to[2].part && r < a.cout)
+        put4(a.to[2], r, ch, make_float4(sd[f][4 * g], sd[f][4 * g + 1], sd[f][4 * g + 2], sd[f][4 * g + 3]));
+    }
+  bsg += __shfl_xor(bsg, 32);
+  bsu += __shfl_xor(bsu, 32);
+  if (lane < 32) {
+    put_col(a.to[0], hid, a.hidden, bsg);
+    put_col(a.to[1], hid, a.hidden, bsu);
+  }
+  meet();   // every wave is done with dgs
+  float* const cols = (float*)dgs;
+  cols[wave * 64 + lane] = bsd;
+  meet();
+  if (wave) return;
+  float t = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) t += cols[w * 64 + lane];
+  put_col(a.to[2], lane, a.cout, t);
+}
+
 // to (+)= the ranges' partial sums, in order.
 struct SumJob {
   const float* part;
@@ -909,6 +1152,7 @@ struct Plan {
   int parts, low;        // of a factor; of h, dg and du (backward)
   long cinp, hidp, coutp;
   long chunk;            // pixels at a time
+  bool slim;             // a backward pass in one launch
   int wide;              // the weights' gradients' tiles
   int ranges, per;       // of the pixels of a chunk, at most
   long stride;           // floats of a range's partial sums
@@ -948,6 +1192,8 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
                                    : p.parts * (p.hidp + p.cinp));
   const long most = (long)128 << 20;
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
+  p.slim = backward && s.dtype == TGP_BF16 && s.cin <= 64 && s.cout <= 64 && s.hidden <= 256;
+  if (p.slim) p.chunk = std::min(rows, 1l << 22);   // (nothing lies between launches)
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -962,9 +1208,10 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
     p.h = take((size_t)2 * p.parts * p.chunk * p.hidp);
   } else {
     p.dy = take((size_t)2 * p.parts * p.chunk * p.coutp);
-    p.h = take((size_t)2 * p.low * p.chunk * p.hidp);
-    p.dg = take((size_t)2 * p.low * p.chunk * p.hidp);
-    p.du = take((size_t)2 * p.low * p.chunk * p.hidp);
+    const size_t plane = p.slim ? 0 : (size_t)2 * p.low * p.chunk * p.hidp;
+    p.h = take(plane);
+    p.dg = take(plane);
+    p.du = take(plane);
     auto tiles = [&](long t) { return 2 * cdiv(s.hidden, t) * (long)cdiv(s.cin, t) + cdiv(s.cout, t) * (long)cdiv(s.hidden, t); };
     const long large = tiles(128);
     // as large as leave enough of them, with the ranges' help, and are not mostly padding
@@ -972,8 +1219,9 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
     p.wide = 8 * 4 * x <= 9 * large && 4 * x * runs >= 3 * kFill ? 256 : large * runs >= kFill ? 128 : 64;
     const long n = tiles(p.wide), fill = p.wide == 256 ? kFill : 2 * kFill;
     // ranges of four stages at least, as many as fill the chip; one where the tiles do
-    const long want = 4 * n >= 3 * kFill ? 1 : std::max<long>(1, std::min<long>(fill / n, p.chunk / 256));
-    p.per = (int)round_up((p.chunk + want - 1) / want, 64);
+    const long want = p.slim ? std::min<long>(kFill, cdiv(p.chunk, 64))
+                      : 4 * n >= 3 * kFill ? 1 : std::max<long>(1, std::min<long>(fill / n, p.chunk / 256));
+    p.per = (int)round_up((p.chunk + want - 1) / std::max<long>(want, 1), 64);
     p.ranges = ranges_of(p.chunk, p.per);
     p.stride = 2 * (long)s.hidden * round_up(s.cin, 4) + (long)s.cout * round_up(s.hidden, 4) +
                2 * round_up(s.hidden, 4) + round_up(s.cout, 4);
@@ -1243,11 +1491,57 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
   const Matrix wd = c.operand(g.w.down, s.hidden, s.cout, s.hidden, p.wd, s.cout);
   const Matrix h = matrix_at(ws, p.h, L, p.chunk, p.hidp), dg = matrix_at(ws, p.dg, L, p.chunk, p.hidp),
                du = matrix_at(ws, p.du, L, p.chunk, p.hidp);
+  auto add_up = [&](SumArgs& m) {
+    const bool deep = m.ranges >= 8;
+    int sb = 0;
+    for (int k = 0; k < m.jobs; ++k) {
+      m.j[k].blk0 = sb;
+      sb += cdiv((long)m.j[k].rows * (m.j[k].ldp / 4), deep ? 64 : 256);
+    }
+    ProfScope ps("gated_sum", 0, 4.0 * m.ranges * p.stride, st);
+    if (deep) TGP_LAUNCH(ps, sum_k<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
+    else TGP_LAUNCH(ps, sum_k<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
+  };
   for (long r0 = 0; r0 < g.rows; r0 += p.chunk) {
     const long rows = std::min(p.chunk, g.rows - r0);
     const Matrix xm = c.operand(x + r0 * ldx, ldx, rows, s.cin, p.x, p.chunk);
     const Matrix dym = c.operand(dy + r0 * lddy, lddy, rows, s.cout, p.dy, p.chunk);
     if (hipError_t e = c.flush(); e != hipSuccess) return e;
+    if constexpr (sizeof(T) == 2) {
+      if (p.slim) {
+        SumArgs m{};
+        m.ranges = ranges_of(rows, p.per);
+        m.stride = p.stride;
+        m.add = !overwrite || r0 > 0;
+        const bool direct = p.ranges == 1;
+        float* at = (float*)((char*)ws + p.part);
+        auto sink = [&](int rows_w, int cols_w, float* w, float* b) {
+          const int ldp = (int)round_up(cols_w, 4);
+          const Sink t = direct ? Sink{w, b, cols_w, cols_w, at16(w, cols_w, 4)}
+                                : Sink{w ? at : nullptr, b ? at + (long)rows_w * ldp : nullptr, ldp, cols_w, 1};
+          if (w) m.j[m.jobs++] = {t.part, w, rows_w, cols_w, ldp, 0};
+          if (b) m.j[m.jobs++] = {t.cols, b, 1, rows_w, (int)round_up(rows_w, 4), 0};
+          at += (long)rows_w * ldp + round_up(rows_w, 4);
+          return t;
+        };
+        SlimArgs a{xm.part[0], dym.part[0], wg.part[0], wu.part[0], wd.part[0], xm.ld, dym.ld, wg.ld, wd.ld, (int)rows,
+                   p.per, s.cin, s.hidden, s.cout, g.w.b_gate, g.w.b_up, {}, p.stride, direct && m.add,
+                   dx ? dx + r0 * lddx : nullptr, lddx, 0};
+        a.vec = at16(a.dx, lddx, 2);
+        a.to[0] = sink(s.hidden, s.cin, gr.gate, gr.b_gate);
+        a.to[1] = sink(s.hidden, s.cin, gr.up, gr.b_up);
+        a.to[2] = sink(s.cout, s.hidden, gr.down, gr.b_down);
+        with_act(s.act, [&](auto act) {
+          ProfScope ps("gated_slim", 2.0 * rows * (8 * s.cin + 3 * s.cout) * s.hidden,
+                       2.0 * rows * (2 * s.cin + s.cout) + 4.0 * m.ranges * p.stride, st);
+          constexpr int ACT = decltype(act)::value;
+          if (grads) TGP_LAUNCH(ps, (slim_k<ACT, true>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
+          else TGP_LAUNCH(ps, (slim_k<ACT, false>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
+        });
+        if (grads && !direct) add_up(m);
+        continue;
+      }
+    }
     HiddenArgs a = hidden_args(c, xm, wg, wu, rows);
     add_pairs(&a.d, dym, P, wd, P);
     a.lddy = dym.ld;
@@ -1325,17 +1619,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
         else if (p.wide == 128) TGP_LAUNCH(ps, outer_k<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
         else TGP_LAUNCH(ps, outer_k<OuterX>, dim3((unsigned)blocks), dim3(OuterX::T), 0, st, o);
       }
-      if (!direct) {
-        const bool deep = m.ranges >= 8;
-        int sb = 0;
-        for (int k = 0; k < m.jobs; ++k) {
-          m.j[k].blk0 = sb;
-          sb += cdiv((long)m.j[k].rows * (m.j[k].ldp / 4), deep ? 64 : 256);
-        }
-        ProfScope ps("gated_sum", 0, 4.0 * m.ranges * p.stride, st);
-        if (deep) TGP_LAUNCH(ps, sum_k<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
-        else TGP_LAUNCH(ps, sum_k<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
-      }
+      if (!direct) add_up(m);
     }
     if (dx) {   // last: it may be written over x or dy
       OutArgs o{};
