@@ -933,6 +933,7 @@ __global__ __launch_bounds__(512, 2) void slim_k(SlimArgs a) {
         g = mfma32(as_bf16x8(x), as_bf16x8(F::frag(wgs, F::place(32 * wave), h)), g);
         u = mfma32(as_bf16x8(x), as_bf16x8(F::frag(wus, F::place(32 * wave), h)), u);
         d = mfma32(as_bf16x8(y), as_bf16x8(wd[h]), d);
+        if (h & 1) __builtin_amdgcn_sched_barrier(0);
       }
       const int left = hi - i0 - 32 * i - 4 * half;
 #pragma unroll
@@ -952,37 +953,39 @@ __global__ __launch_bounds__(512, 2) void slim_k(SlimArgs a) {
       for (int k = 0; k < 2; ++k) {
         __builtin_amdgcn_sched_barrier(0);
         const int s16 = (2 * i + k) * 2048;
-        u32x4 part[3][2];
+        // pixels 8 (2 k) + 4 half on, and 8 (2 k + 1) + 4 half on
+        const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 4 * i + 2 * k;
 #pragma unroll
-        for (int m = 0; m < 3; ++m)
+        for (int m = 0; m < 3; ++m) {
+          u32x4 top, low;
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             const f32x16_t& w = m == 0 ? g : m == 1 ? u : d;
             const float e = w[8 * k + 2 * z], f = w[8 * k + 2 * z + 1];
             const unsigned p = pack_bf16(e, f);
-            part[m][0][z] = p;
+            top[z] = p;
             const float he = __uint_as_float(p << 16), hf = __uint_as_float(p & 0xffff0000u);
             const bool ie = (p & 0x7f80u) == 0x7f80u, jf = (p & 0x7f800000u) == 0x7f800000u;
-            part[m][1][z] = pack_bf16(ie ? 0.f : e - he, jf ? 0.f : f - hf);
+            low[z] = pack_bf16(ie ? 0.f : e - he, jf ? 0.f : f - hf);
           }
-        if (a.dx) {
-          // pixels 8 (2 k) + 4 half on, and 8 (2 k + 1) + 4 half on
-          const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 4 * i + 2 * k;
-          *(uint2*)(dgs + to + ((c ^ sw) << 4)) = make_uint2(part[0][0][0], part[0][0][1]);
-          *(uint2*)(dgs + to + (((c + 1) ^ sw) << 4)) = make_uint2(part[0][0][2], part[0][0][3]);
-          *(uint2*)(dus + to + ((c ^ sw) << 4)) = make_uint2(part[1][0][0], part[1][0][1]);
-          *(uint2*)(dus + to + (((c + 1) ^ sw) << 4)) = make_uint2(part[1][0][2], part[1][0][3]);
-        }
-        if constexpr (GRADS)
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const u32x4 x = column(xt + s16, f), y = column(yt + s16, f);
-#pragma unroll
-          for (int w = 1; w >= 0; --w) {
-            sg[f] = mfma32(as_bf16x8(x), as_bf16x8(part[0][w]), sg[f]);
-            su[f] = mfma32(as_bf16x8(x), as_bf16x8(part[1][w]), su[f]);
-            sd[f] = mfma32(as_bf16x8(part[2][w]), as_bf16x8(y), sd[f]);
+          if (m < 2 && a.dx) {
+            unsigned char* const ds = m ? dus : dgs;
+            *(uint2*)(ds + to + ((c ^ sw) << 4)) = make_uint2(top[0], top[1]);
+            *(uint2*)(ds + to + (((c + 1) ^ sw) << 4)) = make_uint2(top[2], top[3]);
           }
+          if constexpr (GRADS)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const u32x4 x = column((m < 2 ? xt : yt) + s16, f);
+#pragma unroll
+              for (int w = 1; w >= 0; --w) {
+                const bf16x8_t e = as_bf16x8(w ? low : top);
+                if (m == 0) sg[f] = mfma32(as_bf16x8(x), e, sg[f]);
+                else if (m == 1) su[f] = mfma32(as_bf16x8(x), e, su[f]);
+                else sd[f] = mfma32(e, as_bf16x8(x), sd[f]);
+              }
+            }
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
