@@ -71,7 +71,9 @@ KERNEL_FILES = {
     "conv1x1_res": "conv_mfma.hip", "conv_fwd_dma": "conv_mfma.hip",
     "conv_wgrad_mfma": "conv_mfma.hip", "splitk_reduce": "conv_mfma.hip",
     "wtransform": "conv_mfma.hip", "norm_": "layer_norm.hip", "muon_": "muon.hip",
-    "weight_step": "weight_step.hip", "adamw": "weight_step.hip", "": "elementwise.hip",
+    "weight_step": "weight_step.hip", "adamw": "weight_step.hip",
+    "adamw8": "adamw8.hip", "gated_": "gated.hip", "res_": "residual_norm.hip", "residual_norm": "residual_norm.hip",
+    "": "elementwise.hip",
 }
 
 

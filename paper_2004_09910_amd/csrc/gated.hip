@@ -1,13 +1,18 @@
 // A gated feed-forward block over the channels of each pixel, forward and
 // backward: y = (act(x Wg^T + bg) * (x Wu^T + bu)) Wd^T + bd.
 //
-// Forward: one launch has both projections of a tile of hidden channels in
-// registers and leaves h = act(g) u; a second multiplies it by Wd^T.
+// Forward: up to 256 channels (float32: 128) on both sides one launch (gated_narrow) keeps a
+// tile's hidden channels in LDS; for at most 64 pixels two (gated_few) read the weights
+// once, straight into registers; else one launch has both projections of a tile of
+// hidden channels in registers and leaves h = act(g) u, and a second multiplies it by
+// Wd^T.
 // Backward, from x and dy: one launch has g, u and dh = dy Wd of a tile and leaves
-// h, dg = dh u act'(g) and du = dh act(g); one takes dx = dg Wg + du Wu as one sum
-// over twice the hidden channels; one takes the three weight gradients, sums over
-// pixels, in ranges whose partial tiles the last adds up in order, together
-// with the column sums of dg, du and dy (a product of the left factor with ones).
+// h, dg = dh u act'(g) and du = dh act(g); one takes the three weight gradients, sums
+// over pixels, together with the column sums of dg, du and dy (a product of the left
+// factor with ones), where the tiles are few in ranges whose partial sums another adds
+// up in order; one takes dx = dg Wg + du Wu as one sum over twice the hidden channels.
+// Up to 64 channels on both sides and 256 hidden ones of bfloat16 all that is one launch
+// (gated_slim) and the ranges' sums.
 //
 // Matrix instructions take bfloat16.  Of a TGP_BF16 network x, dy and the weights
 // are that; h, dg and du are rounded once for y and dx, which are rounded to
@@ -63,7 +68,7 @@ struct Copies {
 // Memory bounds it: eight values a thread.  A float32 is split by rounding to
 // bfloat16 and rounding what is left; an infinity or NaN has no rest.
 template <typename T>
-__global__ __launch_bounds__(kT) void copy_k(Copies c) {
+__global__ __launch_bounds__(kT) void gated_copy(Copies c) {
   int k = 0;
   while (k + 1 < c.n && (long)blockIdx.x >= c.j[k + 1].blk0) ++k;
   const CopyJob j = c.j[k];
@@ -159,7 +164,7 @@ __device__ __forceinline__ void biases(const float* b, int c, int n, float (&v)[
 
 // h of a tile.  P: parts of a factor.
 template <typename PR, int ACT, int P>
-__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void hidden_k(HiddenArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_hidden(HiddenArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
   int ti, tj;
   tile_of(xcd_remap(blockIdx.x, gridDim.x), a.tm, a.tn, &ti, &tj);
@@ -191,7 +196,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 // h, dg and du of a tile, each in P parts (one, and no h, where no weight's gradient
 // is wanted).
 template <typename PR, typename PD, int ACT, int P, bool GRADS>
-__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void back_k(HiddenArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_back(HiddenArgs a) {
   static_assert(PR::BM == PD::BM && PR::BN == PD::BN && PR::MT == PD::MT && PR::WN == PD::WN, "one tile");
   __shared__ __align__(1024) unsigned char ring[PR::LDS > PD::LDS ? PR::LDS : PD::LDS];
   int ti, tj;
@@ -288,7 +293,7 @@ __device__ __forceinline__ void put_out(const f32x16_t& acc, const float (&b)[16
 
 // SPLIT: ranges of `per` of the sum, each into rows of its own at part.
 template <typename PR, typename T, bool SPLIT>
-__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void out_k(OutArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_out(OutArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
   const int tiles = a.tm * a.tn, blk = xcd_remap(blockIdx.x, gridDim.x), q = SPLIT ? blk / tiles : 0;
   const int k0 = SPLIT ? q * a.per : 0, k1 = SPLIT ? min(a.k, k0 + a.per) : a.k;
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 
 // y = the ranges' sums, in order, + bias; four columns a thread.
 template <typename T>
-__global__ __launch_bounds__(kT) void join_k(OutArgs a, int ranges) {
+__global__ __launch_bounds__(kT) void gated_join(OutArgs a, int ranges) {
   const int per = a.ldp / 4, e = blockIdx.x * kT + threadIdx.x, r = e / per, c = (e - r * per) * 4;
   if (r >= a.rows) return;
   const float* p = a.part + (long)r * a.ldp + c;
@@ -382,7 +387,7 @@ __device__ __forceinline__ void wave_biases(const float* b, int c, int n, float 
 // that of rows of 64), and a wave that sends four at once waits that long.  12544 x
 // 256, 1024 hidden channels: 58 us with the loads before the products.
 template <int P, int KSX, int NW, int CG, int ACT, typename T>
-__global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void narrow_k(NarrowArgs a) {
+__global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowArgs a) {
   // from three stages of 64 channels on the pixels stay in LDS, which leaves the ring
   // less, and the fragments of one are in registers: all of them spill
   constexpr bool XL = P == 1 && KSX >= 3;
@@ -681,9 +686,10 @@ struct FewArgs {
 // matrices (two: h, else y).  Weights are read once, straight into fragments, and what
 // bounds it is how many of their loads are on their way at a time: as many waves as a
 // block has, and blocks of fewer channels (the other rows of their fragments are zeros)
-// where 32 each leave CUs without one.
+// where 32 each leave CUs without one (1 x 1024 through 4096 and back 23.8 us, with 32
+// channels a block 41; its 24 MB come in at 1.0 TB/s).
 template <typename T, int M, int MF, int NW, int ACT>
-__global__ __launch_bounds__(64 * NW) void few_k(FewArgs a) {
+__global__ __launch_bounds__(64 * NW) void gated_few(FewArgs a) {
   constexpr int U = M == 1 && MF == 1 && sizeof(T) == 2 ? 8 : 4;   // steps of 16 whose loads go out together
   __shared__ float red[NW][M * MF][16][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -772,7 +778,7 @@ struct OuterArgs {
 };
 
 template <typename PR>
-__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void outer_k(OuterArgs a) {
+__global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_outer(OuterArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
   const int blk = xcd_remap(blockIdx.x, gridDim.x);
   int k = 0;
@@ -855,9 +861,10 @@ struct SlimArgs {
 // + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
 // For dx, dg and du go through LDS, rows of hidden channels beside the weights' rows.
 // What bounds it are the activations and the splitting in two parts, some 60 operations
-// a value of the hidden channels.
+// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 134 us and 11 for the
+// ranges' sums; by a launch for h, dg and du, one for the weights and one for dx 365).
 template <int ACT, bool GRADS>
-__global__ __launch_bounds__(512, 2) void slim_k(SlimArgs a) {
+__global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
   typedef Feed<64, 64, false, 2> F;   // (its layout: rows of 64 values)
   constexpr int TILE = 8192, WS = 32768;
   __shared__ __align__(1024) unsigned char lds[4 * WS + 4 * TILE];
@@ -1086,7 +1093,7 @@ struct SumArgs {
 
 // Four columns a thread; with many ranges four waves share them (WAVES = 4).
 template <int WAVES>
-__global__ __launch_bounds__(256) void sum_k(SumArgs a) {
+__global__ __launch_bounds__(256) void gated_sum(SumArgs a) {
   __shared__ float4 sh[WAVES][64];
   int k = 0;
   while (k + 1 < a.jobs && (int)blockIdx.x >= a.j[k + 1].blk0) ++k;
@@ -1124,15 +1131,21 @@ __global__ __launch_bounds__(256) void sum_k(SumArgs a) {
     if (c + z < j.n) to[z] = a.add ? to[z] + v[z] : v[z];
 }
 
-__global__ void zero_k(float* p, long n) {
+__global__ void gated_zero(float* p, long n) {
   const long i = (long)blockIdx.x * kT + threadIdx.x;
   if (i < n) p[i] = 0.f;
 }
 
 // ------------------------------------------------- plans
 
-// Large and small tiles of each launch; the large ones of y and dx with a deep ring, a
-// block a CU, and with a shallow one, two.
+// Large and small tiles of each launch.  A CU takes 55 bytes a clock from DMA, so a stage
+// of 128 x 128 tiles (64 values, 32 KB, 582 clocks) comes in slower than its 512 clocks of
+// products: tiles of 256 rows where there are enough of them.  4096 pixels x 1024, 4096
+// hidden: h 84 us (815 TFLOP/s; tiles of 128 x 128, two blocks a CU, 90), h, dg and du
+// 148 (two blocks of 128 x 64 a CU 163), the weights' gradients 213 (967; 128 x 128 255),
+// y 50 and dx 78 (885).  Stages of 32 pixels where both factors are read by columns: the
+// fragments of one of 64 spill (787).  y and dx of 128 x 128 with a deep ring, a block a
+// CU, and with a shallow one, two.
 typedef Product<2, 2, 4, 2, 64, 2, false, false, 2> HidL;
 typedef Product<1, 1, 2, 2, 64, 3, false, false, 2> HidS;
 typedef Product<2, 1, 2, 4, 64, 3, false, false, 2> BackL;
@@ -1166,7 +1179,7 @@ int ranges_of(long rows, int per) { return (int)((rows + per - 1) / per); }
 
 // A long sum for few tiles of 64 x 64: ranges of `per` of its k values, four stages each
 // at least, that the tiles' blocks fill the chip with; their partial sums are joined by a
-// launch of its own (144 x 1024, k 4096: 20.6 us as 48 blocks).
+// launch of its own (144 x 1024, k 4096: 20.6 us as 48 blocks, 7.5 and 4 as 240).
 struct Split {
   int n, per;
 };
@@ -1281,8 +1294,8 @@ struct Call {
   hipError_t flush() {
     if (!copies.n) return hipSuccess;
     ProfScope ps("gated_copy", 0, copy_bytes, st);
-    if (g.s.dtype == TGP_BF16) TGP_LAUNCH(ps, copy_k<bf16_t>, dim3((unsigned)copy_blocks), dim3(kT), 0, st, copies);
-    else TGP_LAUNCH(ps, copy_k<float>, dim3((unsigned)copy_blocks), dim3(kT), 0, st, copies);
+    if (g.s.dtype == TGP_BF16) TGP_LAUNCH(ps, gated_copy<bf16_t>, dim3((unsigned)copy_blocks), dim3(kT), 0, st, copies);
+    else TGP_LAUNCH(ps, gated_copy<float>, dim3((unsigned)copy_blocks), dim3(kT), 0, st, copies);
     copies.n = 0;
     copy_blocks = 0;
     copy_bytes = 0;
@@ -1310,7 +1323,7 @@ void launch_out(const char* name, OutArgs a, hipStream_t st) {
   a.tm = cdiv(a.rows, PR::BM);
   a.tn = cdiv(a.n, PR::BN);
   ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * (a.k + a.n), st);
-  TGP_LAUNCH(ps, (out_k<PR, T, false>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
+  TGP_LAUNCH(ps, (gated_out<PR, T, false>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
 }
 
 // y or dx, by the number of tiles: more than a block a CU (two shallow rings, 147456 x 64
@@ -1330,10 +1343,10 @@ void launch_sum(const char* name, const char* name_join, OutArgs a, void* join, 
   a.tn = cdiv(a.n, PRS::BN);
   {
     ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * a.k + 4.0 * d.n * a.rows * a.n, st);
-    TGP_LAUNCH(ps, (out_k<PRS, T, true>), dim3((unsigned)a.tm * a.tn * d.n), dim3(PRS::T), 0, st, a);
+    TGP_LAUNCH(ps, (gated_out<PRS, T, true>), dim3((unsigned)a.tm * a.tn * d.n), dim3(PRS::T), 0, st, a);
   }
   ProfScope ps(name_join, 0, (4.0 * d.n + 2) * a.rows * a.n, st);
-  TGP_LAUNCH(ps, join_k<T>, dim3((unsigned)cdiv((long)a.rows * (a.ldp / 4), kT)), dim3(kT), 0, st, a, d.n);
+  TGP_LAUNCH(ps, gated_join<T>, dim3((unsigned)cdiv((long)a.rows * (a.ldp / 4), kT)), dim3(kT), 0, st, a, d.n);
 }
 
 HiddenArgs hidden_args(const Call& c, const Matrix& x, const Matrix& wg, const Matrix& wu, long rows) {
@@ -1379,7 +1392,7 @@ void launch_narrow(const NarrowArgs& a, hipStream_t st) {
                2.0 * a.rows * (a.cin + a.cout), st);
   auto go = [&](auto ksx, auto nw, auto cg) {
     constexpr int KSX = decltype(ksx)::value, NW = decltype(nw)::value, CG = decltype(cg)::value;
-    TGP_LAUNCH(ps, (narrow_k<P, KSX, NW, CG, ACT, T>), dim3(cdiv(a.rows, 64)), dim3(64 * NW), 0, st, a);
+    TGP_LAUNCH(ps, (gated_narrow<P, KSX, NW, CG, ACT, T>), dim3(cdiv(a.rows, 64)), dim3(64 * NW), 0, st, a);
   };
   typedef std::integral_constant<int, 2> two;
   typedef std::integral_constant<int, 4> four;
@@ -1419,10 +1432,10 @@ hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, T* 
     constexpr int MF = decltype(mf)::value, NO = MF * sizeof(T) == 8 ? 8 : 16;   // (registers)
     with_act(s.act, [&](auto act) {
       ProfScope ps("gated_few_hidden", 4.0 * rows * s.cin * s.hidden, 2.0 * e * s.cin * s.hidden, st);
-      TGP_LAUNCH(ps, (few_k<T, 2, MF, 8, decltype(act)::value>), dim3(cdiv(s.hidden, a.cw)), dim3(512), 0, st, a);
+      TGP_LAUNCH(ps, (gated_few<T, 2, MF, 8, decltype(act)::value>), dim3(cdiv(s.hidden, a.cw)), dim3(512), 0, st, a);
     });
     ProfScope ps("gated_few_out", 2.0 * rows * s.cout * s.hidden, (double)e * s.cout * s.hidden, st);
-    TGP_LAUNCH(ps, (few_k<T, 1, MF, NO, 0>), dim3(cdiv(s.cout, o.cw)), dim3(64 * NO), 0, st, o);
+    TGP_LAUNCH(ps, (gated_few<T, 1, MF, NO, 0>), dim3(cdiv(s.cout, o.cw)), dim3(64 * NO), 0, st, o);
   };
   if (rows <= 32) go(std::integral_constant<int, 1>());
   else go(std::integral_constant<int, 2>());
@@ -1459,7 +1472,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
       a.tm = cdiv(rows, PR::BM);
       a.tn = cdiv(s.hidden, PR::BN);
       ProfScope ps("gated_hidden", 4.0 * rows * s.cin * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.hidden), st);
-      TGP_LAUNCH(ps, (hidden_k<PR, decltype(act)::value, P>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
+      TGP_LAUNCH(ps, (gated_hidden<PR, decltype(act)::value, P>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
     };
     with_act(s.act, [&](auto act) {
       if (fills(rows, s.hidden)) hidden(HidL(), act);
@@ -1502,8 +1515,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       sb += cdiv((long)m.j[k].rows * (m.j[k].ldp / 4), deep ? 64 : 256);
     }
     ProfScope ps("gated_sum", 0, 4.0 * m.ranges * p.stride, st);
-    if (deep) TGP_LAUNCH(ps, sum_k<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
-    else TGP_LAUNCH(ps, sum_k<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
+    if (deep) TGP_LAUNCH(ps, gated_sum<4>, dim3((unsigned)sb), dim3(256), 0, st, m);
+    else TGP_LAUNCH(ps, gated_sum<1>, dim3((unsigned)sb), dim3(256), 0, st, m);
   };
   for (long r0 = 0; r0 < g.rows; r0 += p.chunk) {
     const long rows = std::min(p.chunk, g.rows - r0);
@@ -1538,8 +1551,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
           ProfScope ps("gated_slim", 2.0 * rows * (8 * s.cin + 3 * s.cout) * s.hidden,
                        2.0 * rows * (2 * s.cin + s.cout) + 4.0 * m.ranges * p.stride, st);
           constexpr int ACT = decltype(act)::value;
-          if (grads) TGP_LAUNCH(ps, (slim_k<ACT, true>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
-          else TGP_LAUNCH(ps, (slim_k<ACT, false>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
+          if (grads) TGP_LAUNCH(ps, (gated_slim<ACT, true>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
+          else TGP_LAUNCH(ps, (gated_slim<ACT, false>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
         });
         if (grads && !direct) add_up(m);
         continue;
@@ -1557,7 +1570,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       a.tm = cdiv(rows, PR::BM);
       a.tn = cdiv(s.hidden, PR::BN);
       ProfScope ps("gated_back", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
-      TGP_LAUNCH(ps, (back_k<PR, decltype(pd), decltype(act)::value, L, decltype(all)::value>),
+      TGP_LAUNCH(ps, (gated_back<PR, decltype(pd), decltype(act)::value, L, decltype(all)::value>),
                  dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
     };
     with_act(s.act, [&](auto act) {
@@ -1618,9 +1631,9 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       job(dym, P, s.cout, h, L, s.hidden, gr.down, gr.b_down);
       {
         ProfScope ps("gated_outer", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * o.j[0].s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
-        if (p.wide == 64) TGP_LAUNCH(ps, outer_k<OuterS>, dim3((unsigned)blocks), dim3(OuterS::T), 0, st, o);
-        else if (p.wide == 128) TGP_LAUNCH(ps, outer_k<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
-        else TGP_LAUNCH(ps, outer_k<OuterX>, dim3((unsigned)blocks), dim3(OuterX::T), 0, st, o);
+        if (p.wide == 64) TGP_LAUNCH(ps, gated_outer<OuterS>, dim3((unsigned)blocks), dim3(OuterS::T), 0, st, o);
+        else if (p.wide == 128) TGP_LAUNCH(ps, gated_outer<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
+        else TGP_LAUNCH(ps, gated_outer<OuterX>, dim3((unsigned)blocks), dim3(OuterX::T), 0, st, o);
       }
       if (!direct) add_up(m);
     }
@@ -1662,7 +1675,7 @@ hipError_t gated_backward(const Gated& g, const void* dy, long lddy, const void*
     for (const auto& a : all) {
       if (!a.first) continue;
       ProfScope ps("gated_zero", 0, 4.0 * a.second, st);
-      TGP_LAUNCH(ps, zero_k, dim3((unsigned)((a.second + kT - 1) / kT)), dim3(kT), 0, st, a.first, a.second);
+      TGP_LAUNCH(ps, gated_zero, dim3((unsigned)((a.second + kT - 1) / kT)), dim3(kT), 0, st, a.first, a.second);
     }
     return launch_status();
   }
