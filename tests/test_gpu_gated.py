@@ -154,6 +154,11 @@ def test_large_tiles_and_ranges(rows, cin, hidden, cout, dt):
         assert ref.rel(g, 2 * once.cpu().double()) <= (2.5 * 2.0 ** -24 if dt == "fp32" else 0.0), name
 
 
+def test_pixels_in_two_parts_of_one_launch_each():
+    """4194374 pixels of few channels; sums of so many terms have a random walk of 2048 x 2^-24."""
+    Block((1 << 22) + 70, 8, 16, 8, "bf16").check(2048 * 2.0 ** -24)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows", [3, 150])
 @pytest.mark.parametrize("cin,hidden,cout,ldx,ldy,offx,offy,offw", [
@@ -264,7 +269,8 @@ def test_micro_batches_add_up():
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows,cin,hidden,cout", [(1, 64, 128, 64), (20, 65, 40, 33), (500, 64, 200, 72)])
+@pytest.mark.parametrize("rows,cin,hidden,cout", [(1, 64, 128, 64), (20, 65, 40, 33), (500, 64, 200, 72), (700, 48, 250, 64),
+                                                  (144, 264, 1000, 300)])
 def test_side_stream_and_graph(rows, cin, hidden, cout, dt):
     """On another stream, and captured: every replay gives the eager call's bits, with eager calls between."""
     b = Block(rows, cin, hidden, cout, dt)
