@@ -11,7 +11,7 @@
 // over pixels, together with the column sums of dg, du and dy (a product of the left
 // factor with ones), where the tiles are few in ranges whose partial sums another adds
 // up in order; one takes dx = dg Wg + du Wu as one sum over twice the hidden channels.
-// Up to 64 channels on both sides and 256 hidden ones of bfloat16 all that is one launch
+// Up to 64 channels on both sides and 65 to 256 hidden ones of bfloat16 all that is one launch
 // (gated_slim) and the ranges' sums.
 //
 // Matrix instructions take bfloat16.  Of a TGP_BF16 network x, dy and the weights
@@ -861,7 +861,7 @@ struct SlimArgs {
 // + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
 // For dx, dg and du go through LDS, rows of hidden channels beside the weights' rows.
 // What bounds it are the activations and the splitting in two parts, some 60 operations
-// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 134 us and 11 for the
+// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 128 us and 11 for the
 // ranges' sums; by a launch for h, dg and du, one for the weights and one for dx 365).
 template <int ACT, bool GRADS>
 __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
@@ -903,15 +903,19 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
   const int hid = 32 * wave + (lane & 31);   // the lane's hidden channel
   const float bg = a.bg && hid < a.hidden ? a.bg[hid] : 0.f, bu = a.bu && hid < a.hidden ? a.bu[hid] : 0.f;
   u32x4 wd[4];   // a row of Wd^T
+  {
+    // (every lane loads, from inside the matrix: behind conditions the loads would wait for
+    // one another)
+    const bf16_t* const from = a.wd + min(hid, a.hidden - 1);
+    unsigned e[32];
 #pragma unroll
-  for (int h = 0; h < 4; ++h)
+    for (int k = 0; k < 32; ++k) e[k] = from[min(16 * (k / 8) + 8 * half + k % 8, a.cout - 1) * a.ldwd];
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      const int c = 16 * h + 8 * half + 2 * z;
-      const unsigned e = hid < a.hidden && c < a.cout ? a.wd[c * a.ldwd + hid] : 0u;
-      const unsigned f = hid < a.hidden && c + 1 < a.cout ? a.wd[(c + 1) * a.ldwd + hid] : 0u;
-      wd[h][z] = e | f << 16;
-    }
+    for (int k = 0; k < 32; ++k)
+      if (hid >= a.hidden || 16 * (k / 8) + 8 * half + k % 8 >= a.cout) e[k] = 0u;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) wd[k / 4][k % 4] = e[2 * k] | e[2 * k + 1] << 16;
+  }
   // reads by columns: rows r0 and r0 + 8 of sixteen, 8 bytes of this lane's part
   const int r0 = 4 * half + ((lane & 15) >> 2), q0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   const int at0 = r0 * 128 + ((q0 ^ F::swz(r0)) << 4) + 8 * (lane & 1);
@@ -1027,22 +1031,33 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
     }
   }
   if constexpr (!GRADS) return;
-  // the sums: rows of hidden channels (of Wd's: of cout), a lane each
+  // The sums, a matrix at a time through LDS (64 KB): rows of hidden channels (of Wd's: of
+  // cout), chunks of four columns XORed with the row.  (Straight from the registers the
+  // stores are 16 KB of instructions, which one block after the other fetches.)
   const long off = blockIdx.x * a.stride;
-  auto put4 = [&](const Sink& t, int r, int c, float4 v) __attribute__((always_inline)) {
-    float* to = t.part + off + (long)r * t.ldp + c;
-    if (t.vec) {
-      if (c >= t.ldp) return;
-      if (a.add) {
-        const float4 e = *(const float4*)to;
-        v = make_float4(e.x + v.x, e.y + v.y, e.z + v.z, e.w + v.w);
-      }
-      *(float4*)to = v;
-    } else {
-      const float w[4] = {v.x, v.y, v.z, v.w};
+  auto place = [&](int r, int chunk, int wide) __attribute__((always_inline)) {
+    return (float4*)(dgs + (r * wide + (chunk ^ (r & 15))) * 16);
+  };
+  auto put = [&](const Sink& t, int rows, int wide) __attribute__((always_inline)) {
+    meet();
+#pragma unroll 1
+    for (int e = threadIdx.x; e < 4096; e += 512) {
+      const int r = e / wide, c = 4 * (e % wide);
+      if (r >= rows || c >= t.n) continue;
+      float4 v = *place(r, e % wide, wide);
+      float* to = t.part + off + (long)r * t.ldp + c;
+      if (t.vec) {
+        if (a.add) {
+          const float4 o = *(const float4*)to;
+          v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+        }
+        *(float4*)to = v;
+      } else {
+        const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int z = 0; z < 4; ++z)
-        if (c + z < t.n) to[z] = a.add ? to[z] + w[z] : w[z];
+        for (int z = 0; z < 4; ++z)
+          if (c + z < t.n) to[z] = a.add ? to[z] + w[z] : w[z];
+      }
     }
   };
   auto put_col = [&](const Sink& t, int r, int n, float v) __attribute__((always_inline)) {
@@ -1051,17 +1066,21 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
     *to = a.add ? *to + v : v;
   };
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
+  for (int m = 0; m < 3; ++m) {
+    if (!a.to[m].part) continue;
+    meet();   // every wave is done with dgs and dus
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int c = 32 * f + 8 * g + 4 * half, r = 32 * f + (lane & 31), ch = 32 * wave + 8 * g + 4 * half;
-      if (a.to[0].part && hid < a.hidden)
-        put4(a.to[0], hid, c, make_float4(sg[f][4 * g], sg[f][4 * g + 1], sg[f][4 * g + 2], sg[f][4 * g + 3]));
-      if (a.to[1].part && hid < a.hidden)
-        put4(a.to[1], hid, c, make_float4(su[f][4 * g], su[f][4 * g + 1], su[f][4 * g + 2], su[f][4 * g + 3]));
-      if (a.to[2].part && r < a.cout)
-        put4(a.to[2], r, ch, make_float4(sd[f][4 * g], sd[f][4 * g + 1], sd[f][4 * g + 2], sd[f][4 * g + 3]));
-    }
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x16_t& w = m == 0 ? sg[f] : m == 1 ? su[f] : sd[f];
+        float4* const to = m < 2 ? place(hid, 8 * f + 2 * g + half, 16)
+                                 : place(32 * f + (lane & 31), 8 * wave + 2 * g + half, 64);
+        *to = make_float4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+      }
+    if (m < 2) put(a.to[m], a.hidden, 16);
+    else put(a.to[m], a.cout, 64);
+  }
   bsg += __shfl_xor(bsg, 32);
   bsu += __shfl_xor(bsu, 32);
   if (lane < 32) {
@@ -1208,7 +1227,11 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
                                    : p.parts * (p.hidp + p.cinp));
   const long most = (long)128 << 20;
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
-  p.slim = backward && s.dtype == TGP_BF16 && s.cin <= 64 && s.cout <= 64 && s.hidden <= 256;
+  // (64 channels, 256 hidden: 1 pixel 18.7 us and in three launches 24.1, 64 18.7 and 18.5,
+  // 1000 23.4 and 27.3, 12544 35.7 and 41.1, 147456 143 and 365; with few hidden channels
+  // most waves of a block have none: 300 x 32, 64 hidden 21.0 and 18.4, 12544 x 16, 32
+  // hidden 28.2 and 23.5, 100000 x 16 78 and 88)
+  p.slim = backward && s.dtype == TGP_BF16 && s.cin <= 64 && s.cout <= 64 && s.hidden > 64 && s.hidden <= 256;
   if (p.slim) p.chunk = std::min(rows, 1l << 22);   // (nothing lies between launches)
   size_t at = 0;
   auto take = [&](size_t n) {

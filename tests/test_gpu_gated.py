@@ -156,7 +156,7 @@ def test_large_tiles_and_ranges(rows, cin, hidden, cout, dt):
 
 def test_pixels_in_two_parts_of_one_launch_each():
     """4194374 pixels of few channels; sums of so many terms have a random walk of 2048 x 2^-24."""
-    Block((1 << 22) + 70, 8, 16, 8, "bf16").check(2048 * 2.0 ** -24)
+    Block((1 << 22) + 70, 8, 72, 8, "bf16").check(2048 * 2.0 ** -24)
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
