@@ -861,7 +861,7 @@ struct SlimArgs {
 // + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
 // For dx, dg and du go through LDS, rows of hidden channels beside the weights' rows.
 // What bounds it are the activations and the splitting in two parts, some 60 operations
-// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 128 us and 11 for the
+// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 121 us and 11 for the
 // ranges' sums; by a launch for h, dg and du, one for the weights and one for dx 365).
 template <int ACT, bool GRADS>
 __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
