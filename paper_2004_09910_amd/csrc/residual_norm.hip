@@ -19,6 +19,7 @@
 
 #include "common.h"
 #include "prof.h"
+#include "row_plan.h"
 #include "row_regs.h"
 #include "train_ops.h"
 
@@ -702,44 +703,24 @@ Vectors vectors(const tgp_residual_params& p) {
 constexpr int kFwdBlocks = 2048;   // most blocks of a forward launch
 constexpr int kBlocks = 1024;      // most ranges of a backward one
 constexpr int kAnyBlocks = 512;
+static_assert(kRowThreads == kT, "lanes of a block");
 
 bool any_sum(const tgp_residual_grads& g) {
   return g.scale || g.post_gain || g.post_bias || g.pre_gain || g.pre_bias;
 }
 
-// How registers hold a row: vb bytes an access, nv of them a lane, g lanes a row (0:
-// the block); vb = 0: not at all.
-struct Plan {
-  int vb, nv, g;
-};
-
-// The widest accesses that every row's start and length allow, at most `most` values a
-// lane; then the lanes that leave fewest idle, more lanes where two leave the same.
-// near: a wave's rows are within 32 bits of each other; else it takes one at a time.
-Plan plan_of(int esz, int C, uintptr_t bits, int most, int widest, bool near) {
-  bits |= (uintptr_t)C * esz;
-  const int vb = bits % widest == 0 ? widest : bits % 4 == 0 ? 4 : 2, nvec = C * esz / vb, top = most * esz / vb;
-  Plan best{vb, 0, 64};
-  int room = 1 << 30;
-  for (int g = 64; g >= (near ? 1 : 64); g >>= 1) {
-    const int nv = cdiv(nvec, g);
-    if (nv > std::min(4, top)) break;
-    if (nv * g < room) room = nv * g, best = {vb, nv, g};
-  }
-  if (best.nv) return best;
-  const int nv = cdiv(nvec, kT);
-  if (nv > top) return {0, 0, 0};
-  return {vb, nv <= 4 ? nv : nv <= 8 ? 8 : 16, 0};
-}
-
-// Calls f(VB, NV, BLK as constants); MOST: values a lane.
+// Calls f(VB, NV, BLK as constants); MOST: values a lane.  False: no kernel holds such a row.
 template <int ESZ, int MOST, int WIDE, typename F>
-void with_plan(const Plan& p, F f) {
+bool with_plan(const RowPlan& p, F f) {
+  bool done = false;
   auto nv = [&](auto vb, auto blk) {
     constexpr int TOP = MOST * ESZ / decltype(vb)::value;
     constexpr bool BLK = decltype(blk)::value;
     auto go = [&](auto n) {
-      if constexpr (decltype(n)::value <= TOP && (BLK || decltype(n)::value <= 4)) f(vb, n, blk);
+      if constexpr (decltype(n)::value <= TOP && (BLK || decltype(n)::value <= 4)) {
+        f(vb, n, blk);
+        done = true;
+      }
     };
     switch (p.nv) {
       case 1: return go(std::integral_constant<int, 1>());
@@ -747,7 +728,7 @@ void with_plan(const Plan& p, F f) {
       case 3: return go(std::integral_constant<int, 3>());
       case 4: return go(std::integral_constant<int, 4>());
       case 8: return go(std::integral_constant<int, 8>());
-      default: return go(std::integral_constant<int, 16>());
+      case kMostVectors: return go(std::integral_constant<int, kMostVectors>());
     }
   };
   auto vec = [&](auto blk) {
@@ -757,6 +738,7 @@ void with_plan(const Plan& p, F f) {
   };
   if (p.g) vec(std::false_type());
   else vec(std::true_type());
+  return done;
 }
 
 // f(whether there is a post norm, as a constant)
@@ -778,13 +760,12 @@ bool near_rows(std::initializer_list<Rows> all) {
 template <typename T>
 uintptr_t place(const Rows& r) { return r.p ? (uintptr_t)r.p | (uintptr_t)r.ld * sizeof(T) : 0; }
 
-constexpr int kFwdValues = 32, kBwdValues = 16;   // of a row, a lane
-
 template <typename T>
 hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
   const double n = (double)a.s.rows * a.s.C;
-  const Plan p = plan_of(sizeof(T), a.s.C, place<T>(a.r) | place<T>(a.f) | place<T>(a.gate) | place<T>(a.out) | place<T>(a.z),
-                         kFwdValues, 16, near_rows<T>({a.r, a.f, a.out, a.z}));
+  constexpr int WIDE = fwd_widest(sizeof(T));
+  const RowPlan p = row_plan(sizeof(T), a.s.C, place<T>(a.r) | place<T>(a.f) | place<T>(a.gate) | place<T>(a.out) | place<T>(a.z),
+                             kFwdValues, WIDE, near_rows<T>({a.r, a.f, a.out, a.z}));
   if (!p.vb || (a.gate.p && a.s.group > 0x7fffffff)) {
     ProfScope ps("residual_norm_fwd_any", 20 * n, 4 * n * sizeof(T), st);
     TGP_LAUNCH(ps, res_fwd_any<T>, dim3((unsigned)std::min<long>(a.s.rows, 2048)), dim3(kT),
@@ -796,24 +777,25 @@ hipError_t forward_t(const ResidualForward& a, hipStream_t st) {
   const FwdArgs k{a.r.p, a.f.p, a.gate.p, a.out.p, a.z.p, a.r.ld, a.f.ld, a.gate.ld, a.out.ld, a.z.ld, (long)a.s.rows,
                   (unsigned)a.s.group, vectors(a.w), a.s.eps, (float4*)a.stats, a.s.C, p.g};
   const unsigned grid = even_grid(a.s.rows, p.g == 0 ? 1 : 4 * (64 / p.g), kFwdBlocks);
+  bool done = false;
   with_post(a.s.post, [&](auto post) {
-    with_plan<sizeof(T), kFwdValues, 16>(p, [&](auto vb, auto nv, auto blk) {
+    done = with_plan<sizeof(T), kFwdValues, WIDE>(p, [&](auto vb, auto nv, auto blk) {
       constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
       constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
       ProfScope ps("residual_norm_fwd", 20 * n, (a.z.p ? 4 : 3) * n * sizeof(T), st);
       TGP_LAUNCH(ps, (res_fwd<T, VB, NV, BLK, POST>), dim3(grid), dim3(kT), 0, st, k);
     });
   });
-  return launch_status();
+  return done ? launch_status() : hipErrorNotSupported;
 }
 
 template <typename T>
 hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
-  constexpr int WIDE = 4 * sizeof(T);   // bytes of an access: four values
+  constexpr int WIDE = bwd_widest(sizeof(T));
   const double n = (double)a.s.rows * a.s.C;
   const long rows = a.s.rows, group = a.gate.p ? (long)a.s.group : 1;
   const bool sums = any_sum(a.g), shared = group > 1;
-  const Plan p = plan_of(sizeof(T), a.s.C,
+  const RowPlan p = row_plan(sizeof(T), a.s.C,
                          place<T>(a.dz) | place<T>(a.dout) | (a.dz.p ? place<T>(a.out) : 0) | place<T>(a.f) | place<T>(a.gate) |
                              place<T>(a.dr) | place<T>(a.df) | place<T>(a.dgate),
                          kBwdValues, WIDE,
@@ -860,8 +842,9 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   }
   const bool join = shared && !whole && (sums || a.dgate.p);
   if (sums || join) k.part = a.part;
+  bool done = false;
   with_post(a.s.post, [&](auto post) {
-    with_plan<sizeof(T), kBwdValues, WIDE>(p, [&](auto vb, auto nv, auto blk) {
+    done = with_plan<sizeof(T), kBwdValues, WIDE>(p, [&](auto vb, auto nv, auto blk) {
       constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
       constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
       ProfScope ps("residual_norm_bwd", 40 * n, (3 + (a.dout.p ? 1 : 0) + (a.dz.p ? 2 : 0)) * n * sizeof(T), st);
@@ -869,6 +852,7 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
       else TGP_LAUNCH(ps, (res_bwd<T, VB, NV, BLK, POST, false>), dim3(grid), dim3(kT), 0, st, k);
     });
   });
+  if (!done) return hipErrorNotSupported;
   if (join) {
     ProfScope ps("residual_norm_gates", 4.0 * grid * a.s.C, 16.0 * grid * a.s.C, st);
     auto go = [&](auto many) {
