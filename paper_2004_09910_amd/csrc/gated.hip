@@ -98,21 +98,42 @@ __global__ __launch_bounds__(kT) void gated_copy(Copies c) {
 
 // ------------------------------------------------- hidden channels
 
-// act(g) and act'(g), to float32's accuracy.  GELU's Phi(g) = (1 + erf(g / sqrt 2)) /
-// 2 is by the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook
-// (1.5e-7), whose exponential act' has as well.
-template <int ACT>
+// 2^(c v) for v the sum of `v` and `rest`, c the sum of `c` and `tail`.  FINE: to some 2^-22
+// of itself; else of c v alone, whose rounding is up to 2^-24 |c v| of it.
+template <bool FINE>
+__device__ __forceinline__ float exp2_of(float v, float rest, float c, float tail) {
+  const float y = v * c, e = __builtin_amdgcn_exp2f(y);
+  if constexpr (!FINE) return e;
+  const float d = fmaf(v, c, -y) + (v * tail + rest * c);
+  return fabsf(y) < 126.f ? fmaf(e, d * 0.69314718f, e) : e;   // (no inf - inf)
+}
+
+// act(g) and act'(g), relative to themselves also where g is far below zero.  SiLU is g p,
+// p = 1 / (1 + exp(-g)).  GELU is g Phi(g) with Phi(-|g|) = exp(-g g / 2) R(|g|) and R as
+// t times a polynomial in t = 1 / (1 + 0.265 |g|), a least-squares fit of erfcx(|g| / sqrt
+// 2) / 2 whose largest relative error up to |g| = 15 was brought down to 1.6e-8; in float32
+// arithmetic 4e-7.  Without FINE the exponential adds 5e-8 g g of the value (2e-6 at -6),
+// which two bfloat16s do not see.
+template <int ACT, bool FINE>
 __device__ __forceinline__ void act_of(float g, float* a, float* slope) {
   if constexpr (ACT == TGP_ACT_SILU) {
-    const float p = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+    const float p = __builtin_amdgcn_rcpf(1.f + exp2_of<FINE>(g, 0.f, -1.44269502f, -1.92596303e-8f));
     *a = g * p;
     *slope = p + *a * (1.f - p);
   } else {
-    const float e = __builtin_amdgcn_exp2f(g * g * -0.72134752f);
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * fabsf(g));
-    const float q =
-        0.5f * e * t *
-        (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float s = g * g, rest = FINE ? fmaf(g, g, -s) : 0.f;
+    const float e = exp2_of<FINE>(s, rest, -0.72134751f, -9.62981517e-9f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.265f, fabsf(g), 1.f));
+    float r = 0.0304386261f;
+    r = fmaf(r, t, -0.142422333f);
+    r = fmaf(r, t, 0.214186966f);
+    r = fmaf(r, t, -0.112326354f);
+    r = fmaf(r, t, 0.135238826f);
+    r = fmaf(r, t, 0.0614404269f);
+    r = fmaf(r, t, 0.102419138f);
+    r = fmaf(r, t, 0.105285376f);
+    r = fmaf(r, t, 0.105739325f);
+    const float q = e * t * r;
     const float p = g < 0.f ? q : 1.f - q;
     *a = g * p;
     *slope = p + g * e * 0.39894228f;
@@ -185,7 +206,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 #pragma unroll
       for (int z = 0; z < 16; ++z) {
         float act, slope;
-        act_of<ACT>(p.acc[0][i][j][z] + bg[z], &act, &slope);
+        act_of<ACT, P == 3>(p.acc[0][i][j][z] + bg[z], &act, &slope);
         v[z] = act * (p.acc[1][i][j][z] + bu[z]);
       }
       put_parts<P>(a.h, r, c, r < a.rows, a.ldh, v);
@@ -222,7 +243,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 #pragma unroll
       for (int z = 0; z < 16; ++z) {
         float act, slope;
-        act_of<ACT>(p.acc[0][i][j][z] + bg[z], &act, &slope);
+        act_of<ACT, P == 3>(p.acc[0][i][j][z] + bg[z], &act, &slope);
         const float u = p.acc[1][i][j][z] + bu[z], dh = d.acc[0][i][j][z];
         h[z] = act * u;
         dg[z] = dh * u * slope;
@@ -532,7 +553,7 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowAr
 #pragma unroll
       for (int z = 0; z < 16; ++z) {
         float act, slope;
-        act_of<ACT>(g[i][z] + bg[z], &act, &slope);
+        act_of<ACT, P == 3>(g[i][z] + bg[z], &act, &slope);
         v[z] = act * (u[i][z] + bu[z]);
       }
       const int row = 32 * i + (lane & 31);
@@ -750,7 +771,7 @@ __global__ __launch_bounds__(64 * NW) void gated_few(FewArgs a) {
     }
     if constexpr (M == 2) {
       float act, slope;
-      act_of<ACT>(s[0], &act, &slope);
+      act_of<ACT, sizeof(T) == 4>(s[0], &act, &slope);
       s[0] = act * s[1];
     }
     Elt<T>::st((T*)a.y + r * a.ldy + j0 + n, s[0]);
@@ -950,7 +971,7 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         float act, slope;
-        act_of<ACT>(g[v] + bg, &act, &slope);
+        act_of<ACT, false>(g[v] + bg, &act, &slope);
         const float up = u[v] + bu, dh = d[v];
         const bool in = 8 * (v / 4) + v % 4 < left;   // (a bias may be infinite)
         g[v] = in ? dh * up * slope : 0.f;
