@@ -27,6 +27,7 @@
 // thousands at a time, so that what one launch leaves for the next stays in the
 // caches.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "common.h"
@@ -657,6 +658,27 @@ struct Eight<float> {
     }
   }
 };
+// A value as two bfloat16s, in the order of fragments: sixteen channels of 32 MF pixels
+// are MF times 64 lanes' eight values; the second parts `plane` values behind the first.
+struct Pair {
+  bf16_t at;
+};
+template <>
+struct Eight<Pair> {
+  u32x4 p[2];
+  // n: channels from the lane's first on; in: whether the lane's pixel is there
+  __device__ __forceinline__ void load(const bf16_t* at, long plane, int n, bool in) {
+    p[0] = p[1] = u32x4{};
+    if (!in || n <= 0) return;
+    p[0] = *(const u32x4*)at;
+    p[1] = *(const u32x4*)(at + plane);
+    if (n >= 8) return;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) p[q][z] = 2 * z + 1 < n ? p[q][z] : 2 * z < n ? p[q][z] & 0xffffu : 0u;
+  }
+};
 template <typename T>
 struct Frag {
   static constexpr int P = sizeof(T) == 2 ? 1 : 3;
@@ -681,18 +703,27 @@ struct Frag {
         }
     }
   }
-  // c + this fragment's rows times b's
-  __device__ __forceinline__ f32x16_t times(const Frag& b, f32x16_t c) const {
-    if constexpr (P == 3) {
-      c = mfma32(as_bf16x8(p[2]), as_bf16x8(b.p[0]), c);
-      c = mfma32(as_bf16x8(p[1]), as_bf16x8(b.p[1]), c);
-      c = mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[2]), c);
-      c = mfma32(as_bf16x8(p[1]), as_bf16x8(b.p[0]), c);
-      c = mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[1]), c);
-    }
-    return mfma32(as_bf16x8(p[0]), as_bf16x8(b.p[0]), c);
+};
+template <>
+struct Frag<Pair> {
+  static constexpr int P = 2;
+  u32x4 p[P];
+  __device__ __forceinline__ void set(const Eight<Pair>& e) {
+    p[0] = e.p[0];
+    p[1] = e.p[1];
   }
 };
+// c + a's rows times b's: the pairs of parts that a float32 product needs, small ones first
+template <typename TA, typename TB>
+__device__ __forceinline__ f32x16_t times(const Frag<TA>& a, const Frag<TB>& b, f32x16_t c) {
+  constexpr int PA = Frag<TA>::P, PB = Frag<TB>::P;
+#pragma unroll
+  for (int d = 2; d >= 0; --d)
+#pragma unroll
+    for (int i = d; i >= 0; --i)
+      if (i < PA && d - i < PB) c = mfma32(as_bf16x8(a.p[i < PA ? i : 0]), as_bf16x8(b.p[d - i < PB ? d - i : 0]), c);
+  return c;
+}
 
 struct FewArgs {
   const void *x, *w[2];
@@ -700,18 +731,21 @@ struct FewArgs {
   void* y;
   long ldx, ldw, ldy;
   int rows, k, n, vx, vw;
-  int cw;   // channels of a block
+  int cw;       // channels of a block
+  long plane;   // from the first parts of h to the second (Pair)
 };
 
 // Up to 32 MF pixels: cw channels of the result a block, NW waves that share the sum; M
 // matrices (two: h, else y).  Weights are read once, straight into fragments, and what
 // bounds it is how many of their loads are on their way at a time: as many waves as a
 // block has, and blocks of fewer channels (the other rows of their fragments are zeros)
-// where 32 each leave CUs without one (1 x 1024 through 4096 and back 23.8 us, with 32
-// channels a block 41; its 24 MB come in at 1.0 TB/s).
-template <typename T, int M, int MF, int NW, int ACT>
+// where 32 each leave CUs without one (1 x 1024 through 4096 and back 22.8 us, with 32
+// channels a block 41; its 24 MB come in at 1.1 TB/s).  Of a bfloat16 network h is two
+// parts in the order of fragments, loads of 1 KB (60 such pixels 43.8 us; in rows, whose
+// loads take 32 bytes each of 32 rows, 59.9, and one part in rows 43.8).
+template <typename TX, typename TW, typename TY, int M, int MF, int NW, int ACT>
 __global__ __launch_bounds__(64 * NW) void gated_few(FewArgs a) {
-  constexpr int U = M == 1 && MF == 1 && sizeof(T) == 2 ? 8 : 4;   // steps of 16 whose loads go out together
+  constexpr int U = M == 1 && MF == 1 && sizeof(TW) == 2 ? 8 : 4;   // steps of 16 whose loads go out together
   __shared__ float red[NW][M * MF][16][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j0 = blockIdx.x * a.cw, col = j0 + (lane & 31), per = ((a.k + NW - 1) / NW + 15) / 16 * 16;
@@ -723,28 +757,33 @@ __global__ __launch_bounds__(64 * NW) void gated_few(FewArgs a) {
 #pragma unroll
     for (int f = 0; f < MF; ++f) acc[m][f] = f32x16_t{};
   for (int k0 = wave * per; k0 < k1; k0 += 16 * U) {
-    Eight<T> vw[U][M], vx[U][MF];
+    Eight<TW> vw[U][M];
+    Eight<TX> vx[U][MF];
 #pragma unroll
     for (int s = 0; s < U; ++s) {
       const int k = k0 + 16 * s + 8 * (lane >> 5);
 #pragma unroll
-      for (int m = 0; m < M; ++m) vw[s][m].load((const T*)a.w[m] + col * a.ldw, k, k1, here, a.vw);
+      for (int m = 0; m < M; ++m) vw[s][m].load((const TW*)a.w[m] + col * a.ldw, k, k1, here, a.vw);
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         const int r = 32 * f + (lane & 31);
-        vx[s][f].load((const T*)a.x + r * a.ldx, k, k1, r < a.rows, a.vx);
+        if constexpr (std::is_same<TX, Pair>::value)
+          vx[s][f].load((const bf16_t*)a.x + ((k0 / 16 + s) * MF + f) * 512L + 8 * lane, a.plane, k1 - k, r < a.rows);
+        else
+          vx[s][f].load((const TX*)a.x + r * a.ldx, k, k1, r < a.rows, a.vx);
       }
     }
 #pragma unroll
     for (int s = 0; s < U; ++s) {
-      Frag<T> w[M], x;
+      Frag<TW> w[M];
+      Frag<TX> x;
 #pragma unroll
       for (int m = 0; m < M; ++m) w[m].set(vw[s][m]);
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         x.set(vx[s][f]);
 #pragma unroll
-        for (int m = 0; m < M; ++m) acc[m][f] = w[m].times(x, acc[m][f]);
+        for (int m = 0; m < M; ++m) acc[m][f] = times(w[m], x, acc[m][f]);
       }
     }
   }
@@ -771,10 +810,19 @@ __global__ __launch_bounds__(64 * NW) void gated_few(FewArgs a) {
     }
     if constexpr (M == 2) {
       float act, slope;
-      act_of<ACT, sizeof(T) == 4>(s[0], &act, &slope);
+      act_of<ACT, sizeof(TW) == 4>(s[0], &act, &slope);
       s[0] = act * s[1];
     }
-    Elt<T>::st((T*)a.y + r * a.ldy + j0 + n, s[0]);
+    if constexpr (std::is_same<TY, Pair>::value) {
+      const uint32_t top = f2bf(s[0]);
+      const bool fine = (top & 0x7f80u) != 0x7f80u;   // an infinity or NaN has no rest
+      const int c = j0 + n;
+      bf16_t* to = (bf16_t*)a.y + ((c / 16 * MF + f) * 64L + (r & 31) + 32 * (c >> 3 & 1)) * 8 + (c & 7);
+      to[0] = (bf16_t)top;
+      to[a.plane] = (bf16_t)(fine ? f2bf(s[0] - bf2f(top)) : 0u);
+    } else {
+      Elt<TY>::st((TY*)a.y + r * a.ldy + j0 + n, s[0]);
+    }
   }
 }
 
@@ -1215,6 +1263,18 @@ struct Plan {
   size_t x, dy, wg, wu, wd, h, dg, du, part, join, bytes;   // offsets
 };
 
+constexpr int kFewRows = 64;
+
+// Whether one launch takes a forward pass whole: what its registers and LDS hold.
+bool narrow(const tgp_gated_shape& s, long rows) {
+  const int most = s.dtype == TGP_BF16 ? 256 : 128;
+  return s.cin <= most && s.cout <= most && (rows > kFewRows || s.hidden <= 256);
+}
+
+// Whether two launches take it, whose weights go straight into registers.
+bool few(const tgp_gated_shape& s, long rows) { return rows <= kFewRows && !narrow(s, rows); }
+long few_pixels(long rows) { return rows <= 32 ? 32 : 64; }   // of its fragments
+
 int ranges_of(long rows, int per) { return (int)((rows + per - 1) / per); }
 
 // A long sum for few tiles of 64 x 64: ranges of `per` of its k values, four stages each
@@ -1265,7 +1325,7 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   p.wd = take((size_t)2 * p.parts * s.cout * p.hidp);
   p.x = take((size_t)2 * p.parts * p.chunk * p.cinp);
   if (!backward) {
-    p.h = take((size_t)2 * p.parts * p.chunk * p.hidp);
+    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.parts * p.chunk * p.hidp);
   } else {
     p.dy = take((size_t)2 * p.parts * p.chunk * p.coutp);
     const size_t plane = p.slim ? 0 : (size_t)2 * p.low * p.chunk * p.hidp;
@@ -1422,14 +1482,6 @@ void with_act(int act, F f) {
 
 bool at16(const void* p, long ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
 
-constexpr int kFewRows = 64;
-
-// Whether one launch takes a forward pass whole: what its registers and LDS hold.
-bool narrow(const tgp_gated_shape& s, long rows) {
-  const int most = s.dtype == TGP_BF16 ? 256 : 128;
-  return s.cin <= most && s.cout <= most && (rows > kFewRows || s.hidden <= 256);
-}
-
 template <int P, int ACT, typename T>
 void launch_narrow(const NarrowArgs& a, hipStream_t st) {
   ProfScope ps("gated_narrow", 2.0 * a.rows * a.hidden * (2 * a.cin + a.cout) * (P == 1 ? 1 : 6),
@@ -1464,24 +1516,26 @@ void launch_narrow(const NarrowArgs& a, hipStream_t st) {
 }
 
 template <typename T>
-hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, T* h, long ldh, hipStream_t st) {
+hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, void* h, long ldh, hipStream_t st) {
+  typedef std::conditional_t<sizeof(T) == 2, Pair, float> H;
   const tgp_gated_shape& s = g.s;
   const int rows = (int)g.rows, e = sizeof(T);
+  const long plane = few_pixels(rows) * round_up(s.hidden, 16);
   auto width = [](int n) { return n >= 32 * 256 ? 32 : n >= 16 * 256 ? 16 : n >= 8 * 128 ? 8 : 4; };
   const FewArgs a{x, {g.w.gate, g.w.up}, {g.w.b_gate, g.w.b_up}, h, ldx, s.cin, ldh, rows, s.cin, s.hidden,
-                  at16(x, ldx, e), at16(g.w.gate, s.cin, e) && at16(g.w.up, s.cin, e), width(s.hidden)};
+                  at16(x, ldx, e), at16(g.w.gate, s.cin, e) && at16(g.w.up, s.cin, e), width(s.hidden), plane};
   const FewArgs o{h, {g.w.down, nullptr}, {g.w.b_down, nullptr}, y, ldh, s.hidden, ldy, rows, s.hidden, s.cout,
-                  at16(h, ldh, e), at16(g.w.down, s.hidden, e), width(s.cout)};
+                  at16(h, ldh, 4), at16(g.w.down, s.hidden, e), width(s.cout), plane};
   auto go = [&](auto mf) {
-    constexpr int MF = decltype(mf)::value, NO = MF * sizeof(T) == 8 ? 8 : 16;   // (registers)
+    constexpr int MF = decltype(mf)::value, NO = MF == 2 ? 8 : 16;   // (registers)
     with_act(s.act, [&](auto act) {
       ProfScope ps("gated_few_hidden", 4.0 * rows * s.cin * s.hidden, 2.0 * e * s.cin * s.hidden, st);
-      TGP_LAUNCH(ps, (gated_few<T, 2, MF, 8, decltype(act)::value>), dim3(cdiv(s.hidden, a.cw)), dim3(512), 0, st, a);
+      TGP_LAUNCH(ps, (gated_few<T, T, H, 2, MF, 8, decltype(act)::value>), dim3(cdiv(s.hidden, a.cw)), dim3(512), 0, st, a);
     });
     ProfScope ps("gated_few_out", 2.0 * rows * s.cout * s.hidden, (double)e * s.cout * s.hidden, st);
-    TGP_LAUNCH(ps, (gated_few<T, 1, MF, NO, 0>), dim3(cdiv(s.cout, o.cw)), dim3(64 * NO), 0, st, o);
+    TGP_LAUNCH(ps, (gated_few<H, T, T, 1, MF, NO, 0>), dim3(cdiv(s.cout, o.cw)), dim3(64 * NO), 0, st, o);
   };
-  if (rows <= 32) go(std::integral_constant<int, 1>());
+  if (few_pixels(rows) == 32) go(std::integral_constant<int, 1>());
   else go(std::integral_constant<int, 2>());
   return launch_status();
 }
@@ -1491,8 +1545,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
   constexpr int P = sizeof(T) == 2 ? 1 : 3;
   const tgp_gated_shape& s = g.s;
   Call c{g, plan_of(s, g.rows, false), (char*)ws, st};
-  if (g.rows <= kFewRows && !narrow(s, g.rows))
-    return forward_few<T>(g, x, ldx, y, ldy, (T*)((char*)ws + c.p.h), c.p.hidp, st);
+  if (few(s, g.rows)) return forward_few<T>(g, x, ldx, y, ldy, (char*)ws + c.p.h, c.p.hidp, st);
   const Matrix wg = c.operand(g.w.gate, s.cin, s.hidden, s.cin, c.p.wg, s.hidden);
   const Matrix wu = c.operand(g.w.up, s.cin, s.hidden, s.cin, c.p.wu, s.hidden);
   const Matrix wd = c.operand(g.w.down, s.hidden, s.cout, s.hidden, c.p.wd, s.cout);
