@@ -414,15 +414,23 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowAr
   // less, and the fragments of one are in registers: all of them spill
   constexpr bool XL = P == 1 && KSX >= 3;
   constexpr int XK = XL ? 1 : KSX;   // stages of pixels in registers
-  constexpr int NS = XL ? 3 : P == 1 ? 4 : 6, BK = 64, BH = 32 * NW, KG = NW / CG, H = BK / 16, L = 4;
+  // Of bfloat16 h is two parts, 16 bits, so that y is rounded once.  A ring of three leaves
+  // LDS for them; where the pixels take that as well, it holds half of the tile's channels
+  // at a time.  (131072 x 128, 512 hidden channels: 116 us, with a ring of four and halves
+  // 132, with h in one part, errors of twice a rounding's, 92.)
+  constexpr int Q = P == 1 ? 2 : P;
+  constexpr bool HALF = XL;
+  constexpr int NS = P == 1 ? 3 : 6, BK = 64, BH = 32 * NW, KG = NW / CG, H = BK / 16, L = 4;
+  constexpr int HK = BH / (HALF ? 128 : 64);   // 64s of channels that LDS holds
   typedef Feed<BH, BK, false, NW> FW;
   typedef Feed<64, BK, false, 2> FH;   // (its layout)
   constexpr int SLOT = FW::BYTES, HB = FH::BYTES, DUAL = 2 * P * KSX, SPT = DUAL + P * CG / 2;
   static_assert(FW::LOADS == L && H == L && KSX * HB <= SLOT && P < NS, "a load between the products of a step");
-  __shared__ __align__(1024) unsigned char ring[NS * SLOT + P * (BH / 64) * HB + XL * SLOT];
+  __shared__ __align__(1024) unsigned char ring[NS * SLOT + Q * HK * HB + XL * SLOT];
+  static_assert(!HALF || (P == 1 && CG >= 4), "two stages of Wd at least");
   static_assert(sizeof(ring) <= 160 * 1024 && NS * SLOT >= NW * 8192, "LDS");
   unsigned char* const hs = ring + NS * SLOT;   // [part][64 channels], as stages of 64 rows
-  unsigned char* const xs = XL ? hs + P * (BH / 64) * HB : ring;   // the pixels, [64 channels][64 rows]
+  unsigned char* const xs = XL ? hs + Q * HK * HB : ring;   // the pixels, [64 channels][64 rows]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i0 = blockIdx.x * 64;
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
@@ -547,7 +555,7 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowAr
     float bg[16], bu[16];
     wave_biases(a.bg, c, a.hidden, bg);
     wave_biases(a.bu, c, a.hidden, bu);
-    // (every wave has met a barrier since the last product read h)
+    unsigned hp[2][Q][8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float v[16];
@@ -557,41 +565,66 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowAr
         act_of<ACT, P == 3>(g[i][z] + bg[z], &act, &slope);
         v[z] = act * (u[i][z] + bu[z]);
       }
-      const int row = 32 * i + (lane & 31);
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        unsigned pk[8];
+      for (int p = 0; p < Q; ++p) {
 #pragma unroll
-        for (int z = 0; z < 8; ++z) pk[z] = pack_bf16(v[2 * z], v[2 * z + 1]);
-        put8(pk, [&](int h, u32x4 w) {
-          const int q = (wave & 1) * 4 + 2 * h + (lane >> 5);
-          *(u32x4*)(hs + (p * (BH / 64) + (wave >> 1)) * HB + row * 128 + ((q ^ FH::swz(row)) << 4)) = w;
-        });
-        if (p + 1 < P)
+        for (int z = 0; z < 8; ++z) hp[i][p][z] = pack_bf16(v[2 * z], v[2 * z + 1]);
+        if (p + 1 < Q)
 #pragma unroll
           for (int z = 0; z < 16; ++z) {
-            const float hi = z & 1 ? __uint_as_float(pk[z / 2] & 0xffff0000u) : __uint_as_float(pk[z / 2] << 16);
+            const unsigned w = hp[i][p][z / 2];
+            const float hi = z & 1 ? __uint_as_float(w & 0xffff0000u) : __uint_as_float(w << 16);
             v[z] = (__float_as_uint(hi) & 0x7f800000u) == 0x7f800000u ? 0.f : v[z] - hi;
           }
       }
+      __builtin_amdgcn_sched_barrier(0);   // one fragment's values at a time: registers
     }
-    u32x4 hf[P][H][2];
+    auto put_h = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = 32 * i + (lane & 31);
+#pragma unroll
+        for (int p = 0; p < Q; ++p)
+          put8(hp[i][p], [&](int h, u32x4 w) {
+            const int q = (wave & 1) * 4 + 2 * h + (lane >> 5);
+            *(u32x4*)(hs + (p * HK + (wave >> 1) % HK) * HB + row * 128 + ((q ^ FH::swz(row)) << 4)) = w;
+          });
+      }
+    };
+    // (every wave has met a barrier since the last product read h)
+    if (!HALF || wave < NW / 2) put_h();
+    // fragments of h: a stage's for its P turns, or (bfloat16) of one step and the next
+    constexpr int HF = P == 1 ? 2 : H;
+    u32x4 hf[HF][Q][2];
+    auto read_h = [&](int o, int z) __attribute__((always_inline)) {
+#pragma unroll
+      for (int p = 0; p < Q; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          hf[z % HF][p][i] = FH::frag(hs + (p * HK + (o * KG + wave / CG) % HK) * HB, FH::place(32 * i), z);
+    };
     each<P * CG / 2>([&](auto sc) {
       constexpr int s = decltype(sc)::value, o = s / P, j = P - 1 - s % P;
+      constexpr bool fresh = o == 0 || (HALF && o == CG / 4);   // h is not what the turn before read
+      constexpr bool more = s + 1 < P * CG / 2 && !(HALF && o + 1 == CG / 4);
+      if constexpr (HALF && o == CG / 4) {   // the other half, when every wave has read the first
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        ring_barrier();
+        if (wave >= NW / 2) put_h();
+      }
       turn(std::integral_constant<int, DUAL + s>(), ht, [&](int h) __attribute__((always_inline)) {
-        if (h == 0 && j == P - 1) {
+        if constexpr (P == 1) {
+          if (fresh && h == 0) read_h(o, 0);
+          if (h + 1 < H) read_h(o, h + 1);
+          else if (more) read_h(o + 1, 0);
+        } else if (h == 0 && j == P - 1) {
 #pragma unroll
-          for (int z = 0; z < H; ++z)
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                hf[p][z][i] = FH::frag(hs + (p * (BH / 64) + o * KG + wave / CG) * HB, FH::place(32 * i), z);
+          for (int z = 0; z < H; ++z) read_h(o, z);
         }
 #pragma unroll
-        for (int p = P - 1 - j; p >= 0; --p)
+        for (int p = Q - 1 - j; p >= 0; --p)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) y[i] = mfma32(as_bf16x8(b[h]), as_bf16x8(hf[p][h][i]), y[i]);
+          for (int i = 0; i < 2; ++i) y[i] = mfma32(as_bf16x8(b[h]), as_bf16x8(hf[h % HF][p][i]), y[i]);
       });
     });
   }
@@ -1503,8 +1536,7 @@ void launch_narrow(const NarrowArgs& a, hipStream_t st) {
   };
   if constexpr (P == 1) {
     auto wide = [&](auto ksx) {
-      if (a.cout <= 64) go(ksx, eight(), two());
-      else if (a.cout <= 128) go(ksx, eight(), four());
+      if (a.cout <= 128) go(ksx, eight(), four());
       else go(ksx, eight(), eight());
     };
     if (k == 4) return wide(std::integral_constant<int, 4>());

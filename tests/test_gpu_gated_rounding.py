@@ -69,3 +69,19 @@ def _check(rows, cin, hidden, cout, forward=True, backward=False, **kw):
                                                   (33, 64, 1031, 300), (64, 320, 72, 24)])
 def test_few_pixels(rows, cin, hidden, cout):
     _check(rows, cin, hidden, cout)
+
+
+# every pair of widths that one launch of few channels is made for, hidden channels of several tiles and an odd end
+@pytest.mark.parametrize("cout", [40, 64, 72, 128, 136, 250, 256])
+@pytest.mark.parametrize("cin", [24, 64, 72, 128, 129, 192, 200, 256])
+def test_narrow(cin, cout):
+    _check(70, cin, 520, cout)
+    _check(203, cin, 1031 - 2 * cin, cout)
+
+
+@pytest.mark.parametrize("cout", [24, 64, 65, 128])
+@pytest.mark.parametrize("cin", [24, 64, 65, 128])
+@pytest.mark.parametrize("hidden", [256, 270, 520])
+def test_narrow_float32(cin, cout, hidden):
+    """The same of a float32 network, by test_gpu_gated.py's bounds."""
+    Block(131, cin, hidden, cout, "fp32", (cin + hidden) % 2).check()
