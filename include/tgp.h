@@ -402,8 +402,8 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * cin, Wd cout x hidden, dense, of the type `dtype` (1x1 convolutions' weights as
  * tgp_bind_params takes them); biases float32 (NULL: zeros).  Consecutive rows of
  * x and y are ldx and ldy elements apart.  Products run on bfloat16 matrix
- * instructions with float32 sums.  TGP_BF16: h is rounded to bfloat16 before the
- * last product, y once more.  TGP_FP32: every factor is split into three
+ * instructions with float32 sums.  TGP_BF16: h enters the last product as two
+ * bfloat16s (16 bits), y is rounded once.  TGP_FP32: every factor is split into three
  * bfloat16s, of whose nine products the six largest are summed, which keeps
  * float32's accuracy.  A factor that is infinite or NaN makes what is summed with
  * it NaN or infinite, and nothing else.

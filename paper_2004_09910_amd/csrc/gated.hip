@@ -15,9 +15,10 @@
 // (gated_slim) and the ranges' sums.
 //
 // Matrix instructions take bfloat16.  Of a TGP_BF16 network x, dy and the weights
-// are that; h, dg and du are rounded once for y and dx, which are rounded to
-// bfloat16 themselves, and kept as two bfloat16s (16 bits) for the weights'
-// gradients, float32 sums.  Of a TGP_FP32 network every factor is three
+// are that, and h, dg and du two bfloat16s each (16 bits, 2^-16 of a value): y and dx
+// are then rounded once, and the weights' gradients, float32 sums, 3e-6 of their norm
+// off (three parts, half as many products again, would bring that to float32's 1e-7;
+// one part, half of them, has 2e-3).  Of a TGP_FP32 network every factor is three
 // bfloat16s, its 24 bits, and six of the nine products are summed, small ones
 // first: what is left out is 2^-24 of a term.  A sum over split factors is one
 // sum over pairs of their parts.
@@ -184,7 +185,7 @@ __device__ __forceinline__ void biases(const float* b, int c, int n, float (&v)[
   }
 }
 
-// h of a tile.  P: parts of a factor.
+// h of a tile, in P parts (three where the factors have as many, else two).
 template <typename PR, int ACT, int P>
 __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_hidden(HiddenArgs a) {
   __shared__ __align__(1024) unsigned char ring[PR::LDS];
@@ -215,8 +216,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
   }
 }
 
-// h, dg and du of a tile, each in P parts (one, and no h, where no weight's gradient
-// is wanted).
+// h, dg and du of a tile, each in P parts (no h where no weight's gradient is wanted).
 template <typename PR, typename PD, int ACT, int P, bool GRADS>
 __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_back(HiddenArgs a) {
   static_assert(PR::BM == PD::BM && PR::BN == PD::BN && PR::MT == PD::MT && PR::WN == PD::WN, "one tile");
@@ -250,10 +250,9 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
         dg[z] = dh * u * slope;
         du[z] = dh * act;
       }
-      constexpr int Q = GRADS ? P : (P == 2 ? 1 : P);
-      if constexpr (GRADS) put_parts<Q>(a.h, r, c, r < a.rows, a.ldh, h);
-      put_parts<Q>(a.dg, r, c, r < a.rows, a.ldh, dg);
-      put_parts<Q>(a.du, r, c, r < a.rows, a.ldh, du);
+      if constexpr (GRADS) put_parts<P>(a.h, r, c, r < a.rows, a.ldh, h);
+      put_parts<P>(a.dg, r, c, r < a.rows, a.ldh, dg);
+      put_parts<P>(a.du, r, c, r < a.rows, a.ldh, du);
       __builtin_amdgcn_sched_barrier(0);   // one fragment's values at a time: registers
     }
   }
@@ -262,7 +261,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 // ------------------------------------------------- y, dx
 
 struct OutArgs {
-  Segs<1> s;
+  Segs<1, 2> s;        // (of bfloat16 both parts of the left factor at once)
   long lda, ldb;
   int rows, k, n;
   const float* bias;
@@ -1262,22 +1261,29 @@ __global__ void gated_zero(float* p, long n) {
 // Large and small tiles of each launch.  A CU takes 55 bytes a clock from DMA, so a stage
 // of 128 x 128 tiles (64 values, 32 KB, 582 clocks) comes in slower than its 512 clocks of
 // products: tiles of 256 rows where there are enough of them.  4096 pixels x 1024, 4096
-// hidden: h 84 us (815 TFLOP/s; tiles of 128 x 128, two blocks a CU, 90), h, dg and du
-// 148 (two blocks of 128 x 64 a CU 163), the weights' gradients 213 (967; 128 x 128 255),
-// y 50 and dx 78 (885).  Stages of 32 pixels where both factors are read by columns: the
-// fragments of one of 64 spill (787).  y and dx of 128 x 128 with a deep ring, a block a
-// CU, and with a shallow one, two.
+// hidden: h 86 us (798 TFLOP/s; tiles of 128 x 128, two blocks a CU, 90), h, dg and du
+// 156 (two blocks of 128 x 64 a CU 163), the weights' gradients 215 (957; 128 x 128 255),
+// y 67 and dx 134 (1028).  Stages of 32 pixels where both factors are read by columns: the
+// fragments of one of 64 spill (787).  y and dx take a left factor's two parts in one
+// stage, 48 KB of a 128 x 128 tile for twice the products (y part by part, the right
+// factor read twice: 96 us).
 typedef Product<2, 2, 4, 2, 64, 2, false, false, 2> HidL;
 typedef Product<1, 1, 2, 2, 64, 3, false, false, 2> HidS;
 typedef Product<2, 1, 2, 4, 64, 3, false, false, 2> BackL;
 typedef Product<2, 1, 2, 4, 64, 3, false, true, 1> DhL;
 typedef Product<1, 1, 2, 2, 64, 3, false, true, 1> DhS;
-typedef Product<2, 2, 2, 2, 64, 4, false, false, 1> OutL;
-typedef Product<2, 2, 2, 2, 64, 2, false, false, 1> OutL2;
-typedef Product<1, 1, 2, 2, 64, 4, false, false, 1> OutS;
-typedef Product<2, 2, 2, 2, 64, 4, false, true, 1> DxL;
-typedef Product<2, 2, 2, 2, 64, 2, false, true, 1> DxL2;
-typedef Product<1, 1, 2, 2, 64, 4, false, true, 1> DxS;
+// BKS: the right factor's rows are the sum's; NA: the left factor's parts that are taken at once
+template <bool BKS, int NA> struct Sums;
+template <bool BKS> struct Sums<BKS, 1> {
+  typedef Product<2, 2, 2, 2, 64, 4, false, BKS, 1> L;
+  typedef Product<2, 2, 2, 2, 64, 2, false, BKS, 1> L2;
+  typedef Product<1, 1, 2, 2, 64, 4, false, BKS, 1> S;
+};
+template <bool BKS> struct Sums<BKS, 2> {
+  typedef Product<2, 2, 2, 2, 64, 3, false, BKS, 1, 2> L;
+  typedef Product<2, 2, 4, 2, 64, 2, false, BKS, 1, 2> L2;
+  typedef Product<1, 1, 2, 2, 64, 3, false, BKS, 1, 2> S;
+};
 typedef Product<2, 4, 4, 2, 32, 4, true, true, 1> OuterX;
 typedef Product<2, 2, 2, 2, 32, 4, true, true, 1> OuterL;
 typedef Product<1, 1, 2, 2, 64, 4, true, true, 1> OuterS;
@@ -1286,7 +1292,7 @@ constexpr long kFill = 256;   // tiles that fill the chip
 
 // A call's workspace and how its pixels are taken.
 struct Plan {
-  int parts, low;        // of a factor; of h, dg and du (backward)
+  int parts, low;        // of a factor; of h, dg and du
   long cinp, hidp, coutp;
   long chunk;            // pixels at a time
   bool slim;             // a backward pass in one launch
@@ -1338,7 +1344,7 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   // so many pixels that what lies between launches stays in the caches, but that
   // a launch fills the chip
   const long a_row = 2 * (backward ? 3 * p.low * p.hidp + p.parts * (p.cinp + p.coutp)
-                                   : p.parts * (p.hidp + p.cinp));
+                                   : p.low * p.hidp + p.parts * p.cinp);
   const long most = (long)128 << 20;
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
   // (64 channels, 256 hidden: 1 pixel 18.7 us and in three launches 24.1, 64 18.7 and 18.5,
@@ -1358,7 +1364,7 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   p.wd = take((size_t)2 * p.parts * s.cout * p.hidp);
   p.x = take((size_t)2 * p.parts * p.chunk * p.cinp);
   if (!backward) {
-    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.parts * p.chunk * p.hidp);
+    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.low * p.chunk * p.hidp);
   } else {
     p.dy = take((size_t)2 * p.parts * p.chunk * p.coutp);
     const size_t plane = p.slim ? 0 : (size_t)2 * p.low * p.chunk * p.hidp;
@@ -1382,7 +1388,7 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   }
   const long rest = p.chunk ? rows % p.chunk : 0;
   auto room = [&](long r) {
-    const int n = p.parts == 1 ? 1 : 6;
+    const int n = p.parts == 1 ? 1 : 6;   // pairs that add_sum makes
     return !r ? 0 : backward ? split_bytes(r, s.cin, s.hidden, 2 * n) : split_bytes(r, s.cout, s.hidden, n);
   };
   p.join = take(std::max(room(p.chunk), room(rest)));
@@ -1448,9 +1454,24 @@ void pairs(int na, int nb, F f) {
 }
 void add_pairs(Segs<1>* s, const Matrix& a, int na, const Matrix& b, int nb) {
   pairs(na, nb, [&](int i, int j) {
-    s->a[s->n] = a.part[i];
+    s->a[s->n][0] = a.part[i];
     s->b[s->n++][0] = b.part[j];
   });
+}
+// The same of a float32 network; of bfloat16 a's two parts as one pair with b.
+template <typename T>
+void add_sum(OutArgs* o, const Matrix& a, const Matrix& b) {
+  Segs<1, 2>& s = o->s;
+  if constexpr (sizeof(T) == 2) {
+    s.a[s.n][0] = a.part[0];
+    s.a[s.n][1] = a.part[1];
+    s.b[s.n++][0] = b.part[0];
+  } else {
+    pairs(3, 3, [&](int i, int j) {
+      s.a[s.n][0] = a.part[i];
+      s.b[s.n++][0] = b.part[j];
+    });
+  }
 }
 
 bool fills(long rows, long cols) { return (long)cdiv(rows, 128) * cdiv(cols, 128) >= kFill; }
@@ -1459,15 +1480,19 @@ template <typename PR, typename T>
 void launch_out(const char* name, OutArgs a, hipStream_t st) {
   a.tm = cdiv(a.rows, PR::BM);
   a.tn = cdiv(a.n, PR::BN);
-  ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * (a.k + a.n), st);
+  ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n * PR::NA, 2.0 * a.rows * (a.k * PR::NA + a.n), st);
   TGP_LAUNCH(ps, (gated_out<PR, T, false>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
 }
 
-// y or dx, by the number of tiles: more than a block a CU (two shallow rings, 147456 x 64
-// of 256: 12.4 us, a deep one 16.0), one (4096 x 1024 of 4096: 50.5 us, shallow 59),
-// less, much less.
-template <typename PRL2, typename PRL, typename PRS, typename T>
+// y or dx, by the number of tiles of 128 x 128: more than one a CU (bfloat16: 256 x 128 a
+// block, 40000 x 304 of 600 58 us and by tiles of 128 x 128 62; float32: two shallow rings
+// a CU), one, less, much less.
+template <bool BKS, typename T>
 void launch_sum(const char* name, const char* name_join, OutArgs a, void* join, hipStream_t st) {
+  typedef Sums<BKS, sizeof(T) == 2 ? 2 : 1> PR;
+  typedef typename PR::L2 PRL2;
+  typedef typename PR::L PRL;
+  typedef typename PR::S PRS;
   const long tiles = (long)cdiv(a.rows, 128) * cdiv(a.n, 128);
   if (tiles > kFill) return launch_out<PRL2, T>(name, a, st);
   if (tiles == kFill) return launch_out<PRL, T>(name, a, st);
@@ -1479,7 +1504,7 @@ void launch_sum(const char* name, const char* name_join, OutArgs a, void* join, 
   a.tm = cdiv(a.rows, PRS::BM);
   a.tn = cdiv(a.n, PRS::BN);
   {
-    ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n, 2.0 * a.rows * a.k + 4.0 * d.n * a.rows * a.n, st);
+    ProfScope ps(name, 2.0 * a.rows * a.k * a.n * a.s.n * PRS::NA, 2.0 * a.rows * a.k * PRS::NA + 4.0 * d.n * a.rows * a.n, st);
     TGP_LAUNCH(ps, (gated_out<PRS, T, true>), dim3((unsigned)a.tm * a.tn * d.n), dim3(PRS::T), 0, st, a);
   }
   ProfScope ps(name_join, 0, (4.0 * d.n + 2) * a.rows * a.n, st);
@@ -1490,7 +1515,7 @@ HiddenArgs hidden_args(const Call& c, const Matrix& x, const Matrix& wg, const M
   const tgp_gated_shape& s = c.g.s;
   HiddenArgs a{};
   pairs(c.p.parts, c.p.parts, [&](int i, int j) {
-    a.s.a[a.s.n] = x.part[i];
+    a.s.a[a.s.n][0] = x.part[i];
     a.s.b[a.s.n][0] = wg.part[j];
     a.s.b[a.s.n++][1] = wu.part[j];
   });
@@ -1574,14 +1599,14 @@ hipError_t forward_few(const Gated& g, const T* x, long ldx, T* y, long ldy, voi
 
 template <typename T>
 hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void* ws, hipStream_t st) {
-  constexpr int P = sizeof(T) == 2 ? 1 : 3;
+  constexpr int P = sizeof(T) == 2 ? 1 : 3, L = sizeof(T) == 2 ? 2 : 3;
   const tgp_gated_shape& s = g.s;
   Call c{g, plan_of(s, g.rows, false), (char*)ws, st};
   if (few(s, g.rows)) return forward_few<T>(g, x, ldx, y, ldy, (char*)ws + c.p.h, c.p.hidp, st);
   const Matrix wg = c.operand(g.w.gate, s.cin, s.hidden, s.cin, c.p.wg, s.hidden);
   const Matrix wu = c.operand(g.w.up, s.cin, s.hidden, s.cin, c.p.wu, s.hidden);
   const Matrix wd = c.operand(g.w.down, s.hidden, s.cout, s.hidden, c.p.wd, s.cout);
-  const Matrix h = matrix_at(ws, c.p.h, P, c.p.chunk, c.p.hidp);
+  const Matrix h = matrix_at(ws, c.p.h, L, c.p.chunk, c.p.hidp);
   for (long r0 = 0; r0 < g.rows; r0 += c.p.chunk) {
     const long rows = std::min(c.p.chunk, g.rows - r0);
     const Matrix xm = c.operand(x + r0 * ldx, ldx, rows, s.cin, c.p.x, c.p.chunk);
@@ -1600,15 +1625,15 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
       typedef decltype(pr) PR;
       a.tm = cdiv(rows, PR::BM);
       a.tn = cdiv(s.hidden, PR::BN);
-      ProfScope ps("gated_hidden", 4.0 * rows * s.cin * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.hidden), st);
-      TGP_LAUNCH(ps, (gated_hidden<PR, decltype(act)::value, P>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
+      ProfScope ps("gated_hidden", 4.0 * rows * s.cin * s.hidden * a.s.n, 2.0 * rows * (s.cin + L * s.hidden), st);
+      TGP_LAUNCH(ps, (gated_hidden<PR, decltype(act)::value, L>), dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
     };
     with_act(s.act, [&](auto act) {
       if (fills(rows, s.hidden)) hidden(HidL(), act);
       else hidden(HidS(), act);
     });
     OutArgs o{};
-    add_pairs(&o.s, h, P, wd, P);
+    add_sum<T>(&o, h, wd);
     o.lda = h.ld;
     o.ldb = wd.ld;
     o.rows = (int)rows;
@@ -1618,7 +1643,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
     o.y = y + r0 * ldy;
     o.ldy = ldy;
     o.vec = at16(o.y, ldy, sizeof(T));
-    launch_sum<OutL2, OutL, OutS, T>("gated_out", "gated_out_join", o, (char*)ws + c.p.join, st);
+    launch_sum<false, T>("gated_out", "gated_out_join", o, (char*)ws + c.p.join, st);
   }
   return launch_status();
 }
@@ -1768,9 +1793,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
     }
     if (dx) {   // last: it may be written over x or dy
       OutArgs o{};
-      const int nd = sizeof(T) == 2 ? 1 : 3;
-      add_pairs(&o.s, dg, nd, wg, P);
-      add_pairs(&o.s, du, nd, wu, P);
+      add_sum<T>(&o, dg, wg);
+      add_sum<T>(&o, du, wu);
       o.lda = p.hidp;
       o.ldb = wg.ld;
       o.rows = (int)rows;
@@ -1779,7 +1803,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       o.y = dx + r0 * lddx;
       o.ldy = lddx;
       o.vec = at16(o.y, lddx, sizeof(T));
-      launch_sum<DxL2, DxL, DxS, T>("gated_dx", "gated_dx_join", o, (char*)ws + p.join, st);
+      launch_sum<true, T>("gated_dx", "gated_dx_join", o, (char*)ws + p.join, st);
     }
   }
   return launch_status();

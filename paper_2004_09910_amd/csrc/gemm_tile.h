@@ -143,23 +143,23 @@ struct Feed {
 // What one launch's tile products run over: `segs` pairs of matrices of the same
 // shape one after the other (parts of a sum whose factors are split).
 constexpr int kMaxSegs = 12;
-template <int NB>
+template <int NB, int NA = 1>
 struct Segs {
-  const bf16_t* a[kMaxSegs];
+  const bf16_t* a[kMaxSegs][NA];
   const bf16_t* b[kMaxSegs][NB];
   int n;
 };
 
 // WM x WN waves of MT x NT fragments of 32 x 32, for each of NB right factors that
-// share the left one; NS slots.  Lane l of a wave holds row l % 32 of a fragment and
+// share the left one, whose NA parts are summed; NS slots.  Lane l of a wave holds row l % 32 of a fragment and
 // its columns 8 (v / 4) + 4 (l / 32) + v % 4.
-template <int MT_, int NT_, int WM_, int WN_, int BK_, int NS_, bool AKS, bool BKS, int NB_>
+template <int MT_, int NT_, int WM_, int WN_, int BK_, int NS_, bool AKS, bool BKS, int NB_, int NA_ = 1>
 struct Product {
-  static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, BK = BK_, NS = NS_, NB = NB_;
+  static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, BK = BK_, NS = NS_, NB = NB_, NA = NA_;
   static constexpr int NW = WM * WN, T = 64 * NW, BM = 32 * MT * WM, BN = 32 * NT * WN;
   typedef Feed<BM, BK, AKS, NW> FA;
   typedef Feed<BN, BK, BKS, NW> FB;
-  static constexpr int SLOT = FA::BYTES + NB * FB::BYTES, LPS = FA::LOADS + NB * FB::LOADS;
+  static constexpr int SLOT = NA * FA::BYTES + NB * FB::BYTES, LPS = NA * FA::LOADS + NB * FB::LOADS;
   static constexpr int LDS = NS * SLOT;
   static_assert(LDS <= 160 * 1024 && NS >= 2, "LDS ring");
 
@@ -177,27 +177,31 @@ struct Product {
   // The sums over values k0 .. k1 (k0 a multiple of BK) of every pair of `s`: rows
   // i0 .. of A (m in all), columns j0 .. of B (n).  extra(a, i, p): more products of a
   // left fragment (u32x4, fragment row i) of pair p.
-  template <typename X>
-  __device__ __forceinline__ void run(unsigned char* ring, const Segs<NB>& s, long lda, long ldb, int m, int n, int i0,
+  template <int SA, typename X>
+  __device__ __forceinline__ void run(unsigned char* ring, const Segs<NB, SA>& s, long lda, long ldb, int m, int n, int i0,
                                       int j0, int k0, int k1, X extra) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    FA fa;
+    static_assert(SA >= NA, "parts");
+    FA fa[NA];
     FB fb[NB];
-    fa.init(lda, m - i0);
+#pragma unroll
+    for (int q = 0; q < NA; ++q) fa[q].init(lda, m - i0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) fb[b].init(ldb, n - j0);
     const int per = (k1 - k0 + BK - 1) / BK, total = per * s.n;
     const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)TGP_LDS(ring) + wave * 1024);
     int seg = 0, left = k1 - k0;   // of the next stage to be sent for
     auto seek = [&]() {
-      fa.seek(s.a[seg], i0, k0);
+#pragma unroll
+      for (int q = 0; q < NA; ++q) fa[q].seek(s.a[seg][q], i0, k0);
 #pragma unroll
       for (int b = 0; b < NB; ++b) fb[b].seek(s.b[seg][b], j0, k0);
     };
     seek();
     auto next = [&]() __attribute__((always_inline)) {
-      fa.next(left);
+#pragma unroll
+      for (int q = 0; q < NA; ++q) fa[q].next(left);
 #pragma unroll
       for (int b = 0; b < NB; ++b) fb[b].next(left);
       left -= BK;
@@ -209,18 +213,19 @@ struct Product {
     auto load = [&](auto uc, int slot) __attribute__((always_inline)) {   // load u of its LPS
       constexpr int u = decltype(uc)::value;
       const unsigned d = lds + slot * SLOT;
-      if constexpr (u < FA::LOADS) {
-        fa.template load<u>(d);
+      if constexpr (u < NA * FA::LOADS) {
+        constexpr int q = u / FA::LOADS;
+        fa[q].template load<u % FA::LOADS>(d + q * FA::BYTES);
       } else {
-        constexpr int v = u - FA::LOADS, b = v / FB::LOADS;
-        fb[b].template load<v % FB::LOADS>(d + FA::BYTES + b * FB::BYTES);
+        constexpr int v = u - NA * FA::LOADS, b = v / FB::LOADS;
+        fb[b].template load<v % FB::LOADS>(d + NA * FA::BYTES + b * FB::BYTES);
       }
     };
     int pa[MT], pb[NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) pa[i] = FA::place((wm * MT + i) * 32);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) pb[j] = FA::BYTES + FB::place((wn * NT + j) * 32);
+    for (int j = 0; j < NT; ++j) pb[j] = NA * FA::BYTES + FB::place((wn * NT + j) * 32);
 #pragma unroll
     for (int k = 0; k < NS; ++k)
       if (k < total) {
@@ -229,10 +234,12 @@ struct Product {
       }
     // the fragments of the stage to be multiplied
     constexpr int H = BK / 16;
-    u32x4 a[H][MT], b[H][NB][NT];
+    u32x4 a[H][NA][MT], b[H][NB][NT];
     auto read = [&](int h, const unsigned char* st) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[h][i] = FA::frag(st, pa[i], h);
+      for (int q = 0; q < NA; ++q)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) a[h][q][i] = FA::frag(st + q * FA::BYTES, pa[i], h);
 #pragma unroll
       for (int q = 0; q < NB; ++q)
 #pragma unroll
@@ -261,12 +268,14 @@ struct Product {
 #pragma unroll
         for (int q = 0; q < NB; ++q)
 #pragma unroll
-          for (int i = 0; i < MT; ++i)
+          for (int r = NA - 1; r >= 0; --r)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-              acc[q][i][j] = mfma32(as_bf16x8(b[h][q][j]), as_bf16x8(a[h][i]), acc[q][i][j]);
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) extra(a[h][i], i, pair);
+              for (int j = 0; j < NT; ++j)
+                acc[q][i][j] = mfma32(as_bf16x8(b[h][q][j]), as_bf16x8(a[h][r][i]), acc[q][i][j]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) extra(a[h][0][i], i, pair);
         read(h, ring + nslot * SLOT);
         if (send) each<(h + 1) * LPS / H - h * LPS / H>([&](auto u) {
           load(std::integral_constant<int, h * LPS / H + decltype(u)::value>(), slot);

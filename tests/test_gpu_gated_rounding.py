@@ -85,3 +85,16 @@ def test_narrow(cin, cout):
 def test_narrow_float32(cin, cout, hidden):
     """The same of a float32 network, by test_gpu_gated.py's bounds."""
     Block(131, cin, hidden, cout, "fp32", (cin + hidden) % 2).check()
+
+
+# small tiles, a split sum, large tiles with one and with several a compute unit
+@pytest.mark.parametrize("rows,cin,hidden,cout", [(65, 257, 40, 24), (300, 264, 200, 72), (150, 300, 1500, 264), (2100, 264, 520, 2048),
+                                                  (4200, 264, 1100, 1100)])
+def test_wide(rows, cin, hidden, cout):
+    _check(rows, cin, hidden, cout)
+
+
+@pytest.mark.parametrize("rows,cin,hidden,cout", [(3, 8, 16, 8), (65, 257, 40, 24), (300, 264, 200, 72), (150, 300, 1500, 264),
+                                                  (1100, 2048, 264, 264), (2100, 2048, 264, 40), (4200, 1100, 520, 136)])
+def test_backward(rows, cin, hidden, cout):
+    _check(rows, cin, hidden, cout, forward=False, backward=True)
