@@ -420,8 +420,8 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * 1 for a step's first micro-batch, 0 to add to them.  dx NULL: not wanted.  dx
  * may be dy or x itself at the same row distance and width; y and dx may not
  * overlap x or dy otherwise (EINVAL).  Of a TGP_BF16 network dg, du and h enter
- * dx rounded to bfloat16, and the weights' gradients as two bfloat16s each (16
- * bits; 3e-6 of the gradient's norm).
+ * these products as two bfloat16s each (16 bits; the weights' gradients are 3e-6
+ * of their norm off), and dx is rounded once.
  * rows = 0 leaves the accumulators as they are, or zeroes them (overwrite).
  * Sums over rows run in an order fixed by the shape, rows and alignment.
  *

@@ -960,10 +960,13 @@ struct SlimArgs {
 // the weights' gradients' products over pixels take h, dg and du, with the rows of x and
 // dy read from LDS in the order that those have (values j of a lane are pixels 4 (l / 32)
 // + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
-// For dx, dg and du go through LDS, rows of hidden channels beside the weights' rows.
-// What bounds it are the activations and the splitting in two parts, some 60 operations
-// a value of the hidden channels (147456 x 64, 256 hidden, GELU: 121 us and 11 for the
-// ranges' sums; by a launch for h, dg and du, one for the weights and one for dx 365).
+// For dx, dg and du go through LDS, 32 pixels at a time in their two parts, rows of hidden
+// channels beside the weights' rows.
+// What bounds it are the activations, the splitting in two parts and the products, one
+// after the other (147456 x 64, 256 hidden: SiLU 109 us, GELU 135, and 11 for the ranges'
+// sums; dx of first parts alone took 16 less, its values up to 25 times what a rounding
+// allows; by a launch for h, dg and du, one for the weights and one for dx the pass is
+// 365).  The two halves of 64 pixels are a loop: unrolled, 39 registers spill (154).
 template <int ACT, bool GRADS>
 __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
   typedef Feed<64, 64, false, 2> F;   // (its layout: rows of 64 values)
@@ -1035,7 +1038,7 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
     meet();
     if (i0 + 64 < hi) send(i0 + 64, slot ^ 1);
     const unsigned char *const xt = xs + slot * 2 * TILE, *const yt = xt + TILE;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       __builtin_amdgcn_sched_barrier(0);   // one fragment's values at a time: registers
       f32x16_t g{}, u{}, d{};
@@ -1060,13 +1063,15 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
         bsg += g[v];
         bsu += u[v];
       }
+      if (i && a.dx) meet();   // the first 32 pixels' sums are out of dgs
       // 16 pixels' parts of dg, du and h, and their products
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         __builtin_amdgcn_sched_barrier(0);
         const int s16 = (2 * i + k) * 2048;
-        // pixels 8 (2 k) + 4 half on, and 8 (2 k + 1) + 4 half on
-        const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 4 * i + 2 * k;
+        // of the 32 pixels' first parts chunks 0 .. 3, of their second 4 .. 7: pixels 8 (2 k) +
+        // 4 half on, and 8 (2 k + 1) + 4 half on
+        const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 2 * k;
 #pragma unroll
         for (int m = 0; m < 3; ++m) {
           u32x4 top, low;
@@ -1084,6 +1089,8 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
             unsigned char* const ds = m ? dus : dgs;
             *(uint2*)(ds + to + ((c ^ sw) << 4)) = make_uint2(top[0], top[1]);
             *(uint2*)(ds + to + (((c + 1) ^ sw) << 4)) = make_uint2(top[2], top[3]);
+            *(uint2*)(ds + to + (((c + 4) ^ sw) << 4)) = make_uint2(low[0], low[1]);
+            *(uint2*)(ds + to + (((c + 5) ^ sw) << 4)) = make_uint2(low[2], low[3]);
           }
           if constexpr (GRADS)
 #pragma unroll
@@ -1100,6 +1107,32 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+      if (!a.dx) continue;
+      meet();
+      // a fragment of dx a wave: of dg Wg (waves 0 to 3) or du Wu, of first or second parts
+      const int part = wave >> 1 & 1, cf = wave & 1;
+      const unsigned char *const ds = wave < 4 ? dgs : dus, *const ws = wave < 4 ? wgs : wus;
+      f32x16_t o{};
+#pragma unroll 2
+      for (int h = 0; h < 16; ++h)
+        o = mfma32(as_bf16x8(column(ws + h * 2048, cf)), as_bf16x8(column(ds + h * 2048, part)), o);
+      meet();
+      float* const rest = (float*)dgs + lane;   // [wave - 2][value][lane]
+      if (wave >= 2)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) rest[(wave - 2) * 1024 + v * 64] = o[v];
+      meet();
+      if (wave < 2) {
+        // beside waves 0 and 1: the first parts of du, the second of dg and of du
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float* const q = rest + wave * 1024 + v * 64;
+          o[v] = (o[v] + q[2 * 1024]) + (q[0] + q[4 * 1024]);
+        }
+        const float none[16] = {};
+        const int r = i0 + 32 * i + (lane & 31);
+        put_out<bf16_t>(o, none, a.dx + r * a.lddx, r < hi, 32 * cf, a.cin, a.vec);
+      }
     }
     // column sums of dy: eight pixels a wave
     if constexpr (GRADS)
@@ -1107,28 +1140,6 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
     for (int z = 0; z < 8; ++z) {
       const int r = 8 * wave + z;
       bsd += bf2f(*(const bf16_t*)(yt + r * 128 + (((lane >> 3) ^ F::swz(r)) << 4) + 2 * (lane & 7)));
-    }
-    meet();
-    if (!a.dx) continue;
-    // a fragment of dx a wave, of dg Wg (waves 0 to 3) or du Wu
-    const int pf = wave >> 1 & 1, cf = wave & 1;
-    const unsigned char *const ds = wave < 4 ? dgs : dus, *const ws = wave < 4 ? wgs : wus;
-    f32x16_t o{};
-#pragma unroll 2
-    for (int h = 0; h < 16; ++h)
-      o = mfma32(as_bf16x8(column(ws + h * 2048, cf)), as_bf16x8(column(ds + h * 2048, pf)), o);
-    meet();
-    float* const half2 = (float*)dgs + (wave & 3) * 1024 + lane;
-    if (wave >= 4)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) half2[v * 64] = o[v];
-    meet();
-    if (wave < 4) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[v] += half2[v * 64];
-      const float none[16] = {};
-      const int r = i0 + 32 * pf + (lane & 31);
-      put_out<bf16_t>(o, none, a.dx + r * a.lddx, r < hi, 32 * cf, a.cin, a.vec);
     }
   }
   if constexpr (!GRADS) return;

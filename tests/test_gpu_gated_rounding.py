@@ -94,6 +94,12 @@ def test_wide(rows, cin, hidden, cout):
     _check(rows, cin, hidden, cout)
 
 
+@pytest.mark.parametrize("rows", [1, 33, 64, 100, 3000])
+@pytest.mark.parametrize("cin,hidden,cout", [(64, 256, 64), (24, 72, 40), (33, 250, 61), (64, 129, 1), (1, 65, 64)])
+def test_narrow_backward(rows, cin, hidden, cout):
+    _check(rows, cin, hidden, cout, forward=False, backward=True)
+
+
 @pytest.mark.parametrize("rows,cin,hidden,cout", [(3, 8, 16, 8), (65, 257, 40, 24), (300, 264, 200, 72), (150, 300, 1500, 264),
                                                   (1100, 2048, 264, 264), (2100, 2048, 264, 40), (4200, 1100, 520, 136)])
 def test_backward(rows, cin, hidden, cout):
