@@ -419,9 +419,9 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * tgp_bind_params' (each may be NULL: not wanted; grads NULL: none): overwrite =
  * 1 for a step's first micro-batch, 0 to add to them.  dx NULL: not wanted.  dx
  * may be dy or x itself at the same row distance and width; y and dx may not
- * overlap x or dy otherwise (EINVAL).  Of a TGP_BF16 network dg, du and h enter
- * these products as two bfloat16s each (16 bits; the weights' gradients are 3e-6
- * of their norm off), and dx is rounded once.
+ * overlap x or dy otherwise (EINVAL).  Of a TGP_BF16 network dg and du enter dx
+ * as two bfloat16s each (16 bits), which is rounded once, and dg, du and h the
+ * weights' gradients as three (24 bits).
  * rows = 0 leaves the accumulators as they are, or zeroes them (overwrite).
  * Sums over rows run in an order fixed by the shape, rows and alignment.
  *

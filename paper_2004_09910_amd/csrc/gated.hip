@@ -15,10 +15,10 @@
 // (gated_slim) and the ranges' sums.
 //
 // Matrix instructions take bfloat16.  Of a TGP_BF16 network x, dy and the weights
-// are that, and h, dg and du two bfloat16s each (16 bits, 2^-16 of a value): y and dx
-// are then rounded once, and the weights' gradients, float32 sums, 3e-6 of their norm
-// off (three parts, half as many products again, would bring that to float32's 1e-7;
-// one part, half of them, has 2e-3).  Of a TGP_FP32 network every factor is three
+// are that.  h, dg and du are two bfloat16s each (16 bits, 2^-16 of a value) for y and
+// dx, which are then rounded once, and three, their 24 bits, for the weights' gradients,
+// float32 sums (two parts, a third of the products less, leave 3e-6 of a gradient's
+// norm where float32 sums have 1e-7; one part 2e-3).  Of a TGP_FP32 network every factor is three
 // bfloat16s, its 24 bits, and six of the nine products are summed, small ones
 // first: what is left out is 2^-24 of a term.  A sum over split factors is one
 // sum over pairs of their parts.
@@ -114,8 +114,8 @@ __device__ __forceinline__ float exp2_of(float v, float rest, float c, float tai
 // p = 1 / (1 + exp(-g)).  GELU is g Phi(g) with Phi(-|g|) = exp(-g g / 2) R(|g|) and R as
 // t times a polynomial in t = 1 / (1 + 0.265 |g|), a least-squares fit of erfcx(|g| / sqrt
 // 2) / 2 whose largest relative error up to |g| = 15 was brought down to 1.6e-8; in float32
-// arithmetic 4e-7.  Without FINE the exponential adds 5e-8 g g of the value (2e-6 at -6),
-// which two bfloat16s do not see.
+// arithmetic 4e-7.  Without FINE the exponential adds 5e-8 g g of the value (2e-6 at -6):
+// for y of bfloat16, whose h is two bfloat16s.
 template <int ACT, bool FINE>
 __device__ __forceinline__ void act_of(float g, float* a, float* slope) {
   if constexpr (ACT == TGP_ACT_SILU) {
@@ -216,7 +216,8 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
   }
 }
 
-// h, dg and du of a tile, each in P parts (no h where no weight's gradient is wanted).
+// h, dg and du of a tile, each in P parts: three, or of bfloat16 two, and no h, where no
+// weight's gradient is wanted.
 template <typename PR, typename PD, int ACT, int P, bool GRADS>
 __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1) void gated_back(HiddenArgs a) {
   static_assert(PR::BM == PD::BM && PR::BN == PD::BN && PR::MT == PD::MT && PR::WN == PD::WN, "one tile");
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(PR::T, PR::NW == 8 || PR::LDS <= 80 * 1024 ? 2 : 1)
 #pragma unroll
       for (int z = 0; z < 16; ++z) {
         float act, slope;
-        act_of<ACT, P == 3>(p.acc[0][i][j][z] + bg[z], &act, &slope);
+        act_of<ACT, true>(p.acc[0][i][j][z] + bg[z], &act, &slope);
         const float u = p.acc[1][i][j][z] + bu[z], dh = d.acc[0][i][j][z];
         h[z] = act * u;
         dg[z] = dh * u * slope;
@@ -962,11 +963,10 @@ struct SlimArgs {
 // + j and, from j = 4 on, 4 more).  The gradients' sums stay in registers to the end.
 // For dx, dg and du go through LDS, 32 pixels at a time in their two parts, rows of hidden
 // channels beside the weights' rows.
-// What bounds it are the activations, the splitting in two parts and the products, one
-// after the other (147456 x 64, 256 hidden: SiLU 109 us, GELU 135, and 11 for the ranges'
-// sums; dx of first parts alone took 16 less, its values up to 25 times what a rounding
-// allows; by a launch for h, dg and du, one for the weights and one for dx the pass is
-// 365).  The two halves of 64 pixels are a loop: unrolled, 39 registers spill (154).
+// What bounds it are the activations, the splitting in parts and the products, one after
+// the other (147456 x 64, 256 hidden, GELU: 123 us, and 11 for the ranges' sums; by a launch
+// for h, dg and du, one for the weights and one for dx 365).  The two halves of 64 pixels
+// are a loop: unrolled, 39 registers spill (16 us).
 template <int ACT, bool GRADS>
 __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
   typedef Feed<64, 64, false, 2> F;   // (its layout: rows of 64 values)
@@ -1054,7 +1054,7 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         float act, slope;
-        act_of<ACT, false>(g[v] + bg, &act, &slope);
+        act_of<ACT, true>(g[v] + bg, &act, &slope);
         const float up = u[v] + bu, dh = d[v];
         const bool in = 8 * (v / 4) + v % 4 < left;   // (a bias may be infinite)
         g[v] = in ? dh * up * slope : 0.f;
@@ -1074,31 +1074,34 @@ __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
         const int to = hid * 128 + 8 * half, sw = F::swz(hid), c = 2 * k;
 #pragma unroll
         for (int m = 0; m < 3; ++m) {
-          u32x4 top, low;
+          constexpr int Q = GRADS ? 3 : 2;
+          u32x4 q[Q];
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             const f32x16_t& w = m == 0 ? g : m == 1 ? u : d;
-            const float e = w[8 * k + 2 * z], f = w[8 * k + 2 * z + 1];
-            const unsigned p = pack_bf16(e, f);
-            top[z] = p;
-            const float he = __uint_as_float(p << 16), hf = __uint_as_float(p & 0xffff0000u);
-            const bool ie = (p & 0x7f80u) == 0x7f80u, jf = (p & 0x7f800000u) == 0x7f800000u;
-            low[z] = pack_bf16(ie ? 0.f : e - he, jf ? 0.f : f - hf);
+            float e = w[8 * k + 2 * z], f = w[8 * k + 2 * z + 1];
+#pragma unroll
+            for (int n = 0; n < Q; ++n) {   // (an infinity leaves NaN)
+              q[n][z] = pack_bf16(e, f);
+              e -= __uint_as_float(q[n][z] << 16);
+              f -= __uint_as_float(q[n][z] & 0xffff0000u);
+            }
           }
           if (m < 2 && a.dx) {
             unsigned char* const ds = m ? dus : dgs;
-            *(uint2*)(ds + to + ((c ^ sw) << 4)) = make_uint2(top[0], top[1]);
-            *(uint2*)(ds + to + (((c + 1) ^ sw) << 4)) = make_uint2(top[2], top[3]);
-            *(uint2*)(ds + to + (((c + 4) ^ sw) << 4)) = make_uint2(low[0], low[1]);
-            *(uint2*)(ds + to + (((c + 5) ^ sw) << 4)) = make_uint2(low[2], low[3]);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              *(uint2*)(ds + to + (((c + 4 * n) ^ sw) << 4)) = make_uint2(q[n][0], q[n][1]);
+              *(uint2*)(ds + to + (((c + 4 * n + 1) ^ sw) << 4)) = make_uint2(q[n][2], q[n][3]);
+            }
           }
           if constexpr (GRADS)
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
               const u32x4 x = column((m < 2 ? xt : yt) + s16, f);
 #pragma unroll
-              for (int w = 1; w >= 0; --w) {
-                const bf16x8_t e = as_bf16x8(w ? low : top);
+              for (int w = Q - 1; w >= 0; --w) {
+                const bf16x8_t e = as_bf16x8(q[w]);
                 if (m == 0) sg[f] = mfma32(as_bf16x8(x), e, sg[f]);
                 else if (m == 1) su[f] = mfma32(as_bf16x8(x), e, su[f]);
                 else sd[f] = mfma32(e, as_bf16x8(x), sd[f]);
@@ -1303,7 +1306,7 @@ constexpr long kFill = 256;   // tiles that fill the chip
 
 // A call's workspace and how its pixels are taken.
 struct Plan {
-  int parts, low;        // of a factor; of h, dg and du
+  int parts, hparts;     // of a factor; of h, dg and du
   long cinp, hidp, coutp;
   long chunk;            // pixels at a time
   bool slim;             // a backward pass in one launch
@@ -1348,15 +1351,15 @@ size_t split_bytes(long rows, long cols, int k, int pairs) {
 Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   Plan p{};
   p.parts = s.dtype == TGP_BF16 ? 1 : 3;
-  p.low = s.dtype == TGP_BF16 ? 2 : 3;
+  p.hparts = s.dtype == TGP_BF16 && !backward ? 2 : 3;
   p.cinp = round_up(s.cin, 8);
   p.hidp = round_up(s.hidden, 8);
   p.coutp = round_up(s.cout, 8);
   // so many pixels that what lies between launches stays in the caches, but that
   // a launch fills the chip
-  const long a_row = 2 * (backward ? 3 * p.low * p.hidp + p.parts * (p.cinp + p.coutp)
-                                   : p.low * p.hidp + p.parts * p.cinp);
-  const long most = (long)128 << 20;
+  const long a_row = 2 * (backward ? 3 * p.hparts * p.hidp + p.parts * (p.cinp + p.coutp)
+                                   : p.hparts * p.hidp + p.parts * p.cinp);
+  const long most = (long)(backward && p.parts == 1 ? 192 : 128) << 20;   // (of 256 MB)
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
   // (64 channels, 256 hidden: 1 pixel 18.7 us and in three launches 24.1, 64 18.7 and 18.5,
   // 1000 23.4 and 27.3, 12544 35.7 and 41.1, 147456 143 and 365; with few hidden channels
@@ -1375,10 +1378,10 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   p.wd = take((size_t)2 * p.parts * s.cout * p.hidp);
   p.x = take((size_t)2 * p.parts * p.chunk * p.cinp);
   if (!backward) {
-    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.low * p.chunk * p.hidp);
+    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.hparts * p.chunk * p.hidp);
   } else {
     p.dy = take((size_t)2 * p.parts * p.chunk * p.coutp);
-    const size_t plane = p.slim ? 0 : (size_t)2 * p.low * p.chunk * p.hidp;
+    const size_t plane = p.slim ? 0 : (size_t)2 * p.hparts * p.chunk * p.hidp;
     p.h = take(plane);
     p.dg = take(plane);
     p.du = take(plane);
@@ -1662,7 +1665,7 @@ hipError_t forward_t(const Gated& g, const T* x, long ldx, T* y, long ldy, void*
 template <typename T>
 hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long ldx, T* dx, long lddx,
                       const tgp_gated_grads& gr, bool overwrite, void* ws, hipStream_t st) {
-  constexpr int P = sizeof(T) == 2 ? 1 : 3, L = sizeof(T) == 2 ? 2 : 3;
+  constexpr int P = sizeof(T) == 2 ? 1 : 3, L = 3;
   const tgp_gated_shape& s = g.s;
   const bool grads = gr.gate || gr.up || gr.down || gr.b_gate || gr.b_up || gr.b_down;
   Call c{g, plan_of(s, g.rows, true), (char*)ws, st};
@@ -1735,7 +1738,8 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       a.tm = cdiv(rows, PR::BM);
       a.tn = cdiv(s.hidden, PR::BN);
       ProfScope ps("gated_back", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
-      TGP_LAUNCH(ps, (gated_back<PR, decltype(pd), decltype(act)::value, L, decltype(all)::value>),
+      constexpr bool ALL = decltype(all)::value;
+      TGP_LAUNCH(ps, (gated_back<PR, decltype(pd), decltype(act)::value, ALL ? L : sizeof(T) == 2 ? 2 : 3, ALL>),
                  dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
     };
     with_act(s.act, [&](auto act) {

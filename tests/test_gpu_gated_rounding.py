@@ -15,7 +15,7 @@ import torch
 
 import block_ops_ref as ref
 from gpu_util import say
-from test_gpu_gated import Block
+from test_gpu_gated import NAMES, Block
 
 pytestmark = pytest.mark.gpu
 U, SURE = 2.0 ** -24, 7.0
@@ -104,3 +104,17 @@ def test_narrow_backward(rows, cin, hidden, cout):
                                                   (1100, 2048, 264, 264), (2100, 2048, 264, 40), (4200, 1100, 520, 136)])
 def test_backward(rows, cin, hidden, cout):
     _check(rows, cin, hidden, cout, forward=False, backward=True)
+
+
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("rows,cin,hidden,cout", [(16, 16, 72, 16), (40, 8, 200, 24), (70, 12, 256, 9),       # one launch
+                                                  (16, 16, 300, 16), (33, 8, 24, 8), (300, 16, 300, 8)])     # tile products
+def test_weights_gradients(rows, cin, hidden, cout, act):
+    """Float32 sums of factors with 24 bits: off by sqrt(K) 2^-24 of their norm for the sum over the pixels, for g and
+    u and for dh, and by 8 x 2^-24 for the activation's arithmetic."""
+    say("gated, weights' gradients", rows, cin, hidden, cout, act)
+    b = Block(rows, cin, hidden, cout, "bf16", act)
+    tol = U * (rows ** 0.5 + 2 * cin ** 0.5 + cout ** 0.5 + 8)
+    want = ref.gated(b.x.cpu(), b.host(), act, b.dy.cpu())
+    for name, p, q in zip(NAMES, b.backward()[1:], want[1:]):
+        assert ref.rel(p, q) <= tol, (name, ref.rel(p, q), tol)
