@@ -84,87 +84,106 @@ __global__ __launch_bounds__(kT) void res_fwd_any(const T* r, long ldr, const T*
   }
 }
 
-// One gate's pixels (without a gate: one pixel) a block at a time, G of a row in
-// LDS; a column's sums belong to one thread of the block and lie in part[block][6][C]:
-// dz ohat, dz, S1, S2, and U1 and U2 of the present gate.
-template <typename T>
-__global__ __launch_bounds__(kT) void res_bwd_any(const T* dz, long lddz, const T* dout, long lddout, const T* out,
-                                                  long ldout, const T* f, long ldf, const T* gate, long ldgate,
-                                                  long group, Vectors w, int post, const float4* stats, T* dr,
-                                                  long lddr, T* df, long lddf, T* dgate, long lddgate, float* part,
-                                                  long rows, int C) {
+// Which pixels a block takes.  Ranges: `ranges` blocks for each of the groups of
+// pixels that share a gate (one group of all pixels where none do), `per` pixels
+// each.  Whole: whole groups by a wave (a block, where a row is a block's), side
+// by side in parts of `part` lanes' rows (a power of two) where they are small.
+struct BwdArgs {
+  const void *dz, *dout, *out, *f, *gate;
+  void *dr, *df, *dgate;
+  long lddz, lddout, ldout, ldf, ldgate, lddr, lddf, lddgate, rows, group, per;
+  Vectors w;
+  const float4* stats;
+  float* part;   // [block][4][C]: dz ohat, dz, S1, S2 (ranges of a shared gate: U1, U2)
+  int C, G, ranges, slots;
+  int shared;    // a gate for several pixels
+};
+
+// A row a block at a time, G of it in LDS; a column's sums belong to one thread of the
+// block and lie in part, of whole groups with U1 and U2 of the present one behind them
+// (six a block).  (32768 x 4104 bfloat16, a gate for 8192 pixels: 2.7 ms, by a block a
+// gate 341.)
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kT) void res_bwd_any(BwdArgs a, int post) {
   extern __shared__ float row[];
   __shared__ float s4[4];
-  float* mine = part + (long)blockIdx.x * 6 * C;
+  const T *dz = (const T*)a.dz, *dout = (const T*)a.dout, *out = (const T*)a.out, *f = (const T*)a.f;
+  const int C = a.C;
+  const Vectors& w = a.w;
+  float* mine = a.part + (long)blockIdx.x * (WHOLE ? 6 : 4) * C;
   float *P0 = mine, *P1 = P0 + C, *S1 = P1 + C, *S2 = S1 + C, *U1 = S2 + C, *U2 = U1 + C;
   for (int c = threadIdx.x; c < C; c += kT) P0[c] = P1[c] = S1[c] = S2[c] = 0.f;
   const float inv_c = 1.f / C;
-  for (long u = blockIdx.x; u * group < rows; u += gridDim.x) {
-    const T* q = gate ? gate + u * ldgate : nullptr;
-    for (int c = threadIdx.x; c < C; c += kT) U1[c] = U2[c] = 0.f;
-    for (long p = u * group; p < (u + 1) * group; ++p) {
-      const float4 st = stats[p];
-      float ms = 0.f, mp = 0.f;
-      if (dz) {
-        for (int c = threadIdx.x; c < C; c += kT) {
-          const float d = Elt<T>::ld(dz + p * lddz + c), a = d * at_or(w.pre_gain, c, 1.f);
-          const float o = (Elt<T>::ld(out + p * ldout + c) - st.z) * st.w;
-          ms += a;
-          mp += a * o;
-          P0[c] += d * o;
-          P1[c] += d;
-        }
-        ms = block_sum(ms, s4) * inv_c;
-        mp = block_sum(mp, s4) * inv_c;
-      }
-      float ns = 0.f, np = 0.f;
+  // pixel p with its gate at q; A1 and A2 take G fhat and G (times the gate, where it is the pixel's own)
+  auto take = [&](long p, const T* q, float* A1, float* A2) {
+    const float4 st = a.stats[p];
+    float ms = 0.f, mp = 0.f;
+    if (dz) {
       for (int c = threadIdx.x; c < C; c += kT) {
-        float G = dout ? Elt<T>::ld(dout + p * lddout + c) : 0.f;
-        if (dz) {
-          const float a = Elt<T>::ld(dz + p * lddz + c) * at_or(w.pre_gain, c, 1.f);
-          const float o = (Elt<T>::ld(out + p * ldout + c) - st.z) * st.w;
-          G += st.w * (a - ms - o * mp);
-        }
-        row[c] = G;
-        if (!post) continue;
-        const float fh = (Elt<T>::ld(f + p * ldf + c) - st.x) * st.y;
-        const float b = G * at_or(w.scale, c, 1.f) * (q ? Elt<T>::ld(q + c) : 1.f) * at_or(w.post_gain, c, 1.f);
-        ns += b;
-        np += b * fh;
+        const float d = Elt<T>::ld(dz + p * a.lddz + c), e = d * at_or(w.pre_gain, c, 1.f);
+        const float o = (Elt<T>::ld(out + p * a.ldout + c) - st.z) * st.w;
+        ms += e;
+        mp += e * o;
+        P0[c] += d * o;
+        P1[c] += d;
       }
-      if (post) {
-        ns = block_sum(ns, s4) * inv_c;
-        np = block_sum(np, s4) * inv_c;
-      }
-      // all that a thread reads of a channel before what it writes there: outputs may lie on inputs
-      for (int c = threadIdx.x; c < C; c += kT) {
-        const float G = row[c], sc = at_or(w.scale, c, 1.f), g = q ? Elt<T>::ld(q + c) : 1.f;
-        float fh = Elt<T>::ld(f + p * ldf + c), v = G * sc * g, n = fh;
-        if (post) {
-          const float pg = at_or(w.post_gain, c, 1.f);
-          fh = (fh - st.x) * st.y;
-          n = pg * fh + at_or(w.post_bias, c, 0.f);
-          v = st.y * (v * pg - ns - fh * np);
-        }
-        if (group == 1) {
-          S1[c] += g * G * fh;
-          S2[c] += g * G;
-          if (dgate) Elt<T>::st(dgate + p * lddgate + c, sc * G * n);
-        } else {
-          U1[c] += G * fh;
-          U2[c] += G;
-        }
-        Elt<T>::st(dr + p * lddr + c, G);
-        Elt<T>::st(df + p * lddf + c, v);
-      }
+      ms = block_sum(ms, s4) * inv_c;
+      mp = block_sum(mp, s4) * inv_c;
     }
-    for (int c = threadIdx.x; c < C && group > 1; c += kT) {
-      const float g = q ? Elt<T>::ld(q + c) : 1.f;
-      S1[c] += g * U1[c];
-      S2[c] += g * U2[c];
-      if (dgate) {
-        const float n = post ? at_or(w.post_gain, c, 1.f) * U1[c] + at_or(w.post_bias, c, 0.f) * U2[c] : U1[c];
-        Elt<T>::st(dgate + u * lddgate + c, at_or(w.scale, c, 1.f) * n);
+    float ns = 0.f, np = 0.f;
+    for (int c = threadIdx.x; c < C; c += kT) {
+      float G = dout ? Elt<T>::ld(dout + p * a.lddout + c) : 0.f;
+      if (dz) {
+        const float e = Elt<T>::ld(dz + p * a.lddz + c) * at_or(w.pre_gain, c, 1.f);
+        const float o = (Elt<T>::ld(out + p * a.ldout + c) - st.z) * st.w;
+        G += st.w * (e - ms - o * mp);
+      }
+      row[c] = G;
+      if (!post) continue;
+      const float fh = (Elt<T>::ld(f + p * a.ldf + c) - st.x) * st.y;
+      const float b = G * at_or(w.scale, c, 1.f) * (q ? Elt<T>::ld(q + c) : 1.f) * at_or(w.post_gain, c, 1.f);
+      ns += b;
+      np += b * fh;
+    }
+    if (post) {
+      ns = block_sum(ns, s4) * inv_c;
+      np = block_sum(np, s4) * inv_c;
+    }
+    // all that a thread reads of a channel before what it writes there: outputs may lie on inputs
+    for (int c = threadIdx.x; c < C; c += kT) {
+      const float G = row[c], sc = at_or(w.scale, c, 1.f), g = q ? Elt<T>::ld(q + c) : 1.f;
+      float fh = Elt<T>::ld(f + p * a.ldf + c), v = G * sc * g, n = fh;
+      if (post) {
+        const float pg = at_or(w.post_gain, c, 1.f);
+        fh = (fh - st.x) * st.y;
+        n = pg * fh + at_or(w.post_bias, c, 0.f);
+        v = st.y * (v * pg - ns - fh * np);
+      }
+      const float h = a.shared ? G : g * G;
+      A1[c] += h * fh;
+      A2[c] += h;
+      if (a.dgate && !a.shared) Elt<T>::st((T*)a.dgate + p * a.lddgate + c, sc * G * n);
+      Elt<T>::st((T*)a.dr + p * a.lddr + c, G);
+      Elt<T>::st((T*)a.df + p * a.lddf + c, v);
+    }
+  };
+  if constexpr (!WHOLE) {
+    const long g = blockIdx.x / (unsigned)a.ranges;
+    const long lo = g * a.group + (blockIdx.x - g * a.ranges) * a.per, hi = min(lo + a.per, (g + 1) * a.group);
+    for (long p = lo; p < hi; ++p) take(p, a.gate ? (const T*)a.gate + (a.shared ? g : p) * a.ldgate : nullptr, S1, S2);
+  } else {
+    for (long u = blockIdx.x; u * a.group < a.rows; u += gridDim.x) {
+      const T* q = (const T*)a.gate + u * a.ldgate;
+      for (int c = threadIdx.x; c < C; c += kT) U1[c] = U2[c] = 0.f;
+      for (long p = u * a.group; p < (u + 1) * a.group; ++p) take(p, q, U1, U2);
+      for (int c = threadIdx.x; c < C; c += kT) {
+        const float g = Elt<T>::ld(q + c);
+        S1[c] += g * U1[c];
+        S2[c] += g * U2[c];
+        if (a.dgate) {
+          const float n = post ? at_or(w.post_gain, c, 1.f) * U1[c] + at_or(w.post_bias, c, 0.f) * U2[c] : U1[c];
+          Elt<T>::st((T*)a.dgate + u * a.lddgate + c, at_or(w.scale, c, 1.f) * n);
+        }
       }
     }
   }
@@ -345,21 +364,6 @@ __global__ __launch_bounds__(kT) void res_fwd(FwdArgs a) {
     if (in && a.stats && sh.l == 0) a.stats[p] = make_float4(st.x, st.y, so.x, so.y);
   }
 }
-
-// Which pixels a block takes.  Ranges: `ranges` blocks for each of the groups of
-// pixels that share a gate (one group of all pixels where none do), `per` pixels
-// each.  Whole: whole groups by a wave (a block, where a row is a block's), side
-// by side in parts of `part` lanes' rows (a power of two) where they are small.
-struct BwdArgs {
-  const void *dz, *dout, *out, *f, *gate;
-  void *dr, *df, *dgate;
-  long lddz, lddout, ldout, ldf, ldgate, lddr, lddf, lddgate, rows, group, per;
-  Vectors w;
-  const float4* stats;
-  float* part;   // [block][4][C]: dz ohat, dz, S1, S2 (ranges of a shared gate: U1, U2)
-  int C, G, ranges, slots;
-  int shared;    // a gate for several pixels
-};
 
 // The four sums over rows stay in registers to a block's end, and the next row's loads
 // are on their way while one is worked on (131072 x 128 bfloat16, rows 384 apart, with
@@ -805,18 +809,6 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
     TGP_LAUNCH(ps, res_sums, dim3(cdiv(a.s.C, 16), 2), dim3(1024), 0, st, a.part, S, stride, vectors(a.w), a.s.post, a.g,
                (int)a.overwrite, a.s.C);
   };
-  if (!p.vb) {
-    const int S = (int)std::min<long>(kAnyBlocks, rows / group);
-    {
-      ProfScope ps("residual_norm_bwd_any", 40 * n, 6 * n * sizeof(T), st);
-      TGP_LAUNCH(ps, res_bwd_any<T>, dim3(S), dim3(kT), a.s.C * sizeof(float), st, (const T*)a.dz.p, a.dz.ld,
-                 (const T*)a.dout.p, a.dout.ld, (const T*)a.out.p, a.out.ld, (const T*)a.f.p, a.f.ld,
-                 (const T*)a.gate.p, a.gate.ld, group, vectors(a.w), a.s.post, (const float4*)a.stats, (T*)a.dr.p,
-                 a.dr.ld, (T*)a.df.p, a.df.ld, (T*)a.dgate.p, a.dgate.ld, a.part, rows, a.s.C);
-    }
-    if (sums) add_up(S, 6);
-    return launch_status();
-  }
   BwdArgs k{a.dz.p, a.dout.p, a.out.p, a.f.p, a.gate.p, a.dr.p, a.df.p, a.dgate.p, a.dz.ld, a.dout.ld, a.out.ld, a.f.ld,
             a.gate.ld, a.dr.ld, a.df.ld, a.dgate.ld, rows, shared ? group : rows, 0, vectors(a.w), (const float4*)a.stats,
             nullptr, a.s.C, p.g, 1, 1, shared};
@@ -826,9 +818,11 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
   // channel); of eight where a block takes a row at a time and waits for it
   const long most = std::min<long>(kBlocks, std::max<long>(256, rows / (p.g ? 24 : 8)));
   // whole groups where a wave (block) each fills the chip, or takes one in one turn
-  const bool whole = shared && (groups >= (p.g ? 1024 : 512) || k.group <= rpw);
+  const bool any = !p.vb, whole = shared && (groups >= (p.g ? 1024 : 512) || k.group <= rpw);
   unsigned grid;
-  if (whole) {
+  if (whole && any) {
+    grid = (unsigned)std::min<long>(kAnyBlocks, groups);
+  } else if (whole) {
     int part = 1;
     while (part < k.group && part < rpw) part <<= 1;
     k.slots = rpw / part;
@@ -841,9 +835,14 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
     grid = (unsigned)(groups * k.ranges);
   }
   const bool join = shared && !whole && (sums || a.dgate.p);
-  if (sums || join) k.part = a.part;
-  bool done = false;
-  with_post(a.s.post, [&](auto post) {
+  if (sums || join || any) k.part = a.part;
+  if (any) {
+    ProfScope ps("residual_norm_bwd_any", 40 * n, 6 * n * sizeof(T), st);
+    if (whole) TGP_LAUNCH(ps, (res_bwd_any<T, true>), dim3(grid), dim3(kT), a.s.C * sizeof(float), st, k, a.s.post);
+    else TGP_LAUNCH(ps, (res_bwd_any<T, false>), dim3(grid), dim3(kT), a.s.C * sizeof(float), st, k, a.s.post);
+  }
+  bool done = any;
+  if (!any) with_post(a.s.post, [&](auto post) {
     done = with_plan<sizeof(T), kBwdValues, WIDE>(p, [&](auto vb, auto nv, auto blk) {
       constexpr int VB = decltype(vb)::value, NV = decltype(nv)::value;
       constexpr bool BLK = decltype(blk)::value, POST = decltype(post)::value;
@@ -865,7 +864,7 @@ hipError_t backward_t(const ResidualBackward& a, hipStream_t st) {
     else go(std::false_type());
   }
   if (sums && join) add_up((int)groups, 4 * k.ranges);
-  else if (sums) add_up((int)grid, 4);
+  else if (sums) add_up((int)grid, any && whole ? 6 : 4);
   return launch_status();
 }
 
