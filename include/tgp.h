@@ -426,8 +426,10 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * Sums over rows run in an order fixed by the shape, rows and alignment.
  *
  * ws: device memory of at least what tgp_gated_workspace returns for the call
- * (backward 0 or 1), at a multiple of 256 bytes; ENOSPACE if smaller.  Nothing
- * in it needs to start at zero, and nothing is kept in it between calls.
+ * (backward 0 or 1), at a multiple of 256 bytes; ENOSPACE if smaller.  It holds
+ * copies of tensors and weights of any alignment (below) and what one launch leaves
+ * for the next, of some thousand pixels at a time.  Nothing in it needs to start
+ * at zero, and nothing is kept in it between calls.
  * Alignment: elements of x, y, dy, dx and weights at multiples of their size,
  * biases and gradients at 4 bytes.  Tensors of a TGP_BF16 network whose address,
  * rows and row distances are multiples of 16 bytes are read as they are, others

@@ -1355,10 +1355,11 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
   p.cinp = round_up(s.cin, 8);
   p.hidp = round_up(s.hidden, 8);
   p.coutp = round_up(s.cout, 8);
+  const bool alone = !backward && narrow(s, rows);   // nothing lies between launches
   // so many pixels that what lies between launches stays in the caches, but that
   // a launch fills the chip
   const long a_row = 2 * (backward ? 3 * p.hparts * p.hidp + p.parts * (p.cinp + p.coutp)
-                                   : p.hparts * p.hidp + p.parts * p.cinp);
+                                   : (alone ? 0 : p.hparts * p.hidp) + p.parts * p.cinp);
   const long most = (long)(backward && p.parts == 1 ? 192 : 128) << 20;   // (of 256 MB)
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
   // (64 channels, 256 hidden: 1 pixel 18.7 us and in three launches 24.1, 64 18.7 and 18.5,
@@ -1373,12 +1374,18 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
     at += (n + 255) / 256 * 256;
     return here;
   };
+  if (!backward && few(s, rows)) {   // reads all its operands where they are
+    p.h = take((size_t)4 * few_pixels(rows) * round_up(s.hidden, 16));
+    p.bytes = at;
+    return p;
+  }
+  // copies of what does not lie in 16-byte pieces, which the query cannot see
   p.wg = take((size_t)2 * p.parts * s.hidden * p.cinp);
   p.wu = take((size_t)2 * p.parts * s.hidden * p.cinp);
   p.wd = take((size_t)2 * p.parts * s.cout * p.hidp);
   p.x = take((size_t)2 * p.parts * p.chunk * p.cinp);
   if (!backward) {
-    p.h = take(few(s, rows) ? (size_t)4 * few_pixels(rows) * round_up(s.hidden, 16) : (size_t)2 * p.hparts * p.chunk * p.hidp);
+    p.h = take(alone ? 0 : (size_t)2 * p.hparts * p.chunk * p.hidp);
   } else {
     p.dy = take((size_t)2 * p.parts * p.chunk * p.coutp);
     const size_t plane = p.slim ? 0 : (size_t)2 * p.hparts * p.chunk * p.hidp;
@@ -1405,7 +1412,7 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
     const int n = p.parts == 1 ? 1 : 6;   // pairs that add_sum makes
     return !r ? 0 : backward ? split_bytes(r, s.cin, s.hidden, 2 * n) : split_bytes(r, s.cout, s.hidden, n);
   };
-  p.join = take(std::max(room(p.chunk), room(rest)));
+  p.join = take(alone || p.slim ? 0 : std::max(room(p.chunk), room(rest)));
   p.bytes = at;
   return p;
 }

@@ -94,8 +94,10 @@ def test_wide(rows, cin, hidden, cout):
     _check(rows, cin, hidden, cout)
 
 
+# on both sides of where one launch takes it
 @pytest.mark.parametrize("rows", [1, 33, 64, 100, 3000])
-@pytest.mark.parametrize("cin,hidden,cout", [(64, 256, 64), (24, 72, 40), (33, 250, 61), (64, 129, 1), (1, 65, 64)])
+@pytest.mark.parametrize("cin,hidden,cout", [(64, 256, 64), (24, 72, 40), (33, 250, 61), (64, 129, 1), (1, 65, 64),
+                                             (64, 64, 64), (64, 257, 64), (65, 256, 64), (64, 256, 65)])
 def test_narrow_backward(rows, cin, hidden, cout):
     _check(rows, cin, hidden, cout, forward=False, backward=True)
 
