@@ -343,7 +343,10 @@ tgp_status tgp_schedule_trace(int m, int n, int ckpt_mode, int32_t* ops, int cap
  * These calls keep no state of their own: tensors, statistics and workspaces
  * are the caller's, every argument check runs on the host before anything is
  * enqueued, and work goes to `stream`.  They may be captured into a HIP
- * graph.  Calls with different buffers may run from several threads.
+ * graph.  Calls with different buffers may run from several threads.  Which tensors
+ * may lie on each other is said and checked call by call; weights, vectors over
+ * channels, statistics, gradients and workspaces may share memory with nothing that
+ * the call writes, which is the caller's part.
  *
  * Layer normalisation over the channels of each pixel (no statistic crosses
  * a pixel, so a micro-batched run equals the full-batch one, and a recompute
@@ -405,11 +408,13 @@ tgp_status tgp_layer_norm_backward(int64_t rows, int C, int dtype, const void* d
  * instructions with float32 sums.  TGP_BF16: h enters the last product as two
  * bfloat16s (16 bits), y is rounded once.  TGP_FP32: every factor is split into three
  * bfloat16s, of whose nine products the six largest are summed, which keeps
- * float32's accuracy.  A factor that is infinite or NaN makes what is summed with
- * it NaN or infinite, and nothing else.
+ * float32's accuracy; a value over bfloat16's largest (3.39e38) counts as infinite,
+ * and one under 2^-100 may lose its last bits.  act is accurate relative to itself.
+ * A factor that is infinite or NaN makes what is summed with it NaN or infinite,
+ * and nothing else.
  *
- * The backward starts from x and dy alone (g, u and h are computed again, with
- * the forward's bits, as a stage's F' does):
+ * The backward starts from x and dy alone (g, u and h are computed again, as a
+ * stage's F' does, and equal the forward's but for the order of float32 sums):
  *
  *   dh = dy Wd      dg = dh u act'(g)      du = dh act(g)
  *   dx = dg Wg + du Wu      dWg (+)= dg^T x      dWu (+)= du^T x      dWd (+)= dy^T h
@@ -496,8 +501,8 @@ tgp_status tgp_gated_backward(const tgp_gated_shape* shape, int64_t rows,
  * smaller; it may be NULL where that is 0).
  *
  * An output may be an input itself at the same row distance (of the gates: where
- * group = 1); any other overlap of an output with an input or output is refused
- * (EINVAL).  An infinity or NaN in a row of r or f makes that row NaN and no
+ * group = 1); any other overlap of an output tensor (out, z, dr, df, dgate) with an
+ * input or output tensor is refused (EINVAL).  An infinity or NaN in a row of r or f makes that row NaN and no
  * other; in the backward it reaches its row of dr and df and the sums it is in.
  * Alignment as of tgp_layer_norm_forward, stats at 16 bytes.  EUNSUPPORTED where
  * C is over 32768. */

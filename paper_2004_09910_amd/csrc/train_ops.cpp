@@ -183,8 +183,7 @@ tgp_status check_residual_params(const char* who, const tgp_residual_params* w) 
   return TGP_OK;
 }
 
-// Each of outs against every in and every other out; gates: places of a gate or its
-// gradient, which may lie on each other alone, and only where every pixel has one.
+// Each of outs against every in, on which it may lie row by row, and every other out.
 tgp_status check_places(const char* who, const Place* ins, int n_in, const Place* outs, int n_out, int dtype) {
   for (int o = 0; o < n_out; ++o) {
     for (int i = 0; i < n_in; ++i) TRY(check_apart(who, outs[o], ins[i], dtype));

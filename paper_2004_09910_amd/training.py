@@ -226,7 +226,11 @@ class GatedPipeline(NormPipeline):
         t = norm(x)    f = gated(t)    r = x + scale post_norm(f)    partition j reads pre_norm(r)
 
     Its matrices are of the network's type, everything else float32; AdamW with 8-bit states updates all of it.  The
-    blocks of a new partition are kept and started as the norms are."""
+    blocks of a new partition are kept and started as the norms are.
+
+    The gated block's backward computes its hidden channels again in every mode; t, f and r of all micro-batches are
+    kept in every mode, as the norms' inputs and outputs are, three tensors of a partition's input beside them.
+    balance_by_time measures the partitions' layers, not the blocks."""
 
     VECTORS = ("b_gate", "b_up", "b_down", "scale", "post_gain", "post_bias", "pre_gain", "pre_bias")
 
