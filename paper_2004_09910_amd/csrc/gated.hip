@@ -416,8 +416,8 @@ __global__ __launch_bounds__(64 * NW, P == 1 ? 2 : 1) void gated_narrow(NarrowAr
   constexpr int XK = XL ? 1 : KSX;   // stages of pixels in registers
   // Of bfloat16 h is two parts, 16 bits, so that y is rounded once.  A ring of three leaves
   // LDS for them; where the pixels take that as well, it holds half of the tile's channels
-  // at a time.  (131072 x 128, 512 hidden channels: 116 us, with a ring of four and halves
-  // 132, with h in one part, errors of twice a rounding's, 92.)
+  // at a time.  (131072 x 128, 512 hidden channels, as two launches: 116 us, with a ring of
+  // four and halves 132, with h in one part, which single values of y show, 92; as one 106.)
   constexpr int Q = P == 1 ? 2 : P;
   constexpr bool HALF = XL;
   constexpr int NS = P == 1 ? 3 : 6, BK = 64, BH = 32 * NW, KG = NW / CG, H = BK / 16, L = 4;
@@ -964,9 +964,9 @@ struct SlimArgs {
 // For dx, dg and du go through LDS, 32 pixels at a time in their two parts, rows of hidden
 // channels beside the weights' rows.
 // What bounds it are the activations, the splitting in parts and the products, one after
-// the other (147456 x 64, 256 hidden, GELU: 123 us, and 11 for the ranges' sums; by a launch
-// for h, dg and du, one for the weights and one for dx 365).  The two halves of 64 pixels
-// are a loop: unrolled, 39 registers spill (16 us).
+// the other (147456 x 64, 256 hidden, GELU: 124 of a pass's 135 us, the rest the ranges'
+// sums; a launch for h, dg and du, one for the weights and one for dx take three times as
+// long).  The two halves of 64 pixels are a loop: unrolled, 39 registers spill (16 us).
 template <int ACT, bool GRADS>
 __global__ __launch_bounds__(512, 2) void gated_slim(SlimArgs a) {
   typedef Feed<64, 64, false, 2> F;   // (its layout: rows of 64 values)
@@ -1275,9 +1275,9 @@ __global__ void gated_zero(float* p, long n) {
 // Large and small tiles of each launch.  A CU takes 55 bytes a clock from DMA, so a stage
 // of 128 x 128 tiles (64 values, 32 KB, 582 clocks) comes in slower than its 512 clocks of
 // products: tiles of 256 rows where there are enough of them.  4096 pixels x 1024, 4096
-// hidden: h 86 us (798 TFLOP/s; tiles of 128 x 128, two blocks a CU, 90), h, dg and du
-// 156 (two blocks of 128 x 64 a CU 163), the weights' gradients 215 (957; 128 x 128 255),
-// y 67 and dx 134 (1028).  Stages of 32 pixels where both factors are read by columns: the
+// hidden: h 88 us (785 TFLOP/s), h, dg and du 174 (in two parts 156, and by two blocks of
+// 128 x 64 a CU 163), the weights' gradients 317 (976; in two parts 215, and by tiles of
+// 128 x 128 255), y 69 (988) and dx 136 (1011).  Stages of 32 pixels where both factors are read by columns: the
 // fragments of one of 64 spill (787).  y and dx take a left factor's two parts in one
 // stage, 48 KB of a 128 x 128 tile for twice the products (y part by part, the right
 // factor read twice: 96 us).
@@ -1362,10 +1362,10 @@ Plan plan_of(const tgp_gated_shape& s, long rows, bool backward) {
                                    : (alone ? 0 : p.hparts * p.hidp) + p.parts * p.cinp);
   const long most = (long)(backward && p.parts == 1 ? 192 : 128) << 20;   // (of 256 MB)
   p.chunk = std::min(rows, std::max<long>(4096, most / a_row / 128 * 128));
-  // (64 channels, 256 hidden: 1 pixel 18.7 us and in three launches 24.1, 64 18.7 and 18.5,
-  // 1000 23.4 and 27.3, 12544 35.7 and 41.1, 147456 143 and 365; with few hidden channels
-  // most waves of a block have none: 300 x 32, 64 hidden 21.0 and 18.4, 12544 x 16, 32
-  // hidden 28.2 and 23.5, 100000 x 16 78 and 88)
+  // (64 channels, 256 hidden, short runs of GELU: 1 pixel 21.9 us and in three launches 21.1,
+  // 64 22.2 and 21.2, 1000 26.9 and 32.4, 12544 39.0 and 50.1, 147456 160 and 484; with few
+  // hidden channels most waves of a block have none: 300 x 32, 64 hidden 24.6 and 21.2,
+  // 12544 x 16, 32 hidden 30.5 and 26.8, 100000 x 16 93 and 114)
   p.slim = backward && s.dtype == TGP_BF16 && s.cin <= 64 && s.cout <= 64 && s.hidden > 64 && s.hidden <= 256;
   if (p.slim) p.chunk = std::min(rows, 1l << 22);   // (nothing lies between launches)
   size_t at = 0;
@@ -1574,8 +1574,8 @@ void launch_narrow(const NarrowArgs& a, hipStream_t st) {
   typedef std::integral_constant<int, 8> eight;
   const int k = cdiv(a.cin, 64);
   // up to 128 channels four waves a block, of bfloat16 two blocks a CU: one's first loads
-  // and activations beside the other's products (147456 x 64, 256 hidden channels: 65 us
-  // with eight waves)
+  // and activations beside the other's products (147456 x 64, 256 hidden channels: 51 us;
+  // with h in one part 44, and so with eight waves 65)
   auto cols = [&](auto ksx) {
     if (a.cout <= 64) go(ksx, four(), two());
     else go(ksx, four(), four());
@@ -1723,7 +1723,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
         a.to[1] = sink(s.hidden, s.cin, gr.up, gr.b_up);
         a.to[2] = sink(s.cout, s.hidden, gr.down, gr.b_down);
         with_act(s.act, [&](auto act) {
-          ProfScope ps("gated_slim", 2.0 * rows * (8 * s.cin + 3 * s.cout) * s.hidden,
+          ProfScope ps("gated_slim", 2.0 * rows * (12 * s.cin + 4 * s.cout) * s.hidden,
                        2.0 * rows * (2 * s.cin + s.cout) + 4.0 * m.ranges * p.stride, st);
           constexpr int ACT = decltype(act)::value;
           if (grads) TGP_LAUNCH(ps, (gated_slim<ACT, true>), dim3((unsigned)m.ranges), dim3(512), 0, st, a);
@@ -1744,7 +1744,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       typedef decltype(pr) PR;
       a.tm = cdiv(rows, PR::BM);
       a.tn = cdiv(s.hidden, PR::BN);
-      ProfScope ps("gated_back", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
+      ProfScope ps("gated_back", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * a.s.n, 2.0 * rows * (s.cin + s.cout + 3 * L * s.hidden), st);
       constexpr bool ALL = decltype(all)::value;
       TGP_LAUNCH(ps, (gated_back<PR, decltype(pd), decltype(act)::value, ALL ? L : sizeof(T) == 2 ? 2 : 3, ALL>),
                  dim3((unsigned)a.tm * a.tn), dim3(PR::T), 0, st, a);
@@ -1806,7 +1806,7 @@ hipError_t backward_t(const Gated& g, const T* dy, long lddy, const T* x, long l
       job(du, L, s.hidden, xm, P, s.cin, gr.up, gr.b_up);
       job(dym, P, s.cout, h, L, s.hidden, gr.down, gr.b_down);
       {
-        ProfScope ps("gated_outer", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * o.j[0].s.n, 2.0 * rows * (s.cin + s.cout + 6 * s.hidden), st);
+        ProfScope ps("gated_outer", 2.0 * rows * (2 * s.cin + s.cout) * s.hidden * o.j[0].s.n, 2.0 * rows * (s.cin + s.cout + 3 * L * s.hidden), st);
         if (p.wide == 64) TGP_LAUNCH(ps, gated_outer<OuterS>, dim3((unsigned)blocks), dim3(OuterS::T), 0, st, o);
         else if (p.wide == 128) TGP_LAUNCH(ps, gated_outer<OuterL>, dim3((unsigned)blocks), dim3(OuterL::T), 0, st, o);
         else TGP_LAUNCH(ps, gated_outer<OuterX>, dim3((unsigned)blocks), dim3(OuterX::T), 0, st, o);

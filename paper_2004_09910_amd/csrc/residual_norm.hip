@@ -368,7 +368,8 @@ __global__ __launch_bounds__(kT) void res_fwd(FwdArgs a) {
 // The four sums over rows stay in registers to a block's end, and the next row's loads
 // are on their way while one is worked on (131072 x 128 bfloat16, rows 384 apart, with
 // the sums' launches: 82.6 us with a row's loads one after the other and none ahead, 54
-// so).  Memory bounds it (45 us, 4.4 TB/s), and the sums' launches, 4 us each.
+// so).  Memory bounds it (46 us on tensors that are new to the caches, 4.4 TB/s, 36.5 on
+// ones that are not), and the sums' launches, 4 to 5 us each.
 template <typename T, int VB, int NV, bool BLK, bool POST, bool WHOLE>
 __global__ __launch_bounds__(kT) void res_bwd(BwdArgs a) {
   typedef Vec<T, VB> VT;
